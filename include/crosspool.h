@@ -246,8 +246,9 @@ cp_status cp_request_close(cp_pool *pool, int32_t req_id);
 cp_status cp_request_len(cp_pool *pool, int32_t req_id, int64_t *ctx_len);
 
 /* The request's layer cursor (Section 3.2): the layer its next decode step
- * reads, in [0, n_layers), and whether a new token is in flight (placed at
- * the first layer's step, committed after the last layer's). */
+ * reads, in [0, n_layers), and how many new tokens are in flight (placed at
+ * the first layer's step, committed after the last layer's; at most 1 but
+ * for the chunks of cp_attn_extend_step). */
 cp_status cp_request_cursor(cp_pool *pool, int32_t req_id, int32_t *layer, int32_t *in_flight);
 
 /* Copy the request's page-table entries of pages [first, first + count) to
@@ -461,6 +462,210 @@ cp_status cp_request_layer_state(cp_pool *pool, int32_t req_id, int32_t *layer, 
  * cp_kv_append. Errors: CP_EINVAL (range outside the committed [0,
  * ctx_len)), CP_ESTATE (host-only pool), CP_EHIP. */
 cp_status cp_kv_gather(cp_pool *pool, int32_t req_id, int64_t start, int64_t n_tok, void *dst, void *hip_stream);
+
+/* --------------------------------------------------------------- branches */
+
+/* Make each destination request a copy of a prefix of a source request: dst
+ * holds the same first n_tok[i] tokens in every layer, without the caller
+ * moving their rows. Whole pages are shared (one physical page, counted once
+ * against the budget, read through both page tables); a page that the prefix
+ * ends in is copied, because both requests may go on writing there. The
+ * requests are independent afterwards: either may be appended to, decoded,
+ * truncated, forked again or closed in any order; a page goes back to the
+ * pool with its last user. Continuations sampled from one prompt, beams that
+ * change parents (truncate to 0, then fork) and prompts with a common prefix
+ * are the uses (Section 3.1: pages are physical memory behind a logical
+ * address space, so two logical ranges can show the same page).
+ *
+ *   src_ids  host, n entries, open requests; one source may appear several
+ *            times, but not also as a destination of the call.
+ *   dst_ids  host, n distinct entries: open, empty requests (0 tokens) of
+ *            the source's model, whose own reservation holds the prefix.
+ *   n_tok    host, n entries in [0, source's committed tokens], or NULL: all
+ *            of the source's committed tokens.
+ * A destination's reservation then counts only the pages it does not share:
+ * a fork never fails for want of budget, and gives budget back (a virtual
+ * pool keeps the chunks mapped until a close of the model). One launch writes
+ * the page-table entries and copies the partial pages, on hip_stream; work
+ * on the requests on other streams must have been ordered before it. With
+ * device_pages this call waits for the device where steps took pages that
+ * the host has not read back, or where the model's stack must shrink.
+ * Errors: CP_EINVAL (unknown id, another model, a destination that is not
+ * empty, a prefix past the source or the reservation, a token in flight,
+ * the same id twice), CP_EHIP. */
+cp_status cp_request_fork(cp_pool *pool, int32_t n, const int32_t *src_ids, const int32_t *dst_ids,
+                          const int64_t *n_tok, void *hip_stream);
+
+/* Cut requests back to their first new_len[i] tokens (0 <= new_len[i] <=
+ * committed tokens), in every layer; pages behind them go back to the pool,
+ * for this request's next tokens or any other's. For drafted tokens that
+ * were not accepted, prompts that run again from some point, and beams
+ * (before a fork). The reservation stays. Where the new end lies inside a
+ * page that another request shares, the page is copied (on hip_stream), so
+ * that the next tokens can be written; later calls must be ordered after
+ * work already enqueued on the requests, as those on the same stream are.
+ * Giving up shared pages takes their place in the budget again, since the
+ * reservation must be able to fill it with pages of its own: CP_ENOSPC if it
+ * is not there (nothing changed).
+ * Errors: CP_EINVAL (unknown or duplicate id, a length out of range, a token
+ * in flight), CP_ENOSPC, CP_ENOMEM (a virtual pool could not map chunks),
+ * CP_EHIP. On a device_pages pool it may wait for the device as
+ * cp_request_fork does. */
+cp_status cp_request_truncate(cp_pool *pool, int32_t n, const int32_t *ids, const int64_t *new_len,
+                              void *hip_stream);
+
+/* -------------------------------------------------------- rotary positions */
+
+typedef enum {
+  CP_ROPE_HALF = 0,       /* pair i is elements (i, i + rot_dim / 2) */
+  CP_ROPE_INTERLEAVED = 1 /* pair i is elements (2 i, 2 i + 1) */
+} cp_rope_layout;
+
+/* Frequencies, as angle per position of pair i: f_i = base^(-2 i / rot_dim),
+ * and for contexts longer than the trained one */
+typedef enum {
+  CP_ROPE_PLAIN = 0,  /* f_i */
+  CP_ROPE_LINEAR = 1, /* f_i / factor (positions interpolated) */
+  CP_ROPE_NTK = 2,    /* base * factor^(rot_dim / (rot_dim - 2)) as the base */
+  /* by wavelength: r_i = orig_len f_i / (2 pi) is the number of turns over
+   * the trained context and w = clamp((r_i - low_turns) / (high_turns -
+   * low_turns), 0, 1); f_i w + (f_i / factor) (1 - w) */
+  CP_ROPE_PARTS = 3,
+  CP_ROPE_TABLE = 4   /* table[i], rot_dim / 2 angles per position */
+} cp_rope_scaling;
+
+typedef struct {
+  int32_t rot_dim; /* rotated elements of a head: even, in [2, 1024] (NTK: from 4 on) */
+  int32_t layout;  /* cp_rope_layout */
+  int32_t scaling; /* cp_rope_scaling */
+  int32_t reserved0;
+  double base;     /* > 0 (10000 is usual); TABLE: ignored */
+  double factor;   /* LINEAR, NTK, PARTS: > 0 */
+  double orig_len; /* PARTS: trained context, > 0 */
+  double low_turns, high_turns; /* PARTS: low_turns < high_turns */
+  double magnitude;    /* multiplies sine and cosine; 0 means 1 */
+  const double *table; /* TABLE: host, rot_dim / 2 finite angles (not retained) */
+} cp_rope_desc;
+
+typedef struct cp_rope cp_rope; /* opaque; immutable once created */
+
+/* A rotation on a device (-1: host only, for cp_rope_angles). Angles are
+ * formed in 64 bits, pos * f_i reduced to one turn, so far positions keep
+ * their precision. Errors: CP_EINVAL, CP_ENOMEM, CP_EHIP. */
+cp_status cp_rope_create(const cp_rope_desc *desc, int32_t device, cp_rope **out);
+
+/* The caller must have synchronised every stream used with it. */
+cp_status cp_rope_destroy(cp_rope *rope);
+
+/* The angles per position, rot_dim / 2 of them, to host memory. */
+cp_status cp_rope_angles(const cp_rope *rope, double *angles);
+
+typedef enum { CP_ROPE_BF16 = 0, CP_ROPE_F32 = 1 } cp_rope_dtype;
+
+/* A tensor [n_tokens][heads][width] in device memory; strides in elements,
+ * the last dimension contiguous. Elements [offset, offset + rot_dim) of each
+ * head are rotated, the others copied. dst may be src (same strides), and
+ * must not overlap it otherwise; distinct tokens and heads of dst must not
+ * overlap. Any alignment of whole elements works; 16-byte aligned rows are
+ * faster. */
+typedef struct {
+  const void *src;
+  void *dst;
+  int64_t src_token, src_head, dst_token, dst_head; /* strides, >= 0 */
+  int32_t heads, width, offset, dtype;              /* cp_rope_dtype */
+} cp_rope_tensor;
+
+/* Rotate 1 to 16 tensors of the same tokens in one launch: with angle t =
+ * pos * f_i and (a, b) the elements of pair i,
+ *     (a, b) <- magnitude (a cos t - b sin t, a sin t + b cos t),
+ * computed in 32 bits and rounded once. inverse != 0 turns by -t (the
+ * rotation's transpose, which is also its gradient): the magnitude
+ * multiplies in both directions.
+ *   positions  device, n_tokens int32 (any sign), or NULL: token k is at
+ *              position first + k.
+ * Errors: CP_EINVAL, CP_ESTATE (host-only rotation), CP_EHIP. */
+cp_status cp_rope_apply(const cp_rope *rope, int32_t n_tensors, const cp_rope_tensor *tensors, int64_t n_tokens,
+                        const int32_t *positions, int64_t first, int32_t inverse, void *hip_stream);
+
+/* cp_kv_append of rows whose keys are not yet rotated: each row's K heads
+ * (GQA: elements [0, rot_dim) of every K head; MLA: the first rot_dim
+ * elements of the rope part) are rotated at the token's position in the
+ * request on the way into the pool; V, and what lies outside, is copied bit
+ * for bit. The same checks, plus CP_EINVAL for a rotation wider than the
+ * head (MLA: than the rope part) or on another device. */
+cp_status cp_kv_append_rope(cp_pool *pool, int32_t n, const int32_t *req_ids, const int32_t *n_new, const void *rows,
+                            const cp_rope *rope, void *hip_stream);
+
+/* ------------------------------------------------- attention of token chunks */
+
+typedef struct {
+  /* > 0: scores s become softcap * tanh(s / softcap); 0: uncapped. */
+  float softcap;
+  /* W >= 1: a token at position p sees positions > p - W only; 0: all. */
+  int32_t window;
+  /* Device, [n_q_heads] float, or NULL: slopes[h] * |p - j| is subtracted
+   * from the (capped) score of position j. */
+  const float *slopes;
+  /* Host, n entries, or NULL: the first prefix[i] tokens of request i are
+   * seen by every query (a prompt read in both directions); >= 0, lengths
+   * past the context count as the context. Window and documents still
+   * limit what is seen. */
+  const int32_t *prefix;
+  /* Device, one int32 per query token (in the order of q), or NULL: the
+   * position at which the token's document starts; earlier ones are not
+   * seen. A start past the token's own position, and past its prefix,
+   * leaves the row empty. */
+  const int32_t *doc_begin;
+  /* 0: the planner cuts long contexts into ranges where there are few
+   * rows; k >= 1 forces at most k ranges per request. */
+  int32_t num_splits;
+  int32_t path; /* cp_path: AUTO, or VALU to force the vector kernel */
+  /* cp_attn_extend_step: rotates the new rows' keys as they are placed, as
+   * cp_kv_append_rope does; NULL: rows are stored as they are. Queries
+   * always come rotated. cp_attn_extend: must be NULL. */
+  const cp_rope *rope;
+} cp_extend_opts;
+
+/* Attention of the last n_q[i] tokens of each request (a prompt chunk, a
+ * few drafted tokens, or one) over the request's KV in the pool. All
+ * requests of a call belong to one model. Query token t of request i stands
+ * at position p = context - n_q[i] + t (a context with tokens in flight, of
+ * the current layer, as in cp_attn_decode) and sees positions j with
+ *     max(p - window + 1, doc_begin) <= j < max(p + 1, prefix[i]):
+ *     s_j = cap(scale * <q_h, K_j>) - slopes[h] |p - j|;
+ *     out_h = sum_j softmax(s)_j V_j;  lse_h = ln sum_j exp(s_j).
+ * A row that sees nothing (or whose scores are all -inf) gives out = 0 and
+ * lse = -inf. What lies in positions that a row does not see does not reach
+ * it, infinities and NaN included.
+ *   n_q  host, n entries, 0 <= n_q[i] <= context of request i.
+ *   q    device, bf16, [sum n_q][n_q_heads][d_k] in call order; 16-byte
+ *        aligned. out [sum n_q][n_q_heads][d_v] bf16 (8-byte aligned) and
+ *        lse [sum n_q][n_q_heads] float likewise.
+ *   opts may be NULL (causal attention).
+ * Scores, statistics and sums are held in 32 bits; the matrix-core kernels
+ * round probabilities to bf16 for prompt chunks (more than 32 rows, a row
+ * being a token and a query head of one KV head) and take them in two bf16 parts for fewer. Results depend on the logical KV
+ * and the call only, never on page placement. The cursor does not move.
+ * Errors: CP_EINVAL, CP_ESTATE (host-only pool), CP_ENOMEM (workspace), CP_EHIP. */
+cp_status cp_attn_extend(cp_pool *pool, int32_t n, const int32_t *req_ids, const int32_t *n_q, const void *q,
+                         void *out, float *lse, void *hip_stream, const cp_extend_opts *opts);
+
+/* Place chunks of new tokens and attend: for each request the current
+ * layer's rows of n_new[i] tokens are appended and the same tokens' queries
+ * attend over the context with them, as cp_attn_extend. Multi-layer models
+ * are taken layer by layer as in cp_attn_decode_step: at the first layer
+ * n_new[i] >= 0 places the chunk (pages of every layer), at later layers
+ * n_new[i] must be the tokens in flight; the cursor moves on with each call
+ * and the chunk is committed after the last layer. Requests with n_new[i] =
+ * 0 contribute no rows, but their cursor moves on too.
+ *   rows  device, bf16, [sum n_new][row_elems] in call order (one layer).
+ * Errors: those of cp_kv_append and cp_attn_extend, plus CP_EINVAL for an
+ * n_new that is not the tokens in flight. A refused call changes nothing;
+ * after a HIP failure the tokens are placed and the cursors moved, and the
+ * pool should be closed. */
+cp_status cp_attn_extend_step(cp_pool *pool, int32_t n, const int32_t *req_ids, const int32_t *n_new,
+                              const void *rows, const void *q, void *out, float *lse, void *hip_stream,
+                              const cp_extend_opts *opts);
 
 /* ---------------------------------------------------------------------
  * KV-cache planner (Section 3.1, "KV-cache Planner and Virtualizer",

@@ -22,6 +22,9 @@ CP_KIND_MLA, CP_KIND_GQA = 0, 1
 CP_PATH_AUTO, CP_PATH_VALU, CP_PATH_MFMA = 0, 1, 2
 CP_SCHED_BALANCED, CP_SCHED_QUEUE, CP_SCHED_GRID = 0, 1, 2
 CP_BACKING_BUFFER, CP_BACKING_VIRTUAL = 0, 1
+CP_ROPE_HALF, CP_ROPE_INTERLEAVED = 0, 1
+CP_ROPE_PLAIN, CP_ROPE_LINEAR, CP_ROPE_NTK, CP_ROPE_PARTS, CP_ROPE_TABLE = 0, 1, 2, 3, 4
+CP_ROPE_BF16, CP_ROPE_F32 = 0, 1
 _NAMES = {0: "CP_OK", -1: "CP_EINVAL", -2: "CP_ENOMEM", -3: "CP_ENOSPC", -4: "CP_EHIP", -5: "CP_ESTATE"}
 
 
@@ -98,6 +101,50 @@ class cp_decode_opts(C.Structure):
     ]
 
 
+class cp_rope_desc(C.Structure):
+    _fields_ = [
+        ("rot_dim", C.c_int32),
+        ("layout", C.c_int32),
+        ("scaling", C.c_int32),
+        ("reserved0", C.c_int32),
+        ("base", C.c_double),
+        ("factor", C.c_double),
+        ("orig_len", C.c_double),
+        ("low_turns", C.c_double),
+        ("high_turns", C.c_double),
+        ("magnitude", C.c_double),
+        ("table", C.POINTER(C.c_double)),
+    ]
+
+
+class cp_rope_tensor(C.Structure):
+    _fields_ = [
+        ("src", C.c_void_p),
+        ("dst", C.c_void_p),
+        ("src_token", C.c_int64),
+        ("src_head", C.c_int64),
+        ("dst_token", C.c_int64),
+        ("dst_head", C.c_int64),
+        ("heads", C.c_int32),
+        ("width", C.c_int32),
+        ("offset", C.c_int32),
+        ("dtype", C.c_int32),
+    ]
+
+
+class cp_extend_opts(C.Structure):
+    _fields_ = [
+        ("softcap", C.c_float),
+        ("window", C.c_int32),
+        ("slopes", C.c_void_p),
+        ("prefix", C.c_void_p),
+        ("doc_begin", C.c_void_p),
+        ("num_splits", C.c_int32),
+        ("path", C.c_int32),
+        ("rope", C.c_void_p),
+    ]
+
+
 class cp_plan_model(C.Structure):
     _fields_ = [("kappa_bytes", C.c_double), ("arrival_rate", C.c_double), ("n_samples", C.c_int64),
                 ("prompt_tokens", C.POINTER(C.c_int64)), ("output_tokens", C.POINTER(C.c_int64)),
@@ -149,6 +196,15 @@ def _load() -> C.CDLL:
                                    C.POINTER(cp_decode_opts)], I32),
         "cp_request_layer_state": ([P, I32, C.POINTER(I32), C.POINTER(I64)], I32),
         "cp_kv_gather": ([P, I32, I64, I64, VP, VP], I32),
+        "cp_request_fork": ([P, I32, VP, VP, VP, VP], I32),
+        "cp_request_truncate": ([P, I32, VP, VP, VP], I32),
+        "cp_rope_create": ([C.POINTER(cp_rope_desc), I32, C.POINTER(P)], I32),
+        "cp_rope_destroy": ([P], I32),
+        "cp_rope_angles": ([P, C.POINTER(C.c_double)], I32),
+        "cp_rope_apply": ([P, I32, VP, I64, VP, I64, I32, VP], I32),
+        "cp_kv_append_rope": ([P, I32, VP, VP, VP, P, VP], I32),
+        "cp_attn_extend": ([P, I32, VP, VP, VP, VP, VP, VP, C.POINTER(cp_extend_opts)], I32),
+        "cp_attn_extend_step": ([P, I32, VP, VP, VP, VP, VP, VP, VP, C.POINTER(cp_extend_opts)], I32),
         "cp_plan_pool": ([C.POINTER(cp_plan_model), I32, C.POINTER(cp_plan_opts), C.POINTER(cp_plan_result)], I32),
     }
     for name, (args, res) in sig.items():
@@ -170,6 +226,15 @@ def i32_array(xs: Sequence[int]):
     """A host int32 array argument built once, for callers that repeat a
     call with the same request ids (it is passed as it is)."""
     return (C.c_int32 * len(xs))(*[int(x) for x in xs])
+
+
+def i64_array(xs: Sequence[int]):
+    """The same of int64, for lengths."""
+    return (C.c_int64 * len(xs))(*[int(x) for x in xs])
+
+
+def _i64_array(xs):
+    return xs if xs is None or isinstance(xs, C.Array) else i64_array(xs)
 
 
 def _i32_array(xs: Sequence[int]):
@@ -354,6 +419,125 @@ def cp_kv_gather(pool: int, req_id: int, start: int, n_tok: int, dst, stream=Non
     _check(LIB.cp_kv_gather(pool, req_id, start, n_tok, _ptr(dst), _stream(stream)))
 
 
+def cp_request_fork(pool: int, src_ids: Sequence[int], dst_ids: Sequence[int], n_tok=None, stream=None) -> None:
+    n = len(dst_ids)
+    if len(src_ids) != n or (n_tok is not None and len(n_tok) != n):
+        raise ValueError("src_ids, dst_ids and n_tok differ in length")
+    _check(LIB.cp_request_fork(pool, n, _i32_array(src_ids), _i32_array(dst_ids), _i64_array(n_tok), _stream(stream)))
+
+
+def cp_request_truncate(pool: int, req_ids: Sequence[int], new_len: Sequence[int], stream=None) -> None:
+    n = len(req_ids)
+    if len(new_len) != n:
+        raise ValueError("req_ids and new_len differ in length")
+    _check(LIB.cp_request_truncate(pool, n, _i32_array(req_ids), _i64_array(new_len), _stream(stream)))
+
+
+def cp_rope_create(rot_dim: int, device: int = 0, layout: int = CP_ROPE_HALF, scaling: int = CP_ROPE_PLAIN,
+                   base: float = 10000.0, factor: float = 1.0, orig_len: float = 0.0, low_turns: float = 1.0,
+                   high_turns: float = 32.0, magnitude: float = 0.0, table=None) -> int:
+    tab = None if table is None else (C.c_double * len(table))(*[float(x) for x in table])
+    if tab is not None and len(tab) != rot_dim // 2:
+        raise ValueError("table holds rot_dim / 2 angles")
+    d = cp_rope_desc(rot_dim, layout, scaling, 0, base, factor, orig_len, low_turns, high_turns, magnitude, tab)
+    out = C.c_void_p()
+    _check(LIB.cp_rope_create(C.byref(d), device, C.byref(out)))
+    return out.value
+
+
+def cp_rope_destroy(rope: int) -> None:
+    _check(LIB.cp_rope_destroy(rope))
+
+
+def cp_rope_angles(rope: int, rot_dim: int) -> np.ndarray:
+    out = np.zeros(rot_dim // 2)
+    _check(LIB.cp_rope_angles(rope, out.ctypes.data_as(C.POINTER(C.c_double))))
+    return out
+
+
+def rope_parts(pairs, offset: int = 0):
+    """The tensor records of cp_rope_apply, built once for callers that repeat
+    a call: (src, dst) tensors [tokens][heads][width], bf16 or float32, whose
+    last dimension is contiguous; dst may be src. Elements [offset, offset +
+    rot_dim) of each head are rotated."""
+    import torch
+
+    pairs = list(pairs)
+    arr = (cp_rope_tensor * len(pairs))()
+    tokens = None
+    for i, (s, d) in enumerate(pairs):
+        if s.dim() != 3 or s.shape != d.shape or s.dtype != d.dtype:
+            raise ValueError("src and dst are [tokens][heads][width] of one dtype")
+        if s.dtype not in (torch.bfloat16, torch.float32):
+            raise ValueError("rotated tensors are bf16 or float32")
+        if any(t.stride(2) != 1 and t.shape[2] > 1 for t in (s, d)):
+            raise ValueError("the last dimension must be contiguous")
+        if tokens not in (None, s.shape[0]):
+            raise ValueError("the tensors differ in tokens")
+        if s.device != d.device:
+            raise ValueError("src and dst are on different devices")
+        tokens = s.shape[0]
+        arr[i] = cp_rope_tensor(s.data_ptr(), d.data_ptr(), s.stride(0), s.stride(1), d.stride(0), d.stride(1),
+                                s.shape[1], s.shape[2], offset, CP_ROPE_F32 if s.dtype == torch.float32 else CP_ROPE_BF16)
+    arr.tokens, arr.keep = tokens or 0, pairs
+    return arr
+
+
+def cp_rope_apply(rope: int, parts, positions=None, first: int = 0, inverse: bool = False, stream=None) -> None:
+    """parts: from rope_parts. positions: int32 device tensor (or address) with
+    one entry per token, or None: first, first + 1, ..."""
+    if hasattr(positions, "dtype") and (str(positions.dtype) != "torch.int32" or positions.numel() != parts.tokens):
+        raise ValueError("positions holds one int32 per token")
+    _check(LIB.cp_rope_apply(rope, len(parts), parts, parts.tokens, _ptr(positions), first, int(inverse),
+                             _stream(stream)))
+
+
+def _rope(rope) -> Optional[int]:
+    return rope.handle if isinstance(rope, Rope) else rope
+
+
+def cp_kv_append_rope(pool: int, req_ids: Sequence[int], n_new: Sequence[int], rows, rope, stream=None) -> None:
+    n = len(req_ids)
+    if len(n_new) != n:
+        raise ValueError("req_ids and n_new differ in length")
+    _check(LIB.cp_kv_append_rope(pool, n, _i32_array(req_ids), _i32_array(n_new), _ptr(rows), _rope(rope),
+                                 _stream(stream)))
+
+
+def _extend_opts(n, softcap, window, slopes, prefix, doc_begin, num_splits, path, rope):
+    if prefix is not None:
+        if len(prefix) != n:
+            raise ValueError("prefix and req_ids differ in length")
+        prefix = _i32_array(prefix)
+    o = cp_extend_opts(softcap, window, _ptr(slopes), None, _ptr(doc_begin), num_splits, path, _rope(rope))
+    if prefix is not None:
+        o.prefix = prefix if isinstance(prefix, int) else C.addressof(prefix)
+        o.keep = prefix
+    return o
+
+
+def cp_attn_extend(pool: int, req_ids: Sequence[int], n_q: Sequence[int], q, out, lse, stream=None, *,
+                   softcap: float = 0.0, window: int = 0, slopes=None, prefix=None, doc_begin=None,
+                   num_splits: int = 0, path: int = CP_PATH_AUTO) -> None:
+    n = len(req_ids)
+    if len(n_q) != n:
+        raise ValueError("req_ids and n_q differ in length")
+    o = _extend_opts(n, softcap, window, slopes, prefix, doc_begin, num_splits, path, None)
+    _check(LIB.cp_attn_extend(pool, n, _i32_array(req_ids), _i32_array(n_q), _ptr(q), _ptr(out), _ptr(lse),
+                              _stream(stream), C.byref(o)))
+
+
+def cp_attn_extend_step(pool: int, req_ids: Sequence[int], n_new: Sequence[int], rows, q, out, lse, stream=None, *,
+                        rope=None, softcap: float = 0.0, window: int = 0, slopes=None, prefix=None, doc_begin=None,
+                        num_splits: int = 0, path: int = CP_PATH_AUTO) -> None:
+    n = len(req_ids)
+    if len(n_new) != n:
+        raise ValueError("req_ids and n_new differ in length")
+    o = _extend_opts(n, softcap, window, slopes, prefix, doc_begin, num_splits, path, rope)
+    _check(LIB.cp_attn_extend_step(pool, n, _i32_array(req_ids), _i32_array(n_new), _ptr(rows), _ptr(q), _ptr(out),
+                                   _ptr(lse), _stream(stream), C.byref(o)))
+
+
 def cp_plan_pool(models, horizon_s: float, n_obs: int, quantile: float, seed: int, chunk_bytes: int = 2 << 20) -> dict:
     """models: sequence of dicts with kappa_bytes, arrival_rate and equal-length
     prompt_tokens / output_tokens / service_time_s sequences (trace records)."""
@@ -375,6 +559,33 @@ def cp_plan_pool(models, horizon_s: float, n_obs: int, quantile: float, seed: in
 
 
 # -------------------------------------------------------- convenience ----
+
+class Rope:
+    """Owns one cp_rope handle. layout: "half" or "interleaved"; scaling:
+    "none", "linear", "ntk", "parts" or "table"."""
+
+    _LAYOUT = {"half": CP_ROPE_HALF, "interleaved": CP_ROPE_INTERLEAVED}
+    _SCALING = {"none": CP_ROPE_PLAIN, "linear": CP_ROPE_LINEAR, "ntk": CP_ROPE_NTK, "parts": CP_ROPE_PARTS,
+                "table": CP_ROPE_TABLE}
+
+    def __init__(self, rot_dim: int, device: int = 0, layout: str = "half", scaling: str = "none", **desc):
+        self.handle = None
+        if layout not in self._LAYOUT or scaling not in self._SCALING:
+            raise ValueError(f"unknown layout {layout!r} or scaling {scaling!r}")
+        self.rot_dim, self.device = rot_dim, device
+        self.handle = cp_rope_create(rot_dim, device, self._LAYOUT[layout], self._SCALING[scaling], **desc)
+
+    def angles(self) -> np.ndarray:
+        return cp_rope_angles(self.handle, self.rot_dim)
+
+    def apply(self, parts, positions=None, first: int = 0, inverse: bool = False, stream=None) -> None:
+        cp_rope_apply(self.handle, parts, positions, first, inverse, stream)
+
+    def destroy(self) -> None:
+        if self.handle:
+            cp_rope_destroy(self.handle)
+            self.handle = None
+
 
 class Pool:
     """Owns one cp_pool handle; methods forward to the C names above."""
@@ -435,6 +646,21 @@ class Pool:
 
     def decode_layers(self, req_ids, n_new, rows, q, out, lse, stream=None, **opts) -> None:
         cp_attn_decode_layers(self.handle, req_ids, n_new, rows, q, out, lse, stream, **opts)
+
+    def append_rope(self, req_ids, n_new, rows, rope, stream=None) -> None:
+        cp_kv_append_rope(self.handle, req_ids, n_new, rows, rope, stream)
+
+    def extend(self, req_ids, n_q, q, out, lse, stream=None, **opts) -> None:
+        cp_attn_extend(self.handle, req_ids, n_q, q, out, lse, stream, **opts)
+
+    def extend_step(self, req_ids, n_new, rows, q, out, lse, stream=None, **opts) -> None:
+        cp_attn_extend_step(self.handle, req_ids, n_new, rows, q, out, lse, stream, **opts)
+
+    def fork(self, src_ids, dst_ids, n_tok=None, stream=None) -> None:
+        cp_request_fork(self.handle, src_ids, dst_ids, n_tok, stream)
+
+    def truncate(self, req_ids, new_len, stream=None) -> None:
+        cp_request_truncate(self.handle, req_ids, new_len, stream)
 
     def layer_state(self, req_id: int):
         return cp_request_layer_state(self.handle, req_id)

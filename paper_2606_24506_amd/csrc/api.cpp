@@ -14,13 +14,16 @@
 
 #include "cost_line.hpp"
 #include "crosspool.h"
+#include "extend.h"
 #include "kargs.h"
 static_assert(cp::kNoAllocScratchBytes == CP_NOALLOC_WORKSPACE_BYTES, "the header states the fixed workspace size");
 #include "status.hpp"
 #include "pool.hpp"
+#include "rope.hpp"
 
 namespace cp {
 hipError_t launch_append(const AppendArgs &a, hipStream_t stream);
+hipError_t launch_append_rope(const AppendArgs &a, const RopeK &rope, hipStream_t stream);
 hipError_t launch_gather(const GatherArgs &a, hipStream_t stream);
 hipError_t launch_decode(const DecodeArgs &a, int grid, uint32_t mask, hipStream_t stream, hipEvent_t ev0,
                          hipEvent_t ev1);
@@ -30,6 +33,9 @@ int decode_wgs_per_cu(uint32_t mask);
 int matrix_streams(int variant);
 int matrix_step_tokens(int variant, int hkv);
 hipError_t launch_merge(const MergeArgs &a, hipStream_t stream);
+hipError_t launch_extend(const ExtArgs &a, int32_t kind, hipStream_t stream);
+hipError_t launch_ext_merge(const ExtMergeArgs &a, uint32_t rows, hipStream_t stream);
+hipError_t launch_page_copy(const PageCopyArgs &a, hipStream_t stream);
 hipError_t launch_stack_push(const StackPushArgs &a, hipStream_t stream);
 hipError_t scratch_device_address(int device, void **out);
 }  // namespace cp
@@ -82,6 +88,9 @@ struct AppendPlan {
 };
 cp_status decode_impl(cp_pool *p, int32_t n, const int32_t *req_ids, const void *q, void *out, float *lse,
                       void *hip_stream, const cp_decode_opts *opts);
+cp_status check_ids(cp_pool *p, int32_t n, const int32_t *ids);
+cp_status launch_page_items(cp_pool *p, const std::vector<PageItem> &items, const std::vector<int32_t> &models,
+                            hipStream_t s);
 }  // namespace
 
 struct cp_pool {
@@ -313,6 +322,12 @@ cp_status prepare_growth(cp_pool *p, int32_t n, const int32_t *ids, const int32_
   }
   std::vector<int32_t> carved;
   for (int32_t m = 0; m < p->st.n_models(); ++m) {
+    if (p->dev_pages && need[(size_t)m] > 0) {
+      // pages waiting in the device stack may be the last of the budget: it
+      // keeps no more than requests may take behind this growth
+      cp_status rc = drain_stack(p, m, p->st.room_to_grow(m) - need[(size_t)m]);
+      if (rc) return rc;
+    }
     if (need[(size_t)m] > 0 && !p->st.ensure_slots(m, need[(size_t)m], &carved)) {
       p->st.release_empty(carved);
       return fail(CP_ENOMEM, "could not map physical memory for %lld new pages of model %d",
@@ -538,6 +553,113 @@ cp_status cp_request_close(cp_pool *p, int32_t req_id) {
   return CP_OK;
 }
 
+cp_status cp_request_fork(cp_pool *p, int32_t n, const int32_t *src, const int32_t *dst, const int64_t *n_tok,
+                          void *hip_stream) {
+  if (!p) return fail(CP_EINVAL, "null pool");
+  cp_status rc = check_ids(p, n, dst);
+  if (rc) return rc;
+  if (n > 0 && !src) return fail(CP_EINVAL, "null src_ids");
+  if (p->broken) return fail(CP_ESTATE, "a failed decode step left the device page stacks out of step; destroy the pool");
+  const int32_t P = p->st.page_tokens();
+  std::vector<int64_t> len((size_t)n), tails((size_t)p->st.n_models(), 0), shown((size_t)p->st.n_models(), 0);
+  std::vector<int32_t> sorted(dst, dst + n);
+  std::sort(sorted.begin(), sorted.end());
+  for (int32_t i = 0; i < n; ++i) {
+    if (!p->st.valid_open(src[i])) return fail(CP_EINVAL, "request %d is not open", src[i]);
+    if (std::binary_search(sorted.begin(), sorted.end(), src[i]))
+      return fail(CP_EINVAL, "request %d is both a source and a destination", src[i]);
+    const Request &s = p->st.req(src[i]), &d = p->st.req(dst[i]);
+    if (s.model != d.model) return fail(CP_EINVAL, "requests %d and %d are of different models", src[i], dst[i]);
+    if (s.cursor != 0 || s.inflight || d.cursor != 0 || d.inflight)
+      return fail(CP_EINVAL, "request %d or %d has a token in flight; finish its decode steps first", src[i], dst[i]);
+    if (d.ctx_len != 0) return fail(CP_EINVAL, "request %d is not empty", dst[i]);
+    len[(size_t)i] = n_tok ? n_tok[i] : s.ctx_len;
+    if (len[(size_t)i] < 0 || len[(size_t)i] > s.ctx_len)
+      return fail(CP_EINVAL, "a prefix of %lld tokens of request %d, which has %lld", (long long)len[(size_t)i], src[i],
+                  (long long)s.ctx_len);
+    if (!p->st.fits_reservation(dst[i], len[(size_t)i]))
+      return fail(CP_EINVAL, "a prefix of %lld tokens is past request %d's reservation", (long long)len[(size_t)i], dst[i]);
+    shown[(size_t)d.model] += (len[(size_t)i] + P - 1) / P * d.layers;
+    if (len[(size_t)i] % P) tails[(size_t)d.model] += d.layers;
+  }
+  rc = reconcile_pages(p);
+  if (rc) return rc;
+  std::vector<int32_t> carved;
+  for (int32_t m = 0; m < p->st.n_models(); ++m) {
+    if (p->dev_pages) {  // the stack keeps what requests may still take then
+      rc = drain_stack(p, m, p->st.room_to_grow(m) - shown[(size_t)m]);
+      if (rc) return rc;
+    }
+    if (!p->st.ensure_slots(m, tails[(size_t)m], &carved)) {
+      p->st.release_empty(carved);
+      return fail(CP_ENOMEM, "could not map physical memory for %lld pages of model %d", (long long)tails[(size_t)m], m);
+    }
+  }
+  std::vector<PageItem> items;
+  std::vector<int32_t> models;
+  for (int32_t i = 0; i < n; ++i) {
+    if (len[(size_t)i] == 0) continue;
+    p->st.fork(src[i], dst[i], len[(size_t)i]);
+    const Request &s = p->st.req(src[i]), &d = p->st.req(dst[i]);
+    const uint32_t whole = (uint32_t)(len[(size_t)i] / P), tail = (uint32_t)(len[(size_t)i] % P);
+    const uint32_t *pt = p->st.pte_mirror();
+    for (int32_t l = 0; l < d.layers; ++l) {
+      items.push_back(PageItem{s.plane_base(l), d.plane_base(l), whole, tail, tail ? pt[s.plane_base(l) + whole] : 0u,
+                               tail ? pt[d.plane_base(l) + whole] : 0u, 0u, 0u});
+      models.push_back(d.model);
+    }
+  }
+  return launch_page_items(p, items, models, (hipStream_t)hip_stream);
+}
+
+cp_status cp_request_truncate(cp_pool *p, int32_t n, const int32_t *ids, const int64_t *new_len, void *hip_stream) {
+  if (!p) return fail(CP_EINVAL, "null pool");
+  cp_status rc = check_ids(p, n, ids);
+  if (rc) return rc;
+  if (n > 0 && !new_len) return fail(CP_EINVAL, "null new_len");
+  if (p->broken) return fail(CP_ESTATE, "a failed decode step left the device page stacks out of step; destroy the pool");
+  bool any = false;
+  for (int32_t i = 0; i < n; ++i) {
+    const Request &r = p->st.req(ids[i]);
+    if (new_len[i] < 0 || new_len[i] > r.ctx_len)
+      return fail(CP_EINVAL, "request %d of %lld tokens cannot be cut to %lld", ids[i], (long long)r.ctx_len,
+                  (long long)new_len[i]);
+    if (r.cursor != 0 || r.inflight)
+      return fail(CP_EINVAL, "request %d has a token in flight; finish its decode steps first", ids[i]);
+    any = any || new_len[i] < r.ctx_len;
+  }
+  if (!any) return CP_OK;
+  rc = reconcile_pages(p);
+  if (rc) return rc;
+  std::vector<int64_t> more, pages;
+  p->st.truncate_cost(n, ids, new_len, &more, &pages);
+  if (!p->st.fits_budget(more))
+    return fail(CP_ENOSPC, "the pool page budget cannot take back the shared pages' place");
+  std::vector<int32_t> carved;
+  for (int32_t m = 0; m < p->st.n_models(); ++m) {
+    // a virtual pool backs whole reservations; otherwise the copies' pages
+    const int64_t slots = p->st.virt() && more[(size_t)m] ? p->st.reserved(m) + more[(size_t)m] - p->st.allocated(m)
+                                                          : pages[(size_t)m];
+    if (!p->st.ensure_slots(m, slots, &carved)) {
+      p->st.release_empty(carved);
+      return fail(CP_ENOMEM, "could not map physical memory for %lld pages of model %d", (long long)slots, m);
+    }
+  }
+  std::vector<PageItem> items;
+  std::vector<int32_t> models;
+  std::vector<PoolState::OwnPage> copies;
+  for (int32_t i = 0; i < n; ++i) {
+    copies.clear();
+    p->st.truncate_own(ids[i], new_len[i], &copies);
+    for (const PoolState::OwnPage &c : copies) {
+      items.push_back(PageItem{c.slot, c.slot, 0u, (uint32_t)(new_len[i] % p->st.page_tokens()), c.from, c.to, 0u, 0u});
+      models.push_back(p->st.req(ids[i]).model);
+    }
+  }
+  for (int32_t i = 0; i < n; ++i) p->st.truncate(ids[i], new_len[i]);
+  return launch_page_items(p, items, models, (hipStream_t)hip_stream);
+}
+
 cp_status cp_request_len(cp_pool *p, int32_t req_id, int64_t *ctx_len) {
   if (!p || !ctx_len) return fail(CP_EINVAL, "null argument");
   if (!p->st.valid_open(req_id)) return fail(CP_EINVAL, "request %d is not open", req_id);
@@ -624,8 +746,10 @@ struct AppItem {
 };
 
 // Append launches for rows already accounted for in the host tables, in
-// groups of at most kMaxReqPerLaunch items and kMaxLaunchModels models.
-cp_status launch_appends(cp_pool *p, const std::vector<AppItem> &items, const void *rows, hipStream_t s) {
+// groups of at most kMaxReqPerLaunch items and kMaxLaunchModels models; with
+// keys rotated on the way where a rotation is given.
+cp_status launch_appends(cp_pool *p, const std::vector<AppItem> &items, const void *rows, hipStream_t s,
+                         const cp_rope *rope = nullptr) {
   const int32_t P = p->st.page_tokens();
   size_t i = 0;
   while (i < items.size()) {
@@ -665,19 +789,59 @@ cp_status launch_appends(cp_pool *p, const std::vector<AppItem> &items, const vo
     }
     a.n_blocks = (int32_t)blocks;
     if (a.n_req > 0) {
-      hipError_t e = launch_append(a, s);
+      hipError_t e = rope ? launch_append_rope(a, rope_k(*rope, false), s) : launch_append(a, s);
       if (e != hipSuccess) return hip_fail(e, "append launch");
     }
   }
   return CP_OK;
 }
 
-}  // namespace
+// Launches the page-table and partial-page copies of forks and truncations
+// already accounted for in the host tables.
+cp_status launch_page_items(cp_pool *p, const std::vector<PageItem> &items, const std::vector<int32_t> &models,
+                            hipStream_t s) {
+  if (p->host_only || items.empty()) return CP_OK;
+  DeviceGuard g(p->device);
+  size_t i = 0;
+  while (i < items.size()) {
+    PageCopyArgs a{};
+    a.pool = p->dev_pool;
+    a.pte = p->dev_pte;
+    int32_t nm = 0, model_map[16];
+    for (int k = 0; k < 16; ++k) model_map[k] = -1;
+    uint32_t blocks = 0;
+    for (; i < items.size() && a.n_items < kMaxPageItems; ++i) {
+      int32_t mi = model_map[models[i]];
+      if (mi < 0) {
+        if (nm == kMaxLaunchModels) break;
+        mi = model_map[models[i]] = nm;
+        a.geom[nm++] = geom_k(p->st.model(models[i]), p->st.page_tokens());
+      }
+      PageItem &it = a.item[a.n_items++];
+      it = items[i];
+      it.block_begin = blocks;
+      it.model = (uint32_t)mi;
+      const uint32_t segs = it.tail * ((uint32_t)a.geom[mi].row_elems / 8);
+      blocks += std::max({1u, (segs + kPageItemSegs - 1) / kPageItemSegs, (it.whole + kPageItemEntries - 1) / kPageItemEntries});
+    }
+    a.n_blocks = (int32_t)blocks;
+    const hipError_t e = launch_page_copy(a, s);
+    if (e != hipSuccess) return hip_fail(e, "page copy launch");
+  }
+  return CP_OK;
+}
 
-extern "C" {
+// A rotation fits a model's keys: the pool's device, and no wider than the
+// head (MLA: than the rope part).
+cp_status check_rope(const cp_pool *p, const Geom &g, const cp_rope *rope) {
+  if (rope->device != p->device) return fail(CP_EINVAL, "the rotation is on device %d, the pool on %d", rope->device, p->device);
+  const int32_t room = g.kind == kMLA ? g.rope : g.head_dim;
+  if (rope->rot > room) return fail(CP_EINVAL, "rotation of %d elements is wider than the %d of a key", rope->rot, room);
+  return CP_OK;
+}
 
-cp_status cp_kv_append(cp_pool *p, int32_t n, const int32_t *req_ids, const int32_t *n_new, const void *rows,
-                       void *hip_stream) {
+cp_status append_impl(cp_pool *p, int32_t n, const int32_t *req_ids, const int32_t *n_new, const void *rows,
+                      const cp_rope *rope, void *hip_stream) {
   if (!p) return fail(CP_EINVAL, "null pool");
   cp_status rc = check_ids(p, n, req_ids);
   if (rc) return rc;
@@ -698,6 +862,10 @@ cp_status cp_kv_append(cp_pool *p, int32_t n, const int32_t *req_ids, const int3
     if (!p->st.fits_reservation(req_ids[i], nl))
       return fail(CP_EINVAL, "request %d would grow to %lld tokens, past its reservation of %lld pages", req_ids[i],
                   (long long)nl, (long long)r.reserve_pages);
+    if (rope) {
+      rc = check_rope(p, p->st.model(r.model), rope);
+      if (rc) return rc;
+    }
     total += (int64_t)n_new[i] * r.layers;
   }
   if (p->host_only) {
@@ -746,7 +914,22 @@ cp_status cp_kv_append(cp_pool *p, int32_t n, const int32_t *req_ids, const int3
     if (rc) return rc;
     for (AppItem &it : items) it.n_ent = 0;
   }
-  return launch_appends(p, items, rows, s);
+  return launch_appends(p, items, rows, s, rope);
+}
+
+}  // namespace
+
+extern "C" {
+
+cp_status cp_kv_append(cp_pool *p, int32_t n, const int32_t *req_ids, const int32_t *n_new, const void *rows,
+                       void *hip_stream) {
+  return append_impl(p, n, req_ids, n_new, rows, nullptr, hip_stream);
+}
+
+cp_status cp_kv_append_rope(cp_pool *p, int32_t n, const int32_t *req_ids, const int32_t *n_new, const void *rows,
+                            const cp_rope *rope, void *hip_stream) {
+  if (!rope) return fail(CP_EINVAL, "null rope");
+  return append_impl(p, n, req_ids, n_new, rows, rope, hip_stream);
 }
 
 cp_status cp_kv_gather(cp_pool *p, int32_t req_id, int64_t start, int64_t n_tok, void *dst, void *hip_stream) {
@@ -1676,6 +1859,304 @@ cp_status cp_attn_decode_step(cp_pool *p, int32_t n, const int32_t *req_ids, con
   }
   advance_all();
   return CP_OK;
+}
+
+}  // extern "C"
+
+// ------------------------------------------------- attention of token chunks
+
+namespace {
+
+constexpr int64_t kMaxExtUnits = 1 << 23;  // of one launch
+
+// A planned cp_attn_extend: launches by kernel, with their requests.
+struct ExtPlan {
+  struct Launch {
+    int32_t kind = kXVec;
+    std::vector<ExtReq> req;
+    std::vector<int32_t> idx;  // of the call's requests
+    uint32_t units = 0;
+  };
+  int32_t model = -1;
+  Geom geom;
+  std::vector<Launch> launches;
+  uint64_t ws_rows = 0;  // partial rows of split requests
+};
+
+// The kernel of a request with n_q query tokens (extend.h).
+int32_t extend_kind(const Geom &g, int32_t path, int64_t n_q) {
+  if (path == CP_PATH_VALU) return kXVec;
+  if (g.kind == kGQA && (g.head_dim == 64 || g.head_dim == 128)) {
+    const bool few = n_q * g.g <= 32;
+    return g.head_dim == 64 ? (few ? kXFew64 : kXRows64) : (few ? kXFew128 : kXRows128);
+  }
+  return kXVec;
+}
+
+// Checks a call and plans it, at the contexts the requests will have with
+// extra[i] more tokens (NULL: none). Changes nothing.
+cp_status plan_extend(cp_pool *p, int32_t n, const int32_t *ids, const int32_t *n_q, const int32_t *extra,
+                      const void *q, const void *out, const float *lse, const cp_extend_opts &o, ExtPlan *pl) {
+  if (o.softcap < 0.f || !std::isfinite(o.softcap)) return fail(CP_EINVAL, "softcap must be finite and >= 0");
+  if (o.window < 0) return fail(CP_EINVAL, "window must be >= 0");
+  if (o.num_splits < 0) return fail(CP_EINVAL, "num_splits must be >= 0");
+  if (o.path != CP_PATH_AUTO && o.path != CP_PATH_VALU) return fail(CP_EINVAL, "path must be automatic or vector");
+  if (n < 1) return fail(CP_EINVAL, "attention needs at least one request");
+  int64_t total = 0;
+  for (int32_t i = 0; i < n; ++i) {
+    const Request &r = p->st.req(ids[i]);
+    if (i == 0) pl->model = r.model;
+    if (r.model != pl->model) return fail(CP_EINVAL, "the requests of a call belong to one model");
+    const int64_t ctx = r.attend_len() + (extra ? extra[i] : 0);
+    if (n_q[i] < 0 || n_q[i] > ctx)
+      return fail(CP_EINVAL, "request %d has a context of %lld tokens, not %d to ask for", ids[i], (long long)ctx, n_q[i]);
+    if (o.prefix && o.prefix[i] < 0) return fail(CP_EINVAL, "negative prefix for request %d", ids[i]);
+    total += n_q[i];
+  }
+  if (total > 0x7FFFFFFF) return fail(CP_EINVAL, "too many query tokens in one call");
+  if (total > 0 && (!q || !out || !lse)) return fail(CP_EINVAL, "null q, out or lse");
+  if ((uintptr_t)q % 16 || (uintptr_t)out % 8 || (uintptr_t)lse % 4 || (uintptr_t)o.slopes % 4 ||
+      (uintptr_t)o.doc_begin % 4)
+    return fail(CP_EINVAL, "q must be 16-byte aligned, out 8-byte, lse, slopes and doc_begin 4-byte");
+  pl->geom = p->st.model(pl->model);
+  const Geom &g = pl->geom;
+
+  // Steps (of ext_tile_keys keys) of each request's longest tile, and tiles.
+  struct Item {
+    int32_t kind;
+    int64_t tiles, steps;
+  };
+  std::vector<Item> it((size_t)n);
+  int64_t work[kXKinds] = {}, units[kXKinds] = {};
+  for (int32_t i = 0; i < n; ++i) {
+    const int64_t ctx = p->st.req(ids[i]).attend_len() + (extra ? extra[i] : 0);
+    Item &x = it[(size_t)i];
+    x.kind = extend_kind(g, o.path, n_q[i]);
+    const int64_t rows = ext_tile_rows(x.kind), keys = ext_tile_keys(x.kind);
+    x.tiles = ((int64_t)n_q[i] * g.g + rows - 1) / rows;
+    int64_t seen = ctx;
+    if (o.window) seen = std::min<int64_t>(ctx, (int64_t)o.window + std::min<int64_t>(n_q[i], rows / g.g + 2) +
+                                                    (o.prefix ? (int64_t)o.prefix[i] : 0));
+    x.steps = (seen + keys - 1) / keys + (o.window ? 1 : 0);
+    units[x.kind] += x.tiles * g.hkv;
+    work[x.kind] += x.tiles * g.hkv * x.steps;
+  }
+  // Ranges: enough units to fill the CUs twice, none shorter than min_steps.
+  int64_t total_units = 0, total_work = 0;
+  for (int k = 0; k < kXKinds; ++k) {
+    total_units += units[k];
+    total_work += work[k];
+  }
+  const int64_t slots = 2 * (int64_t)p->num_cus;
+  int64_t per = std::max<int64_t>(4, (total_work + slots - 1) / slots);
+  if (total_units >= slots) per = INT64_MAX;
+  std::vector<int64_t> splits((size_t)n, 1);
+  for (;;) {  // longer ranges until the partials fit the pool's cap
+    uint64_t o_floats = 0, l_floats = 0;
+    for (int32_t i = 0; i < n; ++i) {
+      const Item &x = it[(size_t)i];
+      int64_t s = per == INT64_MAX ? 1 : (x.steps + per - 1) / per;
+      if (o.num_splits > 0) s = std::min<int64_t>(o.num_splits, x.steps);
+      splits[(size_t)i] = std::max<int64_t>(1, std::min<int64_t>(s, 4096));
+      if (splits[(size_t)i] > 1) l_floats += ((uint64_t)n_q[i] * g.hq + 1) * (uint64_t)splits[(size_t)i];
+    }
+    o_floats = l_floats * (uint64_t)g.d_v;
+    if (!p->ws_limit || o.num_splits > 0 || l_floats == 0 || pool_ws_bytes(2 * o_floats, l_floats) <= p->ws_limit) break;
+    per = per > (1ll << 40) ? INT64_MAX : per * 2;
+  }
+  uint32_t tok0 = 0;
+  uint64_t ws_row = 0;
+  for (int32_t kind = 0; kind < kXKinds; ++kind) {
+    tok0 = 0;
+    for (int32_t i = 0; i < n; tok0 += (uint32_t)n_q[i], ++i) {
+      const Item &x = it[(size_t)i];
+      if (x.kind != kind || n_q[i] == 0) continue;
+      const int64_t u = x.tiles * g.hkv * splits[(size_t)i];
+      if (u > kMaxExtUnits) return fail(CP_EINVAL, "too many query rows of request %d in one call", ids[i]);
+      if (pl->launches.empty() || pl->launches.back().kind != kind ||
+          (int)pl->launches.back().req.size() == kMaxReqPerLaunch || pl->launches.back().units + u > kMaxExtUnits) {
+        pl->launches.emplace_back();
+        pl->launches.back().kind = kind;
+      }
+      ExtPlan::Launch &l = pl->launches.back();
+      const Request &r = p->st.req(ids[i]);
+      ExtReq e{};
+      e.unit_begin = l.units;
+      e.pte_base = r.plane_base(r.cursor);
+      e.ctx = (uint32_t)(r.attend_len() + (extra ? extra[i] : 0));
+      e.n_q = (uint32_t)n_q[i];
+      e.prefix = o.prefix ? (uint32_t)o.prefix[i] : 0u;
+      e.tok0 = tok0;
+      e.tiles = (uint32_t)x.tiles;
+      e.splits = (uint32_t)splits[(size_t)i];
+      if (e.splits > 1) {
+        // partial rows start at a multiple of the request's own ranges
+        e.ws_row = (ws_row + e.splits - 1) / e.splits;
+        ws_row = (e.ws_row + (uint64_t)n_q[i] * g.hq) * e.splits;
+      }
+      l.req.push_back(e);
+      l.idx.push_back(i);
+      l.units += (uint32_t)u;
+    }
+  }
+  pl->ws_rows = ws_row;
+  return CP_OK;
+}
+
+cp_status run_extend(cp_pool *p, const ExtPlan &pl, const void *q, void *out, float *lse, const cp_extend_opts &o,
+                     hipStream_t s) {
+  const Geom &g = pl.geom;
+  const int32_t P = p->st.page_tokens();
+  for (const ExtPlan::Launch &l : pl.launches) {
+    ExtArgs a{};
+    a.pool = p->dev_pool;
+    a.pte = p->dev_pte;
+    a.q = (const uint16_t *)q;
+    a.out = (uint16_t *)out;
+    a.lse = lse;
+    a.ws_o = (float *)p->ws_o;
+    a.ws_l = p->ws_l;
+    a.slopes = o.slopes;
+    a.doc_begin = o.doc_begin;
+    a.softcap = o.softcap;
+    a.scale = g.scale;
+    a.window = (uint32_t)o.window;
+    a.page_magic = page_magic(P);
+    a.n_req = (int32_t)l.req.size();
+    a.n_units = (int32_t)l.units;
+    a.g = geom_k(g, P);
+    std::copy(l.req.begin(), l.req.end(), a.req);
+    hipError_t e = launch_extend(a, l.kind, s);
+    if (e != hipSuccess) return hip_fail(e, "extend launch");
+    ExtMergeArgs m{};
+    m.ws_o = a.ws_o;
+    m.ws_l = a.ws_l;
+    m.out = a.out;
+    m.lse = lse;
+    m.hq = g.hq;
+    m.d_v = g.d_v;
+    uint32_t rows = 0;
+    for (const ExtReq &r : l.req) {
+      if (r.splits < 2) continue;
+      ExtMergeArgs::Req &x = m.req[m.n_req++];
+      x.row_begin = rows;
+      x.rows = r.n_q * (uint32_t)g.hq;
+      x.ws_row = r.ws_row;
+      x.out_row = (uint64_t)r.tok0 * (uint32_t)g.hq;
+      x.splits = r.splits;
+      rows += x.rows;
+    }
+    e = launch_ext_merge(m, rows, s);
+    if (e != hipSuccess) return hip_fail(e, "extend join launch");
+  }
+  return CP_OK;
+}
+
+cp_status bind_extend_workspace(cp_pool *p, const ExtPlan &pl) {
+  if (pl.ws_rows == 0) return CP_OK;
+  return ensure_ws(p, 2 * pl.ws_rows * (uint64_t)pl.geom.d_v, pl.ws_rows);  // fp32 in bf16 elements
+}
+
+}  // namespace
+
+extern "C" {
+
+cp_status cp_attn_extend(cp_pool *p, int32_t n, const int32_t *req_ids, const int32_t *n_q, const void *q, void *out,
+                         float *lse, void *hip_stream, const cp_extend_opts *opts) {
+  if (!p) return fail(CP_EINVAL, "null pool");
+  if (p->host_only) return fail(CP_ESTATE, "host-only pool cannot attend");
+  if (p->broken) return fail(CP_ESTATE, "a failed decode step left the device page stacks out of step; destroy the pool");
+  cp_status rc = check_ids(p, n, req_ids);
+  if (rc) return rc;
+  if (n > 0 && !n_q) return fail(CP_EINVAL, "null n_q");
+  cp_extend_opts o{};
+  if (opts) o = *opts;
+  if (o.rope) return fail(CP_EINVAL, "cp_attn_extend places no rows: opts.rope must be NULL");
+  ExtPlan pl;
+  rc = plan_extend(p, n, req_ids, n_q, nullptr, q, out, lse, o, &pl);
+  if (rc) return rc;
+  DeviceGuard g(p->device);
+  rc = bind_extend_workspace(p, pl);
+  if (rc) return rc;
+  return run_extend(p, pl, q, out, lse, o, (hipStream_t)hip_stream);
+}
+
+cp_status cp_attn_extend_step(cp_pool *p, int32_t n, const int32_t *req_ids, const int32_t *n_new, const void *rows,
+                              const void *q, void *out, float *lse, void *hip_stream, const cp_extend_opts *opts) {
+  if (!p) return fail(CP_EINVAL, "null pool");
+  if (p->host_only) return fail(CP_ESTATE, "host-only pool cannot attend");
+  if (p->broken) return fail(CP_ESTATE, "a failed decode step left the device page stacks out of step; destroy the pool");
+  cp_status rc = check_ids(p, n, req_ids);
+  if (rc) return rc;
+  if (n > 0 && !n_new) return fail(CP_EINVAL, "null n_new");
+  cp_extend_opts o{};
+  if (opts) o = *opts;
+  bool any = false;
+  std::vector<int32_t> placing((size_t)n, 0);
+  for (int32_t i = 0; i < n; ++i) {
+    const Request &r = p->st.req(req_ids[i]);
+    if (n_new[i] < 0) return fail(CP_EINVAL, "negative n_new for request %d", req_ids[i]);
+    if (r.cursor == 0) {
+      if (r.ctx_len + n_new[i] > 0xFFFFFFF0ll) return fail(CP_EINVAL, "context length overflow");
+      if (!p->st.fits_reservation(req_ids[i], r.ctx_len + n_new[i]))
+        return fail(CP_EINVAL, "request %d would grow past its reservation of %lld pages", req_ids[i],
+                    (long long)r.reserve_pages);
+      placing[(size_t)i] = n_new[i];
+    } else if (n_new[i] != r.inflight) {
+      return fail(CP_EINVAL, "request %d is at layer %d of %d with %d tokens in flight: n_new must be that", req_ids[i],
+                  r.cursor, r.layers, r.inflight);
+    }
+    if (o.rope) {
+      rc = check_rope(p, p->st.model(r.model), o.rope);
+      if (rc) return rc;
+    }
+    any = any || n_new[i] > 0;
+  }
+  if (any && !rows) return fail(CP_EINVAL, "null rows");
+  ExtPlan pl;
+  rc = plan_extend(p, n, req_ids, n_new, placing.data(), q, out, lse, o, &pl);
+  if (rc) return rc;
+  DeviceGuard g(p->device);
+  rc = bind_extend_workspace(p, pl);
+  if (rc) return rc;
+  rc = reconcile_pages(p);  // the page-table copies below must not overwrite popped entries
+  if (rc) return rc;
+  rc = prepare_growth(p, n, req_ids, placing.data());
+  if (rc) return rc;
+
+  // Pages of every plane are taken at the first layer; the entries of the
+  // current plane travel with the append launch where they fit, those of the
+  // other planes by a copy.
+  hipStream_t s = (hipStream_t)hip_stream;
+  const uint64_t row_elems = (uint64_t)pl.geom.row_elems;
+  std::vector<AppItem> items;
+  uint64_t src = 0, lo = UINT64_MAX, hi = 0, entries = 0;
+  bool other_planes = false;
+  for (int32_t i = 0; i < n; ++i) {
+    const Request &r = p->st.req(req_ids[i]);
+    const int64_t used = r.pages_used;
+    uint64_t first = 0, count = 0;
+    if (placing[(size_t)i] > 0) p->st.begin_chunk(req_ids[i], n_new[i], &first, &count);
+    if (count) {
+      lo = std::min(lo, first);
+      hi = std::max(hi, first + count);
+      other_planes = other_planes || r.layers > 1;
+    }
+    if (n_new[i] > 0) {
+      items.push_back(AppItem{r.model, (uint32_t)n_new[i], (uint32_t)r.ctx_len, r.plane_base(r.cursor), src,
+                              r.plane_base(r.cursor) + (uint64_t)used, (uint32_t)(r.pages_used - used)});
+      entries += (uint64_t)(r.pages_used - used);
+      src += (uint64_t)n_new[i] * row_elems;
+    }
+  }
+  if (other_planes || entries > (uint64_t)kAppEntMax) {
+    rc = push_ptes(p, lo, hi, s);
+    for (AppItem &x : items) x.n_ent = 0;
+  }
+  if (rc == CP_OK) rc = launch_appends(p, items, rows, s, o.rope);
+  if (rc == CP_OK) rc = run_extend(p, pl, q, out, lse, o, s);
+  for (int32_t i = 0; i < n; ++i) p->st.advance(req_ids[i]);
+  return rc;
 }
 
 }  // extern "C"

@@ -1,0 +1,74 @@
+// Attention of token chunks (cp_attn_extend): launch records shared by the
+// host planner (api.cpp) and the kernels (extend_kernels.hip), and the device
+// helpers of those kernels.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "kargs.h"
+
+namespace cp {
+
+// Kernels, chosen per call by the model's geometry and its rows per KV head.
+//   kXVec    vector: one wave per row, any geometry.
+//   kXRows*  matrix cores, GQA / MHA of head_dim 64 or 128: tiles of 128 rows.
+//   kXFew*   the same with 32 rows, the four waves taking keys in turn.
+enum : int32_t { kXVec = 0, kXRows64, kXRows128, kXFew64, kXFew128, kXKinds };
+
+constexpr int kExtThreads = 256;
+// Rows (a token and a query head of one KV head) of a tile, and keys of one
+// step, of each kernel.
+constexpr int32_t ext_tile_rows(int32_t kind) { return kind == kXVec ? 4 : kind <= kXRows128 ? 128 : 32; }
+constexpr int32_t ext_tile_keys(int32_t kind) { return kind == kXVec || kind <= kXRows128 ? 64 : 128; }
+
+struct ExtReq {
+  uint32_t unit_begin;  // first work unit of the request
+  uint32_t pte_base;    // page-table entries of the plane
+  uint32_t ctx, n_q;    // context, and how many of its last tokens ask
+  uint32_t prefix;
+  uint32_t tok0;        // its first query token in the call's arrays
+  uint32_t tiles;       // row tiles per KV head
+  uint32_t splits;      // key ranges per tile
+  uint64_t ws_row;      // first partial row (splits > 1)
+};
+
+struct ExtArgs {
+  const uint8_t *pool;
+  const uint32_t *pte;
+  const uint16_t *q;
+  uint16_t *out;
+  float *lse;
+  float *ws_o;  // partial outputs, normalised: [row][split][d_v]
+  float *ws_l;  // partial log-sum-exp (base 2): [row][split]
+  const float *slopes;
+  const int32_t *doc_begin;
+  float softcap, scale;
+  uint32_t window;
+  uint32_t page_magic;  // page_divide
+  int32_t n_req, n_units;
+  GeomK g;
+  ExtReq req[kMaxReqPerLaunch];
+};
+static_assert(sizeof(ExtArgs) <= 3776, "extend kernel arguments too large");
+
+struct ExtMergeArgs {
+  const float *ws_o, *ws_l;
+  uint16_t *out;
+  float *lse;
+  int32_t n_req, hq, d_v, pad;
+  struct Req {
+    uint32_t row_begin, rows;  // rows of the launch before, and of, the request
+    uint64_t ws_row;
+    uint64_t out_row;
+    uint32_t splits, pad;
+  } req[kMaxReqPerLaunch];
+};
+static_assert(sizeof(ExtMergeArgs) <= 3072, "extend merge arguments too large");
+
+// floor(2^32 / P), for page_divide on the device.
+inline uint32_t page_magic(int32_t page_tokens) {
+  return page_tokens == 1 ? 0xFFFFFFFFu : (uint32_t)((1ull << 32) / (uint32_t)page_tokens);
+}
+
+}  // namespace cp

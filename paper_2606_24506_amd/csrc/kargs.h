@@ -208,6 +208,28 @@ struct GatherArgs {
   GeomK geom;
 };
 
+// Page-table entries and partial pages of forked and truncated requests. An
+// item is one KV plane of a request: `whole` entries copied from another
+// plane's, and the first `tail` tokens of page `from` copied to page `to`,
+// whose entry (index `whole` of the plane) is written.
+struct PageItem {
+  uint32_t src_base, dst_base;  // first page-table entries of the planes
+  uint32_t whole, tail;
+  uint32_t from, to;
+  uint32_t block_begin;
+  uint32_t model;  // index into PageCopyArgs::geom
+};
+constexpr int kMaxPageItems = 64;
+constexpr uint32_t kPageItemSegs = 1024;     // 16-byte segments one workgroup copies
+constexpr uint32_t kPageItemEntries = 4096;  // ... and page-table entries
+struct PageCopyArgs {
+  uint8_t *pool;
+  uint32_t *pte;
+  int32_t n_items, n_blocks;
+  GeomK geom[kMaxLaunchModels];
+  PageItem item[kMaxPageItems];
+};
+
 // Refill of a device page stack: n entries written at dst[0..n), then the
 // model's count set to new_top. The entries travel in the arguments, so the
 // host keeps no staging copy alive.
@@ -225,5 +247,6 @@ static_assert(sizeof(StackPushArgs) <= 3072, "stack push arguments too large");
 static_assert(sizeof(DecodeArgs) <= 3776, "decode kernel arguments too large");
 static_assert(sizeof(MergeArgs) <= 3072, "merge kernel arguments too large");
 static_assert(sizeof(AppendArgs) <= 3776, "append kernel arguments too large");
+static_assert(sizeof(PageCopyArgs) <= 3072, "page copy arguments too large");
 
 }  // namespace cp

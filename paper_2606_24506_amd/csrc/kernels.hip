@@ -185,6 +185,44 @@ hipError_t launch_gather(const GatherArgs &a, hipStream_t stream) {
   return hipGetLastError();
 }
 
+// ----------------------------------------------- forks and truncations
+
+// Block b of an item copies the b-th part of its entries and of its partial
+// page's segments. Bound by the launch and one page's latency: a fork moves at most
+// one page per KV plane, whatever the context.
+__global__ __launch_bounds__(kCopyThreads) void page_copy_kernel(const PageCopyArgs a) {
+  const int r = sorted_search(a.n_items, blockIdx.x, [&](int i) { return a.item[i].block_begin; });
+  const PageItem &it = a.item[r];
+  const GeomK &g = a.geom[it.model];
+  const uint32_t b = blockIdx.x - it.block_begin;
+  const uint32_t e1 = min(it.whole, (b + 1) * kPageItemEntries);
+  for (uint32_t i = b * kPageItemEntries + threadIdx.x; i < e1; i += kCopyThreads)
+    a.pte[it.dst_base + i] = a.pte[it.src_base + i];
+  if (it.tail == 0) return;
+  if (b == 0 && threadIdx.x == 0) a.pte[it.dst_base + it.whole] = it.to;
+  const uint32_t nseg = (uint32_t)g.row_elems / 8, s1 = min(it.tail * nseg, (b + 1) * kPageItemSegs);
+  const uint8_t *const from = a.pool + ((uint64_t)it.from << 8);
+  uint8_t *const to = a.pool + ((uint64_t)it.to << 8);
+  constexpr int kEach = kPageItemSegs / kCopyThreads;
+  u32x4c x[kEach];
+  uint64_t at[kEach];
+#pragma unroll
+  for (int u = 0; u < kEach; ++u) {
+    const uint32_t i = b * kPageItemSegs + threadIdx.x + kCopyThreads * u, row = i / nseg;
+    at[u] = i < s1 ? row_seg_offset(g, row, i - row * nseg) : 0;
+    if (i < s1) x[u] = *reinterpret_cast<const u32x4c *>(from + at[u]);
+  }
+#pragma unroll
+  for (int u = 0; u < kEach; ++u)
+    if (b * kPageItemSegs + threadIdx.x + kCopyThreads * u < s1) *reinterpret_cast<u32x4c *>(to + at[u]) = x[u];
+}
+
+hipError_t launch_page_copy(const PageCopyArgs &a, hipStream_t stream) {
+  if (a.n_blocks <= 0) return hipSuccess;
+  hipLaunchKernelGGL(page_copy_kernel, dim3(a.n_blocks), dim3(kCopyThreads), 0, stream, a);
+  return hipGetLastError();
+}
+
 // ------------------------------------------------- decode: vector path
 
 typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));

@@ -3,6 +3,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <unordered_map>
 
 namespace cp {
 
@@ -234,9 +235,10 @@ int PoolState::open(int32_t model, int64_t reserve_tokens, int32_t *id, std::str
 void PoolState::close(int32_t id) {
   Request &r = reqs_[id];
   const int32_t model = r.model;
-  for (int32_t l = 0; l < r.layers; ++l)
-    free_pages(pte_.data() + r.plane_base(l), r.pages_used);
-  acct_[model].reserved -= r.reserve_pages;
+  int64_t freed = 0;
+  for (int32_t l = 0; l < r.layers; ++l) freed += free_pages(pte_.data() + r.plane_base(l), r.pages_used);
+  // pages that other requests still show stay counted
+  acct_[model].reserved -= freed + r.reserve_pages - r.pages_used * r.layers;
   pte_ranges_.release(r.pte_base, (uint64_t)r.reserve_pages);
   r = Request{};
   free_ids_.push_back(id);
@@ -271,9 +273,13 @@ void PoolState::grow(int32_t id, int64_t new_len, uint64_t *first, uint64_t *cou
 }
 
 void PoolState::begin_token(int32_t id, uint64_t *first, uint64_t *count) {
+  begin_chunk(id, 1, first, count);
+}
+
+void PoolState::begin_chunk(int32_t id, int32_t n, uint64_t *first, uint64_t *count) {
   Request &r = reqs_[id];
-  grow_planes(r, r.ctx_len + 1, first, count);
-  r.inflight = 1;
+  grow_planes(r, r.ctx_len + n, first, count);
+  r.inflight = n;
 }
 
 void PoolState::take_pages(int32_t model, int64_t k, std::vector<uint32_t> *out) {
@@ -359,6 +365,7 @@ void PoolState::uncarve(int32_t c) {
   a.held -= 1;
   ch.model = -1;
   ch.bits.clear();
+  ch.more.clear();
   give_chunk(c);
 }
 
@@ -446,8 +453,9 @@ void PoolState::alloc_pages(int32_t model, int64_t k, uint32_t *out) {
   }
 }
 
-void PoolState::free_pages(const uint32_t *ptes, int64_t n) {
+int64_t PoolState::free_pages(const uint32_t *ptes, int64_t n) {
   const uint64_t chunk256 = chunk_bytes_ >> 8;
+  int64_t total = 0;
   for (int64_t i = 0; i < n;) {
     // the pages from i on that lie in one chunk
     const int32_t c = (int32_t)(ptes[i] / chunk256);
@@ -456,20 +464,113 @@ void PoolState::free_pages(const uint32_t *ptes, int64_t n) {
     ModelAcct &a = acct_[ch.model];
     const uint32_t page256 = (uint32_t)((uint64_t)models_[ch.model].page_bytes >> 8);
     int64_t j = i;
+    int32_t freed = 0;
     for (; j < n && ptes[j] >= lo && ptes[j] - lo < chunk256; ++j) {
       const uint32_t slot = (uint32_t)(ptes[j] - lo) / page256;
+      if (!ch.more.empty() && ch.more[slot]) {
+        ch.more[slot] -= 1;
+        continue;
+      }
       ch.bits[slot >> 6] |= 1ull << (slot & 63);
+      freed += 1;
     }
-    const int32_t freed = (int32_t)(j - i);
     ch.used -= freed;
     a.used -= freed;
+    total += freed;
     if (ch.used == 0 && !virt_) {
       uncarve(c);
-    } else {
+    } else if (freed) {
       a.partial[c] += freed;  // a virtual pool's empty chunks wait for trim
     }
     i = j;
   }
+  return total;
+}
+
+uint32_t PoolState::sharers(uint32_t pte) const {
+  const uint64_t chunk256 = chunk_bytes_ >> 8;
+  const Chunk &ch = chunks_[(size_t)(pte / chunk256)];
+  if (ch.more.empty()) return 0;
+  return ch.more[(size_t)((pte % chunk256) / ((uint64_t)models_[ch.model].page_bytes >> 8))];
+}
+
+void PoolState::fork(int32_t src, int32_t dst, int64_t n_tok) {
+  const Request &s = reqs_[src];
+  Request &d = reqs_[dst];
+  const Geom &g = models_[d.model];
+  const uint64_t chunk256 = chunk_bytes_ >> 8, page256 = (uint64_t)g.page_bytes >> 8;
+  const int64_t whole = n_tok / P_, tail = n_tok % P_ ? 1 : 0;
+  for (int32_t l = 0; l < d.layers; ++l) {
+    const uint32_t *from = pte_.data() + s.plane_base(l);
+    uint32_t *to = pte_.data() + d.plane_base(l);
+    for (int64_t i = 0; i < whole; ++i) {
+      Chunk &ch = chunks_[(size_t)(from[i] / chunk256)];
+      if (ch.more.empty()) ch.more.assign((size_t)g.ppc, 0u);
+      ch.more[(size_t)(from[i] % chunk256 / page256)] += 1;
+      to[i] = from[i];
+    }
+    if (tail) alloc_pages(d.model, 1, to + whole);
+  }
+  d.pages_used = whole + tail;
+  d.ctx_len = n_tok;
+  acct_[d.model].reserved -= whole * d.layers;
+}
+
+void PoolState::truncate_own(int32_t id, int64_t new_len, std::vector<OwnPage> *copies) {
+  const Request &r = reqs_[id];
+  if (new_len % P_ == 0) return;
+  for (int32_t l = 0; l < r.layers; ++l) {
+    const uint32_t slot = r.plane_base(l) + (uint32_t)(new_len / P_), old = pte_[slot];
+    if (!sharers(old)) continue;
+    alloc_pages(r.model, 1, &pte_[slot]);
+    free_pages(&old, 1);  // takes this user from it; others remain
+    acct_[r.model].reserved += 1;
+    copies->push_back(OwnPage{slot, old, pte_[slot]});
+  }
+}
+
+void PoolState::truncate(int32_t id, int64_t new_len) {
+  Request &r = reqs_[id];
+  const int64_t keep = ceil_div(new_len, P_), drop = r.pages_used - keep;
+  for (int32_t l = 0; l < r.layers; ++l)
+    acct_[r.model].reserved += drop - free_pages(pte_.data() + r.plane_base(l) + keep, drop);
+  r.pages_used = keep;
+  r.ctx_len = new_len;
+}
+
+void PoolState::truncate_cost(int32_t n, const int32_t *ids, const int64_t *new_len, std::vector<int64_t> *reserved,
+                              std::vector<int64_t> *pages) const {
+  reserved->assign(models_.size(), 0);
+  pages->assign(models_.size(), 0);
+  std::unordered_map<uint32_t, uint32_t> given;  // users taken from shared pages so far
+  auto give_shared = [&](uint32_t pte) {
+    const uint32_t k = sharers(pte);
+    return k > 0 && given[pte]++ < k;
+  };
+  for (int pass = 0; pass < 2; ++pass)  // the two passes of a truncation
+    for (int32_t i = 0; i < n; ++i) {
+      const Request &r = reqs_[ids[i]];
+      const int64_t keep = ceil_div(new_len[i], P_);
+      for (int32_t l = 0; l < r.layers; ++l) {
+        const uint32_t *pt = pte_.data() + r.plane_base(l);
+        if (pass == 0 && new_len[i] % P_ && give_shared(pt[keep - 1])) {
+          (*reserved)[(size_t)r.model] += 1;
+          (*pages)[(size_t)r.model] += 1;
+        }
+        for (int64_t k = keep; pass == 1 && k < r.pages_used; ++k)
+          (*reserved)[(size_t)r.model] += give_shared(pt[k]) ? 1 : 0;
+      }
+    }
+}
+
+bool PoolState::fits_budget(const std::vector<int64_t> &extra) const {
+  uint64_t total = 0;
+  for (size_t m = 0; m < models_.size(); ++m) {
+    const ModelAcct &a = acct_[m];
+    const int64_t owed = a.reserved + extra[m] - a.held * models_[m].ppc;
+    total += (uint64_t)a.held + (owed > 0 ? (uint64_t)ceil_div(owed, models_[m].ppc) : 0);
+  }
+  return total <= n_chunks_;
 }
 
 void PoolState::trim(int32_t model) {

@@ -147,6 +147,8 @@ class PoolState {
   // needed) without committing it: the request's layers then see it one
   // decode step at a time. Requires cursor 0 and no token in flight.
   void begin_token(int32_t id, uint64_t *first, uint64_t *count);
+  // The same for a chunk of n >= 0 tokens.
+  void begin_chunk(int32_t id, int32_t n, uint64_t *first, uint64_t *count);
   // After a decode step at the request's cursor: moves to the next layer;
   // past the last one, commits the token in flight.
   void advance(int32_t id);
@@ -180,6 +182,42 @@ class PoolState {
   // kPendingPte in the mirror until read back. Appends the entries' slots.
   void begin_token_popped(int32_t id, std::vector<uint64_t> *slots);
 
+  // Forking and truncating. A page may have several users: requests that show
+  // it through their page tables. It is allocated once, written by nobody
+  // while shared (a request writes only the page its last token is in, which
+  // fork and truncate keep its own) and freed by its last user. An account's
+  // `reserved` is its allocated pages outside the device stack plus what every
+  // open request may still allocate (reserve_pages less the entries it uses),
+  // so a shared page counts once.
+  //
+  // Makes the empty request dst show the first n_tok tokens of src: whole
+  // pages shared, a page for the rest of its own in every plane (after
+  // ensure_slots).
+  void fork(int32_t src, int32_t dst, int64_t n_tok);
+  // Truncation of requests, in two passes over all of a call's, so that no
+  // page freed by one is another's copy while the launch still reads it.
+  // First: where the new end lies inside a shared page, that page is replaced
+  // by one of the request's own (after ensure_slots); appends one record per
+  // plane. Then: the length is set and the pages behind it given up.
+  struct OwnPage {
+    uint32_t slot;      // the page-table entry
+    uint32_t from, to;  // its old and its new page
+  };
+  void truncate_own(int32_t id, int64_t new_len, std::vector<OwnPage> *copies);
+  void truncate(int32_t id, int64_t new_len);
+  // What truncating these requests adds to each model's `reserved`, and the
+  // pages of its own it allocates for shared ones.
+  void truncate_cost(int32_t n, const int32_t *ids, const int64_t *new_len, std::vector<int64_t> *reserved,
+                     std::vector<int64_t> *pages) const;
+  // Would the budget hold every reservation with these additions (per model)?
+  bool fits_budget(const std::vector<int64_t> &extra) const;
+  // Users of a page beyond its first.
+  uint32_t sharers(uint32_t pte) const;
+  // What open requests of the model may still allocate.
+  int64_t room_to_grow(int32_t model) const { return acct_[model].reserved - acct_[model].used + acct_[model].in_stack; }
+  int64_t reserved(int32_t model) const { return acct_[model].reserved; }
+  int64_t allocated(int32_t model) const { return acct_[model].used; }
+
   const uint32_t *pte_mirror() const { return pte_.data(); }
   uint32_t *pte_mirror_mut() { return pte_.data(); }
 
@@ -195,9 +233,10 @@ class PoolState {
     int32_t model = -1;
     int32_t used = 0;
     std::vector<uint64_t> bits;  // free-slot bitmap while carved
+    std::vector<uint32_t> more;  // per slot, users beyond the first (empty until a page is shared)
   };
   struct ModelAcct {
-    int64_t reserved = 0;   // pages promised to open requests
+    int64_t reserved = 0;   // pages promised to open requests (shared ones once)
     int64_t used = 0;       // pages holding KV
     int64_t held = 0;       // chunks carved for this model
     int64_t in_stack = 0;   // allocated pages held by the model's device stack
@@ -219,8 +258,9 @@ class PoolState {
   // append of 212 pages took 5.0 us with a map update for each page, 3.4
   // now).
   void alloc_pages(int32_t model, int64_t k, uint32_t *out);
-  // Frees pages in order (a chunk goes back when its last page does).
-  void free_pages(const uint32_t *ptes, int64_t n);
+  // Takes a user from pages in order; those without another are freed (a
+  // chunk goes back when its last page does). Returns how many were.
+  int64_t free_pages(const uint32_t *ptes, int64_t n);
   void grow_planes(Request &r, int64_t new_len, uint64_t *first, uint64_t *count);
 
   int32_t P_ = 64;

@@ -1,0 +1,202 @@
+"""Rotary positions against the 64-bit form: layouts, widths, partial
+rotations, strides and alignments, types, scalings, far and negative
+positions, in place and out of place, the inverse; and appends that rotate
+keys on the way into the pool."""
+import math
+
+import pytest
+import torch
+
+from paper_2606_24506_amd import crosspool as cpl
+from prompt_ref import GEOMS, Scene, bits, shape, turn, turn_rows
+
+pytestmark = pytest.mark.gpu
+
+
+def allowed(ref, mag, dtype):
+    """Half a step of the result's type, and what 32 bits lose of the pair's length:
+    sine, cosine, two products and a sum, 2^-24 each (sine and cosine are
+    good to 4 of those)."""
+    half = {torch.bfloat16: 2.0 ** -8, torch.float32: 2.0 ** -24}[dtype]
+    return half * ref.abs() + 12 * 2.0 ** -24 * mag + 1e-30
+
+
+def pair_length(x, layout):
+    x = x.double().cpu()
+    h = x.shape[-1] // 2
+    if layout == "half":
+        m = torch.sqrt(x[..., :h] ** 2 + x[..., h:] ** 2)
+        return torch.cat([m, m], -1)
+    return torch.sqrt(x[..., 0::2] ** 2 + x[..., 1::2] ** 2).repeat_interleave(2, -1)
+
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("tokens,heads,width,rot,offset", [
+    (1, 1, 2, 2, 0), (1, 32, 128, 128, 0), (3, 5, 64, 64, 0), (700, 3, 128, 64, 0), (65, 2, 576, 64, 512),
+    (17, 3, 100, 36, 10), (9, 4, 24, 24, 0), (5, 2, 1024, 1024, 0), (33, 7, 80, 16, 32), (2, 300, 64, 32, 0),
+])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_shapes(layout, dtype, tokens, heads, width, rot, offset, in_place):
+    print(f"[case] rope {layout} {dtype} {tokens}x{heads}x{width} rot {rot} at {offset} in place {in_place}", flush=True)
+    gen = torch.Generator(device="cuda").manual_seed(tokens)
+    x = torch.empty(tokens, heads, width, dtype=dtype, device="cuda").normal_(generator=gen)
+    pos = torch.randint(-5000, 200000, (tokens,), generator=gen, device="cuda", dtype=torch.int32)
+    rope = cpl.Rope(rot, layout=layout, magnitude=1.25)
+    want = x.double().cpu().clone()
+    want[..., offset:offset + rot] = turn(x[..., offset:offset + rot], rope.angles(), pos, layout, 1.25)
+    mag = torch.zeros_like(want)
+    mag[..., offset:offset + rot] = 1.25 * pair_length(x[..., offset:offset + rot], layout)
+    dst = x.clone() if in_place else torch.full_like(x, 9.0)
+    rope.apply(cpl.rope_parts([(dst if in_place else x, dst)], offset=offset), pos)
+    torch.cuda.synchronize()
+    got = dst.double().cpu()
+    assert ((got - want).abs() <= allowed(want, mag, dtype)).all(), ((got - want).abs() / allowed(want, mag, dtype)).max()
+    keep = torch.ones(width, dtype=torch.bool)
+    keep[offset:offset + rot] = False
+    assert torch.equal(got[..., keep], x.double().cpu()[..., keep])
+    rope.destroy()
+
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("shift", [0, 1, 4])
+def test_strided_views_of_one_launch(layout, shift):
+    """Head-major tensors, views into wider rows, elements off 16 bytes, several
+    tensors at once; what lies between the rows stays."""
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    T = 40
+    wide = torch.empty(T, 6, 160, dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    major = torch.empty(3, T, 64, dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    out1 = torch.full((T, 4, 96), 5.0, dtype=torch.bfloat16, device="cuda")
+    out2 = torch.full((3, T, 64), 5.0, dtype=torch.bfloat16, device="cuda")
+    src1, dst1 = wide[:, 1:5, shift:shift + 64], out1[:, :, 8 + shift:72 + shift]
+    src2, dst2 = major.transpose(0, 1), out2.transpose(0, 1)
+    rope = cpl.Rope(64, layout=layout)
+    rope.apply(cpl.rope_parts([(src1, dst1), (src2, dst2)]), first=77777)
+    torch.cuda.synchronize()
+    pos = torch.arange(77777, 77777 + T)
+    for s, d in ((src1, dst1), (src2, dst2)):
+        want = turn(s, rope.angles(), pos, layout)
+        assert ((d.double().cpu() - want).abs() <= allowed(want, pair_length(s, layout), torch.bfloat16)).all()
+    assert (out1[..., :8 + shift] == 5).all() and (out1[..., 72 + shift:] == 5).all()
+    rope.destroy()
+
+
+@pytest.mark.parametrize("scaling", ["none", "linear", "ntk", "parts", "table"])
+def test_far_positions_of_every_scaling(scaling):
+    """Positions up to 2^31 - 1: the angle is reduced in 64 bits (its product
+    is good to 2^31 2^-53 of a turn)."""
+    rot = 64
+    kw = dict(factor=8.0, orig_len=4096) if scaling != "none" else {}
+    if scaling == "table":
+        kw["table"] = [1.0 / (1 + i) for i in range(rot // 2)]
+    rope = cpl.Rope(rot, layout="half", scaling=scaling, **kw)
+    ang = rope.angles()
+    i = torch.arange(rot // 2, dtype=torch.float64)
+    f = 10000.0 ** (-2 * i / rot)
+    if scaling == "linear":
+        f = f / 8
+    elif scaling == "ntk":
+        f = (10000.0 * 8 ** (rot / (rot - 2))) ** (-2 * i / rot)
+    elif scaling == "parts":
+        r = 4096 * f / (2 * math.pi)
+        w = ((r - 1) / 31).clamp(0, 1)
+        f = f * w + f / 8 * (1 - w)
+    elif scaling == "table":
+        f = 1 / (1 + i)
+    assert torch.allclose(torch.as_tensor(ang), f, rtol=1e-14, atol=0)
+    pos = torch.tensor([0, 1, -1, 4095, 1 << 20, (1 << 31) - 1, -(1 << 31)], dtype=torch.int32, device="cuda")
+    x = torch.ones(len(pos), 2, rot, device="cuda")
+    y = torch.zeros_like(x)
+    rope.apply(cpl.rope_parts([(x, y)]), pos)
+    torch.cuda.synchronize()
+    want = turn(x, ang, pos, "half")
+    # 32-bit arithmetic, and 2^31 turns held to 2^-53 on either side (2 pi 2^-21 in the worst case)
+    slack = 2 * math.pi * pos.double().cpu().abs()[:, None, None] * 2.0 ** -51
+    assert ((y.double().cpu() - want).abs() <= 16 * 2.0 ** -24 * math.sqrt(2) + slack).all()
+    rope.destroy()
+
+
+def test_inverse_and_gradient():
+    """The inverse undoes the rotation, and is the gradient of it."""
+    rope = cpl.Rope(32, layout="interleaved")
+    x = torch.randn(50, 3, 48, device="cuda")
+    y, z = torch.zeros_like(x), torch.zeros_like(x)
+    rope.apply(cpl.rope_parts([(x, y)], offset=8), first=1000)
+    rope.apply(cpl.rope_parts([(y, z)], offset=8), first=1000, inverse=True)
+    torch.cuda.synchronize()
+    assert torch.allclose(x, z, atol=1e-5)
+    # <w, R x> differentiated in x is the inverse applied to w
+    w = torch.randn_like(x)
+    g = torch.zeros_like(x)
+    rope.apply(cpl.rope_parts([(w, g)], offset=8), first=1000, inverse=True)
+    torch.cuda.synchronize()
+    dx = torch.randn_like(x)
+    moved, y2 = x + dx, torch.zeros_like(x)  # (the rotation is linear: a difference is exact)
+    rope.apply(cpl.rope_parts([(moved, y2)], offset=8), first=1000)
+    torch.cuda.synchronize()
+    lhs = (w.double() * (y2.double() - y.double())).sum()
+    rhs = (g.double() * (moved.double() - x.double())).sum()
+    assert abs(lhs - rhs) <= 1e-5 * (w.double().norm() * dx.double().norm())
+    rope.destroy()
+
+
+def test_no_tokens():
+    rope = cpl.Rope(32)
+    x = torch.empty(0, 3, 32, device="cuda")
+    rope.apply(cpl.rope_parts([(x, x)]))
+    rope.destroy()
+
+
+@pytest.mark.parametrize("name,rot", [("gqa8x2d128", 128), ("gqa8x2d128", 32), ("gqa6x2d64", 24), ("mla16", 64),
+                                      ("mla16", 12), ("mla4l128r40", 40), ("mha3d64", 2), ("gqa4x2d256", 256)])
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("page_tokens", [4, 64])
+def test_append_rotates_keys(name, rot, layout, page_tokens):
+    """Ragged appends behind what requests hold; V and the unrotated elements
+    bit for bit."""
+    if page_tokens * 2 * shape(name)[4] % 256:
+        pytest.skip("pages of this model are no multiple of 256 bytes")
+    print(f"[case] append rope {name} rot {rot} {layout} P{page_tokens}", flush=True)
+    base, new = [0, 50, 3], [301, 1, 0]
+    sc = Scene(name, base, page_tokens=page_tokens, seed=20, room=310)
+    rope = cpl.Rope(rot, layout=layout)
+    rows = sc.normal(sum(new), sc.row)
+    sc.pool.append_rope(sc.ids, new, rows, rope)
+    at = 0
+    mla = GEOMS[name]["kind"] == cpl.CP_KIND_MLA
+    for rid, b, n, old in zip(sc.ids, base, new, sc.rows):
+        got = sc.held(rid, b + n)
+        torch.cuda.synchronize()
+        assert (bits(got[:b]) == bits(old)).all()
+        x, y = rows[at:at + n], got[b:]
+        want = turn_rows(name, x, rope.angles(), torch.arange(b, b + n), layout)
+        rotated = torch.zeros(sc.row, dtype=torch.bool)
+        if mla:
+            rotated[sc.dv:sc.dv + rot] = True
+        else:
+            rotated[:sc.hkv * sc.dk].view(sc.hkv, sc.dk)[:, :rot] = True
+        assert (bits(y[:, ~rotated]) == bits(x[:, ~rotated])).all()
+        mag = pair_length(x[:, rotated].view(n, sc.hkv, rot), layout).view(n, sc.hkv * rot)
+        err = (y.double().cpu() - want)[:, rotated].abs()
+        assert (err <= allowed(want[:, rotated], mag, torch.bfloat16)).all()
+        at += n
+    rope.destroy()
+    sc.close()
+
+
+def test_append_rope_of_layers_and_many_pages():
+    """Two planes, and more new pages than travel with a launch."""
+    sc = Scene("mha3d64", [5], page_tokens=4, seed=21, room=2000, layers=2)
+    rope = cpl.Rope(64)
+    rows = sc.normal(2, 1900, sc.row)
+    sc.pool.append_rope(sc.ids, [1900], rows, rope)
+    got = sc.held(sc.ids[0], 1905, layers=2)
+    for l in range(2):
+        want = turn_rows("mha3d64", rows[l], rope.angles(), torch.arange(5, 1905), "half")
+        mag = torch.zeros_like(want)
+        k = sc.hkv * sc.dk
+        mag[:, :k] = pair_length(rows[l][:, :k].reshape(1900, sc.hkv, 64), "half").view(1900, k)
+        assert ((got[l, 5:].double().cpu() - want).abs() <= allowed(want, mag, torch.bfloat16)).all()
+    rope.destroy()
+    sc.close()
