@@ -2003,6 +2003,24 @@ cp_status plan_extend(cp_pool *p, int32_t n, const int32_t *ids, const int32_t *
   return CP_OK;
 }
 
+// The factors of the scores (extend.h), formed in 64 bits.
+void set_score_factors(ExtArgs *a, double scale) {
+  const double log2e = 1.4426950408889634;
+  if (!(a->softcap > 0.f)) {
+    a->score_mul = (float)(scale * log2e);
+    return;
+  }
+  const double mul = scale / a->softcap, cap = a->softcap * log2e;
+  a->score_mul = (float)mul;
+  a->cap_mul = (float)cap;
+  a->cap_edge = (float)(kCapEdge / mul);
+  double f = mul * cap;
+  for (int k = 0; k < 6; ++k, f *= mul * mul) {
+    a->cap_k[k] = (float)(kTanh[k] * f);
+    if (!std::isfinite(a->cap_k[k])) a->cap_edge = 0.f;  // a tiny cap: never
+  }
+}
+
 cp_status run_extend(cp_pool *p, const ExtPlan &pl, const void *q, void *out, float *lse, const cp_extend_opts &o,
                      hipStream_t s) {
   const Geom &g = pl.geom;
@@ -2019,7 +2037,7 @@ cp_status run_extend(cp_pool *p, const ExtPlan &pl, const void *q, void *out, fl
     a.slopes = o.slopes;
     a.doc_begin = o.doc_begin;
     a.softcap = o.softcap;
-    a.scale = g.scale;
+    set_score_factors(&a, g.scale);
     a.window = (uint32_t)o.window;
     a.page_magic = page_magic(P);
     a.n_req = (int32_t)l.req.size();

@@ -43,7 +43,11 @@ struct ExtArgs {
   float *ws_l;  // partial log-sum-exp (base 2): [row][split]
   const float *slopes;
   const int32_t *doc_begin;
-  float softcap, scale;
+  float softcap;
+  // Scores from products, in units of log2 e: product * score_mul, or capped
+  // cap_mul * tanh(product * score_mul); while |product| < cap_edge the latter is
+  // product * sum_k cap_k[k] product^2k.
+  float score_mul, cap_mul, cap_edge, cap_k[6];
   uint32_t window;
   uint32_t page_magic;  // page_divide
   int32_t n_req, n_units;
@@ -65,6 +69,11 @@ struct ExtMergeArgs {
   } req[kMaxReqPerLaunch];
 };
 static_assert(sizeof(ExtMergeArgs) <= 3072, "extend merge arguments too large");
+
+// tanh(x) = x + x sum_k kTanh[k] x^2k, to 8e-8 of its value under kCapEdge: a
+// least-squares fit, reweighted towards its largest relative error.
+constexpr float kTanh[6] = {1.f, -3.333329714e-01f, 1.333189099e-01f, -5.378023840e-02f, 2.078145661e-02f, -5.875653302e-03f};
+constexpr float kCapEdge = 0.6f;
 
 // floor(2^32 / P), for page_divide on the device.
 inline uint32_t page_magic(int32_t page_tokens) {

@@ -1,0 +1,451 @@
+// gfx950 kernels of attention of token chunks for GQA and MHA of head_dim 64 and
+// 128, on the matrix cores.
+#include <hip/hip_runtime.h>
+
+#include "extend_device.h"
+
+namespace cp {
+
+// Scores are computed transposed, S^T = K Q^T by 32x32x16 products: a lane
+// then holds scores of one row (its column, lane % 32), 16 of every 32 keys, and
+// the other half of the wave the other 16. So the softmax runs inside lanes, and the
+// same registers, rounded, are the operand P^T of O^T = V^T P^T, the products'
+// contraction taking keys in the order that the first left them in:
+// of 16 keys, half h of the wave has keys 4 h + {0..3} and 8 + 4 h + {0..3}. V^T
+// comes from LDS by transposing reads.
+//
+// LDS rows are not padded but their 16-byte pieces swapped by the row number:
+// K reads touch 16 rows at one piece (all 16 pieces of a 256-byte line), V
+// reads four rows at four pieces.
+//
+// RW = 4: 128 rows, a wave for every 32, all over the same 64 keys a step; the
+// next step's keys travel through registers while this one's are worked on.
+// RW = 1: 32 rows, every wave with 32 keys of its own a step (few rows: bound
+// by reading KV); the waves' sums join at the end.
+template <int D, int RW>
+struct ExtCfg {
+  static constexpr int KW = RW == 4 ? 64 : 32;        // keys of a wave's step
+  static constexpr int KEYS = RW == 4 ? 64 : 128;     // keys of a workgroup's step
+  static constexpr int ROW = 2 * D;                   // bytes
+  static constexpr int CPR = D / 8;                   // 16-byte pieces of a row
+  static constexpr int TILE = KW * ROW;               // bytes of K (or V) of a step of a wave's keys
+  static constexpr int BUFS = RW == 4 ? 2 : 4;        // double buffer, or one for each wave
+  static constexpr int LOADERS = RW == 4 ? 256 : 64;  // threads that fill one
+  static constexpr int RPI = LOADERS / CPR;           // rows that they fill at once
+  static constexpr int NL = KW / RPI;                 // 16-byte loads of K (and of V) of a thread
+  static constexpr int KB = KW / 32;                  // blocks of 32 keys
+  static constexpr int NP = RW == 4 ? 1 : 2;          // bf16 parts of a probability
+  static constexpr int LDS = 2 * TILE * BUFS;
+  static_assert(RW == 4 || LDS >= 4 * 32 * D * 4, "the join reuses the tiles");
+};
+
+// Swapped piece numbers: 16 rows at one piece (K), 4 rows at 4 neighbouring pieces (V).
+template <int D>
+CP_DEV int k_piece(int row, int c) {
+  return D == 128 ? c ^ (row & 15) : c ^ ((row >> 1) & 7);
+}
+template <int D>
+CP_DEV int v_piece(int row, int c) {
+  return D == 128 ? c ^ (4 * (row & 3)) : c ^ (4 * ((row >> 1) & 1));
+}
+
+template <int D, int RW, int MODE>
+__global__ __launch_bounds__(kExtThreads, 2) void extend_rows_kernel(const ExtArgs a) {
+  using C = ExtCfg<D, RW>;
+  constexpr int KS = D / 16, DB = D / 32;
+  __shared__ __attribute__((aligned(16))) char lds[C::LDS];
+  __shared__ uint32_t shared_u[4][4];
+  __shared__ float stats[2][4][32];  // RW 1: the waves' m and l
+  const Unit un = find_unit(a);
+  const ExtReq &rq = *un.rq;
+  const GeomK &g = a.g;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 31, half = lane >> 5, c16 = lane & 15, grp = (lane >> 4) & 1;
+  const uint32_t P = (uint32_t)g.page_tokens;
+
+  // ---- this lane's row, what its wave sees, and what the workgroup sees
+  const uint32_t r = un.tile * (32 * RW) + (RW == 4 ? 32 * wave : 0) + col;
+  const Row x = row_of(a, rq, un.kvh, r);
+  const Sight ws = wave_sight<16>(x);
+  const Sight gs = RW == 4 ? group_sight<4>(ws, wave, lane, shared_u) : ws;
+  // steps of the unit: whole steps from a multiple of KEYS on
+  const uint32_t first = gs.lo / C::KEYS, last = (gs.hi + C::KEYS - 1) / C::KEYS, steps = last - first;
+  const uint32_t s0 = first + (uint32_t)((uint64_t)steps * un.split / rq.splits),
+                 s1 = first + (uint32_t)((uint64_t)steps * (un.split + 1) / rq.splits);
+
+  // ---- Q^T: lane holds row `col`, dims 16 ks + 8 half .. + 7
+  bf16x8 qf[KS];
+  {
+    const uint16_t *const qrow = a.q + (x.tok * (uint32_t)g.hq + x.head) * D + 8 * half;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const bf16x8 *>(qrow + 16 * ks);
+  }
+  const float slope = MODE == kModeAny && a.slopes ? a.slopes[x.head] * kLog2e : 0.f;
+
+  float m = -INFINITY, l = 0.f;
+  f32x16 o[DB];
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+
+  // ---- loads: a thread takes piece lc of rows lr, lr + RPI, ... of a step. Lane
+  // i of every wave looks key i up, a step ahead; keys out of sight are looked up
+  // as the nearest one in sight (they are hidden below, and never stale memory).
+  const int lt = RW == 4 ? (int)threadIdx.x : lane, lc = lt % C::CPR, lr = lt / C::CPR;
+  const uint8_t *const head_base = a.pool + (uint64_t)un.kvh * (4ull * P * D) + 16 * lc;
+  u32x4e kreg[C::NL], vreg[C::NL];
+  // keys of step s: RW 4, [64 s, + 64); RW 1, wave w has [128 s + 32 w, + 32)
+  auto base_of = [&](uint32_t s) { return s * C::KEYS + (RW == 4 ? 0u : 32u * wave); };
+  uint32_t key_pte = 0, key_slot = 0;
+  auto look_up = [&](uint32_t s) {
+    const uint32_t key = min(max(base_of(s) + (lane & (C::KW - 1)), gs.lo), gs.hi - 1);
+    key_pte = a.pte[rq.pte_base + page_divide(key, P, a.page_magic, &key_slot)];
+  };
+  auto load_v = [&](int i, const uint8_t *kp) {
+    const u32x4e *const p = reinterpret_cast<const u32x4e *>(kp + (uint64_t)P * C::ROW);
+    vreg[i] = RW == 4 ? *p : __builtin_nontemporal_load(p);
+  };
+  auto row_ptr = [&](int i) {
+    const int row = lr + C::RPI * i;
+    const uint32_t pte = (uint32_t)__shfl((int)key_pte, row, 64), slot = (uint32_t)__shfl((int)key_slot, row, 64);
+    return head_base + ((uint64_t)pte << 8) + slot * C::ROW;
+  };
+  auto load_keys = [&] {
+#pragma unroll
+    for (int i = 0; i < C::NL; ++i) {
+      const uint8_t *const kp = row_ptr(i);
+      const u32x4e *const p = reinterpret_cast<const u32x4e *>(kp);
+      kreg[i] = RW == 4 ? *p : __builtin_nontemporal_load(p);
+      if (RW == 4) load_v(i, kp);
+    }
+  };
+  // RW 1 asks for the next V once the scores' registers are free: 64 registers of
+  // loads in flight beside them do not fit
+  auto load_values = [&] {
+#pragma unroll
+    for (int i = 0; i < C::NL; ++i) load_v(i, row_ptr(i));
+  };
+  // Are there keys of step s that some row of the workgroup does not see? Then
+  // infinities and NaN of V stay out of the products (0 times those is no
+  // 0), and the steps that had any are gone through again at the end.
+  auto mixed = [&](uint32_t s) {
+    const uint32_t b = base_of(s);
+    return b < gs.all_lo || b + C::KW > gs.all_hi;
+  };
+  uint32_t sp_first = 0xFFFFFFFFu, sp_last = 0;
+  auto store_keys = [&](int buf, uint32_t s) {
+    char *const kt = lds + buf * (2 * C::TILE), *const vt = kt + C::TILE;
+    if (mixed(s)) {
+      bool any = false;
+#pragma unroll
+      for (int i = 0; i < C::NL; ++i) any = any || any_special(vreg[i]);
+      if (__builtin_amdgcn_ballot_w64(any)) {
+        sp_first = min(sp_first, s);
+        sp_last = s;
+#pragma unroll
+        for (int i = 0; i < C::NL; ++i) vreg[i] = without_special(vreg[i]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < C::NL; ++i) {
+      const int row = lr + C::RPI * i;
+      *reinterpret_cast<u32x4e *>(kt + row * C::ROW + 16 * k_piece<D>(row, lc)) = kreg[i];
+      *reinterpret_cast<u32x4e *>(vt + row * C::ROW + 16 * v_piece<D>(row, lc)) = vreg[i];
+    }
+  };
+  // V^T of 16 keys and block d of 32 columns
+  auto v_frag = [&](const char *vt, int kb, int ks, int d) {
+    s16x4 f[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int row = 32 * kb + 16 * ks + 8 * h + 4 * half + (c16 >> 2);
+      const int c = 4 * d + 2 * grp + ((c16 >> 1) & 1);
+      f[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(
+          vt + row * C::ROW + 16 * v_piece<D>(row, c) + 8 * (c16 & 1)));
+    }
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(f[0], f[1], 0, 1, 2, 3, 4, 5, 6, 7));
+  };
+
+  // ---- one step over the keys in a buffer
+  auto compute = [&](int buf, uint32_t s, bool more) {
+    const uint32_t b0 = base_of(s);
+    if (b0 >= ws.hi || b0 + C::KW <= ws.lo) {  // out of this wave's sight
+      if (RW == 1 && more) load_values();
+      return;
+    }
+    const char *const kt = lds + buf * (2 * C::TILE), *const vt = kt + C::TILE;
+    f32x16 sc[C::KB];
+#pragma unroll
+    for (int kb = 0; kb < C::KB; ++kb) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sc[kb][i] = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        const int row = 32 * kb + col;
+        const bf16x8 kf = *reinterpret_cast<const bf16x8 *>(kt + row * C::ROW + 16 * k_piece<D>(row, 2 * ks + half));
+        sc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks], sc[kb], 0, 0, 0);
+      }
+    }
+    // element i of block kb: key b0 + 32 kb + 8 (i / 4) + 4 half + i % 4
+    const uint32_t k0 = b0 + 4 * half;
+    shape_scores<MODE, 16 * C::KB>(a, reinterpret_cast<float(&)[16 * C::KB]>(sc), slope, x.pos, k0,
+                                   b0 + C::KW <= ws.pos + 1,
+                                   [](int i) { return 32 * (i / 16) + 8 * (i % 16 / 4) + i % 4; });
+    if (b0 < ws.all_lo || b0 + C::KW > ws.all_hi) {  // some row of the wave does not see some key
+      const uint32_t lo = x.lo - k0, n = x.hi - x.lo;
+#pragma unroll
+      for (int kb = 0; kb < C::KB; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if ((uint32_t)(32 * kb + 8 * (i / 4) + i % 4) - lo >= n) sc[kb][i] = -INFINITY;
+    }
+    float t = sc[0][0];
+#pragma unroll
+    for (int kb = 0; kb < C::KB; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) t = __builtin_fmaxf(t, sc[kb][i]);
+    if (MODE == kModePlain) t *= a.score_mul;
+    // the reference moves when some row's maximum passes it by 2^kLazy
+    if (__builtin_amdgcn_ballot_w64(t > m + kLazy || (m == -INFINITY && t > m))) {
+      const float mt = __builtin_fmaxf(t, other_half(t));
+      const float mn = mt > m + kLazy || m == -INFINITY ? __builtin_fmaxf(mt, m) : m;
+      const float al = mn == -INFINITY ? 1.f : fast_exp2(m - mn);
+      m = mn;
+      l *= al;
+#pragma unroll
+      for (int d = 0; d < DB; ++d) o[d] *= al;
+    }
+    const float ref = m == -INFINITY ? 0.f : m;
+    uint32_t pw[C::NP][C::KB][8];  // two probabilities each, operand order
+#pragma unroll
+    for (int kb = 0; kb < C::KB; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; i += 2) {
+        const float p0 = weight<MODE>(a, sc[kb][i], ref), p1 = weight<MODE>(a, sc[kb][i + 1], ref);
+        l += p0 + p1;
+        if constexpr (C::NP == 1) {
+          pw[0][kb][i / 2] = pack_bf16x2(p0, p1);
+        } else {
+          // leading 8 bits, and the rest rounded: together 16 bits and a half step
+          const uint32_t h0 = __float_as_uint(p0) & 0xFFFF0000u, h1 = __float_as_uint(p1) & 0xFFFF0000u;
+          pw[0][kb][i / 2] = upper_halves(h0, h1);
+          // (kept above zero: an infinite V times 0 would be NaN)
+          pw[1][kb][i / 2] = pack_bf16x2(__builtin_fmaxf(p0 - __uint_as_float(h0), 1e-37f),
+                                         __builtin_fmaxf(p1 - __uint_as_float(h1), 1e-37f));
+        }
+      }
+    if (RW == 1 && more) load_values();
+#pragma unroll
+    for (int kb = 0; kb < C::KB; ++kb)
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+          const bf16x8 vf = v_frag(vt, kb, ks, d);
+#pragma unroll
+          for (int part = 0; part < C::NP; ++part) {
+            const uint32_t *const w = &pw[part][kb][4 * ks];
+            o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, __builtin_bit_cast(bf16x8, u32x4e{w[0], w[1], w[2], w[3]}),
+                                                           o[d], 0, 0, 0);
+          }
+        }
+  };
+
+  // ---- the steps
+  if (s0 < s1) {
+    look_up(s0);
+    load_keys();
+    if (RW == 1) load_values();
+    if (s0 + 1 < s1) look_up(s0 + 1);
+    if (RW == 4) {
+      store_keys(0, s0);
+      __syncthreads();
+    }
+  }
+#pragma unroll 1
+  for (uint32_t s = s0; s < s1; ++s) {
+    const int buf = RW == 4 ? (s - s0) & 1 : wave;
+    if (RW == 1) store_keys(buf, s);
+    const bool more = s + 1 < s1;
+    if (more) load_keys();
+    if (RW == 4) {
+      if (s + 2 < s1) look_up(s + 2);
+      compute(buf, s, more);
+      if (more) store_keys(buf ^ 1, s + 1);
+      __syncthreads();
+    } else {
+      // a wave's LDS operations run in order: its reads follow its writes
+      __builtin_amdgcn_wave_barrier();
+      compute(buf, s, more);
+      if (s + 2 < s1) look_up(s + 2);
+      __builtin_amdgcn_wave_barrier();
+    }
+  }
+
+  // ---- infinities and NaN of V that not every row sees: which rows see one is a
+  // product of ones, and their sums get it added
+  if (RW == 4) {
+    __syncthreads();
+    if (lane == 0) {
+      shared_u[wave][0] = sp_first;
+      shared_u[wave][1] = sp_last;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      sp_first = min(sp_first, shared_u[w][0]);
+      sp_last = max(sp_last, shared_u[w][1]);
+    }
+  }
+  sp_first = __builtin_amdgcn_readfirstlane(sp_first);
+  sp_last = __builtin_amdgcn_readfirstlane(sp_last);
+  if (__builtin_expect(sp_first <= sp_last, 0)) {
+#pragma unroll 1
+    for (uint32_t s = sp_first; s <= sp_last; ++s) {
+      if (!mixed(s)) continue;
+      char *const vt = lds + (RW == 4 ? 0 : wave) * (2 * C::TILE);
+      look_up(s);
+#pragma unroll
+      for (int i = 0; i < C::NL; ++i) {
+        const int row = lr + C::RPI * i;
+        load_v(i, row_ptr(i));
+        *reinterpret_cast<u32x4e *>(vt + row * C::ROW + 16 * v_piece<D>(row, lc)) = vreg[i];
+      }
+      if (RW == 4) __syncthreads();
+      __builtin_amdgcn_wave_barrier();
+      const uint32_t k0 = base_of(s) + 4 * half, lo = x.lo - k0, n = x.hi - x.lo;
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll 1
+        for (uint32_t sign = 0; sign < 2; ++sign) {
+          f32x16 hit;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) hit[i] = 0.f;
+#pragma unroll
+          for (int kb = 0; kb < C::KB; ++kb)
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks) {
+              u32x4e seen;
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                const uint32_t e = 32 * kb + 16 * ks + 8 * (k / 2) + 2 * (k % 2);
+                seen[k] = (e - lo < n ? 0x3F80u : 0u) | (e + 1 - lo < n ? 0x3F800000u : 0u);
+              }
+              hit = __builtin_amdgcn_mfma_f32_32x32x16_bf16(special_ones(v_frag(vt, kb, ks, d), sign),
+                                                            __builtin_bit_cast(bf16x8, seen), hit, 0, 0, 0);
+            }
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (hit[i] > 0.f) o[d][i] += sign ? -INFINITY : INFINITY;
+        }
+      if (RW == 4) __syncthreads();
+      __builtin_amdgcn_wave_barrier();
+    }
+  }
+
+  // ---- results: column d = 32 db + 8 (i / 4) + 4 half + i % 4 of row `col`
+  l += other_half(l);
+  if (RW == 4) {
+    if (r >= rq.n_q * (uint32_t)g.g) return;
+    const bool none = l == 0.f;  // (all scores NaN: l is NaN, and so are the results)
+    const float inv = none ? 0.f : 1.f / l, lse = none ? -INFINITY : m + fast_log2(l);
+    if (rq.splits > 1) {
+      const uint64_t pr = part_row(a, rq, x, un.split);
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+          const f32x4 w = {o[d][i] * inv, o[d][i + 1] * inv, o[d][i + 2] * inv, o[d][i + 3] * inv};
+          *reinterpret_cast<f32x4 *>(a.ws_o + pr * D + 32 * d + 2 * i + 4 * half) = none ? f32x4{0.f, 0.f, 0.f, 0.f} : w;
+        }
+      if (half == 0) a.ws_l[pr] = lse;
+    } else {
+      const uint64_t orow = x.tok * (uint32_t)g.hq + x.head;
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+          const uint2 w = bf16x4_bits(o[d][i] * inv, o[d][i + 1] * inv, o[d][i + 2] * inv, o[d][i + 3] * inv);
+          *reinterpret_cast<uint2 *>(a.out + orow * D + 32 * d + 2 * i + 4 * half) = none ? uint2{0u, 0u} : w;
+        }
+      if (half == 0) a.lse[orow] = lse * kLn2;
+    }
+  } else {
+    __syncthreads();  // every wave is done with its tile
+    float *const part = reinterpret_cast<float *>(lds) + wave * (32 * D);  // [column][row]
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) part[(32 * d + 8 * (i / 4) + 4 * half + i % 4) * 32 + col] = o[d][i];
+    if (half == 0) {
+      stats[0][wave][col] = m;
+      stats[1][wave][col] = l;
+    }
+    __syncthreads();
+    // thread: row t % 32, D / 8 columns
+    constexpr int NC = D / 8;
+    const int row = threadIdx.x & 31, c0 = (threadIdx.x >> 5) * NC;
+    const uint32_t rr = un.tile * 32 + row;
+    if (rr >= rq.n_q * (uint32_t)g.g) return;
+    const Row y = row_of(a, rq, un.kvh, rr);
+    float mt = stats[0][0][row];
+#pragma unroll
+    for (int w = 1; w < 4; ++w) mt = __builtin_fmaxf(mt, stats[0][w][row]);
+    const float ref = mt == -INFINITY ? 0.f : mt;
+    float f[4], lt4 = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      f[w] = fast_exp2(stats[0][w][row] - ref);
+      lt4 += f[w] * stats[1][w][row];
+    }
+    const bool none = lt4 == 0.f;
+    const float inv = none ? 0.f : 1.f / lt4, lse = none ? -INFINITY : mt + fast_log2(lt4);
+    float v[NC];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      float acc = 0.f;
+#pragma unroll
+      for (int w = 0; w < 4; ++w)  // a wave that saw nothing of the row has nothing to add
+        if (f[w] > 0.f) acc += f[w] * reinterpret_cast<const float *>(lds)[w * 32 * D + (c0 + c) * 32 + row];
+      v[c] = acc * inv;
+    }
+    if (rq.splits > 1) {
+      const uint64_t pr = part_row(a, rq, y, un.split);
+#pragma unroll
+      for (int c = 0; c < NC; c += 4)
+        *reinterpret_cast<f32x4 *>(a.ws_o + pr * D + c0 + c) = f32x4{v[c], v[c + 1], v[c + 2], v[c + 3]};
+      if (c0 == 0) a.ws_l[pr] = lse;
+    } else {
+      const uint64_t orow = y.tok * (uint32_t)g.hq + y.head;
+#pragma unroll
+      for (int c = 0; c < NC; c += 4)
+        *reinterpret_cast<uint2 *>(a.out + orow * D + c0 + c) = bf16x4_bits(v[c], v[c + 1], v[c + 2], v[c + 3]);
+      if (c0 == 0) a.lse[orow] = lse * kLn2;
+    }
+  }
+}
+
+namespace {
+template <int D, int RW>
+void launch_rows(const ExtArgs &a, hipStream_t stream) {
+  const dim3 grid((uint32_t)a.n_units), block(kExtThreads);
+  if (a.slopes)
+    hipLaunchKernelGGL((extend_rows_kernel<D, RW, kModeAny>), grid, block, 0, stream, a);
+  else if (a.softcap > 0.f)
+    hipLaunchKernelGGL((extend_rows_kernel<D, RW, kModeCap>), grid, block, 0, stream, a);
+  else
+    hipLaunchKernelGGL((extend_rows_kernel<D, RW, kModePlain>), grid, block, 0, stream, a);
+}
+}  // namespace
+
+void launch_extend_rows(const ExtArgs &a, int32_t kind, hipStream_t stream) {
+  switch (kind) {
+    case kXRows64: return launch_rows<64, 4>(a, stream);
+    case kXRows128: return launch_rows<128, 4>(a, stream);
+    case kXFew64: return launch_rows<64, 1>(a, stream);
+    default: return launch_rows<128, 1>(a, stream);
+  }
+}
+
+}  // namespace cp
