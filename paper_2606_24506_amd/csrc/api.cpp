@@ -1890,7 +1890,7 @@ int32_t extend_kind(const Geom &g, int32_t path, int64_t n_q) {
     const bool few = n_q * g.g <= 32;
     return g.head_dim == 64 ? (few ? kXFew64 : kXRows64) : (few ? kXFew128 : kXRows128);
   }
-  return kXVec;
+  return g.kind == kMLA && g.latent == 512 && g.rope == 64 ? kXMla : kXVec;
 }
 
 // Checks a call and plans it, at the contexts the requests will have with

@@ -14,13 +14,18 @@ namespace cp {
 //   kXVec    vector: one wave per row, any geometry.
 //   kXRows*  matrix cores, GQA / MHA of head_dim 64 or 128: tiles of 128 rows.
 //   kXFew*   the same with 32 rows, the four waves taking keys in turn.
-enum : int32_t { kXVec = 0, kXRows64, kXRows128, kXFew64, kXFew128, kXKinds };
+//   kXMla    matrix cores, MLA with latent 512 and rotary part 64: 128 rows.
+enum : int32_t { kXVec = 0, kXRows64, kXRows128, kXFew64, kXFew128, kXMla, kXKinds };
 
 constexpr int kExtThreads = 256;
 // Rows (a token and a query head of one KV head) of a tile, and keys of one
 // step, of each kernel.
-constexpr int32_t ext_tile_rows(int32_t kind) { return kind == kXVec ? 4 : kind <= kXRows128 ? 128 : 32; }
-constexpr int32_t ext_tile_keys(int32_t kind) { return kind == kXVec || kind <= kXRows128 ? 64 : 128; }
+constexpr int32_t ext_tile_rows(int32_t kind) {
+  return kind == kXVec ? 4 : kind == kXFew64 || kind == kXFew128 ? 32 : 128;
+}
+constexpr int32_t ext_tile_keys(int32_t kind) {
+  return kind == kXFew64 || kind == kXFew128 ? 128 : kind == kXMla ? 32 : 64;
+}
 
 struct ExtReq {
   uint32_t unit_begin;  // first work unit of the request

@@ -7,6 +7,7 @@
 namespace cp {
 
 void launch_extend_rows(const ExtArgs &a, int32_t kind, hipStream_t stream);
+void launch_extend_mla(const ExtArgs &a, hipStream_t stream);
 
 // ------------------------------------------------------------ vector path
 
@@ -144,6 +145,7 @@ hipError_t launch_extend(const ExtArgs &a, int32_t kind, hipStream_t stream) {
     case kXRows128:
     case kXFew64:
     case kXFew128: launch_extend_rows(a, kind, stream); break;
+    case kXMla: launch_extend_mla(a, stream); break;
     default: return hipErrorInvalidValue;
   }
   return hipGetLastError();

@@ -190,7 +190,7 @@ def rounds_to_16_bits(name, n_q, path=cpl.CP_PATH_AUTO):
         return False
     if g["kind"] == cpl.CP_KIND_GQA and g["head_dim"] in (64, 128):
         return n_q * g["n_q_heads"] // g["n_kv_heads"] > 32
-    return False
+    return g["kind"] == cpl.CP_KIND_MLA and (g["latent_dim"], g["rope_dim"]) == (512, 64)
 
 
 def bits(x):
