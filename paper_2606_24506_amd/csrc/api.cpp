@@ -34,7 +34,7 @@ int matrix_streams(int variant);
 int matrix_step_tokens(int variant, int hkv);
 hipError_t launch_merge(const MergeArgs &a, hipStream_t stream);
 hipError_t launch_extend(const ExtArgs &a, int32_t kind, hipStream_t stream);
-hipError_t launch_ext_merge(const ExtMergeArgs &a, uint32_t rows, hipStream_t stream);
+hipError_t launch_ext_merge(const ExtMergeArgs &a, uint32_t rows, uint32_t most_splits, hipStream_t stream);
 hipError_t launch_page_copy(const PageCopyArgs &a, hipStream_t stream);
 hipError_t launch_stack_push(const StackPushArgs &a, hipStream_t stream);
 hipError_t scratch_device_address(int device, void **out);
@@ -1893,6 +1893,59 @@ int32_t extend_kind(const Geom &g, int32_t path, int64_t n_q) {
   return g.kind == kMLA && g.latent == 512 && g.rope == 64 ? kXMla : kXVec;
 }
 
+// A request of a call: its kernel, rows of all heads, row tiles per KV head, steps of
+// its longest tile, and the ranges that these are cut into.
+struct ExtItem {
+  int32_t kind = 0;
+  int64_t rows = 0, tiles = 0, steps = 0, splits = 1;
+};
+
+// Ranges of each request. Steps per range are tried from few to many, and the
+// shortest estimate taken: the launch takes its work over the workgroups that
+// run at once, or its longest unit, and cut requests cost a second launch
+// and their partial rows' way to memory and back. Units that pass what runs
+// at once by a few start a second turn: then the longest unit comes on top.
+void choose_ranges(const Geom &g, int num_cus, uint64_t cap, std::vector<ExtItem> *items) {
+  // us of a step of the kernel, and workgroups of a CU
+  static constexpr struct { double us; int per_cu; } kCost[kXKinds] = {
+      {2.0, 8}, {1.0, 3}, {1.6, 2}, {2.0, 4}, {3.0, 2}, {1.4, 1}};
+  // a unit's start and end, the second launch, and the way of partial rows
+  constexpr double kUnit = 4.0, kJoin = 5.0, kBytesPerUs = 3.0e6;
+  double most = 1, base = 0, all_units = 0;
+  int per_cu = 8;
+  for (const ExtItem &x : *items) {
+    if (x.rows == 0) continue;
+    most = std::max(most, (double)x.steps);
+    per_cu = std::min(per_cu, kCost[x.kind].per_cu);
+    all_units += (double)(x.tiles * g.hkv);
+    base += (double)(x.tiles * g.hkv) * (double)x.steps * kCost[x.kind].us / kCost[x.kind].per_cu;
+  }
+  const double slots = (double)num_cus * per_cu;
+  double best = 1e300, best_per = most;
+  for (double per = most; per >= 1; per = std::floor(per * 0.75)) {
+    double work = base, longest = 0, rows = 0, units = 0;
+    for (const ExtItem &x : *items) {
+      if (x.rows == 0) continue;
+      const double s = std::min(std::ceil((double)x.steps / per), 4096.0), u = (double)(x.tiles * g.hkv) * s;
+      work += u * kUnit / kCost[x.kind].per_cu;
+      longest = std::max(longest, kUnit + std::ceil((double)x.steps / s) * kCost[x.kind].us);
+      units += u;
+      if (s > 1) rows += (double)(x.rows + 1) * s;
+    }
+    double t = units > slots ? work / num_cus + 0.5 * longest : std::max(longest, work / num_cus);
+    const double join = rows > 0 ? kJoin + rows * g.d_v * 8 / kBytesPerUs : 0;
+    t += join;
+    if (t < best && (rows == 0 || pool_ws_bytes((uint64_t)(2 * rows) * (uint64_t)g.d_v, (uint64_t)rows) <= cap)) {
+      best = t;
+      best_per = per;
+    }
+    // no cut helps a launch that is full without, and shorter ranges only cost from here on
+    if ((per == most && all_units >= 4 * slots) || join + work / num_cus > best) break;
+  }
+  for (ExtItem &x : *items)
+    x.splits = (int64_t)std::max(1.0, std::min(std::ceil((double)x.steps / best_per), 4096.0));
+}
+
 // Checks a call and plans it, at the contexts the requests will have with
 // extra[i] more tokens (NULL: none). Changes nothing.
 cp_status plan_extend(cp_pool *p, int32_t n, const int32_t *ids, const int32_t *n_q, const int32_t *extra,
@@ -1922,56 +1975,41 @@ cp_status plan_extend(cp_pool *p, int32_t n, const int32_t *ids, const int32_t *
   const Geom &g = pl->geom;
 
   // Steps (of ext_tile_keys keys) of each request's longest tile, and tiles.
-  struct Item {
-    int32_t kind;
-    int64_t tiles, steps;
-  };
-  std::vector<Item> it((size_t)n);
-  int64_t work[kXKinds] = {}, units[kXKinds] = {};
+  std::vector<ExtItem> it((size_t)n);
   for (int32_t i = 0; i < n; ++i) {
     const int64_t ctx = p->st.req(ids[i]).attend_len() + (extra ? extra[i] : 0);
-    Item &x = it[(size_t)i];
+    ExtItem &x = it[(size_t)i];
     x.kind = extend_kind(g, o.path, n_q[i]);
     const int64_t rows = ext_tile_rows(x.kind), keys = ext_tile_keys(x.kind);
+    x.rows = (int64_t)n_q[i] * g.hq;
     x.tiles = ((int64_t)n_q[i] * g.g + rows - 1) / rows;
     int64_t seen = ctx;
     if (o.window) seen = std::min<int64_t>(ctx, (int64_t)o.window + std::min<int64_t>(n_q[i], rows / g.g + 2) +
                                                     (o.prefix ? (int64_t)o.prefix[i] : 0));
     x.steps = (seen + keys - 1) / keys + (o.window ? 1 : 0);
-    units[x.kind] += x.tiles * g.hkv;
-    work[x.kind] += x.tiles * g.hkv * x.steps;
   }
-  // Ranges: enough units to fill the CUs twice, none shorter than min_steps.
-  int64_t total_units = 0, total_work = 0;
-  for (int k = 0; k < kXKinds; ++k) {
-    total_units += units[k];
-    total_work += work[k];
+  const uint64_t cap = p->ws_limit ? p->ws_limit : UINT64_MAX;
+  if (o.num_splits > 0) {
+    for (ExtItem &x : it) x.splits = std::max<int64_t>(1, std::min<int64_t>({o.num_splits, x.steps, 4096}));
+  } else {
+    choose_ranges(g, p->num_cus, cap, &it);
   }
-  const int64_t slots = 2 * (int64_t)p->num_cus;
-  int64_t per = std::max<int64_t>(4, (total_work + slots - 1) / slots);
-  if (total_units >= slots) per = INT64_MAX;
-  std::vector<int64_t> splits((size_t)n, 1);
-  for (;;) {  // longer ranges until the partials fit the pool's cap
-    uint64_t o_floats = 0, l_floats = 0;
-    for (int32_t i = 0; i < n; ++i) {
-      const Item &x = it[(size_t)i];
-      int64_t s = per == INT64_MAX ? 1 : (x.steps + per - 1) / per;
-      if (o.num_splits > 0) s = std::min<int64_t>(o.num_splits, x.steps);
-      splits[(size_t)i] = std::max<int64_t>(1, std::min<int64_t>(s, 4096));
-      if (splits[(size_t)i] > 1) l_floats += ((uint64_t)n_q[i] * g.hq + 1) * (uint64_t)splits[(size_t)i];
-    }
-    o_floats = l_floats * (uint64_t)g.d_v;
-    if (!p->ws_limit || o.num_splits > 0 || l_floats == 0 || pool_ws_bytes(2 * o_floats, l_floats) <= p->ws_limit) break;
-    per = per > (1ll << 40) ? INT64_MAX : per * 2;
-  }
-  uint32_t tok0 = 0;
+  // long requests first: theirs are the longest units
+  std::vector<int32_t> order((size_t)n);
+  for (int32_t i = 0; i < n; ++i) order[(size_t)i] = i;
+  std::stable_sort(order.begin(), order.end(), [&](int32_t x, int32_t y) {
+    const ExtItem &u = it[(size_t)x], &v = it[(size_t)y];
+    return u.steps * v.splits > v.steps * u.splits;
+  });
+  std::vector<uint32_t> tok((size_t)n);
+  for (int32_t i = 1; i < n; ++i) tok[(size_t)i] = tok[(size_t)i - 1] + (uint32_t)n_q[i - 1];
+
   uint64_t ws_row = 0;
   for (int32_t kind = 0; kind < kXKinds; ++kind) {
-    tok0 = 0;
-    for (int32_t i = 0; i < n; tok0 += (uint32_t)n_q[i], ++i) {
-      const Item &x = it[(size_t)i];
+    for (int32_t i : order) {
+      const ExtItem &x = it[(size_t)i];
       if (x.kind != kind || n_q[i] == 0) continue;
-      const int64_t u = x.tiles * g.hkv * splits[(size_t)i];
+      const int64_t u = (x.tiles * g.hkv * x.splits + 7) / 8 * 8;
       if (u > kMaxExtUnits) return fail(CP_EINVAL, "too many query rows of request %d in one call", ids[i]);
       if (pl->launches.empty() || pl->launches.back().kind != kind ||
           (int)pl->launches.back().req.size() == kMaxReqPerLaunch || pl->launches.back().units + u > kMaxExtUnits) {
@@ -1986,9 +2024,9 @@ cp_status plan_extend(cp_pool *p, int32_t n, const int32_t *ids, const int32_t *
       e.ctx = (uint32_t)(r.attend_len() + (extra ? extra[i] : 0));
       e.n_q = (uint32_t)n_q[i];
       e.prefix = o.prefix ? (uint32_t)o.prefix[i] : 0u;
-      e.tok0 = tok0;
+      e.tok0 = tok[(size_t)i];
       e.tiles = (uint32_t)x.tiles;
-      e.splits = (uint32_t)splits[(size_t)i];
+      e.splits = (uint32_t)x.splits;
       if (e.splits > 1) {
         // partial rows start at a multiple of the request's own ranges
         e.ws_row = (ws_row + e.splits - 1) / e.splits;
@@ -2015,7 +2053,7 @@ void set_score_factors(ExtArgs *a, double scale) {
   a->cap_mul = (float)cap;
   a->cap_edge = (float)(kCapEdge / mul);
   double f = mul * cap;
-  for (int k = 0; k < 6; ++k, f *= mul * mul) {
+  for (int k = 0; k < kTanhTerms; ++k, f *= mul * mul) {
     a->cap_k[k] = (float)(kTanh[k] * f);
     if (!std::isfinite(a->cap_k[k])) a->cap_edge = 0.f;  // a tiny cap: never
   }
@@ -2051,11 +2089,11 @@ cp_status run_extend(cp_pool *p, const ExtPlan &pl, const void *q, void *out, fl
     m.ws_l = a.ws_l;
     m.out = a.out;
     m.lse = lse;
-    m.hq = g.hq;
     m.d_v = g.d_v;
-    uint32_t rows = 0;
+    uint32_t rows = 0, most = 1;
     for (const ExtReq &r : l.req) {
       if (r.splits < 2) continue;
+      most = std::max(most, r.splits);
       ExtMergeArgs::Req &x = m.req[m.n_req++];
       x.row_begin = rows;
       x.rows = r.n_q * (uint32_t)g.hq;
@@ -2064,7 +2102,7 @@ cp_status run_extend(cp_pool *p, const ExtPlan &pl, const void *q, void *out, fl
       x.splits = r.splits;
       rows += x.rows;
     }
-    e = launch_ext_merge(m, rows, s);
+    e = launch_ext_merge(m, rows, most, s);
     if (e != hipSuccess) return hip_fail(e, "extend join launch");
   }
   return CP_OK;

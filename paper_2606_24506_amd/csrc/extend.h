@@ -27,8 +27,14 @@ constexpr int32_t ext_tile_keys(int32_t kind) {
   return kind == kXFew64 || kind == kXFew128 ? 128 : kind == kXMla ? 32 : 64;
 }
 
+// tanh(x) = x + x sum_{k > 0} kTanh[k] x^2k, to 4e-8 of its value under kCapEdge: a
+// least-squares fit, reweighted towards its largest relative error.
+constexpr int kTanhTerms = 4;
+constexpr float kTanh[kTanhTerms] = {1.f, -3.33326690e-01f, 1.32999740e-01f, -4.91567400e-02f};
+constexpr float kCapEdge = 0.35f;
+
 struct ExtReq {
-  uint32_t unit_begin;  // first work unit of the request
+  uint32_t unit_begin;  // first workgroup of the request (a multiple of 8)
   uint32_t pte_base;    // page-table entries of the plane
   uint32_t ctx, n_q;    // context, and how many of its last tokens ask
   uint32_t prefix;
@@ -52,7 +58,7 @@ struct ExtArgs {
   // Scores from products, in units of log2 e: product * score_mul, or capped
   // cap_mul * tanh(product * score_mul); while |product| < cap_edge the latter is
   // product * sum_k cap_k[k] product^2k.
-  float score_mul, cap_mul, cap_edge, cap_k[6];
+  float score_mul, cap_mul, cap_edge, cap_k[kTanhTerms];
   uint32_t window;
   uint32_t page_magic;  // page_divide
   int32_t n_req, n_units;
@@ -65,7 +71,7 @@ struct ExtMergeArgs {
   const float *ws_o, *ws_l;
   uint16_t *out;
   float *lse;
-  int32_t n_req, hq, d_v, pad;
+  int32_t n_req, d_v, lanes, pad;  // lanes: ranges of a row taken at once
   struct Req {
     uint32_t row_begin, rows;  // rows of the launch before, and of, the request
     uint64_t ws_row;
@@ -74,11 +80,6 @@ struct ExtMergeArgs {
   } req[kMaxReqPerLaunch];
 };
 static_assert(sizeof(ExtMergeArgs) <= 3072, "extend merge arguments too large");
-
-// tanh(x) = x + x sum_k kTanh[k] x^2k, to 8e-8 of its value under kCapEdge: a
-// least-squares fit, reweighted towards its largest relative error.
-constexpr float kTanh[6] = {1.f, -3.333329714e-01f, 1.333189099e-01f, -5.378023840e-02f, 2.078145661e-02f, -5.875653302e-03f};
-constexpr float kCapEdge = 0.6f;
 
 // floor(2^32 / P), for page_divide on the device.
 inline uint32_t page_magic(int32_t page_tokens) {

@@ -37,14 +37,17 @@ CP_DEV uint32_t page_divide(uint32_t x, uint32_t P, uint32_t magic, uint32_t *re
   return q;
 }
 
-// The unit of a workgroup: consecutive units (which share KV) go to one XCD, whose
-// L2 they then share; workgroups are dealt to the eight XCDs in turn.
+// Unit of a request's workgroup b of n: workgroups are dealt to the eight XCDs in
+// turn, and consecutive units (which share KV) go to one XCD, whose L2 they then
+// share. Request by request, so that the XCDs get equal parts of long and short
+// ones: over the launch as a whole, three prompts of 16K, 9K and 4K tokens left
+// the XCDs of the short one idle for half the time.
 CP_DEV uint32_t xcd_unit(uint32_t b, uint32_t n) {
   const uint32_t per = n / 8, rem = n % 8, x = b % 8;
   return x * per + min(x, rem) + b / 8;
 }
 
-// tanh to 1.2e-7 of its value. Under kCapEdge a polynomial in x^2 fitted to tanh(x) / x
+// tanh to 2e-7 of its value. Under kCapEdge a polynomial in x^2 fitted to tanh(x) / x
 // (kTanh; 1 - 2 / (e^2x + 1) loses what the difference cancels, and scores far
 // under the cap are the usual case), above it the quotient.
 CP_DEV float tanh_large(float x) {
@@ -54,9 +57,9 @@ CP_DEV float tanh_large(float x) {
 }
 CP_DEV float cap_tanh(float x) {
   const float y = x * x;
-  float p = kTanh[5];
+  float p = kTanh[kTanhTerms - 1];
 #pragma unroll
-  for (int k = 4; k > 0; --k) p = __builtin_fmaf(p, y, kTanh[k]);
+  for (int k = kTanhTerms - 2; k > 0; --k) p = __builtin_fmaf(p, y, kTanh[k]);
   return __builtin_fabsf(x) < kCapEdge ? __builtin_fmaf(x * y, p, x) : tanh_large(x);  // NaN: the second, NaN too
 }
 
@@ -65,67 +68,18 @@ CP_DEV float cap_tanh(float x) {
 // capped; capped or not, with slopes.
 enum : int { kModePlain = 0, kModeCap, kModeAny };
 
-// Scores of N keys of one row, from products to units of log2 e (kModePlain:
-// left as they are). Element i is key k0 + at(i); behind: no key is past the
-// position `pos` of any row of the wave.
-template <int MODE, int N, class F>
-CP_DEV void shape_scores(const ExtArgs &a, float (&s)[N], float slope, uint32_t pos, uint32_t k0, bool behind, F at) {
-  if constexpr (MODE == kModePlain) return;
-  if (MODE == kModeCap || a.softcap > 0.f) {
-    float big = 0.f;
-#pragma unroll
-    for (int i = 0; i < N; ++i) big = __builtin_fmaxf(big, __builtin_fabsf(s[i]));
-    // (a NaN does not raise `big`: the polynomial keeps it as well)
-    if (__builtin_amdgcn_ballot_w64(big >= a.cap_edge)) {
-#pragma unroll
-      for (int i = 0; i < N; ++i) s[i] = cap_tanh(s[i] * a.score_mul) * a.cap_mul;
-    } else {  // the same polynomial with both factors in its coefficients
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const float y = s[i] * s[i];
-        float p = a.cap_k[5];
-#pragma unroll
-        for (int k = 4; k >= 0; --k) p = __builtin_fmaf(p, y, a.cap_k[k]);
-        s[i] *= p;
-      }
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < N; ++i) s[i] *= a.score_mul;
-  }
-  if constexpr (MODE == kModeAny) {
-    if (behind) {  // slope * (pos - key) in two steps
-      const float far = (float)(pos - k0);
-#pragma unroll
-      for (int i = 0; i < N; ++i) s[i] = __builtin_fmaf(-slope, far - (float)at(i), s[i]);
-    } else {
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const uint32_t key = k0 + at(i);
-        s[i] = __builtin_fmaf(-slope, (float)(max(key, pos) - min(key, pos)), s[i]);
-      }
-    }
-  }
-}
-
-// 2^(score - ref)
-template <int MODE>
-CP_DEV float weight(const ExtArgs &a, float s, float ref) {
-  return fast_exp2(MODE == kModePlain ? __builtin_fmaf(s, a.score_mul, -ref) : s - ref);
-}
-
 struct Unit {
   const ExtReq *rq;
   uint32_t kvh, tile, split;
+  bool none;  // one of the workgroups up to the next multiple of 8
 };
 CP_DEV Unit find_unit(const ExtArgs &a) {
-  const uint32_t v = xcd_unit(blockIdx.x, (uint32_t)a.n_units);
-  const int r = sorted_search(a.n_req, v, [&](int i) { return a.req[i].unit_begin; });
+  const int r = sorted_search(a.n_req, blockIdx.x, [&](int i) { return a.req[i].unit_begin; });
   const ExtReq &rq = a.req[r];
-  const uint32_t w = v - rq.unit_begin, per_head = rq.tiles * rq.splits;
-  const uint32_t kvh = w / per_head, u = w - kvh * per_head;
+  const uint32_t per_head = rq.tiles * rq.splits, n = per_head * (uint32_t)a.g.hkv, b = blockIdx.x - rq.unit_begin;
+  const uint32_t w = xcd_unit(b, n), kvh = w / per_head, u = w - kvh * per_head;
   // later tiles see more keys: they start first
-  return Unit{&rq, kvh, rq.tiles - 1 - u / rq.splits, u % rq.splits};
+  return Unit{&rq, kvh, rq.tiles - 1 - u / rq.splits, u % rq.splits, b >= n};
 }
 
 // What a row sees, and where its results go.
@@ -154,6 +108,94 @@ CP_DEV Row row_of(const ExtArgs &a, const ExtReq &rq, uint32_t kvh, uint32_t r) 
 // Stores of a row's result: NORMAL to the call's arrays, or a range's part.
 CP_DEV uint64_t part_row(const ExtArgs &a, const ExtReq &rq, const Row &x, uint32_t split) {
   return (rq.ws_row + (x.tok - rq.tok0) * (uint32_t)a.g.hq + x.head) * rq.splits + split;
+}
+
+// product * sum_k cap_k product^2k: the capped score, in units of log2 e, of a
+// product under cap_edge. less: subtracted in the last step.
+CP_DEV float small_cap(const ExtArgs &a, float s, float less) {
+  const float y = s * s;
+  float p = a.cap_k[kTanhTerms - 1];
+#pragma unroll
+  for (int k = kTanhTerms - 2; k >= 0; --k) p = __builtin_fmaf(p, y, a.cap_k[k]);
+  return __builtin_fmaf(s, p, -less);
+}
+template <int N>
+CP_DEV bool all_small(const ExtArgs &a, const float (&s)[N]) {
+  float big = 0.f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) big = __builtin_fmaxf(big, __builtin_fabsf(s[i]));
+  return __builtin_amdgcn_ballot_w64(big >= a.cap_edge) == 0;  // (a NaN is not: the polynomial keeps it too)
+}
+
+// Scores of N keys of one row, from products to units of log2 e. Element i is
+// key k0 + at(i); behind: no key is past the position `pos` of any row of the wave.
+template <int MODE, int N, class F>
+CP_DEV void shape_scores(const ExtArgs &a, float (&s)[N], float slope, uint32_t pos, uint32_t k0, bool behind, F at) {
+  if (MODE == kModeCap || a.softcap > 0.f) {
+    if (all_small(a, s)) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) s[i] = small_cap(a, s[i], 0.f);
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) s[i] = cap_tanh(s[i] * a.score_mul) * a.cap_mul;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) s[i] *= a.score_mul;
+  }
+  if constexpr (MODE == kModeAny) {
+    if (behind) {  // slope * (pos - key) in two steps
+      const float far = (float)(pos - k0);
+#pragma unroll
+      for (int i = 0; i < N; ++i) s[i] = __builtin_fmaf(-slope, far - (float)at(i), s[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const uint32_t key = k0 + at(i);
+        s[i] = __builtin_fmaf(-slope, (float)(max(key, pos) - min(key, pos)), s[i]);
+      }
+    }
+  }
+}
+
+// Scores of N keys of one row, with those out of sight made -inf, and their
+// maximum in units of log2 e. hide: some row of the wave does not see some of
+// the keys. Where it can, it leaves the products as they are (returns true), for
+// weight() to scale or cap and take the reference off in one go.
+template <int MODE, int N, class F>
+CP_DEV bool scores_of(const ExtArgs &a, float (&s)[N], float slope, const Row &x, uint32_t k0, bool behind, bool hide,
+                      F at, float *top) {
+  bool raw = MODE == kModePlain || (MODE == kModeCap && !hide && all_small(a, s));
+  if (!raw) shape_scores<MODE, N>(a, s, slope, x.pos, k0, behind, at);
+  if (hide) {
+    const uint32_t lo = x.lo - k0, n = x.hi - x.lo;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if ((uint32_t)at(i) - lo >= n) s[i] = -INFINITY;
+  }
+  float t = s[0];
+#pragma unroll
+  for (int i = 1; i < N; ++i) t = __builtin_fmaxf(t, s[i]);
+  if (MODE == kModePlain) t *= a.score_mul;
+  if (MODE == kModeCap && raw) t = small_cap(a, t, 0.f);
+  *top = t;
+  return raw;
+}
+
+// 2^(score - ref) of N elements in order: each(i, weight of i, weight of i + 1)
+template <int MODE, int N, class E>
+CP_DEV void weights(const ExtArgs &a, const float (&s)[N], bool raw, float ref, E each) {
+  if (MODE == kModePlain) {
+#pragma unroll
+    for (int i = 0; i < N; i += 2)
+      each(i, fast_exp2(__builtin_fmaf(s[i], a.score_mul, -ref)), fast_exp2(__builtin_fmaf(s[i + 1], a.score_mul, -ref)));
+  } else if (MODE == kModeCap && raw) {
+#pragma unroll
+    for (int i = 0; i < N; i += 2) each(i, fast_exp2(small_cap(a, s[i], ref)), fast_exp2(small_cap(a, s[i + 1], ref)));
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; i += 2) each(i, fast_exp2(s[i] - ref), fast_exp2(s[i + 1] - ref));
+  }
 }
 
 // Of some rows: the first key that any sees and the last plus one, the keys that

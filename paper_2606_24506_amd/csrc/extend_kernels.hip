@@ -19,6 +19,7 @@ template <int E>  // V columns per lane
 __global__ __launch_bounds__(kExtThreads) void extend_vec_kernel(const ExtArgs a) {
   extern __shared__ float qs[];  // [4][d_k]
   const Unit un = find_unit(a);
+  if (un.none) return;
   const ExtReq &rq = *un.rq;
   const GeomK &g = a.g;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -98,34 +99,61 @@ __global__ __launch_bounds__(kExtThreads) void extend_vec_kernel(const ExtArgs a
 
 // ----------------------------------------------------------------- join
 
-// One wave per row: weights 2^(lse_s - max) of the ranges, then the columns.
+// Weights 2^(lse_s - max) of the ranges of a row, then the columns: a thread takes
+// four columns of every `lanes`-th range, with four loads in flight, and the lanes'
+// sums meet in LDS. A workgroup takes 256 / (d_v / 4 * lanes) rows.
 __global__ __launch_bounds__(kExtThreads) void ext_merge_kernel(const ExtMergeArgs a) {
-  const int lane = threadIdx.x & 63;
-  const uint32_t row = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int r = sorted_search(a.n_req, row, [&](int i) { return a.req[i].row_begin; });
+  __shared__ float part[kExtThreads][4];
+  __shared__ float lsum[kExtThreads];
+  const uint32_t dv4 = (uint32_t)a.d_v / 4, per_row = dv4 * (uint32_t)a.lanes;
+  const uint32_t sub = threadIdx.x / per_row, t = threadIdx.x - sub * per_row, c = t % dv4, ln = t / dv4;
+  const uint32_t row = blockIdx.x * (kExtThreads / per_row) + sub;
+  // the request of each thread's row: rows of a workgroup may belong to two
+  int r = 0;
+  while (r + 1 < a.n_req && a.req[r + 1].row_begin <= row) ++r;
   const ExtMergeArgs::Req &rq = a.req[r];
   const uint32_t i = row - rq.row_begin;
-  if (i >= rq.rows) return;
-  const uint64_t pr = (rq.ws_row + i) * rq.splits;
+  const bool valid = i < rq.rows;
+  const uint64_t pr = (rq.ws_row + (valid ? i : 0u)) * rq.splits;
   float mx = -INFINITY;
-  for (uint32_t s = lane; s < rq.splits; s += 64) mx = fmaxf(mx, a.ws_l[pr + s]);
-  mx = wave_max(mx);
+  if (valid)
+    for (uint32_t s = 0; s < rq.splits; ++s) mx = fmaxf(mx, a.ws_l[pr + s]);
   const float ref = mx == -INFINITY ? 0.f : mx;
   float sum = 0.f;
-  for (uint32_t s = lane; s < rq.splits; s += 64) sum += fast_exp2(a.ws_l[pr + s] - ref);
-  sum = wave_sum(sum);
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  const f32x4 *const o = reinterpret_cast<const f32x4 *>(a.ws_o) + pr * dv4 + c;
+  if (valid)
+    for (uint32_t s0 = ln; s0 < rq.splits; s0 += 4 * (uint32_t)a.lanes) {
+      f32x4 v[4];
+      float w[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const uint32_t s = s0 + u * (uint32_t)a.lanes;
+        w[u] = s < rq.splits ? fast_exp2(a.ws_l[pr + s] - ref) : 0.f;
+        v[u] = s < rq.splits ? o[(uint64_t)s * dv4] : f32x4{0.f, 0.f, 0.f, 0.f};
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        sum += w[u];
+        if (w[u] > 0.f) acc += w[u] * v[u];  // (a range that saw nothing has nothing to add)
+      }
+    }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) part[threadIdx.x][k] = acc[k];
+  lsum[threadIdx.x] = sum;
+  __syncthreads();
+  if (!valid || ln != 0) return;
+  for (uint32_t k = 1; k < (uint32_t)a.lanes; ++k) {
+    sum += lsum[threadIdx.x + k * dv4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[e] += part[threadIdx.x + k * dv4][e];
+  }
   const bool none = sum == 0.f;
   const float inv = none ? 0.f : 1.f / sum;
-  const uint32_t dv = (uint32_t)a.d_v;
-  for (uint32_t c = lane; c < dv; c += 64) {
-    float acc = 0.f;
-    for (uint32_t s = 0; s < rq.splits; ++s) {
-      const float w = fast_exp2(a.ws_l[pr + s] - ref);
-      if (w > 0.f) acc = __builtin_fmaf(w, a.ws_o[(pr + s) * dv + c], acc);
-    }
-    a.out[(rq.out_row + i) * dv + c] = (uint16_t)f32_to_bf16(acc * inv);
-  }
-  if (lane == 0) a.lse[rq.out_row + i] = none ? -INFINITY : (mx + fast_log2(sum)) * kLn2;
+  const uint64_t orow = rq.out_row + i;
+  *reinterpret_cast<uint2 *>(a.out + orow * (uint32_t)a.d_v + 4 * c) =
+      bf16x4_bits(acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
+  if (c == 0) a.lse[orow] = none ? -INFINITY : (mx + fast_log2(sum)) * kLn2;
 }
 
 hipError_t launch_extend(const ExtArgs &a, int32_t kind, hipStream_t stream) {
@@ -151,9 +179,14 @@ hipError_t launch_extend(const ExtArgs &a, int32_t kind, hipStream_t stream) {
   return hipGetLastError();
 }
 
-hipError_t launch_ext_merge(const ExtMergeArgs &a, uint32_t rows, hipStream_t stream) {
+hipError_t launch_ext_merge(const ExtMergeArgs &in, uint32_t rows, uint32_t most_splits, hipStream_t stream) {
   if (rows == 0) return hipSuccess;
-  hipLaunchKernelGGL(ext_merge_kernel, dim3((rows + 3) / 4), dim3(kExtThreads), 0, stream, a);
+  ExtMergeArgs a = in;
+  const int dv4 = a.d_v / 4;
+  a.lanes = 1;
+  while (a.lanes * 2 * dv4 <= kExtThreads && (uint32_t)a.lanes < most_splits) a.lanes *= 2;
+  const uint32_t per = (uint32_t)(kExtThreads / (dv4 * a.lanes));
+  hipLaunchKernelGGL(ext_merge_kernel, dim3((rows + per - 1) / per), dim3(kExtThreads), 0, stream, a);
   return hipGetLastError();
 }
 

@@ -59,6 +59,7 @@ __global__ __launch_bounds__(64 * ExtMla::WAVES, 2) void extend_mla_kernel(const
   __shared__ uint32_t shared_u[C::WAVES][4];
   uint32_t *const ptab = reinterpret_cast<uint32_t *>(lds + C::OFF_TAB);
   const Unit un = find_unit(a);
+  if (un.none) return;
   const ExtReq &rq = *un.rq;
   const GeomK &g = a.g;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -193,22 +194,10 @@ __global__ __launch_bounds__(64 * ExtMla::WAVES, 2) void extend_mla_kernel(const
       __syncthreads();
     }
     if (!busy) continue;
-    shape_scores<MODE, 8>(a, reinterpret_cast<float(&)[8]>(sc), slope, x.pos, k0, s * C::KEYS + C::KEYS <= ws.pos + 1,
-                          [](int i) { return 16 * (i / 4) + i % 4; });
-    if (mix) {
-      const uint32_t lo = x.lo - k0, n = x.hi - x.lo;
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if ((uint32_t)(16 * u + i) - lo >= n) sc[u][i] = -INFINITY;
-    }
-    float t = sc[0][0];
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) t = __builtin_fmaxf(t, sc[u][i]);
-    if (MODE == kModePlain) t *= a.score_mul;
+    auto &flat = reinterpret_cast<float(&)[8]>(sc);
+    float t;
+    const bool raw = scores_of<MODE, 8>(a, flat, slope, x, k0, s * C::KEYS + C::KEYS <= ws.pos + 1, mix,
+                                        [](int i) { return 16 * (i / 4) + i % 4; }, &t);
     if (__builtin_amdgcn_ballot_w64(t > m + kLazy || (m == -INFINITY && t > m))) {
       const float mt = xor_max_16_32(t);
       const float mn = mt > m + kLazy || m == -INFINITY ? __builtin_fmaxf(mt, m) : m;
@@ -220,12 +209,10 @@ __global__ __launch_bounds__(64 * ExtMla::WAVES, 2) void extend_mla_kernel(const
     }
     const float ref = m == -INFINITY ? 0.f : m;
     uint32_t pw[4];
-#pragma unroll
-    for (int i = 0; i < 8; i += 2) {
-      const float p0 = weight<MODE>(a, sc[i / 4][i % 4], ref), p1 = weight<MODE>(a, sc[i / 4][i % 4 + 1], ref);
+    weights<MODE, 8>(a, flat, raw, ref, [&](int i, float p0, float p1) {
       l += p0 + p1;
       pw[i / 2] = pack_bf16x2(p0, p1);
-    }
+    });
     const bf16x8 pf = __builtin_bit_cast(bf16x8, u32x4e{pw[0], pw[1], pw[2], pw[3]});
 #pragma unroll
     for (int d = 0; d < C::DB; ++d) o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v_frag(tb, d), pf, o[d], 0, 0, 0);

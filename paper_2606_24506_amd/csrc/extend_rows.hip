@@ -57,6 +57,7 @@ __global__ __launch_bounds__(kExtThreads, 2) void extend_rows_kernel(const ExtAr
   __shared__ uint32_t shared_u[4][4];
   __shared__ float stats[2][4][32];  // RW 1: the waves' m and l
   const Unit un = find_unit(a);
+  if (un.none) return;
   const ExtReq &rq = *un.rq;
   const GeomK &g = a.g;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -189,23 +190,11 @@ __global__ __launch_bounds__(kExtThreads, 2) void extend_rows_kernel(const ExtAr
     }
     // element i of block kb: key b0 + 32 kb + 8 (i / 4) + 4 half + i % 4
     const uint32_t k0 = b0 + 4 * half;
-    shape_scores<MODE, 16 * C::KB>(a, reinterpret_cast<float(&)[16 * C::KB]>(sc), slope, x.pos, k0,
-                                   b0 + C::KW <= ws.pos + 1,
-                                   [](int i) { return 32 * (i / 16) + 8 * (i % 16 / 4) + i % 4; });
-    if (b0 < ws.all_lo || b0 + C::KW > ws.all_hi) {  // some row of the wave does not see some key
-      const uint32_t lo = x.lo - k0, n = x.hi - x.lo;
-#pragma unroll
-      for (int kb = 0; kb < C::KB; ++kb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if ((uint32_t)(32 * kb + 8 * (i / 4) + i % 4) - lo >= n) sc[kb][i] = -INFINITY;
-    }
-    float t = sc[0][0];
-#pragma unroll
-    for (int kb = 0; kb < C::KB; ++kb)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) t = __builtin_fmaxf(t, sc[kb][i]);
-    if (MODE == kModePlain) t *= a.score_mul;
+    const bool hide = b0 < ws.all_lo || b0 + C::KW > ws.all_hi;
+    auto &flat = reinterpret_cast<float(&)[16 * C::KB]>(sc);
+    float t;
+    const bool raw = scores_of<MODE, 16 * C::KB>(a, flat, slope, x, k0, b0 + C::KW <= ws.pos + 1, hide,
+                                                 [](int i) { return 32 * (i / 16) + 8 * (i % 16 / 4) + i % 4; }, &t);
     // the reference moves when some row's maximum passes it by 2^kLazy
     if (__builtin_amdgcn_ballot_w64(t > m + kLazy || (m == -INFINITY && t > m))) {
       const float mt = __builtin_fmaxf(t, other_half(t));
@@ -218,23 +207,19 @@ __global__ __launch_bounds__(kExtThreads, 2) void extend_rows_kernel(const ExtAr
     }
     const float ref = m == -INFINITY ? 0.f : m;
     uint32_t pw[C::NP][C::KB][8];  // two probabilities each, operand order
-#pragma unroll
-    for (int kb = 0; kb < C::KB; ++kb)
-#pragma unroll
-      for (int i = 0; i < 16; i += 2) {
-        const float p0 = weight<MODE>(a, sc[kb][i], ref), p1 = weight<MODE>(a, sc[kb][i + 1], ref);
-        l += p0 + p1;
-        if constexpr (C::NP == 1) {
-          pw[0][kb][i / 2] = pack_bf16x2(p0, p1);
-        } else {
-          // leading 8 bits, and the rest rounded: together 16 bits and a half step
-          const uint32_t h0 = __float_as_uint(p0) & 0xFFFF0000u, h1 = __float_as_uint(p1) & 0xFFFF0000u;
-          pw[0][kb][i / 2] = upper_halves(h0, h1);
-          // (kept above zero: an infinite V times 0 would be NaN)
-          pw[1][kb][i / 2] = pack_bf16x2(__builtin_fmaxf(p0 - __uint_as_float(h0), 1e-37f),
-                                         __builtin_fmaxf(p1 - __uint_as_float(h1), 1e-37f));
-        }
+    weights<MODE, 16 * C::KB>(a, flat, raw, ref, [&](int i, float p0, float p1) {
+      l += p0 + p1;
+      if constexpr (C::NP == 1) {
+        pw[0][i / 16][i % 16 / 2] = pack_bf16x2(p0, p1);
+      } else {
+        // leading 8 bits, and the rest rounded: together 16 bits and a half step
+        const uint32_t h0 = __float_as_uint(p0) & 0xFFFF0000u, h1 = __float_as_uint(p1) & 0xFFFF0000u;
+        pw[0][i / 16][i % 16 / 2] = upper_halves(h0, h1);
+        // (kept above zero: an infinite V times 0 would be NaN)
+        pw[1][i / 16][i % 16 / 2] = pack_bf16x2(__builtin_fmaxf(p0 - __uint_as_float(h0), 1e-37f),
+                                                __builtin_fmaxf(p1 - __uint_as_float(h1), 1e-37f));
       }
+    });
     if (RW == 1 && more) load_values();
 #pragma unroll
     for (int kb = 0; kb < C::KB; ++kb)
