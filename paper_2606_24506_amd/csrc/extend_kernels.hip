@@ -99,13 +99,14 @@ __global__ __launch_bounds__(kExtThreads) void extend_vec_kernel(const ExtArgs a
 
 // ----------------------------------------------------------------- join
 
-// Weights 2^(lse_s - max) of the ranges of a row, then the columns: a thread takes
-// four columns of every `lanes`-th range, with four loads in flight, and the lanes'
-// sums meet in LDS. A workgroup takes 256 / (d_v / 4 * lanes) rows.
+// Weights 2^(lse_s - max) of a row's ranges, then the columns: a thread takes four
+// columns of every `lanes`-th range, four loads in flight, with a running maximum as
+// over keys; the lanes' sums meet in LDS. A workgroup takes 256 / (d_v / 4 *
+// lanes) rows.
 __global__ __launch_bounds__(kExtThreads) void ext_merge_kernel(const ExtMergeArgs a) {
-  __shared__ float part[kExtThreads][4];
-  __shared__ float lsum[kExtThreads];
-  const uint32_t dv4 = (uint32_t)a.d_v / 4, per_row = dv4 * (uint32_t)a.lanes;
+  __shared__ float part[4][kExtThreads];
+  __shared__ float stat[2][kExtThreads];
+  const uint32_t dv4 = (uint32_t)a.d_v / 4, lanes = (uint32_t)a.lanes, per_row = dv4 * lanes;
   const uint32_t sub = threadIdx.x / per_row, t = threadIdx.x - sub * per_row, c = t % dv4, ln = t / dv4;
   const uint32_t row = blockIdx.x * (kExtThreads / per_row) + sub;
   // the request of each thread's row: rows of a workgroup may belong to two
@@ -115,38 +116,50 @@ __global__ __launch_bounds__(kExtThreads) void ext_merge_kernel(const ExtMergeAr
   const uint32_t i = row - rq.row_begin;
   const bool valid = i < rq.rows;
   const uint64_t pr = (rq.ws_row + (valid ? i : 0u)) * rq.splits;
-  float mx = -INFINITY;
-  if (valid)
-    for (uint32_t s = 0; s < rq.splits; ++s) mx = fmaxf(mx, a.ws_l[pr + s]);
-  const float ref = mx == -INFINITY ? 0.f : mx;
-  float sum = 0.f;
+  const uint32_t n = valid ? rq.splits : 0u;
+  float m = -INFINITY, sum = 0.f;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
   const f32x4 *const o = reinterpret_cast<const f32x4 *>(a.ws_o) + pr * dv4 + c;
-  if (valid)
-    for (uint32_t s0 = ln; s0 < rq.splits; s0 += 4 * (uint32_t)a.lanes) {
-      f32x4 v[4];
-      float w[4];
+  for (uint32_t s0 = ln; s0 < n; s0 += 4 * lanes) {
+    f32x4 v[4];
+    float e[4];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const uint32_t s = s0 + u * (uint32_t)a.lanes;
-        w[u] = s < rq.splits ? fast_exp2(a.ws_l[pr + s] - ref) : 0.f;
-        v[u] = s < rq.splits ? o[(uint64_t)s * dv4] : f32x4{0.f, 0.f, 0.f, 0.f};
-      }
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        sum += w[u];
-        if (w[u] > 0.f) acc += w[u] * v[u];  // (a range that saw nothing has nothing to add)
-      }
+    for (int u = 0; u < 4; ++u) {
+      const uint32_t s = s0 + u * lanes;
+      e[u] = s < n ? a.ws_l[pr + s] : -INFINITY;
+      v[u] = s < n ? o[(uint64_t)s * dv4] : f32x4{0.f, 0.f, 0.f, 0.f};
     }
+    float mn = m;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) part[threadIdx.x][k] = acc[k];
-  lsum[threadIdx.x] = sum;
+    for (int u = 0; u < 4; ++u) mn = fmaxf(mn, e[u]);
+    const float ref = mn == -INFINITY ? 0.f : mn, al = fast_exp2(m - ref);
+    m = mn;
+    sum *= al;
+    acc *= al;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const float w = fast_exp2(e[u] - ref);
+      sum += w;
+      if (w > 0.f) acc += w * v[u];  // (a range that saw nothing has nothing to add)
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) part[k][threadIdx.x] = acc[k];
+  stat[0][threadIdx.x] = m;
+  stat[1][threadIdx.x] = sum;
   __syncthreads();
   if (!valid || ln != 0) return;
-  for (uint32_t k = 1; k < (uint32_t)a.lanes; ++k) {
-    sum += lsum[threadIdx.x + k * dv4];
+  float mx = m;
+  for (uint32_t k = 1; k < lanes; ++k) mx = fmaxf(mx, stat[0][threadIdx.x + k * dv4]);
+  const float ref = mx == -INFINITY ? 0.f : mx, own = fast_exp2(m - ref);
+  sum *= own;
+  acc *= own;
+  for (uint32_t k = 1; k < lanes; ++k) {
+    const uint32_t at = threadIdx.x + k * dv4;
+    const float w = fast_exp2(stat[0][at] - ref);
+    sum += w * stat[1][at];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) acc[e] += part[threadIdx.x + k * dv4][e];
+    for (int q = 0; q < 4; ++q) acc[q] += w * part[q][at];
   }
   const bool none = sum == 0.f;
   const float inv = none ? 0.f : 1.f / sum;

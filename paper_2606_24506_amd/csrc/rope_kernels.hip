@@ -70,7 +70,8 @@ CP_DEV void rope_item(const RopeArgs &a, const RopePart &p, int64_t tok, uint32_
     E::store(dr + e0, rope_first(x, y, turn[j]));
     E::store(dr + e1, rope_second(x, y, turn[j]));
   } else if (half) {
-    const u32x4r x = *(const u32x4r *)(sr + j * V), y = *(const u32x4r *)(sr + pairs + j * V);
+    const u32x4r x = __builtin_nontemporal_load((const u32x4r *)(sr + j * V)),
+                 y = __builtin_nontemporal_load((const u32x4r *)(sr + pairs + j * V));
     float u[V], w[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
