@@ -166,13 +166,21 @@ __global__ __launch_bounds__(64 * ExtMla::WAVES, 2) void extend_mla_kernel(const
     if (busy) {
 #pragma unroll
       for (int u = 0; u < 2; ++u) sc[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+      // fragments are read KD products ahead, in this order (left to itself the
+      // compiler reads one or two ahead, and the products wait for LDS)
+      constexpr int KD = 5;
+      bf16x8 kf[KD + 1];
+      auto kread = [&](int e) {
+        return *reinterpret_cast<const bf16x8 *>(tb + kat[e / 2 % 2] + 128 * (e / 4) + 16 * (e % 2) * C::ROW);
+      };
 #pragma unroll
-      for (int ks = 0; ks < C::KS; ++ks)
+      for (int e = 0; e < KD; ++e) kf[e] = kread(e);
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const bf16x8 kf = *reinterpret_cast<const bf16x8 *>(tb + kat[ks % 2] + 128 * (ks / 2) + 16 * u * C::ROW);
-          sc[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[ks], sc[u], 0, 0, 0);
-        }
+      for (int e = 0; e < 2 * C::KS; ++e) {
+        if (e + KD < 2 * C::KS) kf[(e + KD) % (KD + 1)] = kread(e + KD);
+        __builtin_amdgcn_sched_barrier(0);
+        sc[e % 2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[e % (KD + 1)], qf[e / 2], sc[e % 2], 0, 0, 0);
+      }
     }
     if (mix) {
       // infinities and NaN of V stay out of the products (0 times those is
@@ -194,6 +202,12 @@ __global__ __launch_bounds__(64 * ExtMla::WAVES, 2) void extend_mla_kernel(const
       __syncthreads();
     }
     if (!busy) continue;
+    // the first fragments of V arrive during the softmax
+    constexpr int VD = 4;
+    bf16x8 vf[VD + 1];
+#pragma unroll
+    for (int d = 0; d < VD; ++d) vf[d] = v_frag(tb, d);
+    __builtin_amdgcn_sched_barrier(0);
     auto &flat = reinterpret_cast<float(&)[8]>(sc);
     float t;
     const bool raw = scores_of<MODE, 8>(a, flat, slope, x, k0, s * C::KEYS + C::KEYS <= ws.pos + 1, mix,
@@ -215,7 +229,11 @@ __global__ __launch_bounds__(64 * ExtMla::WAVES, 2) void extend_mla_kernel(const
     });
     const bf16x8 pf = __builtin_bit_cast(bf16x8, u32x4e{pw[0], pw[1], pw[2], pw[3]});
 #pragma unroll
-    for (int d = 0; d < C::DB; ++d) o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v_frag(tb, d), pf, o[d], 0, 0, 0);
+    for (int d = 0; d < C::DB; ++d) {
+      if (d + VD < C::DB) vf[(d + VD) % (VD + 1)] = v_frag(tb, d + VD);
+      __builtin_amdgcn_sched_barrier(0);
+      o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[d % (VD + 1)], pf, o[d], 0, 0, 0);
+    }
   }
 
   // ---- infinities and NaN of V that not every row sees: which rows see one is a

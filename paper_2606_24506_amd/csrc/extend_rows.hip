@@ -177,6 +177,7 @@ __global__ __launch_bounds__(kExtThreads, 2) void extend_rows_kernel(const ExtAr
     }
     const char *const kt = lds + buf * (2 * C::TILE), *const vt = kt + C::TILE;
     f32x16 sc[C::KB];
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int kb = 0; kb < C::KB; ++kb) {
 #pragma unroll
@@ -188,6 +189,7 @@ __global__ __launch_bounds__(kExtThreads, 2) void extend_rows_kernel(const ExtAr
         sc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks], sc[kb], 0, 0, 0);
       }
     }
+    __builtin_amdgcn_s_setprio(0);
     // element i of block kb: key b0 + 32 kb + 8 (i / 4) + 4 half + i % 4
     const uint32_t k0 = b0 + 4 * half;
     const bool hide = b0 < ws.all_lo || b0 + C::KW > ws.all_hi;
@@ -221,6 +223,7 @@ __global__ __launch_bounds__(kExtThreads, 2) void extend_rows_kernel(const ExtAr
       }
     });
     if (RW == 1 && more) load_values();
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int kb = 0; kb < C::KB; ++kb)
 #pragma unroll
@@ -235,6 +238,7 @@ __global__ __launch_bounds__(kExtThreads, 2) void extend_rows_kernel(const ExtAr
                                                            o[d], 0, 0, 0);
           }
         }
+    __builtin_amdgcn_s_setprio(0);
   };
 
   // ---- the steps
