@@ -179,16 +179,17 @@ __global__ __launch_bounds__(kExtThreads, 2) void extend_rows_kernel(const ExtAr
     f32x16 sc[C::KB];
     __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-    for (int kb = 0; kb < C::KB; ++kb) {
+    for (int kb = 0; kb < C::KB; ++kb)
 #pragma unroll
       for (int i = 0; i < 16; ++i) sc[kb][i] = 0.f;
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+      for (int kb = 0; kb < C::KB; ++kb) {
         const int row = 32 * kb + col;
         const bf16x8 kf = *reinterpret_cast<const bf16x8 *>(kt + row * C::ROW + 16 * k_piece<D>(row, 2 * ks + half));
         sc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks], sc[kb], 0, 0, 0);
       }
-    }
     __builtin_amdgcn_s_setprio(0);
     // element i of block kb: key b0 + 32 kb + 8 (i / 4) + 4 half + i % 4
     const uint32_t k0 = b0 + 4 * half;
