@@ -15,33 +15,42 @@ namespace cp {
 // a product, and four SIMDs ask for twice what LDS gives, so the products run
 // at half their rate at most.
 //
-// KV goes from the pool to LDS directly, NBUF - 1 steps ahead: the lane for a
-// 16-byte place of LDS loads the piece that belongs there, with the pieces of a
-// row swapped by its number (K reads 16 rows at one piece, V reads 8 rows at 2).
+// KV goes from the pool to LDS directly, NBUF - 1 steps ahead, a load for a row's
+// latent part and one for eight rows' rotary parts. The lane for a 16-byte place of
+// LDS loads the piece that belongs there: the pieces of latent row r are swapped by
+// 2 r mod 16, those of rotary row r by r & 6, and both the reads of K (16 rows at
+// one piece) and of V (8 rows at two) meet no bank twice.
 struct ExtMla {
   static constexpr int DK = 576, DV = 512, KEYS = 32, WAVES = 8;
-  static constexpr int ROW = 2 * DK;       // bytes
-  static constexpr int CPR = ROW / 16;     // 16-byte pieces of a row
-  static constexpr int TILE = KEYS * ROW;  // 36 KiB
+  static constexpr int ROW = 2 * DK, MROW = 2 * DV, RROW = ROW - MROW;  // bytes: in the pool; latent; rotary
+  static constexpr int RING = KEYS * MROW;  // a step's latent part, the rotary part behind it
+  static constexpr int TILE = KEYS * ROW;   // 36 KiB
   static constexpr int NBUF = 3;
-  static constexpr int LOADS = TILE / 1024;  // of 1 KiB a step: waves 0 to 3 take five, the others four
   static constexpr int KS = DK / 32, DB = DV / 16;
-  static constexpr int PTAB = 1024;          // page-table entries kept in LDS
+  static constexpr int MLOADS = KEYS / WAVES;  // latent rows of a wave; waves 0 to 3 load eight rotary rows each too
+  static constexpr int PTAB = 1024;            // page-table entries kept in LDS
   static constexpr int OFF_TAB = NBUF * TILE;
   static constexpr int LDS = OFF_TAB + 4 * PTAB;
-  static_assert(LOADS == 36 && LDS + 512 <= 163840, "LDS budget");
+  static_assert(MROW == 1024 && RROW == 128 && LDS + 512 <= 163840, "LDS budget");
 };
-
-// How the pieces of a row are swapped: within each eight by this number.
-CP_DEV int mla_swap(int row) {
-  const int j = (row >> 1) & 7;
-  return ((j & 3) << 1) | (j >> 2);
-}
+CP_DEV int latent_swap(int row) { return (2 * row) & 15; }
+CP_DEV int rotary_swap(int row) { return row & 6; }
 
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
-// 16 bytes a lane from its own address to LDS at base + 16 lane; with the
+// 16 bytes a lane from base + offset to LDS at lds_base + 16 lane; with the
 // non-temporal policy where KV is read once.
+template <bool NT>
+CP_DEV void row_load_lds(uint64_t base, uint32_t offset, uint32_t lds_base) {
+  lds_base = __builtin_amdgcn_readfirstlane(lds_base);
+  if constexpr (NT)
+    asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, %2 nt" ::"v"(offset), "s"(lds_base), "s"(base)
+                 : "memory", "m0");
+  else
+    asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, %2" ::"v"(offset), "s"(lds_base), "s"(base)
+                 : "memory", "m0");
+}
+// The same, every lane with an address of its own.
 template <bool NT>
 CP_DEV void lane_load_lds(uint64_t addr, uint32_t lds_base) {
   lds_base = __builtin_amdgcn_readfirstlane(lds_base);
@@ -97,14 +106,17 @@ __global__ __launch_bounds__(64 * ExtMla::WAVES, 2) void extend_mla_kernel(const
     slot *= C::ROW;
     const uint32_t buf = lds_addr(lds) + ((s - s0) % C::NBUF) * C::TILE;
 #pragma unroll
-    for (int j = 0; j < 5; ++j) {
-      const uint32_t load = wave + C::WAVES * j;
-      if (load >= C::LOADS) break;
-      const uint32_t e = load * 64 + ln, row = e / C::CPR, p = e - row * C::CPR;
-      const uint32_t piece = p ^ mla_swap((int)row);
-      const uint64_t base = (uint64_t)(uint32_t)__shfl((int)pte, (int)row, 64) << 8;
-      const uint32_t off = (uint32_t)__shfl((int)slot, (int)row, 64) + 16 * piece;
-      lane_load_lds<NT>((uint64_t)(uintptr_t)a.pool + base + off, buf + load * 1024);
+    for (int j = 0; j < C::MLOADS; ++j) {
+      const int row = C::MLOADS * wave + j;
+      const uint64_t base = (uint64_t)(uintptr_t)a.pool + ((uint64_t)(uint32_t)__builtin_amdgcn_readlane(pte, row) << 8) +
+                            (uint32_t)__builtin_amdgcn_readlane(slot, row);
+      row_load_lds<NT>(base, 16u * (uint32_t)(ln ^ latent_swap(row)), buf + row * C::MROW);
+    }
+    if (wave < 4) {
+      const int row = 8 * wave + (ln >> 3);
+      const uint64_t base = (uint64_t)(uintptr_t)a.pool + ((uint64_t)(uint32_t)__shfl((int)pte, row, 64) << 8) +
+                            (uint32_t)__shfl((int)slot, row, 64) + C::MROW + 16 * ((ln & 7) ^ rotary_swap(row));
+      lane_load_lds<NT>(base, buf + C::RING + 8 * wave * C::RROW);
     }
   };
 
@@ -124,26 +136,30 @@ __global__ __launch_bounds__(64 * ExtMla::WAVES, 2) void extend_mla_kernel(const
 #pragma unroll
   for (int d = 0; d < C::DB; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  // LDS byte offsets in a step's tile. K of keys 16 u + col, dims 32 ks + 8 quad: at
-  // kat[ks % 2] + 128 (ks / 2) + 16 u rows; V of key 4 quad + col / 4 (and 16 on),
-  // columns 16 d + 4 (col % 4): at vat[d % 4] + 128 (d / 4). (Formed so, the
-  // swapped pieces cost six registers, and not one for every fragment.)
-  uint32_t kat[2], vat[4];
-  {
-    const int vr = 4 * quad + (col >> 2);
+  // LDS byte offsets in a step's tile, formed afresh in each step (kept through the loop
+  // they would cost 13 registers). K of keys 16 u + col, dims 32 ks + 8 quad: latent at
+  // k[ks % 4] + 256 (ks / 4) + 16 u rows, rotary (ks 16, 17) at r ^ 64 (ks - 16) + 16 u
+  // rows.
+  struct KAt {
+    uint32_t k[4], r;
+  };
+  auto k_at = [] {
+    const LaneIds L = lane_ids();
+    KAt x;
+    x.r = (uint32_t)(C::RING + L.col * C::RROW + 16 * (L.quad ^ rotary_swap(L.col)));
 #pragma unroll
-    for (int k = 0; k < 2; ++k) kat[k] = (uint32_t)(col * C::ROW + 16 * ((4 * k + quad) ^ mla_swap(col)));
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-      vat[k] = (uint32_t)(vr * C::ROW + 16 * ((2 * k + ((col >> 1) & 1)) ^ mla_swap(vr)) + 8 * (col & 1));
-  }
-  // V^T of a step's keys and block d of 16 columns
-  auto v_frag = [&](const char *tb, int d) {
+    for (int k = 0; k < 4; ++k) x.k[k] = (uint32_t)(L.col * C::MROW + 16 * ((4 * k + L.quad) ^ latent_swap(L.col)));
+    return x;
+  };
+  // V^T of a step's keys 4 quad + {0..3} and 16 on, and block d of 16 columns
+  auto v_frag = [&](const char *tb, const LaneIds &L, int d) {
+    const int vr = 4 * L.quad + (L.col >> 2);
+    const char *const at = tb + vr * C::MROW + 8 * (L.col & 1) +
+                           16 * ((2 * (d % 8) + ((L.col >> 1) & 1)) ^ latent_swap(vr)) + 256 * (d / 8);
     s16x4 f[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h)
-      f[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-          (__attribute__((address_space(3))) s16x4 *)(tb + vat[d % 4] + 128 * (d / 4) + 16 * h * C::ROW));
+      f[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(at + 16 * h * C::MROW));
     return __builtin_bit_cast(bf16x8, __builtin_shufflevector(f[0], f[1], 0, 1, 2, 3, 4, 5, 6, 7));
   };
   // Does some row of the workgroup not see some key of step s?
@@ -168,10 +184,13 @@ __global__ __launch_bounds__(64 * ExtMla::WAVES, 2) void extend_mla_kernel(const
       for (int u = 0; u < 2; ++u) sc[u] = f32x4{0.f, 0.f, 0.f, 0.f};
       // fragments are read KD products ahead, in this order (left to itself the
       // compiler reads one or two ahead, and the products wait for LDS)
-      constexpr int KD = 5;
+      constexpr int KD = 4;
       bf16x8 kf[KD + 1];
+      const KAt at = k_at();
       auto kread = [&](int e) {
-        return *reinterpret_cast<const bf16x8 *>(tb + kat[e / 2 % 2] + 128 * (e / 4) + 16 * (e % 2) * C::ROW);
+        const int ks = e / 2, u = e % 2;
+        return *reinterpret_cast<const bf16x8 *>(
+            tb + (ks < 16 ? at.k[ks % 4] + 256 * (ks / 4) + 16 * u * C::MROW : (at.r ^ (64 * (ks - 16))) + 16 * u * C::RROW));
       };
 #pragma unroll
       for (int e = 0; e < KD; ++e) kf[e] = kread(e);
@@ -188,7 +207,7 @@ __global__ __launch_bounds__(64 * ExtMla::WAVES, 2) void extend_mla_kernel(const
       // the steps that had any are gone through again at the end
       __syncthreads();
       bool any = false;
-      for (int e = threadIdx.x; e < C::TILE / 16; e += 64 * C::WAVES) {
+      for (int e = threadIdx.x; e < C::RING / 16; e += 64 * C::WAVES) {
         u32x4e *const w = reinterpret_cast<u32x4e *>(tb) + e;
         if (any_special(*w)) {
           any = true;
@@ -205,8 +224,9 @@ __global__ __launch_bounds__(64 * ExtMla::WAVES, 2) void extend_mla_kernel(const
     // the first fragments of V arrive during the softmax
     constexpr int VD = 4;
     bf16x8 vf[VD + 1];
+    const LaneIds vl = lane_ids();
 #pragma unroll
-    for (int d = 0; d < VD; ++d) vf[d] = v_frag(tb, d);
+    for (int d = 0; d < VD; ++d) vf[d] = v_frag(tb, vl, d);
     __builtin_amdgcn_sched_barrier(0);
     auto &flat = reinterpret_cast<float(&)[8]>(sc);
     float t;
@@ -230,7 +250,7 @@ __global__ __launch_bounds__(64 * ExtMla::WAVES, 2) void extend_mla_kernel(const
     const bf16x8 pf = __builtin_bit_cast(bf16x8, u32x4e{pw[0], pw[1], pw[2], pw[3]});
 #pragma unroll
     for (int d = 0; d < C::DB; ++d) {
-      if (d + VD < C::DB) vf[(d + VD) % (VD + 1)] = v_frag(tb, d + VD);
+      if (d + VD < C::DB) vf[(d + VD) % (VD + 1)] = v_frag(tb, vl, d + VD);
       __builtin_amdgcn_sched_barrier(0);
       o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[d % (VD + 1)], pf, o[d], 0, 0, 0);
     }
@@ -263,6 +283,7 @@ __global__ __launch_bounds__(64 * ExtMla::WAVES, 2) void extend_mla_kernel(const
       if (!busy) continue;
       const char *const tb = lds + ((s - s0) % C::NBUF) * C::TILE;
       const uint32_t k0 = s * C::KEYS + 4 * quad, lo = x.lo - k0, n = x.hi - x.lo;
+      const LaneIds vl = lane_ids();
       u32x4e seen;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
@@ -274,7 +295,7 @@ __global__ __launch_bounds__(64 * ExtMla::WAVES, 2) void extend_mla_kernel(const
 #pragma unroll 1
         for (uint32_t sign = 0; sign < 2; ++sign) {
           f32x4 hit = {0.f, 0.f, 0.f, 0.f};
-          hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(special_ones(v_frag(tb, d), sign),
+          hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(special_ones(v_frag(tb, vl, d), sign),
                                                         __builtin_bit_cast(bf16x8, seen), hit, 0, 0, 0);
 #pragma unroll
           for (int i = 0; i < 4; ++i)
