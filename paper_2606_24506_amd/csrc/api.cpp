@@ -1869,18 +1869,19 @@ namespace {
 
 constexpr int64_t kMaxExtUnits = 1 << 23;  // of one launch
 
-// A planned cp_attn_extend: launches by kernel, with their requests.
+// A planned cp_attn_extend: launches by kernel, and the rows whose ranges are joined.
 struct ExtPlan {
   struct Launch {
     int32_t kind = kXVec;
     std::vector<ExtReq> req;
-    std::vector<int32_t> idx;  // of the call's requests
+    std::vector<ExtMember> member;
     uint32_t units = 0;
   };
   int32_t model = -1;
   Geom geom;
   std::vector<Launch> launches;
-  uint64_t ws_rows = 0;  // partial rows of split requests
+  std::vector<ExtMergeArgs::Req> joins;
+  uint64_t ws_rows = 0;  // partial rows
 };
 
 // The kernel of a request with n_q query tokens (extend.h).
@@ -1893,10 +1894,14 @@ int32_t extend_kind(const Geom &g, int32_t path, int64_t n_q) {
   return g.kind == kMLA && g.latent == 512 && g.rope == 64 ? kXMla : kXVec;
 }
 
-// A request of a call: its kernel, rows of all heads, row tiles per KV head, steps of
-// its longest tile, and the ranges that these are cut into.
+// An item of a call (extend.h): its kernel, rows of all heads, row tiles per KV head,
+// steps of its longest tile, and the ranges that these are cut into.
 struct ExtItem {
   int32_t kind = 0;
+  int32_t first = 0, count = 1;  // requests of the call
+  int32_t group = -1;            // of requests with shared pages: this is their shared item or a tail
+  bool shared = false;
+  int64_t key_lo = 0, key_hi = 0xFFFFFFFFll;
   int64_t rows = 0, tiles = 0, steps = 0, splits = 1;
 };
 
@@ -1908,7 +1913,8 @@ struct ExtItem {
 // partial rows' way to memory and back. Single tokens of 16 requests over 117K
 // tokens: 88 us with 18 steps a range (one turn), 114 with 15, 96 with 9, 140
 // with 45; 2048 tokens of three prompts: 1.19 ms uncut, 1.32 with 64.
-void choose_ranges(const Geom &g, int num_cus, uint64_t cap, std::vector<ExtItem> *items) {
+// Returns the estimate.
+double choose_ranges(const Geom &g, int num_cus, uint64_t cap, std::vector<ExtItem> *items) {
   // us of a step of the kernel with its CUs full, and workgroups of a CU
   static constexpr struct { double us; int per_cu; } kCost[kXKinds] = {
       {2.0, 8}, {1.4, 2}, {2.8, 2}, {2.7, 2}, {4.6, 2}, {2.6, 1}};
@@ -1936,7 +1942,7 @@ void choose_ranges(const Geom &g, int num_cus, uint64_t cap, std::vector<ExtItem
       longest = std::max(longest, len);
       shortest = std::min(shortest, len);
       units += u;
-      if (s > 1) rows += (double)(x.rows + 1) * s;
+      if (s > 1 || x.group >= 0) rows += (double)(x.rows + 1) * s;
     }
     const double join = rows > 0 ? kJoin + rows * g.d_v * 8 / kBytesPerUs : 0;
     const double t = std::max(longest, work / num_cus) + (units > slots ? shortest : 0.0) + join;
@@ -1959,13 +1965,43 @@ void choose_ranges(const Geom &g, int num_cus, uint64_t cap, std::vector<ExtItem
     for (double per = std::floor(most * 0.75); per >= 1 && consider(per); per = std::floor(per * 0.75)) {}
   }
   for (ExtItem &x : *items) x.splits = (int64_t)std::max(1.0, ranges(x, best_per));
+  return best;
+}
+
+// Whole pages that request ids[i] of a call and those right behind it show alike from
+// the start on, and how many requests do (*count, 1 when it is not worth an
+// item): few rows each, which read their keys at the speed of memory, and at least
+// kShareTokens shared tokens.
+constexpr int64_t kShareTokens = 256, kShareRows = 128;
+int64_t shared_run(const cp_pool *p, int32_t n, const int32_t *ids, const int32_t *n_q, int32_t i, int32_t g,
+                   int32_t *count) {
+  const uint32_t *pt = p->st.pte_mirror();
+  const int64_t P = p->st.page_tokens();
+  const Request &a = p->st.req(ids[i]);
+  int64_t pages = a.ctx_len / P;
+  *count = 1;
+  if (n_q[i] * (int64_t)g > kShareRows) return 0;
+  for (int32_t k = i + 1; k < n && *count < kExtMaxReq; ++k) {
+    const Request &b = p->st.req(ids[k]);
+    if (n_q[k] < 1 || n_q[k] * (int64_t)g > kShareRows) break;
+    const uint32_t *x = pt + a.plane_base(a.cursor), *y = pt + b.plane_base(b.cursor);
+    const int64_t most = std::min(pages, b.ctx_len / P);
+    int64_t same = 0;
+    while (same < most && x[same] == y[same] && x[same] != kPendingPte) ++same;
+    // (a request that shares much less than those before starts the next run)
+    if (same * P < kShareTokens || 2 * same < pages) break;
+    pages = same;
+    *count += 1;
+  }
+  return pages;
 }
 
 // Checks a call and plans it, at the contexts the requests will have with
 // extra[i] more tokens (NULL: none). Changes nothing.
 cp_status plan_extend(cp_pool *p, int32_t n, const int32_t *ids, const int32_t *n_q, const int32_t *extra,
                       const void *q, const void *out, const float *lse, const cp_extend_opts &o, ExtPlan *pl) {
-  if (o.softcap < 0.f || !std::isfinite(o.softcap)) return fail(CP_EINVAL, "softcap must be finite and >= 0");
+  if (o.softcap != 0.f && !(o.softcap >= 1e-18f && o.softcap <= 1e18f))
+    return fail(CP_EINVAL, "softcap must be 0 or in [1e-18, 1e18]");
   if (o.window < 0) return fail(CP_EINVAL, "window must be >= 0");
   if (o.num_splits < 0) return fail(CP_EINVAL, "num_splits must be >= 0");
   if (o.path != CP_PATH_AUTO && o.path != CP_PATH_VALU) return fail(CP_EINVAL, "path must be automatic or vector");
@@ -1989,70 +2025,162 @@ cp_status plan_extend(cp_pool *p, int32_t n, const int32_t *ids, const int32_t *
   pl->geom = p->st.model(pl->model);
   const Geom &g = pl->geom;
 
-  // Steps (of ext_tile_keys keys) of each request's longest tile, and tiles.
-  std::vector<ExtItem> it((size_t)n);
-  for (int32_t i = 0; i < n; ++i) {
-    const int64_t ctx = p->st.req(ids[i]).attend_len() + (extra ? extra[i] : 0);
-    ExtItem &x = it[(size_t)i];
-    x.kind = extend_kind(g, o.path, n_q[i]);
+  std::vector<uint32_t> tok((size_t)n, 0u);
+  for (int32_t i = 1; i < n; ++i) tok[(size_t)i] = tok[(size_t)i - 1] + (uint32_t)n_q[i - 1];
+  auto ctx_of = [&](int32_t i) { return p->st.req(ids[i]).attend_len() + (extra ? extra[i] : 0); };
+  // Items: each request, and, another way, with shared pages taken apart.
+  auto item_of = [&](int32_t first, int32_t count, int64_t key_lo, int64_t key_hi) {
+    ExtItem x;
+    x.first = first;
+    x.count = count;
+    x.key_lo = key_lo;
+    x.key_hi = key_hi;
+    int64_t tokens = 0, lo = INT64_MAX, hi = 0;  // keys that may be seen
+    for (int32_t i = first; i < first + count; ++i) {
+      const int64_t ctx = ctx_of(i);
+      tokens += n_q[i];
+      lo = std::min(lo, o.window ? std::max<int64_t>(0, ctx - n_q[i] - o.window + 1) : 0);
+      hi = std::max(hi, ctx);
+    }
+    x.kind = extend_kind(g, o.path, tokens);
     const int64_t rows = ext_tile_rows(x.kind), keys = ext_tile_keys(x.kind);
-    x.rows = (int64_t)n_q[i] * g.hq;
-    x.tiles = ((int64_t)n_q[i] * g.g + rows - 1) / rows;
-    int64_t seen = ctx;
-    if (o.window) seen = std::min<int64_t>(ctx, (int64_t)o.window + std::min<int64_t>(n_q[i], rows / g.g + 2) +
-                                                    (o.prefix ? (int64_t)o.prefix[i] : 0));
-    x.steps = (seen + keys - 1) / keys + (o.window ? 1 : 0);
-  }
+    x.rows = tokens * g.hq;
+    x.tiles = (tokens * g.g + rows - 1) / rows;
+    int64_t seen = std::min(hi, key_hi) - std::max(lo, key_lo);
+    if (o.window)  // of one tile
+      seen = std::min<int64_t>(seen, (int64_t)o.window + std::min<int64_t>(tokens, rows / g.g + 2) +
+                                         (o.prefix ? (int64_t)o.prefix[first] : 0));
+    x.steps = std::max<int64_t>(1, (seen + keys - 1) / keys + (o.window || key_lo ? 1 : 0));
+    return x;
+  };
+  std::vector<ExtItem> it;
+  for (int32_t i = 0; i < n; ++i)
+    if (n_q[i] > 0) it.push_back(item_of(i, 1, 0, 0xFFFFFFFFll));
   const uint64_t cap = p->ws_limit ? p->ws_limit : UINT64_MAX;
+  int32_t groups = 0;
   if (o.num_splits > 0) {
     for (ExtItem &x : it) x.splits = std::max<int64_t>(1, std::min<int64_t>({o.num_splits, x.steps, 4096}));
   } else {
-    choose_ranges(g, p->num_cus, cap, &it);
+    const double t = choose_ranges(g, p->num_cus, cap, &it);
+    // (under a workspace cap: whole; the estimate does not bound the tails' partials)
+    bool look = false;
+    for (int32_t i = 0; i + 1 < n && o.path == CP_PATH_AUTO && !p->ws_limit; ++i) {
+      const Request &a = p->st.req(ids[i]), &b = p->st.req(ids[i + 1]);
+      look = look || (a.pages_used > 0 && b.pages_used > 0 &&
+                      p->st.pte_mirror()[a.plane_base(a.cursor)] == p->st.pte_mirror()[b.plane_base(b.cursor)]);
+    }
+    std::vector<ExtItem> apart;
+    for (int32_t i = 0; look && i < n;) {
+      int32_t count = 1;
+      int64_t pages = 0;
+      if (n_q[i] > 0) pages = shared_run(p, n, ids, n_q, i, g.g, &count);
+      const int64_t keys = pages * p->st.page_tokens();
+      if (count < 2) {
+        if (n_q[i] > 0) apart.push_back(item_of(i, 1, 0, 0xFFFFFFFFll));
+      } else {
+        apart.push_back(item_of(i, count, 0, keys));
+        apart.back().shared = true;
+        apart.back().group = groups;
+        for (int32_t k = i; k < i + count; ++k) {
+          apart.push_back(item_of(k, 1, keys, 0xFFFFFFFFll));
+          apart.back().group = groups;
+        }
+        groups += 1;
+      }
+      i += count;
+    }
+    if (groups > 0 && choose_ranges(g, p->num_cus, cap, &apart) < t)
+      it.swap(apart);
+    else
+      groups = 0;
   }
-  // long requests first: theirs are the longest units
-  std::vector<int32_t> order((size_t)n);
-  for (int32_t i = 0; i < n; ++i) order[(size_t)i] = i;
+  // A group's tails have one number of ranges, and its rows those and the shared item's.
+  struct Group {
+    int64_t shared = 1, tail = 1;
+    uint64_t ws_row = 0;
+    uint32_t tok0 = 0;
+  };
+  std::vector<Group> grp((size_t)groups);
+  for (const ExtItem &x : it)
+    if (x.group >= 0) (x.shared ? grp[(size_t)x.group].shared : grp[(size_t)x.group].tail) =
+        std::max(x.shared ? 1 : grp[(size_t)x.group].tail, x.splits);
+  // Places of partial rows: those of an item's requests together, at a multiple of
+  // their ranges.
+  auto place = [&](int32_t first, int32_t count, int64_t ranges) {
+    ExtMergeArgs::Req m{};
+    for (int32_t i = first; i < first + count; ++i) m.rows += (uint32_t)n_q[i] * (uint32_t)g.hq;
+    m.splits = (uint32_t)ranges;
+    m.ws_row = (pl->ws_rows + (uint64_t)ranges - 1) / (uint64_t)ranges;
+    m.out_row = (uint64_t)tok[(size_t)first] * (uint64_t)g.hq;
+    pl->ws_rows = (m.ws_row + m.rows) * (uint64_t)ranges;
+    pl->joins.push_back(m);
+    return m.ws_row;
+  };
+  // long units first
+  std::vector<int32_t> order(it.size());
+  for (size_t i = 0; i < it.size(); ++i) order[i] = (int32_t)i;
+  for (ExtItem &x : it) {
+    if (x.group < 0) continue;
+    Group &y = grp[(size_t)x.group];
+    if (!x.shared) {
+      x.splits = y.tail;
+      continue;
+    }
+    y.tok0 = tok[(size_t)x.first];
+    y.ws_row = place(x.first, x.count, y.shared + y.tail);
+  }
   std::stable_sort(order.begin(), order.end(), [&](int32_t x, int32_t y) {
     const ExtItem &u = it[(size_t)x], &v = it[(size_t)y];
     return u.steps * v.splits > v.steps * u.splits;
   });
-  std::vector<uint32_t> tok((size_t)n);
-  for (int32_t i = 1; i < n; ++i) tok[(size_t)i] = tok[(size_t)i - 1] + (uint32_t)n_q[i - 1];
 
-  uint64_t ws_row = 0;
   for (int32_t kind = 0; kind < kXKinds; ++kind) {
-    for (int32_t i : order) {
-      const ExtItem &x = it[(size_t)i];
-      if (x.kind != kind || n_q[i] == 0) continue;
+    for (int32_t k : order) {
+      const ExtItem &x = it[(size_t)k];
+      if (x.kind != kind) continue;
       const int64_t u = (x.tiles * g.hkv * x.splits + 7) / 8 * 8;
-      if (u > kMaxExtUnits) return fail(CP_EINVAL, "too many query rows of request %d in one call", ids[i]);
+      if (u > kMaxExtUnits) return fail(CP_EINVAL, "too many query rows of request %d in one call", ids[x.first]);
+      const size_t members = x.shared ? (size_t)x.count : 0;
       if (pl->launches.empty() || pl->launches.back().kind != kind ||
-          (int)pl->launches.back().req.size() == kMaxReqPerLaunch || pl->launches.back().units + u > kMaxExtUnits) {
+          (int)pl->launches.back().req.size() == kExtMaxReq ||
+          pl->launches.back().member.size() + members > (size_t)kExtMaxReq ||
+          pl->launches.back().units + u > kMaxExtUnits) {
         pl->launches.emplace_back();
         pl->launches.back().kind = kind;
       }
       ExtPlan::Launch &l = pl->launches.back();
-      const Request &r = p->st.req(ids[i]);
+      const Request &r = p->st.req(ids[x.first]);
+      auto prefix = [&](int32_t i) { return o.prefix ? (uint32_t)o.prefix[i] : 0u; };
       ExtReq e{};
       e.unit_begin = l.units;
       e.pte_base = r.plane_base(r.cursor);
-      e.ctx = (uint32_t)(r.attend_len() + (extra ? extra[i] : 0));
-      e.n_q = (uint32_t)n_q[i];
-      e.prefix = o.prefix ? (uint32_t)o.prefix[i] : 0u;
-      e.tok0 = tok[(size_t)i];
+      e.ctx = (uint32_t)ctx_of(x.first);
+      e.n_q = (uint32_t)n_q[x.first];
+      e.prefix = prefix(x.first);
+      e.tok0 = tok[(size_t)x.first];
+      e.n_tok = (uint32_t)(x.rows / g.hq);
+      e.key_lo = (uint32_t)x.key_lo;
+      e.key_hi = (uint32_t)x.key_hi;
       e.tiles = (uint32_t)x.tiles;
-      e.splits = (uint32_t)x.splits;
-      if (e.splits > 1) {
-        // partial rows start at a multiple of the request's own ranges
-        e.ws_row = (ws_row + e.splits - 1) / e.splits;
-        ws_row = (e.ws_row + (uint64_t)n_q[i] * g.hq) * e.splits;
+      e.splits = e.all = (uint32_t)x.splits;
+      if (x.group >= 0) {
+        const Group &y = grp[(size_t)x.group];
+        e.all = (uint32_t)(y.shared + y.tail);
+        e.split0 = x.shared ? 0u : (uint32_t)y.shared;
+        e.ws_row = y.ws_row + (uint64_t)(e.tok0 - y.tok0) * (uint64_t)g.hq;
+        e.member0 = (uint16_t)l.member.size();
+        e.members = (uint16_t)members;
+        for (size_t m = 0; m < members; ++m) {
+          const int32_t i = x.first + (int32_t)m;
+          l.member.push_back(ExtMember{(uint32_t)ctx_of(i), (uint32_t)n_q[i], prefix(i), 0u});
+        }
+      } else if (e.splits > 1) {
+        e.ws_row = place(x.first, 1, x.splits);
       }
       l.req.push_back(e);
-      l.idx.push_back(i);
       l.units += (uint32_t)u;
     }
   }
-  pl->ws_rows = ws_row;
   return CP_OK;
 }
 
@@ -2097,27 +2225,26 @@ cp_status run_extend(cp_pool *p, const ExtPlan &pl, const void *q, void *out, fl
     a.n_units = (int32_t)l.units;
     a.g = geom_k(g, P);
     std::copy(l.req.begin(), l.req.end(), a.req);
-    hipError_t e = launch_extend(a, l.kind, s);
+    std::copy(l.member.begin(), l.member.end(), a.member);
+    const hipError_t e = launch_extend(a, l.kind, s);
     if (e != hipSuccess) return hip_fail(e, "extend launch");
+  }
+  for (size_t i = 0; i < pl.joins.size();) {
     ExtMergeArgs m{};
-    m.ws_o = a.ws_o;
-    m.ws_l = a.ws_l;
-    m.out = a.out;
+    m.ws_o = (const float *)p->ws_o;
+    m.ws_l = p->ws_l;
+    m.out = (uint16_t *)out;
     m.lse = lse;
     m.d_v = g.d_v;
     uint32_t rows = 0, most = 1;
-    for (const ExtReq &r : l.req) {
-      if (r.splits < 2) continue;
-      most = std::max(most, r.splits);
+    for (; i < pl.joins.size() && m.n_req < kMaxReqPerLaunch; ++i) {
       ExtMergeArgs::Req &x = m.req[m.n_req++];
+      x = pl.joins[i];
       x.row_begin = rows;
-      x.rows = r.n_q * (uint32_t)g.hq;
-      x.ws_row = r.ws_row;
-      x.out_row = (uint64_t)r.tok0 * (uint32_t)g.hq;
-      x.splits = r.splits;
       rows += x.rows;
+      most = std::max(most, x.splits);
     }
-    e = launch_ext_merge(m, rows, most, s);
+    const hipError_t e = launch_ext_merge(m, rows, most, s);
     if (e != hipSuccess) return hip_fail(e, "extend join launch");
   }
   return CP_OK;

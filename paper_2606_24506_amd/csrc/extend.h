@@ -33,15 +33,27 @@ constexpr int kTanhTerms = 4;
 constexpr float kTanh[kTanhTerms] = {1.f, -3.33326690e-01f, 1.32999740e-01f, -4.91567400e-02f};
 constexpr float kCapEdge = 0.35f;
 
+constexpr int kExtMaxReq = 40;  // items of a launch, and requests of its shared ones
+
+// One item: a request, or a part of it. Requests that share leading pages
+// (forks) and stand next to each other are taken apart: the shared keys are one
+// item, whose rows are those of all of them, and the keys behind are an item of each.
 struct ExtReq {
-  uint32_t unit_begin;  // first workgroup of the request (a multiple of 8)
+  uint32_t unit_begin;  // first workgroup of the item (a multiple of 8)
   uint32_t pte_base;    // page-table entries of the plane
   uint32_t ctx, n_q;    // context, and how many of its last tokens ask
   uint32_t prefix;
   uint32_t tok0;        // its first query token in the call's arrays
+  uint32_t n_tok;       // query tokens (n_q, or those of all members)
+  uint32_t key_lo, key_hi;  // the item's keys
   uint32_t tiles;       // row tiles per KV head
   uint32_t splits;      // key ranges per tile
-  uint64_t ws_row;      // first partial row (splits > 1)
+  uint32_t split0, all; // the first of its ranges among all of its rows', and how many those have
+  uint16_t member0, members;  // of ExtArgs::member (members 0: a request of its own)
+  uint64_t ws_row;      // first partial row (all > 1)
+};
+struct ExtMember {
+  uint32_t ctx, n_q, prefix, pad;
 };
 
 struct ExtArgs {
@@ -63,7 +75,8 @@ struct ExtArgs {
   uint32_t page_magic;  // page_divide
   int32_t n_req, n_units;
   GeomK g;
-  ExtReq req[kMaxReqPerLaunch];
+  ExtReq req[kExtMaxReq];
+  ExtMember member[kExtMaxReq];
 };
 static_assert(sizeof(ExtArgs) <= 3776, "extend kernel arguments too large");
 
@@ -73,7 +86,7 @@ struct ExtMergeArgs {
   float *lse;
   int32_t n_req, d_v, lanes, pad;  // lanes: ranges of a row taken at once
   struct Req {
-    uint32_t row_begin, rows;  // rows of the launch before, and of, the request
+    uint32_t row_begin, rows;  // rows of the launch before, and of, these requests
     uint64_t ws_row;
     uint64_t out_row;
     uint32_t splits, pad;

@@ -89,14 +89,22 @@ struct Row {
   uint64_t tok;          // query token of the call
 };
 CP_DEV Row row_of(const ExtArgs &a, const ExtReq &rq, uint32_t kvh, uint32_t r) {
-  const uint32_t g = (uint32_t)a.g.g, rows = rq.n_q * g, rc = min(r, rows - 1);
-  const uint32_t t = rc / g;
+  const uint32_t g = (uint32_t)a.g.g, rows = rq.n_tok * g, rc = min(r, rows - 1);
+  uint32_t t = rc / g, ctx = rq.ctx, n_q = rq.n_q, prefix = rq.prefix;
   Row x;
   x.tok = (uint64_t)rq.tok0 + t;
   x.head = kvh * g + (rc - t * g);
-  x.pos = rq.ctx - rq.n_q + t;
-  x.hi = max(x.pos + 1, min(rq.prefix, rq.ctx));
-  x.lo = a.window && x.pos >= a.window ? x.pos - a.window + 1 : 0u;
+  for (uint32_t k = 0; k < rq.members; ++k) {  // the member whose token it is
+    const ExtMember &m = a.member[rq.member0 + k];
+    ctx = m.ctx;
+    n_q = m.n_q;
+    prefix = m.prefix;
+    if (t < n_q) break;
+    t -= n_q;
+  }
+  x.pos = ctx - n_q + t;
+  x.hi = min(max(x.pos + 1, min(prefix, ctx)), rq.key_hi);
+  x.lo = max(a.window && x.pos >= a.window ? x.pos - a.window + 1 : 0u, rq.key_lo);
   if (a.doc_begin) {
     const int32_t d = a.doc_begin[x.tok];
     if (d > 0) x.lo = max(x.lo, (uint32_t)d);
@@ -107,7 +115,7 @@ CP_DEV Row row_of(const ExtArgs &a, const ExtReq &rq, uint32_t kvh, uint32_t r) 
 
 // Stores of a row's result: NORMAL to the call's arrays, or a range's part.
 CP_DEV uint64_t part_row(const ExtArgs &a, const ExtReq &rq, const Row &x, uint32_t split) {
-  return (rq.ws_row + (x.tok - rq.tok0) * (uint32_t)a.g.hq + x.head) * rq.splits + split;
+  return (rq.ws_row + (x.tok - rq.tok0) * (uint32_t)a.g.hq + x.head) * rq.all + rq.split0 + split;
 }
 
 // product * sum_k cap_k product^2k: the capped score, in units of log2 e, of a

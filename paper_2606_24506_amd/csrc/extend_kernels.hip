@@ -24,7 +24,7 @@ __global__ __launch_bounds__(kExtThreads) void extend_vec_kernel(const ExtArgs a
   const GeomK &g = a.g;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t r = un.tile * 4 + wave;
-  if (r >= rq.n_q * (uint32_t)g.g) return;  // no barrier below: waves are on their own
+  if (r >= rq.n_tok * (uint32_t)g.g) return;  // no barrier below: waves are on their own
   const Row x = row_of(a, rq, un.kvh, r);
   const uint32_t dk = (uint32_t)g.d_k, P = (uint32_t)g.page_tokens;
   float *const qw = qs + wave * dk;
@@ -83,7 +83,7 @@ __global__ __launch_bounds__(kExtThreads) void extend_vec_kernel(const ExtArgs a
   const bool none = l == 0.f;  // (all scores NaN: l is NaN, and so are the results)
   const float inv = none ? 0.f : 1.f / l;
   const float lse = none ? -INFINITY : m + fast_log2(l);
-  if (rq.splits > 1) {
+  if (rq.all > 1) {
     const uint64_t pr = part_row(a, rq, x, un.split);
 #pragma unroll
     for (int i = 0; i < E; ++i) a.ws_o[pr * (uint32_t)g.d_v + lane * E + i] = none ? 0.f : o[i] * inv;

@@ -73,7 +73,7 @@ __global__ __launch_bounds__(64 * ExtMla::WAVES, 2) void extend_mla_kernel(const
   const GeomK &g = a.g;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, quad = lane >> 4;
-  const uint32_t P = (uint32_t)g.page_tokens, rows = rq.n_q * (uint32_t)g.g;
+  const uint32_t P = (uint32_t)g.page_tokens, rows = rq.n_tok * (uint32_t)g.g;
 
   const uint32_t r = un.tile * 128 + 16 * wave + col;
   const bool busy = un.tile * 128 + 16 * wave < rows;  // else the wave only loads
@@ -310,7 +310,7 @@ __global__ __launch_bounds__(64 * ExtMla::WAVES, 2) void extend_mla_kernel(const
   if (r >= rows) return;
   const bool none = l == 0.f;  // (all scores NaN: l is NaN, and so are the results)
   const float inv = none ? 0.f : 1.f / l, lse = none ? -INFINITY : m + fast_log2(l);
-  if (rq.splits > 1) {
+  if (rq.all > 1) {
     const uint64_t pr = part_row(a, rq, x, un.split);
 #pragma unroll
     for (int d = 0; d < C::DB; ++d)

@@ -337,10 +337,10 @@ __global__ __launch_bounds__(kExtThreads, 2) void extend_rows_kernel(const ExtAr
   // ---- results: column d = 32 db + 8 (i / 4) + 4 half + i % 4 of row `col`
   l += other_half(l);
   if (RW == 4) {
-    if (r >= rq.n_q * (uint32_t)g.g) return;
+    if (r >= rq.n_tok * (uint32_t)g.g) return;
     const bool none = l == 0.f;  // (all scores NaN: l is NaN, and so are the results)
     const float inv = none ? 0.f : 1.f / l, lse = none ? -INFINITY : m + fast_log2(l);
-    if (rq.splits > 1) {
+    if (rq.all > 1) {
       const uint64_t pr = part_row(a, rq, x, un.split);
 #pragma unroll
       for (int d = 0; d < DB; ++d)
@@ -377,7 +377,7 @@ __global__ __launch_bounds__(kExtThreads, 2) void extend_rows_kernel(const ExtAr
     constexpr int NC = D / 8;
     const int row = threadIdx.x & 31, c0 = (threadIdx.x >> 5) * NC;
     const uint32_t rr = un.tile * 32 + row;
-    if (rr >= rq.n_q * (uint32_t)g.g) return;
+    if (rr >= rq.n_tok * (uint32_t)g.g) return;
     const Row y = row_of(a, rq, un.kvh, rr);
     float mt = stats[0][0][row];
 #pragma unroll
@@ -400,7 +400,7 @@ __global__ __launch_bounds__(kExtThreads, 2) void extend_rows_kernel(const ExtAr
         if (f[w] > 0.f) acc += f[w] * reinterpret_cast<const float *>(lds)[w * 32 * D + (c0 + c) * 32 + row];
       v[c] = acc * inv;
     }
-    if (rq.splits > 1) {
+    if (rq.all > 1) {
       const uint64_t pr = part_row(a, rq, y, un.split);
 #pragma unroll
       for (int c = 0; c < NC; c += 4)

@@ -21,7 +21,9 @@ def run(sc, n_q, ids=None, q=None, **opts):
     return q, buf[1], buf[2]
 
 
-def verify(sc, n_q, label, rows=None, **opts):
+def verify(sc, n_q, label, rows=None, together=False, **opts):
+    """together: rows of several requests share tiles, of more than 32 rows, whose
+    probabilities are rounded to bf16 (off by at most 2^-8 of themselves)."""
     q, out, lse = run(sc, n_q, **opts)
     at = 0
     path = opts.pop("path", cpl.CP_PATH_AUTO)
@@ -32,7 +34,7 @@ def verify(sc, n_q, label, rows=None, **opts):
             continue
         ref = attend(sc.name, (rows or sc.rows)[i], q[at:at + k], prefix=prefix[i] if prefix else 0,
                      doc_begin=docs[at:at + k] if docs is not None else None, **opts)
-        check(out[at:at + k], lse[at:at + k], ref, rounds_to_16_bits(sc.name, k, path), f"{label} request {i}")
+        check(out[at:at + k], lse[at:at + k], ref, together or rounds_to_16_bits(sc.name, k, path), f"{label} request {i}")
         at += k
 
 
@@ -193,6 +195,67 @@ def test_results_do_not_depend_on_placement_or_company():
     assert torch.equal(o2, out[:65]) and torch.equal(l2, lse[:65])
     pool.close(rid)
     pool.destroy()
+    sc.close()
+
+
+@pytest.mark.parametrize("name", ["gqa8x2d128", "gqa6x2d64", "mla16", "mla4l128r40"])
+@pytest.mark.parametrize("mask", ["causal", "all", "window"])
+@pytest.mark.parametrize("shared,n_q", [(640, [1, 1, 1, 1, 1]), (1000, [3, 1, 5, 2, 9]), (300, [40, 1, 7, 2, 1])])
+def test_forks_read_their_shared_pages_once(name, mask, shared, n_q):
+    """Branches of one prompt, with tails and queries of different lengths, next
+    to requests that share nothing; the same as with every request whole."""
+    print(f"[case] extend shared {name} {mask} {shared} {n_q}", flush=True)
+    sc = Scene(name, [shared], page_tokens=64, seed=15, room=100, pool_bytes=256 << 20)
+    kids, rows = [], []
+    for i, k in enumerate(n_q):
+        rid = sc.pool.open(sc.model, shared + 400)
+        keep = shared if i != 3 else shared - 70  # one shares less
+        sc.pool.fork([sc.ids[0]], [rid], [keep])
+        tail = sc.normal(k + 13 * i, sc.row, sigma=0.7)
+        sc.pool.append([rid], [k + 13 * i], tail)
+        kids.append(rid)
+        rows.append(torch.cat([sc.rows[0][:keep], tail]))
+    sc.add(100)
+    ids = kids[:2] + [sc.ids[1]] + kids[2:]
+    held = rows[:2] + [sc.rows[1]] + rows[2:]
+    counts = n_q[:2] + [4] + n_q[2:]
+    sc.ids = ids + [sc.ids[0]]
+    sc.rows = held + [sc.rows[0]]
+    counts.append(2)
+    opts = {}
+    if mask == "window":
+        opts = dict(window=200)
+    if mask == "all":
+        opts = dict(softcap=8.0, window=500, prefix=[50, 0, 30, 5000, 0, 100, 7],
+                    slopes=torch.linspace(0.3, 0.01, sc.hq, device="cuda"),
+                    doc_begin=torch.tensor([(37 * i) % 260 for i in range(sum(counts))], dtype=torch.int32, device="cuda"))
+    q, out, lse = run(sc, counts, **opts)
+    q, o2, l2 = run(sc, counts, q=q, num_splits=1, **opts)
+    at = 0
+    more = {k: v for k, v in opts.items() if k not in ("prefix", "doc_begin")}
+    for i, k in enumerate(counts):
+        ref = attend(name, sc.rows[i], q[at:at + k], prefix=opts["prefix"][i] if "prefix" in opts else 0,
+                     doc_begin=opts["doc_begin"][at:at + k] if "doc_begin" in opts else None, **more)
+        check(out[at:at + k], lse[at:at + k], ref, True, f"{name} {mask} request {i}")  # (all rows together may be many)
+        check(o2[at:at + k], l2[at:at + k], ref, True, f"{name} {mask} request {i} whole")
+        at += k
+    sc.close()
+
+
+def test_many_branches_of_two_prompts():
+    """More branches than a launch holds members of."""
+    sc = Scene("gqa8x2d128", [500, 300], seed=16, room=10, pool_bytes=256 << 20)
+    parents, base = list(sc.ids), list(sc.rows)
+    ids, rows = [], []
+    for p, n in ((0, 90), (1, 15)):
+        kids = [sc.pool.open(sc.model, 600) for _ in range(n)]
+        sc.pool.fork([parents[p]] * n, kids)
+        tails = sc.normal(n, 2, sc.row, sigma=0.7)
+        sc.pool.append(kids, [2] * n, tails)
+        ids += kids
+        rows += [torch.cat([base[p], t]) for t in tails]
+    sc.ids, sc.rows = ids + parents, rows + base
+    verify(sc, [1] * len(sc.ids), "105 branches", together=True)
     sc.close()
 
 
