@@ -632,9 +632,12 @@ cp_status cp_request_truncate(cp_pool *p, int32_t n, const int32_t *ids, const i
   rc = reconcile_pages(p);
   if (rc) return rc;
   std::vector<int64_t> more, pages;
-  p->st.truncate_cost(n, ids, new_len, &more, &pages);
-  if (!p->st.fits_budget(more))
-    return fail(CP_ENOSPC, "the pool page budget cannot take back the shared pages' place");
+  // (the bound first: the exact count costs 20 ns a shared page)
+  p->st.truncate_cost(n, ids, new_len, p->st.virt(), &more, &pages);
+  if (!p->st.fits_budget(more)) {
+    p->st.truncate_cost(n, ids, new_len, true, &more, &pages);
+    if (!p->st.fits_budget(more)) return fail(CP_ENOSPC, "the pool page budget cannot take back the shared pages' place");
+  }
   std::vector<int32_t> carved;
   for (int32_t m = 0; m < p->st.n_models(); ++m) {
     // a virtual pool backs whole reservations; otherwise the copies' pages
@@ -1918,51 +1921,53 @@ double choose_ranges(const Geom &g, int num_cus, uint64_t cap, std::vector<ExtIt
   // us of a step of the kernel with its CUs full, and workgroups of a CU
   static constexpr struct { double us; int per_cu; } kCost[kXKinds] = {
       {2.0, 8}, {1.4, 2}, {2.8, 2}, {2.7, 2}, {4.6, 2}, {2.6, 1}};
-  // a unit's start and end, the second launch, and the way of partial rows
-  constexpr double kUnit = 4.0, kJoin = 5.0, kBytesPerUs = 3.0e6;
-  double most = 1, base = 0, all_units = 0;
-  int per_cu = 8;
+  // a unit's start and end, another launch, and the way of partial rows
+  constexpr double kUnit = 4.0, kLaunch = 5.0, kBytesPerUs = 3.0e6;
+  double most = 1, base[kXKinds] = {}, all_units = 0, all_slots = 1e300;
   for (const ExtItem &x : *items) {
-    if (x.rows == 0) continue;
     most = std::max(most, (double)x.steps);
-    per_cu = std::min(per_cu, kCost[x.kind].per_cu);
+    all_slots = std::min(all_slots, (double)num_cus * kCost[x.kind].per_cu);
     all_units += (double)(x.tiles * g.hkv);
-    base += (double)(x.tiles * g.hkv) * (double)x.steps * kCost[x.kind].us / kCost[x.kind].per_cu;
+    base[x.kind] += (double)(x.tiles * g.hkv) * (double)x.steps * kCost[x.kind].us / kCost[x.kind].per_cu;
   }
-  const double slots = (double)num_cus * per_cu;
   auto ranges = [](const ExtItem &x, double per) { return std::min(std::ceil((double)x.steps / per), 4096.0); };
   auto units_of = [&](const ExtItem &x, double s) { return std::ceil((double)(x.tiles * g.hkv) * s / 8) * 8; };
   double best = 1e300, best_per = most;
   auto consider = [&](double per) {  // false: shorter ranges only cost from here on
-    double work = base, longest = 0, shortest = 1e300, rows = 0, units = 0;
+    double units[kXKinds] = {}, longest[kXKinds] = {}, shortest[kXKinds], rows = 0, t = 0, floor = 0;
+    std::fill(shortest, shortest + kXKinds, 1e300);
     for (const ExtItem &x : *items) {
-      if (x.rows == 0) continue;
-      const double s = ranges(x, per), u = units_of(x, s), len = kUnit + std::ceil((double)x.steps / s) * kCost[x.kind].us;
-      work += u * kUnit / kCost[x.kind].per_cu;
-      longest = std::max(longest, len);
-      shortest = std::min(shortest, len);
-      units += u;
+      const double s = ranges(x, per), len = kUnit + std::ceil((double)x.steps / s) * kCost[x.kind].us;
+      units[x.kind] += units_of(x, s);
+      longest[x.kind] = std::max(longest[x.kind], len);
+      shortest[x.kind] = std::min(shortest[x.kind], len);
       if (s > 1 || x.group >= 0) rows += (double)(x.rows + 1) * s;
     }
-    const double join = rows > 0 ? kJoin + rows * g.d_v * 8 / kBytesPerUs : 0;
-    const double t = std::max(longest, work / num_cus) + (units > slots ? shortest : 0.0) + join;
+    for (int k = 0; k < kXKinds; ++k) {  // one launch each
+      if (units[k] == 0) continue;
+      const double work = (base[k] + units[k] * kUnit / kCost[k].per_cu) / num_cus;
+      t += std::max(longest[k], work) + (units[k] > (double)num_cus * kCost[k].per_cu ? shortest[k] : 0.0) + kLaunch;
+      floor += work;
+    }
+    const double join = rows > 0 ? kLaunch + rows * g.d_v * 8 / kBytesPerUs : 0;
+    t += join;
     if (t < best && (rows == 0 || pool_ws_bytes((uint64_t)(2 * rows) * (uint64_t)g.d_v, (uint64_t)rows) <= cap)) {
       best = t;
       best_per = per;
     }
-    return join + work / num_cus <= best;
+    return join + floor <= best;
   };
-  if (consider(most) && all_units < 4 * slots) {
+  if (consider(most) && all_units < 4 * all_slots) {
     double lo = 1, hi = most;  // the least steps per range of one turn
     while (lo < hi) {
       const double mid = std::floor((lo + hi) / 2);
       double units = 0;
-      for (const ExtItem &x : *items) units += x.rows ? units_of(x, ranges(x, mid)) : 0;
-      if (units <= slots) hi = mid;
+      for (const ExtItem &x : *items) units += units_of(x, ranges(x, mid));
+      if (units <= all_slots) hi = mid;
       else lo = mid + 1;
     }
     consider(lo);
-    for (double per = std::floor(most * 0.75); per >= 1 && consider(per); per = std::floor(per * 0.75)) {}
+    for (double per = std::floor(most * 0.7); per >= 1 && consider(per); per = std::floor(per * 0.7)) {}
   }
   for (ExtItem &x : *items) x.splits = (int64_t)std::max(1.0, ranges(x, best_per));
   return best;
@@ -2029,7 +2034,7 @@ cp_status plan_extend(cp_pool *p, int32_t n, const int32_t *ids, const int32_t *
   for (int32_t i = 1; i < n; ++i) tok[(size_t)i] = tok[(size_t)i - 1] + (uint32_t)n_q[i - 1];
   auto ctx_of = [&](int32_t i) { return p->st.req(ids[i]).attend_len() + (extra ? extra[i] : 0); };
   // Items: each request, and, another way, with shared pages taken apart.
-  auto item_of = [&](int32_t first, int32_t count, int64_t key_lo, int64_t key_hi) {
+  auto item_of = [&](int32_t first, int32_t count, int64_t key_lo, int64_t key_hi, int32_t kind = -1) {
     ExtItem x;
     x.first = first;
     x.count = count;
@@ -2042,7 +2047,7 @@ cp_status plan_extend(cp_pool *p, int32_t n, const int32_t *ids, const int32_t *
       lo = std::min(lo, o.window ? std::max<int64_t>(0, ctx - n_q[i] - o.window + 1) : 0);
       hi = std::max(hi, ctx);
     }
-    x.kind = extend_kind(g, o.path, tokens);
+    x.kind = kind >= 0 ? kind : extend_kind(g, o.path, tokens);
     const int64_t rows = ext_tile_rows(x.kind), keys = ext_tile_keys(x.kind);
     x.rows = tokens * g.hq;
     x.tiles = (tokens * g.g + rows - 1) / rows;
@@ -2080,9 +2085,11 @@ cp_status plan_extend(cp_pool *p, int32_t n, const int32_t *ids, const int32_t *
       } else {
         apart.push_back(item_of(i, count, 0, keys));
         apart.back().shared = true;
+        const int32_t shared_kind = apart.back().kind;
         apart.back().group = groups;
         for (int32_t k = i; k < i + count; ++k) {
-          apart.push_back(item_of(k, 1, keys, 0xFFFFFFFFll));
+          // (by the same kernel, and so in the same launch)
+          apart.push_back(item_of(k, 1, keys, 0xFFFFFFFFll, shared_kind));
           apart.back().group = groups;
         }
         groups += 1;

@@ -538,14 +538,14 @@ void PoolState::truncate(int32_t id, int64_t new_len) {
   r.ctx_len = new_len;
 }
 
-void PoolState::truncate_cost(int32_t n, const int32_t *ids, const int64_t *new_len, std::vector<int64_t> *reserved,
-                              std::vector<int64_t> *pages) const {
+void PoolState::truncate_cost(int32_t n, const int32_t *ids, const int64_t *new_len, bool exact,
+                              std::vector<int64_t> *reserved, std::vector<int64_t> *pages) const {
   reserved->assign(models_.size(), 0);
   pages->assign(models_.size(), 0);
   std::unordered_map<uint32_t, uint32_t> given;  // users taken from shared pages so far
   auto give_shared = [&](uint32_t pte) {
     const uint32_t k = sharers(pte);
-    return k > 0 && given[pte]++ < k;
+    return k > 0 && (!exact || given[pte]++ < k);
   };
   for (int pass = 0; pass < 2; ++pass)  // the two passes of a truncation
     for (int32_t i = 0; i < n; ++i) {

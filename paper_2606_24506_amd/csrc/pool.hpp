@@ -206,9 +206,10 @@ class PoolState {
   void truncate_own(int32_t id, int64_t new_len, std::vector<OwnPage> *copies);
   void truncate(int32_t id, int64_t new_len);
   // What truncating these requests adds to each model's `reserved`, and the
-  // pages of its own it allocates for shared ones.
-  void truncate_cost(int32_t n, const int32_t *ids, const int64_t *new_len, std::vector<int64_t> *reserved,
-                     std::vector<int64_t> *pages) const;
+  // pages of its own it allocates for shared ones; not exact: at most that (a
+  // page that the call's requests share among themselves counts for each).
+  void truncate_cost(int32_t n, const int32_t *ids, const int64_t *new_len, bool exact,
+                     std::vector<int64_t> *reserved, std::vector<int64_t> *pages) const;
   // Would the budget hold every reservation with these additions (per model)?
   bool fits_budget(const std::vector<int64_t> &extra) const;
   // Users of a page beyond its first.
