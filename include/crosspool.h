@@ -599,7 +599,8 @@ cp_status cp_kv_append_rope(cp_pool *pool, int32_t n, const int32_t *req_ids, co
 /* ------------------------------------------------- attention of token chunks */
 
 typedef struct {
-  /* > 0: scores s become softcap * tanh(s / softcap); 0: uncapped. */
+  /* In [1e-18, 1e18]: scores s become softcap * tanh(s / softcap); 0:
+   * uncapped. */
   float softcap;
   /* W >= 1: a token at position p sees positions > p - W only; 0: all. */
   int32_t window;
@@ -617,7 +618,8 @@ typedef struct {
    * leaves the row empty. */
   const int32_t *doc_begin;
   /* 0: the planner cuts long contexts into ranges where there are few
-   * rows; k >= 1 forces at most k ranges per request. */
+   * rows; k >= 1 forces at most k ranges per request (and every request
+   * whole, shared pages or not). */
   int32_t num_splits;
   int32_t path; /* cp_path: AUTO, or VALU to force the vector kernel */
   /* cp_attn_extend_step: rotates the new rows' keys as they are placed, as
@@ -642,11 +644,22 @@ typedef struct {
  *        aligned. out [sum n_q][n_q_heads][d_v] bf16 (8-byte aligned) and
  *        lse [sum n_q][n_q_heads] float likewise.
  *   opts may be NULL (causal attention).
- * Scores, statistics and sums are held in 32 bits; the matrix-core kernels
- * round probabilities to bf16 for prompt chunks (more than 32 rows, a row
- * being a token and a query head of one KV head) and take them in two bf16 parts for fewer. Results depend on the logical KV
- * and the call only, never on page placement. The cursor does not move.
- * Errors: CP_EINVAL, CP_ESTATE (host-only pool), CP_ENOMEM (workspace), CP_EHIP. */
+ * Scores, statistics and sums are held in 32 bits. The matrix-core kernels
+ * (GQA and MHA of head_dim 64 and 128, MLA of 512 + 64) multiply the
+ * probabilities as bf16 numbers, but in two bf16 parts for GQA and MHA
+ * requests of at most 32 rows (a row being a token and a query head of one KV
+ * head); the vector kernel, which serves every other geometry, in fp32.
+ * Requests that share leading pages (cp_request_fork) and stand next to each
+ * other in the call may have those pages read once, by kernels for the rows
+ * of all of them. Results depend on the logical KV, on which pages
+ * requests share, and on the call, never on where pages are placed. The
+ * cursor does not move. The call uses the pool's workspace, as the decode
+ * calls do: it must not overlap with them on the GPU, and before a call is
+ * captured into a graph, the same one must have run once (a capped pool's
+ * graphs are captured anew once a call has needed more workspace).
+ * Errors: CP_EINVAL (also: more than 2^23 units of work of one request:
+ * tiles of 4 rows on the vector path, of 128 otherwise), CP_ESTATE (host-only
+ * pool), CP_ENOMEM (workspace), CP_EHIP. */
 cp_status cp_attn_extend(cp_pool *pool, int32_t n, const int32_t *req_ids, const int32_t *n_q, const void *q,
                          void *out, float *lse, void *hip_stream, const cp_extend_opts *opts);
 

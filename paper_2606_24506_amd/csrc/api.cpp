@@ -555,112 +555,131 @@ cp_status cp_request_close(cp_pool *p, int32_t req_id) {
 
 cp_status cp_request_fork(cp_pool *p, int32_t n, const int32_t *src, const int32_t *dst, const int64_t *n_tok,
                           void *hip_stream) {
-  if (!p) return fail(CP_EINVAL, "null pool");
-  cp_status rc = check_ids(p, n, dst);
-  if (rc) return rc;
-  if (n > 0 && !src) return fail(CP_EINVAL, "null src_ids");
-  if (p->broken) return fail(CP_ESTATE, "a failed decode step left the device page stacks out of step; destroy the pool");
-  const int32_t P = p->st.page_tokens();
-  std::vector<int64_t> len((size_t)n), tails((size_t)p->st.n_models(), 0), shown((size_t)p->st.n_models(), 0);
-  std::vector<int32_t> sorted(dst, dst + n);
-  std::sort(sorted.begin(), sorted.end());
-  for (int32_t i = 0; i < n; ++i) {
-    if (!p->st.valid_open(src[i])) return fail(CP_EINVAL, "request %d is not open", src[i]);
-    if (std::binary_search(sorted.begin(), sorted.end(), src[i]))
-      return fail(CP_EINVAL, "request %d is both a source and a destination", src[i]);
-    const Request &s = p->st.req(src[i]), &d = p->st.req(dst[i]);
-    if (s.model != d.model) return fail(CP_EINVAL, "requests %d and %d are of different models", src[i], dst[i]);
-    if (s.cursor != 0 || s.inflight || d.cursor != 0 || d.inflight)
-      return fail(CP_EINVAL, "request %d or %d has a token in flight; finish its decode steps first", src[i], dst[i]);
-    if (d.ctx_len != 0) return fail(CP_EINVAL, "request %d is not empty", dst[i]);
-    len[(size_t)i] = n_tok ? n_tok[i] : s.ctx_len;
-    if (len[(size_t)i] < 0 || len[(size_t)i] > s.ctx_len)
-      return fail(CP_EINVAL, "a prefix of %lld tokens of request %d, which has %lld", (long long)len[(size_t)i], src[i],
-                  (long long)s.ctx_len);
-    if (!p->st.fits_reservation(dst[i], len[(size_t)i]))
-      return fail(CP_EINVAL, "a prefix of %lld tokens is past request %d's reservation", (long long)len[(size_t)i], dst[i]);
-    shown[(size_t)d.model] += (len[(size_t)i] + P - 1) / P * d.layers;
-    if (len[(size_t)i] % P) tails[(size_t)d.model] += d.layers;
-  }
-  rc = reconcile_pages(p);
-  if (rc) return rc;
-  std::vector<int32_t> carved;
-  for (int32_t m = 0; m < p->st.n_models(); ++m) {
-    if (p->dev_pages) {  // the stack keeps what requests may still take then
-      rc = drain_stack(p, m, p->st.room_to_grow(m) - shown[(size_t)m]);
-      if (rc) return rc;
+  return guarded([&]() -> cp_status {
+    if (!p) return fail(CP_EINVAL, "null pool");
+    cp_status rc = check_ids(p, n, dst);
+    if (rc) return rc;
+    if (n > 0 && !src) return fail(CP_EINVAL, "null src_ids");
+    if (p->broken) return fail(CP_ESTATE, "a failed decode step left the device page stacks out of step; destroy the pool");
+    const int32_t P = p->st.page_tokens();
+    std::vector<int64_t> len((size_t)n), tails((size_t)p->st.n_models(), 0), shown((size_t)p->st.n_models(), 0);
+    std::vector<int32_t> sorted(dst, dst + n);
+    std::sort(sorted.begin(), sorted.end());
+    for (int32_t i = 0; i < n; ++i) {
+      if (!p->st.valid_open(src[i])) return fail(CP_EINVAL, "request %d is not open", src[i]);
+      if (std::binary_search(sorted.begin(), sorted.end(), src[i]))
+        return fail(CP_EINVAL, "request %d is both a source and a destination", src[i]);
+      const Request &s = p->st.req(src[i]), &d = p->st.req(dst[i]);
+      if (s.model != d.model) return fail(CP_EINVAL, "requests %d and %d are of different models", src[i], dst[i]);
+      if (s.cursor != 0 || s.inflight || d.cursor != 0 || d.inflight)
+        return fail(CP_EINVAL, "request %d or %d has a token in flight; finish its decode steps first", src[i], dst[i]);
+      if (d.ctx_len != 0) return fail(CP_EINVAL, "request %d is not empty", dst[i]);
+      len[(size_t)i] = n_tok ? n_tok[i] : s.ctx_len;
+      if (len[(size_t)i] < 0 || len[(size_t)i] > s.ctx_len)
+        return fail(CP_EINVAL, "a prefix of %lld tokens of request %d, which has %lld", (long long)len[(size_t)i], src[i],
+                    (long long)s.ctx_len);
+      if (!p->st.fits_reservation(dst[i], len[(size_t)i]))
+        return fail(CP_EINVAL, "a prefix of %lld tokens is past request %d's reservation", (long long)len[(size_t)i], dst[i]);
+      shown[(size_t)d.model] += (len[(size_t)i] + P - 1) / P * d.layers;
+      if (len[(size_t)i] % P) tails[(size_t)d.model] += d.layers;
     }
-    if (!p->st.ensure_slots(m, tails[(size_t)m], &carved)) {
-      p->st.release_empty(carved);
-      return fail(CP_ENOMEM, "could not map physical memory for %lld pages of model %d", (long long)tails[(size_t)m], m);
+    rc = reconcile_pages(p);
+    if (rc) return rc;
+    std::vector<PageItem> items;
+    std::vector<int32_t> models;
+    size_t planes = 0;  // (what the host must allocate comes before any change)
+    for (int32_t i = 0; i < n; ++i) {
+      p->st.reserve_users(src[i], len[(size_t)i]);
+      planes += (size_t)p->st.req(dst[i]).layers;
     }
-  }
-  std::vector<PageItem> items;
-  std::vector<int32_t> models;
-  for (int32_t i = 0; i < n; ++i) {
-    if (len[(size_t)i] == 0) continue;
-    p->st.fork(src[i], dst[i], len[(size_t)i]);
-    const Request &s = p->st.req(src[i]), &d = p->st.req(dst[i]);
-    const uint32_t whole = (uint32_t)(len[(size_t)i] / P), tail = (uint32_t)(len[(size_t)i] % P);
-    const uint32_t *pt = p->st.pte_mirror();
-    for (int32_t l = 0; l < d.layers; ++l) {
-      items.push_back(PageItem{s.plane_base(l), d.plane_base(l), whole, tail, tail ? pt[s.plane_base(l) + whole] : 0u,
-                               tail ? pt[d.plane_base(l) + whole] : 0u, 0u, 0u});
-      models.push_back(d.model);
+    items.reserve(planes);
+    models.reserve(planes);
+    std::vector<int32_t> carved;
+    for (int32_t m = 0; m < p->st.n_models(); ++m) {
+      if (p->dev_pages) {  // the stack keeps what requests may still take then
+        rc = drain_stack(p, m, p->st.room_to_grow(m) - shown[(size_t)m]);
+        if (rc) return rc;
+      }
+      if (!p->st.ensure_slots(m, tails[(size_t)m], &carved)) {
+        p->st.release_empty(carved);
+        return fail(CP_ENOMEM, "could not map physical memory for %lld pages of model %d", (long long)tails[(size_t)m], m);
+      }
     }
-  }
-  return launch_page_items(p, items, models, (hipStream_t)hip_stream);
+    for (int32_t i = 0; i < n; ++i) {
+      if (len[(size_t)i] == 0) continue;
+      p->st.fork(src[i], dst[i], len[(size_t)i]);
+      const Request &s = p->st.req(src[i]), &d = p->st.req(dst[i]);
+      const uint32_t whole = (uint32_t)(len[(size_t)i] / P), tail = (uint32_t)(len[(size_t)i] % P);
+      const uint32_t *pt = p->st.pte_mirror();
+      for (int32_t l = 0; l < d.layers; ++l) {
+        items.push_back(PageItem{s.plane_base(l), d.plane_base(l), whole, tail, tail ? pt[s.plane_base(l) + whole] : 0u,
+                                 tail ? pt[d.plane_base(l) + whole] : 0u, 0u, 0u});
+        models.push_back(d.model);
+      }
+    }
+    return launch_page_items(p, items, models, (hipStream_t)hip_stream);
+  });
 }
 
 cp_status cp_request_truncate(cp_pool *p, int32_t n, const int32_t *ids, const int64_t *new_len, void *hip_stream) {
-  if (!p) return fail(CP_EINVAL, "null pool");
-  cp_status rc = check_ids(p, n, ids);
-  if (rc) return rc;
-  if (n > 0 && !new_len) return fail(CP_EINVAL, "null new_len");
-  if (p->broken) return fail(CP_ESTATE, "a failed decode step left the device page stacks out of step; destroy the pool");
-  bool any = false;
-  for (int32_t i = 0; i < n; ++i) {
-    const Request &r = p->st.req(ids[i]);
-    if (new_len[i] < 0 || new_len[i] > r.ctx_len)
-      return fail(CP_EINVAL, "request %d of %lld tokens cannot be cut to %lld", ids[i], (long long)r.ctx_len,
-                  (long long)new_len[i]);
-    if (r.cursor != 0 || r.inflight)
-      return fail(CP_EINVAL, "request %d has a token in flight; finish its decode steps first", ids[i]);
-    any = any || new_len[i] < r.ctx_len;
-  }
-  if (!any) return CP_OK;
-  rc = reconcile_pages(p);
-  if (rc) return rc;
-  std::vector<int64_t> more, pages;
-  // (the bound first: the exact count costs 20 ns a shared page)
-  p->st.truncate_cost(n, ids, new_len, p->st.virt(), &more, &pages);
-  if (!p->st.fits_budget(more)) {
-    p->st.truncate_cost(n, ids, new_len, true, &more, &pages);
-    if (!p->st.fits_budget(more)) return fail(CP_ENOSPC, "the pool page budget cannot take back the shared pages' place");
-  }
-  std::vector<int32_t> carved;
-  for (int32_t m = 0; m < p->st.n_models(); ++m) {
-    // a virtual pool backs whole reservations; otherwise the copies' pages
-    const int64_t slots = p->st.virt() && more[(size_t)m] ? p->st.reserved(m) + more[(size_t)m] - p->st.allocated(m)
-                                                          : pages[(size_t)m];
-    if (!p->st.ensure_slots(m, slots, &carved)) {
-      p->st.release_empty(carved);
-      return fail(CP_ENOMEM, "could not map physical memory for %lld pages of model %d", (long long)slots, m);
+  return guarded([&]() -> cp_status {
+    if (!p) return fail(CP_EINVAL, "null pool");
+    cp_status rc = check_ids(p, n, ids);
+    if (rc) return rc;
+    if (n > 0 && !new_len) return fail(CP_EINVAL, "null new_len");
+    if (p->broken) return fail(CP_ESTATE, "a failed decode step left the device page stacks out of step; destroy the pool");
+    bool any = false;
+    for (int32_t i = 0; i < n; ++i) {
+      const Request &r = p->st.req(ids[i]);
+      if (new_len[i] < 0 || new_len[i] > r.ctx_len)
+        return fail(CP_EINVAL, "request %d of %lld tokens cannot be cut to %lld", ids[i], (long long)r.ctx_len,
+                    (long long)new_len[i]);
+      if (r.cursor != 0 || r.inflight)
+        return fail(CP_EINVAL, "request %d has a token in flight; finish its decode steps first", ids[i]);
+      any = any || new_len[i] < r.ctx_len;
     }
-  }
-  std::vector<PageItem> items;
-  std::vector<int32_t> models;
-  std::vector<PoolState::OwnPage> copies;
-  for (int32_t i = 0; i < n; ++i) {
-    copies.clear();
-    p->st.truncate_own(ids[i], new_len[i], &copies);
-    for (const PoolState::OwnPage &c : copies) {
-      items.push_back(PageItem{c.slot, c.slot, 0u, (uint32_t)(new_len[i] % p->st.page_tokens()), c.from, c.to, 0u, 0u});
-      models.push_back(p->st.req(ids[i]).model);
+    if (!any) return CP_OK;
+    rc = reconcile_pages(p);
+    if (rc) return rc;
+    std::vector<int64_t> more, pages;
+    // (the bound first: the exact count costs 20 ns a shared page)
+    p->st.truncate_cost(n, ids, new_len, p->st.virt(), &more, &pages);
+    if (!p->st.fits_budget(more)) {
+      p->st.truncate_cost(n, ids, new_len, true, &more, &pages);
+      if (!p->st.fits_budget(more)) return fail(CP_ENOSPC, "the pool page budget cannot take back the shared pages' place");
     }
-  }
-  for (int32_t i = 0; i < n; ++i) p->st.truncate(ids[i], new_len[i]);
-  return launch_page_items(p, items, models, (hipStream_t)hip_stream);
+    std::vector<PageItem> items;
+    std::vector<int32_t> models;
+    std::vector<PoolState::OwnPage> copies;
+    size_t planes = 0, most = 0;
+    for (int32_t i = 0; i < n; ++i) {
+      planes += (size_t)p->st.req(ids[i]).layers;
+      most = std::max(most, (size_t)p->st.req(ids[i]).layers);
+    }
+    copies.reserve(most);
+    items.reserve(planes);
+    models.reserve(planes);
+    std::vector<int32_t> carved;
+    for (int32_t m = 0; m < p->st.n_models(); ++m) {
+      // a virtual pool backs whole reservations; otherwise the copies' pages
+      const int64_t slots = p->st.virt() && more[(size_t)m] ? p->st.reserved(m) + more[(size_t)m] - p->st.allocated(m)
+                                                            : pages[(size_t)m];
+      if (!p->st.ensure_slots(m, slots, &carved)) {
+        p->st.release_empty(carved);
+        return fail(CP_ENOMEM, "could not map physical memory for %lld pages of model %d", (long long)slots, m);
+      }
+    }
+    for (int32_t i = 0; i < n; ++i) {
+      copies.clear();
+      p->st.truncate_own(ids[i], new_len[i], &copies);
+      for (const PoolState::OwnPage &c : copies) {
+        items.push_back(PageItem{c.slot, c.slot, 0u, (uint32_t)(new_len[i] % p->st.page_tokens()), c.from, c.to, 0u, 0u});
+        models.push_back(p->st.req(ids[i]).model);
+      }
+    }
+    for (int32_t i = 0; i < n; ++i) p->st.truncate(ids[i], new_len[i]);
+    return launch_page_items(p, items, models, (hipStream_t)hip_stream);
+  });
 }
 
 cp_status cp_request_len(cp_pool *p, int32_t req_id, int64_t *ctx_len) {
@@ -931,8 +950,10 @@ cp_status cp_kv_append(cp_pool *p, int32_t n, const int32_t *req_ids, const int3
 
 cp_status cp_kv_append_rope(cp_pool *p, int32_t n, const int32_t *req_ids, const int32_t *n_new, const void *rows,
                             const cp_rope *rope, void *hip_stream) {
-  if (!rope) return fail(CP_EINVAL, "null rope");
-  return append_impl(p, n, req_ids, n_new, rows, rope, hip_stream);
+  return guarded([&]() -> cp_status {
+    if (!rope) return fail(CP_EINVAL, "null rope");
+    return append_impl(p, n, req_ids, n_new, rows, rope, hip_stream);
+  });
 }
 
 cp_status cp_kv_gather(cp_pool *p, int32_t req_id, int64_t start, int64_t n_tok, void *dst, void *hip_stream) {
@@ -2268,100 +2289,105 @@ extern "C" {
 
 cp_status cp_attn_extend(cp_pool *p, int32_t n, const int32_t *req_ids, const int32_t *n_q, const void *q, void *out,
                          float *lse, void *hip_stream, const cp_extend_opts *opts) {
-  if (!p) return fail(CP_EINVAL, "null pool");
-  if (p->host_only) return fail(CP_ESTATE, "host-only pool cannot attend");
-  if (p->broken) return fail(CP_ESTATE, "a failed decode step left the device page stacks out of step; destroy the pool");
-  cp_status rc = check_ids(p, n, req_ids);
-  if (rc) return rc;
-  if (n > 0 && !n_q) return fail(CP_EINVAL, "null n_q");
-  cp_extend_opts o{};
-  if (opts) o = *opts;
-  if (o.rope) return fail(CP_EINVAL, "cp_attn_extend places no rows: opts.rope must be NULL");
-  ExtPlan pl;
-  rc = plan_extend(p, n, req_ids, n_q, nullptr, q, out, lse, o, &pl);
-  if (rc) return rc;
-  DeviceGuard g(p->device);
-  rc = bind_extend_workspace(p, pl);
-  if (rc) return rc;
-  return run_extend(p, pl, q, out, lse, o, (hipStream_t)hip_stream);
+  return guarded([&]() -> cp_status {
+    if (!p) return fail(CP_EINVAL, "null pool");
+    if (p->host_only) return fail(CP_ESTATE, "host-only pool cannot attend");
+    if (p->broken) return fail(CP_ESTATE, "a failed decode step left the device page stacks out of step; destroy the pool");
+    cp_status rc = check_ids(p, n, req_ids);
+    if (rc) return rc;
+    if (n > 0 && !n_q) return fail(CP_EINVAL, "null n_q");
+    cp_extend_opts o{};
+    if (opts) o = *opts;
+    if (o.rope) return fail(CP_EINVAL, "cp_attn_extend places no rows: opts.rope must be NULL");
+    ExtPlan pl;
+    rc = plan_extend(p, n, req_ids, n_q, nullptr, q, out, lse, o, &pl);
+    if (rc) return rc;
+    DeviceGuard g(p->device);
+    rc = bind_extend_workspace(p, pl);
+    if (rc) return rc;
+    return run_extend(p, pl, q, out, lse, o, (hipStream_t)hip_stream);
+  });
 }
 
 cp_status cp_attn_extend_step(cp_pool *p, int32_t n, const int32_t *req_ids, const int32_t *n_new, const void *rows,
                               const void *q, void *out, float *lse, void *hip_stream, const cp_extend_opts *opts) {
-  if (!p) return fail(CP_EINVAL, "null pool");
-  if (p->host_only) return fail(CP_ESTATE, "host-only pool cannot attend");
-  if (p->broken) return fail(CP_ESTATE, "a failed decode step left the device page stacks out of step; destroy the pool");
-  cp_status rc = check_ids(p, n, req_ids);
-  if (rc) return rc;
-  if (n > 0 && !n_new) return fail(CP_EINVAL, "null n_new");
-  cp_extend_opts o{};
-  if (opts) o = *opts;
-  bool any = false;
-  std::vector<int32_t> placing((size_t)n, 0);
-  for (int32_t i = 0; i < n; ++i) {
-    const Request &r = p->st.req(req_ids[i]);
-    if (n_new[i] < 0) return fail(CP_EINVAL, "negative n_new for request %d", req_ids[i]);
-    if (r.cursor == 0) {
-      if (r.ctx_len + n_new[i] > 0xFFFFFFF0ll) return fail(CP_EINVAL, "context length overflow");
-      if (!p->st.fits_reservation(req_ids[i], r.ctx_len + n_new[i]))
-        return fail(CP_EINVAL, "request %d would grow past its reservation of %lld pages", req_ids[i],
-                    (long long)r.reserve_pages);
-      placing[(size_t)i] = n_new[i];
-    } else if (n_new[i] != r.inflight) {
-      return fail(CP_EINVAL, "request %d is at layer %d of %d with %d tokens in flight: n_new must be that", req_ids[i],
-                  r.cursor, r.layers, r.inflight);
+  return guarded([&]() -> cp_status {
+    if (!p) return fail(CP_EINVAL, "null pool");
+    if (p->host_only) return fail(CP_ESTATE, "host-only pool cannot attend");
+    if (p->broken) return fail(CP_ESTATE, "a failed decode step left the device page stacks out of step; destroy the pool");
+    cp_status rc = check_ids(p, n, req_ids);
+    if (rc) return rc;
+    if (n > 0 && !n_new) return fail(CP_EINVAL, "null n_new");
+    cp_extend_opts o{};
+    if (opts) o = *opts;
+    bool any = false;
+    std::vector<int32_t> placing((size_t)n, 0);
+    for (int32_t i = 0; i < n; ++i) {
+      const Request &r = p->st.req(req_ids[i]);
+      if (n_new[i] < 0) return fail(CP_EINVAL, "negative n_new for request %d", req_ids[i]);
+      if (r.cursor == 0) {
+        if (r.ctx_len + n_new[i] > 0xFFFFFFF0ll) return fail(CP_EINVAL, "context length overflow");
+        if (!p->st.fits_reservation(req_ids[i], r.ctx_len + n_new[i]))
+          return fail(CP_EINVAL, "request %d would grow past its reservation of %lld pages", req_ids[i],
+                      (long long)r.reserve_pages);
+        placing[(size_t)i] = n_new[i];
+      } else if (n_new[i] != r.inflight) {
+        return fail(CP_EINVAL, "request %d is at layer %d of %d with %d tokens in flight: n_new must be that", req_ids[i],
+                    r.cursor, r.layers, r.inflight);
+      }
+      if (o.rope) {
+        rc = check_rope(p, p->st.model(r.model), o.rope);
+        if (rc) return rc;
+      }
+      any = any || n_new[i] > 0;
     }
-    if (o.rope) {
-      rc = check_rope(p, p->st.model(r.model), o.rope);
-      if (rc) return rc;
-    }
-    any = any || n_new[i] > 0;
-  }
-  if (any && !rows) return fail(CP_EINVAL, "null rows");
-  ExtPlan pl;
-  rc = plan_extend(p, n, req_ids, n_new, placing.data(), q, out, lse, o, &pl);
-  if (rc) return rc;
-  DeviceGuard g(p->device);
-  rc = bind_extend_workspace(p, pl);
-  if (rc) return rc;
-  rc = reconcile_pages(p);  // the page-table copies below must not overwrite popped entries
-  if (rc) return rc;
-  rc = prepare_growth(p, n, req_ids, placing.data());
-  if (rc) return rc;
+    if (any && !rows) return fail(CP_EINVAL, "null rows");
+    ExtPlan pl;
+    rc = plan_extend(p, n, req_ids, n_new, placing.data(), q, out, lse, o, &pl);
+    if (rc) return rc;
+    DeviceGuard g(p->device);
+    rc = bind_extend_workspace(p, pl);
+    if (rc) return rc;
+    rc = reconcile_pages(p);  // the page-table copies below must not overwrite popped entries
+    if (rc) return rc;
+    std::vector<AppItem> items;
+    items.reserve((size_t)n);
+    rc = prepare_growth(p, n, req_ids, placing.data());
+    if (rc) return rc;
 
-  // Pages of every plane are taken at the first layer; the entries of the
-  // current plane travel with the append launch where they fit, those of the
-  // other planes by a copy.
-  hipStream_t s = (hipStream_t)hip_stream;
-  const uint64_t row_elems = (uint64_t)pl.geom.row_elems;
-  std::vector<AppItem> items;
-  uint64_t src = 0, lo = UINT64_MAX, hi = 0, entries = 0;
-  bool other_planes = false;
-  for (int32_t i = 0; i < n; ++i) {
-    const Request &r = p->st.req(req_ids[i]);
-    const int64_t used = r.pages_used;
-    uint64_t first = 0, count = 0;
-    if (placing[(size_t)i] > 0) p->st.begin_chunk(req_ids[i], n_new[i], &first, &count);
-    if (count) {
-      lo = std::min(lo, first);
-      hi = std::max(hi, first + count);
-      other_planes = other_planes || r.layers > 1;
+    // Pages of every plane are taken at the first layer; the entries of the
+    // current plane travel with the append launch where they fit, those of the
+    // other planes by a copy.
+    hipStream_t s = (hipStream_t)hip_stream;
+    const uint64_t row_elems = (uint64_t)pl.geom.row_elems;
+    uint64_t src = 0, lo = UINT64_MAX, hi = 0, entries = 0;
+    bool other_planes = false;
+    for (int32_t i = 0; i < n; ++i) {
+      const Request &r = p->st.req(req_ids[i]);
+      const int64_t used = r.pages_used;
+      uint64_t first = 0, count = 0;
+      if (placing[(size_t)i] > 0) p->st.begin_chunk(req_ids[i], n_new[i], &first, &count);
+      if (count) {
+        lo = std::min(lo, first);
+        hi = std::max(hi, first + count);
+        other_planes = other_planes || r.layers > 1;
+      }
+      if (n_new[i] > 0) {
+        items.push_back(AppItem{r.model, (uint32_t)n_new[i], (uint32_t)r.ctx_len, r.plane_base(r.cursor), src,
+                                r.plane_base(r.cursor) + (uint64_t)used, (uint32_t)(r.pages_used - used)});
+        entries += (uint64_t)(r.pages_used - used);
+        src += (uint64_t)n_new[i] * row_elems;
+      }
     }
-    if (n_new[i] > 0) {
-      items.push_back(AppItem{r.model, (uint32_t)n_new[i], (uint32_t)r.ctx_len, r.plane_base(r.cursor), src,
-                              r.plane_base(r.cursor) + (uint64_t)used, (uint32_t)(r.pages_used - used)});
-      entries += (uint64_t)(r.pages_used - used);
-      src += (uint64_t)n_new[i] * row_elems;
+    if (other_planes || entries > (uint64_t)kAppEntMax) {
+      rc = push_ptes(p, lo, hi, s);
+      for (AppItem &x : items) x.n_ent = 0;
     }
-  }
-  if (other_planes || entries > (uint64_t)kAppEntMax) {
-    rc = push_ptes(p, lo, hi, s);
-    for (AppItem &x : items) x.n_ent = 0;
-  }
-  if (rc == CP_OK) rc = launch_appends(p, items, rows, s, o.rope);
-  if (rc == CP_OK) rc = run_extend(p, pl, q, out, lse, o, s);
-  for (int32_t i = 0; i < n; ++i) p->st.advance(req_ids[i]);
-  return rc;
+    if (rc == CP_OK) rc = launch_appends(p, items, rows, s, o.rope);
+    if (rc == CP_OK) rc = run_extend(p, pl, q, out, lse, o, s);
+    for (int32_t i = 0; i < n; ++i) p->st.advance(req_ids[i]);
+    return rc;
+  });
 }
 
 }  // extern "C"

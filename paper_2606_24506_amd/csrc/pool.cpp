@@ -494,6 +494,16 @@ uint32_t PoolState::sharers(uint32_t pte) const {
   return ch.more[(size_t)((pte % chunk256) / ((uint64_t)models_[ch.model].page_bytes >> 8))];
 }
 
+void PoolState::reserve_users(int32_t src, int64_t n_tok) {
+  const Request &s = reqs_[src];
+  const uint64_t chunk256 = chunk_bytes_ >> 8;
+  for (int32_t l = 0; l < s.layers; ++l)
+    for (int64_t i = 0; i < n_tok / P_; ++i) {
+      Chunk &ch = chunks_[(size_t)(pte_[s.plane_base(l) + (uint64_t)i] / chunk256)];
+      if (ch.more.empty()) ch.more.assign((size_t)models_[s.model].ppc, 0u);
+    }
+}
+
 void PoolState::fork(int32_t src, int32_t dst, int64_t n_tok) {
   const Request &s = reqs_[src];
   Request &d = reqs_[dst];
@@ -504,9 +514,7 @@ void PoolState::fork(int32_t src, int32_t dst, int64_t n_tok) {
     const uint32_t *from = pte_.data() + s.plane_base(l);
     uint32_t *to = pte_.data() + d.plane_base(l);
     for (int64_t i = 0; i < whole; ++i) {
-      Chunk &ch = chunks_[(size_t)(from[i] / chunk256)];
-      if (ch.more.empty()) ch.more.assign((size_t)g.ppc, 0u);
-      ch.more[(size_t)(from[i] % chunk256 / page256)] += 1;
+      chunks_[(size_t)(from[i] / chunk256)].more[(size_t)(from[i] % chunk256 / page256)] += 1;
       to[i] = from[i];
     }
     if (tail) alloc_pages(d.model, 1, to + whole);

@@ -190,9 +190,12 @@ class PoolState {
   // open request may still allocate (reserve_pages less the entries it uses),
   // so a shared page counts once.
   //
+  // Room for the user counts of src's first n_tok tokens' pages, so that fork
+  // itself allocates no memory.
+  void reserve_users(int32_t src, int64_t n_tok);
   // Makes the empty request dst show the first n_tok tokens of src: whole
   // pages shared, a page for the rest of its own in every plane (after
-  // ensure_slots).
+  // ensure_slots and reserve_users).
   void fork(int32_t src, int32_t dst, int64_t n_tok);
   // Truncation of requests, in two passes over all of a call's, so that no
   // page freed by one is another's copy while the launch still reads it.

@@ -74,13 +74,15 @@ cp_status cp_rope_create(const cp_rope_desc *d, int32_t device, cp_rope **out) {
   if (d->layout != CP_ROPE_HALF && d->layout != CP_ROPE_INTERLEAVED) return fail(CP_EINVAL, "unknown layout %d", d->layout);
   if (d->scaling < CP_ROPE_PLAIN || d->scaling > CP_ROPE_TABLE) return fail(CP_EINVAL, "unknown scaling %d", d->scaling);
   if (!std::isfinite(d->magnitude)) return fail(CP_EINVAL, "magnitude must be finite");
+  std::vector<double> turns;
+  const cp_status rc = guarded([&]() -> cp_status {
+    const char *e = angles_of(*d, &turns);
+    return *e ? fail(CP_EINVAL, "%s", e) : CP_OK;
+  });
+  if (rc) return rc;
   cp_rope *r = new (std::nothrow) cp_rope();
   if (!r) return fail(CP_ENOMEM, "host allocation failed");
-  const char *e = angles_of(*d, &r->turns);
-  if (*e) {
-    delete r;
-    return fail(CP_EINVAL, "%s", e);
-  }
+  r->turns.swap(turns);
   for (double &t : r->turns) t /= kTwoPi;
   r->rot = d->rot_dim;
   r->layout = d->layout;

@@ -141,6 +141,27 @@ def test_inverse_and_gradient():
     rope.destroy()
 
 
+def test_graph_replays_on_another_stream():
+    """Captured and replayed, with eager calls of other tensors between."""
+    rope = cpl.Rope(128, layout="half")
+    x = torch.randn(300, 9, 128, device="cuda").bfloat16()
+    pos = torch.arange(300, device="cuda", dtype=torch.int32) * 7
+    eager, got, other = torch.zeros_like(x), torch.zeros_like(x), torch.zeros_like(x)
+    rope.apply(cpl.rope_parts([(x, eager)]), pos)
+    torch.cuda.synchronize()
+    parts, st, graph = cpl.rope_parts([(x, got)]), torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    st.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(st), torch.cuda.graph(graph, stream=st):
+        rope.apply(parts, pos)
+    for _ in range(3):
+        got.zero_()
+        rope.apply(cpl.rope_parts([(got, other)]), first=5)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert (bits(got) == bits(eager)).all()
+    rope.destroy()
+
+
 def test_no_tokens():
     rope = cpl.Rope(32)
     x = torch.empty(0, 3, 32, device="cuda")
