@@ -1912,8 +1912,9 @@ struct ExtPlan {
 int32_t extend_kind(const Geom &g, int32_t path, int64_t n_q) {
   if (path == CP_PATH_VALU) return kXVec;
   if (g.kind == kGQA && (g.head_dim == 64 || g.head_dim == 128)) {
-    const bool few = n_q * g.g <= 32;
-    return g.head_dim == 64 ? (few ? kXFew64 : kXRows64) : (few ? kXFew128 : kXRows128);
+    const int64_t rows = n_q * g.g;
+    if (g.head_dim == 64) return rows <= 16 ? kXFew64 : rows <= 32 ? kXSome64 : kXRows64;
+    return rows <= 16 ? kXFew128 : rows <= 32 ? kXSome128 : kXRows128;
   }
   return g.kind == kMLA && g.latent == 512 && g.rope == 64 ? kXMla : kXVec;
 }
@@ -1941,7 +1942,7 @@ struct ExtItem {
 double choose_ranges(const Geom &g, int num_cus, uint64_t cap, std::vector<ExtItem> *items) {
   // us of a step of the kernel with its CUs full, and workgroups of a CU
   static constexpr struct { double us; int per_cu; } kCost[kXKinds] = {
-      {2.0, 8}, {1.4, 2}, {2.8, 2}, {2.7, 2}, {4.6, 2}, {2.6, 1}};
+      {2.0, 8}, {1.4, 2}, {2.8, 2}, {2.7, 2}, {4.6, 2}, {2.7, 2}, {4.6, 2}, {2.6, 1}};
   // a unit's start and end, another launch, and the way of partial rows
   constexpr double kUnit = 4.0, kLaunch = 5.0, kBytesPerUs = 3.0e6;
   double most = 1, base[kXKinds] = {}, all_units = 0, all_slots = 1e300;

@@ -13,18 +13,19 @@ namespace cp {
 // Kernels, chosen per call by the model's geometry and its rows per KV head.
 //   kXVec    vector: one wave per row, any geometry.
 //   kXRows*  matrix cores, GQA / MHA of head_dim 64 or 128: tiles of 128 rows.
-//   kXFew*   the same with 32 rows, the four waves taking keys in turn.
+//   kXSome*  the same with 32 rows, the four waves taking keys in turn.
+//   kXFew*   ... with 16 rows.
 //   kXMla    matrix cores, MLA with latent 512 and rotary part 64: 128 rows.
-enum : int32_t { kXVec = 0, kXRows64, kXRows128, kXFew64, kXFew128, kXMla, kXKinds };
+enum : int32_t { kXVec = 0, kXRows64, kXRows128, kXSome64, kXSome128, kXFew64, kXFew128, kXMla, kXKinds };
 
 constexpr int kExtThreads = 256;
 // Rows (a token and a query head of one KV head) of a tile, and keys of one
 // step, of each kernel.
 constexpr int32_t ext_tile_rows(int32_t kind) {
-  return kind == kXVec ? 4 : kind == kXFew64 || kind == kXFew128 ? 32 : 128;
+  return kind == kXVec ? 4 : kind == kXSome64 || kind == kXSome128 ? 32 : kind == kXFew64 || kind == kXFew128 ? 16 : 128;
 }
 constexpr int32_t ext_tile_keys(int32_t kind) {
-  return kind == kXFew64 || kind == kXFew128 ? 128 : kind == kXMla ? 32 : 64;
+  return kind >= kXSome64 && kind <= kXFew128 ? 128 : kind == kXMla ? 32 : 64;
 }
 
 // tanh(x) = x + x sum_{k > 0} kTanh[k] x^2k, to 4e-8 of its value under kCapEdge: a

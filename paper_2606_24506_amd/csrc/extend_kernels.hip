@@ -184,6 +184,8 @@ hipError_t launch_extend(const ExtArgs &a, int32_t kind, hipStream_t stream) {
     }
     case kXRows64:
     case kXRows128:
+    case kXSome64:
+    case kXSome128:
     case kXFew64:
     case kXFew128: launch_extend_rows(a, kind, stream); break;
     case kXMla: launch_extend_mla(a, stream); break;

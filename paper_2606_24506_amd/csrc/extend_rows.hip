@@ -49,6 +49,52 @@ CP_DEV int v_piece(int row, int c) {
   return D == 128 ? c ^ (4 * (row & 3)) : c ^ (4 * ((row >> 1) & 1));
 }
 
+// Results of a tile of ROWS rows from its four waves' m, l and sums (parts: [wave][column]
+// [row] in LDS). A thread takes D ROWS / 256 columns of one row.
+template <int D, int ROWS>
+CP_DEV void join_waves(const ExtArgs &a, const ExtReq &rq, const Unit &un, const float *parts,
+                       const float (&stats)[2][4][ROWS]) {
+  constexpr int NC = D * ROWS / kExtThreads;
+  const int row = threadIdx.x % ROWS, c0 = threadIdx.x / ROWS * NC;
+  const uint32_t r = un.tile * ROWS + row;
+  if (r >= rq.n_tok * (uint32_t)a.g.g) return;
+  const Row y = row_of(a, rq, un.kvh, r);
+  float mt = stats[0][0][row];
+#pragma unroll
+  for (int w = 1; w < 4; ++w) mt = __builtin_fmaxf(mt, stats[0][w][row]);
+  const float ref = mt == -INFINITY ? 0.f : mt;
+  float f[4], sum = 0.f;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    f[w] = fast_exp2(stats[0][w][row] - ref);
+    sum += f[w] * stats[1][w][row];
+  }
+  const bool none = sum == 0.f;
+  const float inv = none ? 0.f : 1.f / sum, lse = none ? -INFINITY : mt + fast_log2(sum);
+  float v[NC];
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    float acc = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w)  // a wave that saw nothing of the row has nothing to add
+      if (f[w] > 0.f) acc += f[w] * parts[w * ROWS * D + (c0 + c) * ROWS + row];
+    v[c] = acc * inv;
+  }
+  if (rq.all > 1) {
+    const uint64_t pr = part_row(a, rq, y, un.split);
+#pragma unroll
+    for (int c = 0; c < NC; c += 4)
+      *reinterpret_cast<f32x4 *>(a.ws_o + pr * D + c0 + c) = f32x4{v[c], v[c + 1], v[c + 2], v[c + 3]};
+    if (c0 == 0) a.ws_l[pr] = lse;
+  } else {
+    const uint64_t orow = y.tok * (uint32_t)a.g.hq + y.head;
+#pragma unroll
+    for (int c = 0; c < NC; c += 4)
+      *reinterpret_cast<uint2 *>(a.out + orow * D + c0 + c) = bf16x4_bits(v[c], v[c + 1], v[c + 2], v[c + 3]);
+    if (c0 == 0) a.lse[orow] = lse * kLn2;
+  }
+}
+
 template <int D, int RW, int MODE>
 __global__ __launch_bounds__(kExtThreads, 2) void extend_rows_kernel(const ExtArgs a) {
   using C = ExtCfg<D, RW>;
@@ -373,47 +419,238 @@ __global__ __launch_bounds__(kExtThreads, 2) void extend_rows_kernel(const ExtAr
       stats[1][wave][col] = l;
     }
     __syncthreads();
-    // thread: row t % 32, D / 8 columns
-    constexpr int NC = D / 8;
-    const int row = threadIdx.x & 31, c0 = (threadIdx.x >> 5) * NC;
-    const uint32_t rr = un.tile * 32 + row;
-    if (rr >= rq.n_tok * (uint32_t)g.g) return;
-    const Row y = row_of(a, rq, un.kvh, rr);
-    float mt = stats[0][0][row];
+    join_waves<D, 32>(a, rq, un, reinterpret_cast<const float *>(lds), stats);
+  }
+}
+
+// At most 16 rows a KV head (single tokens of groups to 16 heads): bound by reading
+// KV. As RW = 1 above, but by 16x16x32 products, which leave a lane 8 scores of 32
+// keys and not 16, half of them of rows that are not there: the vector unit's
+// work for one row a tile halves, and so do the registers of queries and
+// sums. Lanes are (row `col` of 16, quarter `quad`); pieces of LDS rows are swapped
+// so that K reads (16 rows at one piece) and V reads (8 rows at two) meet no bank
+// twice.
+template <int D>
+struct ExtFew {
+  static constexpr int KW = 32, KEYS = 128, ROW = 2 * D, CPR = D / 8, TILE = KW * ROW;
+  static constexpr int RPI = 64 / CPR, NL = KW / RPI;
+  static constexpr int KS = D / 32, DB = D / 16;
+  static constexpr int LDS = 8 * TILE;
+  static_assert(LDS >= 4 * 16 * D * 4, "the join reuses the tiles");
+};
+template <int D>
+CP_DEV int few_piece(int row, int c) {
+  return c ^ (D == 128 ? (2 * row) & 15 : row & 6);
+}
+
+template <int D, int MODE>
+__global__ __launch_bounds__(kExtThreads, 2) void extend_few_kernel(const ExtArgs a) {
+  using C = ExtFew<D>;
+  __shared__ __attribute__((aligned(16))) char lds[C::LDS];
+  __shared__ float stats[2][4][16];  // the waves' m and l
+  const Unit un = find_unit(a);
+  if (un.none) return;
+  const ExtReq &rq = *un.rq;
+  const GeomK &g = a.g;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 15, quad = lane >> 4;
+  const uint32_t P = (uint32_t)g.page_tokens;
+
+  const Row x = row_of(a, rq, un.kvh, un.tile * 16 + col);
+  const Sight gs = wave_sight<8>(x);  // every wave has the same rows
+  const uint32_t first = gs.lo / C::KEYS, last = (gs.hi + C::KEYS - 1) / C::KEYS, steps = last - first;
+  const uint32_t s0 = first + (uint32_t)((uint64_t)steps * un.split / rq.splits),
+                 s1 = first + (uint32_t)((uint64_t)steps * (un.split + 1) / rq.splits);
+
+  // ---- loads, as in extend_rows_kernel
+  const int lc = lane % C::CPR, lr = lane / C::CPR;
+  const uint8_t *const head_base = a.pool + (uint64_t)un.kvh * (4ull * P * D) + 16 * lc;
+  u32x4e kreg[C::NL], vreg[C::NL];
+  auto base_of = [&](uint32_t s) { return s * C::KEYS + 32u * wave; };
+  uint32_t key_pte = 0, key_slot = 0;
+  auto look_up = [&](uint32_t s) {
+    const uint32_t key = min(max(base_of(s) + (lane & 31), gs.lo), gs.hi - 1);
+    key_pte = a.pte[rq.pte_base + page_divide(key, P, a.page_magic, &key_slot)];
+  };
+  auto row_ptr = [&](int i) {
+    const int row = lr + C::RPI * i;
+    const uint32_t pte = (uint32_t)__shfl((int)key_pte, row, 64), slot = (uint32_t)__shfl((int)key_slot, row, 64);
+    return reinterpret_cast<const u32x4e *>(head_base + ((uint64_t)pte << 8) + slot * C::ROW);
+  };
+  auto load_keys = [&] {
 #pragma unroll
-    for (int w = 1; w < 4; ++w) mt = __builtin_fmaxf(mt, stats[0][w][row]);
-    const float ref = mt == -INFINITY ? 0.f : mt;
-    float f[4], lt4 = 0.f;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      f[w] = fast_exp2(stats[0][w][row] - ref);
-      lt4 += f[w] * stats[1][w][row];
+    for (int i = 0; i < C::NL; ++i) {
+      const u32x4e *const kp = row_ptr(i);
+      kreg[i] = __builtin_nontemporal_load(kp);
+      vreg[i] = __builtin_nontemporal_load(kp + P * C::CPR);
     }
-    const bool none = lt4 == 0.f;
-    const float inv = none ? 0.f : 1.f / lt4, lse = none ? -INFINITY : mt + fast_log2(lt4);
-    float v[NC];
+  };
+  if (s0 < s1) look_up(s0);
+
+  bf16x8 qf[C::KS];
+  {
+    const uint16_t *const qrow = a.q + (x.tok * (uint32_t)g.hq + x.head) * D + 8 * quad;
 #pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      float acc = 0.f;
+    for (int ks = 0; ks < C::KS; ++ks) qf[ks] = *reinterpret_cast<const bf16x8 *>(qrow + 32 * ks);
+  }
+  const float slope = MODE == kModeAny && a.slopes ? a.slopes[x.head] * kLog2e : 0.f;
+  float m = -INFINITY, l = 0.f;
+  f32x4 o[C::DB];
 #pragma unroll
-      for (int w = 0; w < 4; ++w)  // a wave that saw nothing of the row has nothing to add
-        if (f[w] > 0.f) acc += f[w] * reinterpret_cast<const float *>(lds)[w * 32 * D + (c0 + c) * 32 + row];
-      v[c] = acc * inv;
+  for (int d = 0; d < C::DB; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  char *const kt = lds + wave * (2 * C::TILE), *const vt = kt + C::TILE;
+  auto mixed = [&](uint32_t s) {
+    const uint32_t b = base_of(s);
+    return b < gs.all_lo || b + C::KW > gs.all_hi;
+  };
+  uint32_t sp_first = 0xFFFFFFFFu, sp_last = 0;
+  auto store_v = [&] {
+#pragma unroll
+    for (int i = 0; i < C::NL; ++i) {
+      const int row = lr + C::RPI * i;
+      *reinterpret_cast<u32x4e *>(vt + row * C::ROW + 16 * few_piece<D>(row, lc)) = vreg[i];
     }
-    if (rq.all > 1) {
-      const uint64_t pr = part_row(a, rq, y, un.split);
+  };
+  auto store_keys = [&](uint32_t s) {
+    if (mixed(s)) {
+      bool any = false;
 #pragma unroll
-      for (int c = 0; c < NC; c += 4)
-        *reinterpret_cast<f32x4 *>(a.ws_o + pr * D + c0 + c) = f32x4{v[c], v[c + 1], v[c + 2], v[c + 3]};
-      if (c0 == 0) a.ws_l[pr] = lse;
-    } else {
-      const uint64_t orow = y.tok * (uint32_t)g.hq + y.head;
+      for (int i = 0; i < C::NL; ++i) any = any || any_special(vreg[i]);
+      if (__builtin_amdgcn_ballot_w64(any)) {
+        sp_first = min(sp_first, s);
+        sp_last = s;
 #pragma unroll
-      for (int c = 0; c < NC; c += 4)
-        *reinterpret_cast<uint2 *>(a.out + orow * D + c0 + c) = bf16x4_bits(v[c], v[c + 1], v[c + 2], v[c + 3]);
-      if (c0 == 0) a.lse[orow] = lse * kLn2;
+        for (int i = 0; i < C::NL; ++i) vreg[i] = without_special(vreg[i]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < C::NL; ++i) {
+      const int row = lr + C::RPI * i;
+      *reinterpret_cast<u32x4e *>(kt + row * C::ROW + 16 * few_piece<D>(row, lc)) = kreg[i];
+    }
+    store_v();
+  };
+  // V^T of a step's keys 4 quad + {0..3} and 16 on, and block d of 16 columns
+  auto v_frag = [&](int d) {
+    const int vr = 4 * quad + (col >> 2);
+    s16x4 f[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      f[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(
+          vt + (vr + 16 * h) * C::ROW + 16 * few_piece<D>(vr + 16 * h, 2 * d + ((col >> 1) & 1)) + 8 * (col & 1)));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(f[0], f[1], 0, 1, 2, 3, 4, 5, 6, 7));
+  };
+
+  if (s0 < s1) {
+    load_keys();
+    if (s0 + 1 < s1) look_up(s0 + 1);
+  }
+#pragma unroll 1
+  for (uint32_t s = s0; s < s1; ++s) {
+    store_keys(s);
+    if (s + 1 < s1) {
+      load_keys();
+      if (s + 2 < s1) look_up(s + 2);
+    }
+    // a wave's LDS operations run in order: its reads follow its writes
+    __builtin_amdgcn_wave_barrier();
+    const uint32_t b0 = base_of(s), k0 = b0 + 4 * quad;  // element (u, i): key k0 + 16 u + i
+    if (b0 < gs.hi && b0 + C::KW > gs.lo) {
+      f32x4 sc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+      for (int ks = 0; ks < C::KS; ++ks)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const int row = 16 * u + col;
+          const bf16x8 kf = *reinterpret_cast<const bf16x8 *>(kt + row * C::ROW + 16 * few_piece<D>(row, 4 * ks + quad));
+          sc[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[ks], sc[u], 0, 0, 0);
+        }
+      auto &flat = reinterpret_cast<float(&)[8]>(sc);
+      float t;
+      const bool raw = scores_of<MODE, 8>(a, flat, slope, x, k0, b0 + C::KW <= gs.pos + 1, mixed(s),
+                                          [](int i) { return 16 * (i / 4) + i % 4; }, &t);
+      // the reference moves when some row's maximum passes it by 2^kLazy
+      if (__builtin_amdgcn_ballot_w64(t > m + kLazy || (m == -INFINITY && t > m))) {
+        const float mt = xor_max_16_32(t);
+        const float mn = mt > m + kLazy || m == -INFINITY ? __builtin_fmaxf(mt, m) : m;
+        const float al = mn == -INFINITY ? 1.f : fast_exp2(m - mn);
+        m = mn;
+        l *= al;
+#pragma unroll
+        for (int d = 0; d < C::DB; ++d) o[d] *= al;
+      }
+      const float ref = m == -INFINITY ? 0.f : m;
+      uint32_t pw[2][4];
+      weights<MODE, 8>(a, flat, raw, ref, [&](int i, float p0, float p1) {
+        l += p0 + p1;
+        // leading 8 bits, and the rest rounded: together 16 bits and a half step
+        const uint32_t h0 = __float_as_uint(p0) & 0xFFFF0000u, h1 = __float_as_uint(p1) & 0xFFFF0000u;
+        pw[0][i / 2] = upper_halves(h0, h1);
+        // (kept above zero: an infinite V times 0 would be NaN)
+        pw[1][i / 2] = pack_bf16x2(__builtin_fmaxf(p0 - __uint_as_float(h0), 1e-37f),
+                                   __builtin_fmaxf(p1 - __uint_as_float(h1), 1e-37f));
+      });
+#pragma unroll
+      for (int d = 0; d < C::DB; ++d) {
+        const bf16x8 vf = v_frag(d);
+#pragma unroll
+        for (int part = 0; part < 2; ++part)
+          o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+              vf, __builtin_bit_cast(bf16x8, u32x4e{pw[part][0], pw[part][1], pw[part][2], pw[part][3]}), o[d], 0, 0, 0);
+      }
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+
+  // ---- infinities and NaN of V that not every row sees (as in extend_rows_kernel)
+  sp_first = __builtin_amdgcn_readfirstlane(sp_first);
+  sp_last = __builtin_amdgcn_readfirstlane(sp_last);
+  if (__builtin_expect(sp_first <= sp_last, 0)) {
+#pragma unroll 1
+    for (uint32_t s = sp_first; s <= sp_last; ++s) {
+      if (!mixed(s)) continue;
+      look_up(s);
+#pragma unroll
+      for (int i = 0; i < C::NL; ++i) vreg[i] = row_ptr(i)[P * C::CPR];
+      store_v();
+      __builtin_amdgcn_wave_barrier();
+      const uint32_t k0 = base_of(s) + 4 * quad, lo = x.lo - k0, n = x.hi - x.lo;
+      u32x4e seen;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const uint32_t e = 16 * (k / 2) + 2 * (k % 2);
+        seen[k] = (e - lo < n ? 0x3F80u : 0u) | (e + 1 - lo < n ? 0x3F800000u : 0u);
+      }
+#pragma unroll
+      for (int d = 0; d < C::DB; ++d)
+#pragma unroll 1
+        for (uint32_t sign = 0; sign < 2; ++sign) {
+          f32x4 hit = {0.f, 0.f, 0.f, 0.f};
+          hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(special_ones(v_frag(d), sign), __builtin_bit_cast(bf16x8, seen),
+                                                        hit, 0, 0, 0);
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (hit[i] > 0.f) o[d][i] += sign ? -INFINITY : INFINITY;
+        }
+      __builtin_amdgcn_wave_barrier();
     }
   }
+
+  // ---- the waves' sums joined: columns 16 d + 4 quad + {0..3} of row `col`
+  l = xor_sum_16_32(l);
+  __syncthreads();  // every wave is done with its tile
+  float *const part = reinterpret_cast<float *>(lds) + wave * (16 * D);  // [column][row]
+#pragma unroll
+  for (int d = 0; d < C::DB; ++d)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) part[(16 * d + 4 * quad + i) * 16 + col] = o[d][i];
+  if (quad == 0) {
+    stats[0][wave][col] = m;
+    stats[1][wave][col] = l;
+  }
+  __syncthreads();
+  join_waves<D, 16>(a, rq, un, reinterpret_cast<const float *>(lds), stats);
 }
 
 namespace {
@@ -427,14 +664,26 @@ void launch_rows(const ExtArgs &a, hipStream_t stream) {
   else
     hipLaunchKernelGGL((extend_rows_kernel<D, RW, kModePlain>), grid, block, 0, stream, a);
 }
+template <int D>
+void launch_few(const ExtArgs &a, hipStream_t stream) {
+  const dim3 grid((uint32_t)a.n_units), block(kExtThreads);
+  if (a.slopes)
+    hipLaunchKernelGGL((extend_few_kernel<D, kModeAny>), grid, block, 0, stream, a);
+  else if (a.softcap > 0.f)
+    hipLaunchKernelGGL((extend_few_kernel<D, kModeCap>), grid, block, 0, stream, a);
+  else
+    hipLaunchKernelGGL((extend_few_kernel<D, kModePlain>), grid, block, 0, stream, a);
+}
 }  // namespace
 
 void launch_extend_rows(const ExtArgs &a, int32_t kind, hipStream_t stream) {
   switch (kind) {
     case kXRows64: return launch_rows<64, 4>(a, stream);
     case kXRows128: return launch_rows<128, 4>(a, stream);
-    case kXFew64: return launch_rows<64, 1>(a, stream);
-    default: return launch_rows<128, 1>(a, stream);
+    case kXSome64: return launch_rows<64, 1>(a, stream);
+    case kXSome128: return launch_rows<128, 1>(a, stream);
+    case kXFew64: return launch_few<64>(a, stream);
+    default: return launch_few<128>(a, stream);
   }
 }
 
