@@ -657,7 +657,7 @@ typedef struct {
  * calls do: it must not overlap with them on the GPU, and before a call is
  * captured into a graph, the same one must have run once (a capped pool's
  * graphs are captured anew once a call has needed more workspace).
- * Errors: CP_EINVAL (also: more than 2^23 units of work of one request:
+ * Errors: CP_EINVAL (also: more than 2^22 units of work of one request:
  * tiles of 4 rows on the vector path, of 128 otherwise), CP_ESTATE (host-only
  * pool), CP_ENOMEM (workspace), CP_EHIP. */
 cp_status cp_attn_extend(cp_pool *pool, int32_t n, const int32_t *req_ids, const int32_t *n_q, const void *q,

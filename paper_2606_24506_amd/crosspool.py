@@ -474,12 +474,12 @@ def rope_parts(pairs, offset: int = 0):
             raise ValueError("the last dimension must be contiguous")
         if tokens not in (None, s.shape[0]):
             raise ValueError("the tensors differ in tokens")
-        if s.device != d.device:
-            raise ValueError("src and dst are on different devices")
+        if s.device != d.device or s.device.type != "cuda" or s.device != pairs[0][0].device:
+            raise ValueError("the tensors are on one GPU")
         tokens = s.shape[0]
         arr[i] = cp_rope_tensor(s.data_ptr(), d.data_ptr(), s.stride(0), s.stride(1), d.stride(0), d.stride(1),
                                 s.shape[1], s.shape[2], offset, CP_ROPE_F32 if s.dtype == torch.float32 else CP_ROPE_BF16)
-    arr.tokens, arr.keep = tokens or 0, pairs
+    arr.tokens, arr.keep, arr.device = tokens or 0, pairs, pairs[0][0].device.index if pairs else None
     return arr
 
 
@@ -579,6 +579,8 @@ class Rope:
         return cp_rope_angles(self.handle, self.rot_dim)
 
     def apply(self, parts, positions=None, first: int = 0, inverse: bool = False, stream=None) -> None:
+        if parts.device not in (None, self.device):
+            raise ValueError(f"the rotation is on device {self.device}, the tensors on {parts.device}")
         cp_rope_apply(self.handle, parts, positions, first, inverse, stream)
 
     def destroy(self) -> None:

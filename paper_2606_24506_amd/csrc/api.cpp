@@ -1891,7 +1891,9 @@ cp_status cp_attn_decode_step(cp_pool *p, int32_t n, const int32_t *req_ids, con
 
 namespace {
 
-constexpr int64_t kMaxExtUnits = 1 << 23;  // of one launch
+// Workgroups, and joined rows, of one launch, which has less than 2^32 threads.
+constexpr int64_t kMaxExtUnits = 1 << 22;
+constexpr uint32_t kMaxJoinRows = 1u << 22;
 
 // A planned cp_attn_extend: launches by kernel, and the rows whose ranges are joined.
 struct ExtPlan {
@@ -2142,8 +2144,12 @@ cp_status plan_extend(cp_pool *p, int32_t n, const int32_t *ids, const int32_t *
     m.ws_row = (pl->ws_rows + (uint64_t)ranges - 1) / (uint64_t)ranges;
     m.out_row = (uint64_t)tok[(size_t)first] * (uint64_t)g.hq;
     pl->ws_rows = (m.ws_row + m.rows) * (uint64_t)ranges;
-    pl->joins.push_back(m);
-    return m.ws_row;
+    const uint64_t at = m.ws_row;
+    for (uint32_t left = m.rows; left > 0; left -= m.rows, m.ws_row += m.rows, m.out_row += m.rows) {
+      m.rows = std::min(left, kMaxJoinRows);
+      pl->joins.push_back(m);
+    }
+    return at;
   };
   // long units first
   std::vector<int32_t> order(it.size());
@@ -2266,7 +2272,7 @@ cp_status run_extend(cp_pool *p, const ExtPlan &pl, const void *q, void *out, fl
     m.lse = lse;
     m.d_v = g.d_v;
     uint32_t rows = 0, most = 1;
-    for (; i < pl.joins.size() && m.n_req < kMaxReqPerLaunch; ++i) {
+    for (; i < pl.joins.size() && m.n_req < kMaxReqPerLaunch && rows + pl.joins[i].rows <= 2 * kMaxJoinRows; ++i) {
       ExtMergeArgs::Req &x = m.req[m.n_req++];
       x = pl.joins[i];
       x.row_begin = rows;

@@ -122,16 +122,32 @@ hipError_t launch_rope(const RopeArgs &in, int32_t items, bool f32, hipStream_t 
   RopeArgs a = in;
   // fewer tokens where the items of one would pass 2^31 / tokens
   a.tokens = (int32_t)std::max<int64_t>(1, std::min<int64_t>({kRopeThreads / a.rope.pairs, a.n_tokens, 0x3FFFFFFF / items}));
-  const int64_t blocks = (a.n_tokens + a.tokens - 1) / a.tokens, rounds = ((int64_t)a.tokens * items + kRopeThreads - 1) / kRopeThreads;
-  // few tokens: one round of items per workgroup (latency); many: up to eight
-  const int64_t per = blocks * rounds <= 2048 ? 1 : 8;
-  const dim3 grid((uint32_t)blocks, (uint32_t)std::min<int64_t>(65535, (rounds + per - 1) / per));
+  const int64_t rounds = ((int64_t)a.tokens * items + kRopeThreads - 1) / kRopeThreads;
   const size_t lds = (size_t)a.tokens * a.rope.pairs * sizeof(float2);
-  if (f32)
-    hipLaunchKernelGGL(rope_kernel<true>, grid, dim3(kRopeThreads), lds, stream, a);
-  else
-    hipLaunchKernelGGL(rope_kernel<false>, grid, dim3(kRopeThreads), lds, stream, a);
-  return hipGetLastError();
+  const int64_t size = f32 ? 4 : 2;
+  for (int64_t done = 0; done < in.n_tokens;) {
+    const int64_t blocks = (in.n_tokens - done + a.tokens - 1) / a.tokens;
+    // few tokens: one round of items per workgroup (latency); many: up to eight
+    const int64_t per = blocks * rounds <= 2048 ? 1 : 8, slices = std::min<int64_t>(65535, (rounds + per - 1) / per);
+    // (a launch has less than 2^32 threads)
+    const int64_t most = std::max<int64_t>(1, ((1 << 24) - 1) / slices), now = std::min(blocks, most);
+    a.n_tokens = std::min(in.n_tokens - done, now * a.tokens);
+    a.first = in.first + done;
+    a.pos = in.pos ? in.pos + done : nullptr;
+    for (int i = 0; i < a.n_parts; ++i) {
+      a.part[i].src = (const char *)in.part[i].src + done * in.part[i].src_tok * size;
+      a.part[i].dst = (char *)in.part[i].dst + done * in.part[i].dst_tok * size;
+    }
+    const dim3 grid((uint32_t)now, (uint32_t)slices);
+    if (f32)
+      hipLaunchKernelGGL(rope_kernel<true>, grid, dim3(kRopeThreads), lds, stream, a);
+    else
+      hipLaunchKernelGGL(rope_kernel<false>, grid, dim3(kRopeThreads), lds, stream, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    done += a.n_tokens;
+  }
+  return hipSuccess;
 }
 
 // ------------------------------------------------------- append, rotated

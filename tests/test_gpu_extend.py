@@ -266,6 +266,28 @@ def test_many_requests_take_several_launches():
     sc.close()
 
 
+def test_more_joined_rows_than_one_launch_takes():
+    """2^22 and some rows in two ranges: the join goes in parts, and gives what
+    whole rows give (each side off by the roundings of its probabilities)."""
+    n = (1 << 14) + 50
+    pool = cpl.Pool(page_tokens=64, pool_bytes=64 << 20, device=0)
+    m = pool.register(cpl.CP_KIND_GQA, 256, 1, head_dim=64)
+    rid = pool.open(m, n)
+    pool.append([rid], [n], torch.randn(n, 128, device="cuda").bfloat16())
+    q = torch.randn(n, 256, 64, device="cuda").bfloat16()
+    out, lse = torch.zeros_like(q), torch.zeros(n, 256, device="cuda")
+    o2, l2 = torch.zeros_like(q), torch.zeros(n, 256, device="cuda")
+    pool.extend([rid], [n], q, out, lse, num_splits=2, window=3000)
+    pool.extend([rid], [n], q, o2, l2, num_splits=1, window=3000)
+    torch.cuda.synchronize()
+    assert torch.allclose(lse, l2, atol=1e-4)
+    # outputs to half a step each, probabilities to 2^-8 of sums of p |v|, where |v| < 6
+    assert ((out.float() - o2.float()).abs() <= 2.0 ** -7 * out.float().abs() + 2 * 2.0 ** -8 * 6).all()
+    assert (out[-1].float() - o2[-1].float()).abs().max() < 0.02 and (o2[-1] != 0).any()
+    pool.close(rid)
+    pool.destroy()
+
+
 def test_long_context_far_positions():
     """One row over 70001 tokens, planned ranges, slopes and a cap."""
     sc = Scene("gqa8x2d128", [70001], seed=13)

@@ -162,6 +162,39 @@ def test_graph_replays_on_another_stream():
     rope.destroy()
 
 
+def test_more_tokens_than_one_launch_takes():
+    """2^24 + 11 tokens, one a workgroup: a launch has less than 2^32 threads."""
+    n = (1 << 24) + 11
+    rope = cpl.Rope(260, layout="interleaved")
+    y = torch.zeros(n, 1, 260, dtype=torch.bfloat16, device="cuda")
+    src = torch.ones(1, 1, 260, dtype=torch.bfloat16, device="cuda").expand(n, 1, 260)  # read over and over
+    rope.apply(cpl.rope_parts([(src, y)]), first=-7)
+    torch.cuda.synchronize()
+    for t in (0, 7, 1 << 23, (1 << 24) - 2, (1 << 24) - 1, 1 << 24, n - 1):
+        want = turn(torch.ones(1, 1, 260), rope.angles(), torch.tensor([t - 7]), "interleaved")
+        got = y[t:t + 1].double().cpu()
+        assert ((got - want).abs() <= allowed(want, torch.full_like(want, 2 ** 0.5), torch.bfloat16)).all(), t
+    rope.destroy()
+
+
+def test_tensors_that_do_not_fit_are_refused():
+    x = torch.zeros(4, 2, 32, device="cuda")
+    rope = cpl.Rope(32)
+    for src, dst in ((x, x.cpu()), (x.cpu(), x.cpu()), (x, x.half()), (x.half(), x.half()), (x, x[:3]),
+                     (x.transpose(1, 2), x.transpose(1, 2)), (x[0], x[0])):
+        with pytest.raises(ValueError):
+            cpl.rope_parts([(src, dst)])
+    with pytest.raises(ValueError):
+        rope.apply(cpl.rope_parts([(x, x)]), torch.zeros(5, dtype=torch.int32, device="cuda"))
+    with pytest.raises(ValueError):
+        rope.apply(cpl.rope_parts([(x, x)]), torch.zeros(4, dtype=torch.int64, device="cuda"))
+    with pytest.raises(cpl.CrossPoolError):
+        rope.apply(cpl.rope_parts([(x, x)], offset=1))
+    with pytest.raises(cpl.CrossPoolError):
+        rope.apply(cpl.rope_parts([(x.expand(4, 2, 32), x.as_strided((4, 2, 32), (0, 32, 1)))]))
+    rope.destroy()
+
+
 def test_no_tokens():
     rope = cpl.Rope(32)
     x = torch.empty(0, 3, 32, device="cuda")
