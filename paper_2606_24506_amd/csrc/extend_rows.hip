@@ -19,9 +19,17 @@ namespace cp {
 // reads four rows at four pieces.
 //
 // RW = 4: 128 rows, a wave for every 32, all over the same 64 keys a step; the
-// next step's keys travel through registers while this one's are worked on.
+// next step's keys go to LDS directly while this one's are worked on (through
+// registers, the loads' shuffles and LDS stores were a fifth of the vector unit's
+// work, and 40 registers). Bound by the vector unit (exponentials, cap) and the
+// matrix cores, which overlap only as far as two workgroups a CU take turns, and by
+// LDS, whose reads for 32 rows take as long as the products at their peak:
+// head_dim 128, chunks of 2,048 over 16 K keys, 847 TFLOP/s plain, 724 to 740 capped,
+// 718 sloped (through registers 810, 726, 732); head_dim 64 680, 550, 538 (636, 520, 549).
+// Steps of 32 keys and three workgroups a CU: 847, 748, 660; and 595, 467, 427.
 // RW = 1: 32 rows, every wave with 32 keys of its own a step (few rows: bound
-// by reading KV); the waves' sums join at the end.
+// by reading KV); the waves' sums join at the end. Its loads pass through
+// registers, because a wave's keys are its own and no barrier is needed.
 template <int D, int RW>
 struct ExtCfg {
   static constexpr int KW = RW == 4 ? 64 : 32;        // keys of a wave's step
@@ -30,9 +38,8 @@ struct ExtCfg {
   static constexpr int CPR = D / 8;                   // 16-byte pieces of a row
   static constexpr int TILE = KW * ROW;               // bytes of K (or V) of a step of a wave's keys
   static constexpr int BUFS = RW == 4 ? 2 : 4;        // double buffer, or one for each wave
-  static constexpr int LOADERS = RW == 4 ? 256 : 64;  // threads that fill one
-  static constexpr int RPI = LOADERS / CPR;           // rows that they fill at once
-  static constexpr int NL = KW / RPI;                 // 16-byte loads of K (and of V) of a thread
+  static constexpr int RPI = 64 / CPR;                // rows that a wave loads at once
+  static constexpr int NL = KW / RPI;                 // 16-byte loads of K (and of V) of a thread (RW 1)
   static constexpr int KB = KW / 32;                  // blocks of 32 keys
   static constexpr int NP = RW == 4 ? 1 : 2;          // bf16 parts of a probability
   static constexpr int LDS = 2 * TILE * BUFS;
@@ -136,10 +143,10 @@ __global__ __launch_bounds__(kExtThreads, 2) void extend_rows_kernel(const ExtAr
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
 
-  // ---- loads: a thread takes piece lc of rows lr, lr + RPI, ... of a step. Lane
+  // ---- loads. RW 1: a lane takes piece lc of rows lr, lr + RPI, ... of a step. Lane
   // i of every wave looks key i up, a step ahead; keys out of sight are looked up
   // as the nearest one in sight (they are hidden below, and never stale memory).
-  const int lt = RW == 4 ? (int)threadIdx.x : lane, lc = lt % C::CPR, lr = lt / C::CPR;
+  const int lc = lane % C::CPR, lr = lane / C::CPR;
   const uint8_t *const head_base = a.pool + (uint64_t)un.kvh * (4ull * P * D) + 16 * lc;
   u32x4e kreg[C::NL], vreg[C::NL];
   // keys of step s: RW 4, [64 s, + 64); RW 1, wave w has [128 s + 32 w, + 32)
@@ -151,7 +158,7 @@ __global__ __launch_bounds__(kExtThreads, 2) void extend_rows_kernel(const ExtAr
   };
   auto load_v = [&](int i, const uint8_t *kp) {
     const u32x4e *const p = reinterpret_cast<const u32x4e *>(kp + (uint64_t)P * C::ROW);
-    vreg[i] = RW == 4 ? *p : __builtin_nontemporal_load(p);
+    vreg[i] = __builtin_nontemporal_load(p);
   };
   auto row_ptr = [&](int i) {
     const int row = lr + C::RPI * i;
@@ -163,8 +170,7 @@ __global__ __launch_bounds__(kExtThreads, 2) void extend_rows_kernel(const ExtAr
     for (int i = 0; i < C::NL; ++i) {
       const uint8_t *const kp = row_ptr(i);
       const u32x4e *const p = reinterpret_cast<const u32x4e *>(kp);
-      kreg[i] = RW == 4 ? *p : __builtin_nontemporal_load(p);
-      if (RW == 4) load_v(i, kp);
+      kreg[i] = __builtin_nontemporal_load(p);
     }
   };
   // RW 1 asks for the next V once the scores' registers are free: 64 registers of
@@ -172,6 +178,21 @@ __global__ __launch_bounds__(kExtThreads, 2) void extend_rows_kernel(const ExtAr
   auto load_values = [&] {
 #pragma unroll
     for (int i = 0; i < C::NL; ++i) load_v(i, row_ptr(i));
+  };
+  // RW 4: a wave's quarter of a step straight to LDS, 1 KiB a load. The lane for a
+  // 16-byte place of LDS loads the piece that belongs there (the swaps undo themselves).
+  auto issue = [&](int buf, bool keys, bool values) {
+    const uint32_t kt = lds_addr(lds) + buf * (2 * C::TILE), vt = kt + C::TILE;
+    const int ln = lane_ids().lane;     // (counted afresh: formed here, not kept through the loop)
+#pragma unroll
+    for (int i = 0; i < C::KW / 4 / C::RPI; ++i) {
+      const int row0 = wave * (C::KW / 4) + C::RPI * i, row = row0 + ln / C::CPR, p = ln % C::CPR;
+      const uint64_t base = (uint64_t)(uintptr_t)a.pool + (uint64_t)un.kvh * (4ull * P * D) +
+                            ((uint64_t)(uint32_t)__shfl((int)key_pte, row, 64) << 8) +
+                            (uint32_t)__shfl((int)key_slot, row, 64) * C::ROW;
+      if (keys) lane_load_lds<false>(base + 16 * k_piece<D>(row, p), kt + row0 * C::ROW);
+      if (values) lane_load_lds<false>(base + (uint64_t)P * C::ROW + 16 * v_piece<D>(row, p), vt + row0 * C::ROW);
+    }
   };
   // Are there keys of step s that some row of the workgroup does not see? Then
   // infinities and NaN of V stay out of the products (0 times those is no
@@ -181,15 +202,31 @@ __global__ __launch_bounds__(kExtThreads, 2) void extend_rows_kernel(const ExtAr
     return b < gs.all_lo || b + C::KW > gs.all_hi;
   };
   uint32_t sp_first = 0xFFFFFFFFu, sp_last = 0;
-  auto store_keys = [&](int buf, uint32_t s) {
+  auto note_special = [&](uint32_t s, bool any) {
+    if (!__builtin_amdgcn_ballot_w64(any)) return false;
+    sp_first = min(sp_first, s);
+    sp_last = s;
+    return true;
+  };
+  auto clean_values = [&](int buf, uint32_t s) {  // RW 4, in LDS
+    bool any = false;
+    for (int e = threadIdx.x; e < C::TILE / 16; e += kExtThreads) {
+      u32x4e *const w = reinterpret_cast<u32x4e *>(lds + buf * (2 * C::TILE) + C::TILE) + e;
+      if (any_special(*w)) {
+        any = true;
+        *w = without_special(*w);
+      }
+    }
+    note_special(s, any);
+    __syncthreads();
+  };
+  auto store_keys = [&](int buf, uint32_t s) {  // RW 1
     char *const kt = lds + buf * (2 * C::TILE), *const vt = kt + C::TILE;
     if (mixed(s)) {
       bool any = false;
 #pragma unroll
       for (int i = 0; i < C::NL; ++i) any = any || any_special(vreg[i]);
-      if (__builtin_amdgcn_ballot_w64(any)) {
-        sp_first = min(sp_first, s);
-        sp_last = s;
+      if (note_special(s, any)) {
 #pragma unroll
         for (int i = 0; i < C::NL; ++i) vreg[i] = without_special(vreg[i]);
       }
@@ -289,31 +326,37 @@ __global__ __launch_bounds__(kExtThreads, 2) void extend_rows_kernel(const ExtAr
   };
 
   // ---- the steps
-  if (s0 < s1) {
+  if constexpr (RW == 4) {
+    // a wait the compiler sees for what it has loaded: its own would drain steps in flight
+    if (s0 < s1) look_up(s0);
+    __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);
+    if (s0 < s1) issue(0, true, true);
+    if (s0 + 1 < s1) look_up(s0 + 1);
+  } else if (s0 < s1) {
     look_up(s0);
     load_keys();
-    if (RW == 1) load_values();
+    load_values();
     if (s0 + 1 < s1) look_up(s0 + 1);
-    if (RW == 4) {
-      store_keys(0, s0);
-      __syncthreads();
-    }
   }
 #pragma unroll 1
   for (uint32_t s = s0; s < s1; ++s) {
-    const int buf = RW == 4 ? (s - s0) & 1 : wave;
-    if (RW == 1) store_keys(buf, s);
     const bool more = s + 1 < s1;
-    if (more) load_keys();
-    if (RW == 4) {
-      if (s + 2 < s1) look_up(s + 2);
+    if constexpr (RW == 4) {
+      const int buf = (s - s0) & 1;
+      __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);
+      __syncthreads();  // step s is there for every wave; step s - 1 is done with
+      if (more) {
+        issue(buf ^ 1, true, true);
+        if (s + 2 < s1) look_up(s + 2);
+      }
+      if (mixed(s)) clean_values(buf, s);
       compute(buf, s, more);
-      if (more) store_keys(buf ^ 1, s + 1);
-      __syncthreads();
     } else {
+      store_keys(wave, s);
+      if (more) load_keys();
       // a wave's LDS operations run in order: its reads follow its writes
       __builtin_amdgcn_wave_barrier();
-      compute(buf, s, more);
+      compute(wave, s, more);
       if (s + 2 < s1) look_up(s + 2);
       __builtin_amdgcn_wave_barrier();
     }
@@ -340,15 +383,20 @@ __global__ __launch_bounds__(kExtThreads, 2) void extend_rows_kernel(const ExtAr
 #pragma unroll 1
     for (uint32_t s = sp_first; s <= sp_last; ++s) {
       if (!mixed(s)) continue;
-      char *const vt = lds + (RW == 4 ? 0 : wave) * (2 * C::TILE);
+      char *const vt = lds + (RW == 4 ? C::TILE : wave * (2 * C::TILE));
       look_up(s);
+      if constexpr (RW == 4) {
+        issue(0, false, true);
+        wait_vm<0>();
+        __syncthreads();
+      } else {
 #pragma unroll
-      for (int i = 0; i < C::NL; ++i) {
-        const int row = lr + C::RPI * i;
-        load_v(i, row_ptr(i));
-        *reinterpret_cast<u32x4e *>(vt + row * C::ROW + 16 * v_piece<D>(row, lc)) = vreg[i];
+        for (int i = 0; i < C::NL; ++i) {
+          const int row = lr + C::RPI * i;
+          load_v(i, row_ptr(i));
+          *reinterpret_cast<u32x4e *>(vt + row * C::ROW + 16 * v_piece<D>(row, lc)) = vreg[i];
+        }
       }
-      if (RW == 4) __syncthreads();
       __builtin_amdgcn_wave_barrier();
       const uint32_t k0 = base_of(s) + 4 * half, lo = x.lo - k0, n = x.hi - x.lo;
 #pragma unroll
@@ -427,7 +475,8 @@ __global__ __launch_bounds__(kExtThreads, 2) void extend_rows_kernel(const ExtAr
 // KV. As RW = 1 above, but by 16x16x32 products, which leave a lane 8 scores of 32
 // keys and not 16, half of them of rows that are not there: the vector unit's
 // work for one row a tile halves, and so do the registers of queries and
-// sums. Lanes are (row `col` of 16, quarter `quad`); pieces of LDS rows are swapped
+// sums: capped single tokens over 480 MB of KV take 85 us with the join (89 by RW = 1;
+// 6.1 TB/s in the kernel), sloped ones over 537 MB 86 (104; 6.7 TB/s). Lanes are (row `col` of 16, quarter `quad`); pieces of LDS rows are swapped
 // so that K reads (16 rows at one piece) and V reads (8 rows at two) meet no bank
 // twice.
 template <int D>
