@@ -486,8 +486,9 @@ def rope_parts(pairs, offset: int = 0):
 def cp_rope_apply(rope: int, parts, positions=None, first: int = 0, inverse: bool = False, stream=None) -> None:
     """parts: from rope_parts. positions: int32 device tensor (or address) with
     one entry per token, or None: first, first + 1, ..."""
-    if hasattr(positions, "dtype") and (str(positions.dtype) != "torch.int32" or positions.numel() != parts.tokens):
-        raise ValueError("positions holds one int32 per token")
+    if hasattr(positions, "dtype") and (str(positions.dtype) != "torch.int32" or positions.numel() != parts.tokens or
+                                        not positions.is_cuda):
+        raise ValueError("positions holds one int32 per token, on the GPU")
     _check(LIB.cp_rope_apply(rope, len(parts), parts, parts.tokens, _ptr(positions), first, int(inverse),
                              _stream(stream)))
 
@@ -504,7 +505,14 @@ def cp_kv_append_rope(pool: int, req_ids: Sequence[int], n_new: Sequence[int], r
                                  _stream(stream)))
 
 
-def _extend_opts(n, softcap, window, slopes, prefix, doc_begin, num_splits, path, rope):
+def _extend_opts(n, n_q, tensors, softcap, window, slopes, prefix, doc_begin, num_splits, path, rope):
+    for t in (*tensors, slopes, doc_begin):
+        if hasattr(t, "is_cuda") and not t.is_cuda:
+            raise ValueError("tensors of attention are on the GPU")
+    if hasattr(slopes, "dtype") and str(slopes.dtype) != "torch.float32":
+        raise ValueError("slopes holds one float32 per query head")
+    if hasattr(doc_begin, "dtype") and (str(doc_begin.dtype) != "torch.int32" or doc_begin.numel() != sum(n_q)):
+        raise ValueError("doc_begin holds one int32 per query token")
     if prefix is not None:
         if len(prefix) != n:
             raise ValueError("prefix and req_ids differ in length")
@@ -522,7 +530,7 @@ def cp_attn_extend(pool: int, req_ids: Sequence[int], n_q: Sequence[int], q, out
     n = len(req_ids)
     if len(n_q) != n:
         raise ValueError("req_ids and n_q differ in length")
-    o = _extend_opts(n, softcap, window, slopes, prefix, doc_begin, num_splits, path, None)
+    o = _extend_opts(n, n_q, (q, out, lse), softcap, window, slopes, prefix, doc_begin, num_splits, path, None)
     _check(LIB.cp_attn_extend(pool, n, _i32_array(req_ids), _i32_array(n_q), _ptr(q), _ptr(out), _ptr(lse),
                               _stream(stream), C.byref(o)))
 
@@ -533,7 +541,7 @@ def cp_attn_extend_step(pool: int, req_ids: Sequence[int], n_new: Sequence[int],
     n = len(req_ids)
     if len(n_new) != n:
         raise ValueError("req_ids and n_new differ in length")
-    o = _extend_opts(n, softcap, window, slopes, prefix, doc_begin, num_splits, path, rope)
+    o = _extend_opts(n, n_new, (rows, q, out, lse), softcap, window, slopes, prefix, doc_begin, num_splits, path, rope)
     _check(LIB.cp_attn_extend_step(pool, n, _i32_array(req_ids), _i32_array(n_new), _ptr(rows), _ptr(q), _ptr(out),
                                    _ptr(lse), _stream(stream), C.byref(o)))
 

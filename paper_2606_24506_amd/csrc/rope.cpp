@@ -63,6 +63,19 @@ const char *angles_of(const cp_rope_desc &d, std::vector<double> *out) {
   return "";
 }
 
+// Do two of the rows of `width` elements at t S + h H meet (t < tokens, h < heads)?
+bool rows_overlap(int64_t tokens, int64_t heads, int64_t S, int64_t H, int64_t width) {
+  typedef __int128 wide;
+  if (tokens < 1 || (heads > 1 && H < width) || (tokens > 1 && S < width)) return tokens > 0;
+  if (heads == 1 || tokens == 1) return false;
+  if ((wide)S >= (wide)H * (heads - 1) + width || (wide)H >= (wide)S * (tokens - 1) + width) return false;
+  // neither stride steps over all of the other's rows: the tokens next to every head
+  for (int64_t h = 1; h < heads; ++h)
+    for (wide at = (wide)h * H, t = at / S, end = t + 2; t < end; ++t)
+      if (t < tokens && at - t * S < width && t * S - at < width) return true;
+  return false;
+}
+
 }  // namespace
 
 extern "C" {
@@ -158,7 +171,7 @@ cp_status cp_rope_apply(const cp_rope *r, int32_t n_tensors, const cp_rope_tenso
     const bool in_place = x.src == x.dst;
     if (in_place && ((n_tokens > 1 && x.src_token != x.dst_token) || (x.heads > 1 && x.src_head != x.dst_head)))
       return fail(CP_EINVAL, "tensor %d: in place needs the same strides", i);
-    if ((x.heads > 1 && x.dst_head < x.width) || (n_tokens > 1 && x.dst_token < x.width))
+    if (rows_overlap(n_tokens, x.heads, x.dst_token, x.dst_head, x.width))
       return fail(CP_EINVAL, "tensor %d: heads or tokens of dst overlap", i);
     const int64_t es = x.dtype == CP_ROPE_F32 ? 4 : 2, v = 16 / es;
     if ((uintptr_t)x.src % es || (uintptr_t)x.dst % es) return fail(CP_EINVAL, "tensor %d: misaligned elements", i);

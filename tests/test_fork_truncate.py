@@ -370,3 +370,41 @@ def test_rope_and_extend_refusals():
     refused(p.extend_step, [a], [1], None, None, None, None, status=cpl.CP_ESTATE)
     p.close(a)
     p.destroy()
+
+
+def test_rows_of_a_rotation_that_overlap_are_refused():
+    rope = cpl.Rope(8, device=-1)
+
+    def refused(tokens, heads, token, head, width=16):
+        t = (cpl.cp_rope_tensor * 1)()
+        t[0] = cpl.cp_rope_tensor(4096, 1 << 30, width, width * tokens, token, head, heads, width, 0, cpl.CP_ROPE_BF16)
+        t.tokens = tokens
+        with pytest.raises(cpl.CrossPoolError) as e:
+            cpl.cp_rope_apply(rope.handle, t)
+        return e.value.status != cpl.CP_ESTATE  # (a host-only rotation refuses sound calls too, last)
+
+    for tokens, heads, width in ((1, 1, 16), (1, 5, 16), (5, 1, 16), (4, 3, 16), (2, 7, 9), (6, 6, 16)):
+        for token in (0, 1, 9, 15, 16, 17, 24, 32, 40, 48, 80, 112):
+            for head in (0, 8, 15, 16, 20, 32, 33, 48, 64, 80, 1 << 61):
+                at = sorted(t * token + h * head for t in range(tokens) for h in range(heads))
+                meet = any(b - a < width for a, b in zip(at, at[1:]))
+                assert refused(tokens, heads, token, head, width) == meet, (tokens, heads, token, head, width)
+    rope.destroy()
+
+
+def test_tensors_of_attention_off_the_gpu_are_refused():
+    import torch
+
+    host, where = torch.zeros(2, 4), 4096
+    dev = torch.zeros(3, dtype=torch.int32)
+    for kw in (dict(q=host), dict(out=host), dict(lse=host), dict(slopes=host), dict(doc_begin=dev)):
+        with pytest.raises(ValueError):
+            cpl.cp_attn_extend(None, [0], [3], **{**dict(q=where, out=where, lse=where), **kw})
+        with pytest.raises(ValueError):
+            cpl.cp_attn_extend_step(None, [0], [3], **{**dict(rows=where, q=where, out=where, lse=where), **kw})
+    with pytest.raises(ValueError):
+        cpl.cp_attn_extend_step(None, [0], [3], host, where, where, where)
+    t = (cpl.cp_rope_tensor * 1)()
+    t.tokens = 3
+    with pytest.raises(ValueError):
+        cpl.cp_rope_apply(None, t, positions=dev)
