@@ -24,9 +24,10 @@ namespace cp {
 // work, and 40 registers). Bound by the vector unit (exponentials, cap) and the
 // matrix cores, which overlap only as far as two workgroups a CU take turns, and by
 // LDS, whose reads for 32 rows take as long as the products at their peak:
-// head_dim 128, chunks of 2,048 over 16 K keys, 847 TFLOP/s plain, 724 to 740 capped,
-// 718 sloped (through registers 810, 726, 732); head_dim 64 680, 550, 538 (636, 520, 549).
-// Steps of 32 keys and three workgroups a CU: 847, 748, 660; and 595, 467, 427.
+// head_dim 128, chunks of 2,048 over 16 K keys, 886 TFLOP/s plain, 782 capped, 774
+// sloped (with loads through registers and no fragments read ahead 810, 726, 732; with
+// the first of these changed 847, 730, 718); head_dim 64 730, 563, 560 (636, 520, 549).
+// Steps of 32 keys and three workgroups a CU gained nothing (660 sloped; head_dim 64 595).
 // RW = 1: 32 rows, every wave with 32 keys of its own a step (few rows: bound
 // by reading KV); the waves' sums join at the end. Its loads pass through
 // registers, because a wave's keys are its own and no barrier is needed.
@@ -183,15 +184,25 @@ __global__ __launch_bounds__(kExtThreads, 2) void extend_rows_kernel(const ExtAr
   // 16-byte place of LDS loads the piece that belongs there (the swaps undo themselves).
   auto issue = [&](int buf, bool keys, bool values) {
     const uint32_t kt = lds_addr(lds) + buf * (2 * C::TILE), vt = kt + C::TILE;
-    const int ln = lane_ids().lane;     // (counted afresh: formed here, not kept through the loop)
+    const uint32_t ln = (uint32_t)lane_ids().lane;  // (counted afresh: formed here, not kept through the loop)
+    const uint32_t row0 = wave * (C::KW / 4), r0 = row0 + ln / C::CPR, p = ln % C::CPR;
+    constexpr int N = C::KW / 4 / C::RPI;
+    // rows of 256 bytes have one number for page and slot, in units of the page table
+    const uint32_t key_at = C::ROW == 256 ? key_pte + key_slot : key_pte;
+    uint32_t at[N], slot[N];
 #pragma unroll
-    for (int i = 0; i < C::KW / 4 / C::RPI; ++i) {
-      const int row0 = wave * (C::KW / 4) + C::RPI * i, row = row0 + ln / C::CPR, p = ln % C::CPR;
-      const uint64_t base = (uint64_t)(uintptr_t)a.pool + (uint64_t)un.kvh * (4ull * P * D) +
-                            ((uint64_t)(uint32_t)__shfl((int)key_pte, row, 64) << 8) +
-                            (uint32_t)__shfl((int)key_slot, row, 64) * C::ROW;
-      if (keys) lane_load_lds<false>(base + 16 * k_piece<D>(row, p), kt + row0 * C::ROW);
-      if (values) lane_load_lds<false>(base + (uint64_t)P * C::ROW + 16 * v_piece<D>(row, p), vt + row0 * C::ROW);
+    for (int i = 0; i < N; ++i) {
+      at[i] = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * (r0 + C::RPI * i), (int)key_at);
+      slot[i] = C::ROW == 256 ? 0u : (uint32_t)__builtin_amdgcn_ds_bpermute(4 * (r0 + C::RPI * i), (int)key_slot);
+    }
+    const uint64_t head = (uint64_t)(uintptr_t)a.pool + (uint64_t)un.kvh * (4ull * P * D);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const uint32_t row = r0 + C::RPI * i, to = (row0 + C::RPI * i) * C::ROW;
+      const uint64_t base = head + ((uint64_t)at[i] << 8);
+      const uint32_t in_page = slot[i] * C::ROW;
+      if (keys) lane_load_lds<false>(base + (in_page + 16u * k_piece<D>(row, p)), kt + to);
+      if (values) lane_load_lds<false>(base + (uint64_t)P * C::ROW + (in_page + 16u * v_piece<D>(row, p)), vt + to);
     }
   };
   // Are there keys of step s that some row of the workgroup does not see? Then
@@ -252,6 +263,7 @@ __global__ __launch_bounds__(kExtThreads, 2) void extend_rows_kernel(const ExtAr
   };
 
   // ---- one step over the keys in a buffer
+  constexpr int AHEAD = RW == 1 ? 0 : D == 128 ? 4 : 2;  // (6 and 2: the same; 4 with head_dim 64: 1% slower)
   auto compute = [&](int buf, uint32_t s, bool more) {
     const uint32_t b0 = base_of(s);
     if (b0 >= ws.hi || b0 + C::KW <= ws.lo) {  // out of this wave's sight
@@ -265,15 +277,32 @@ __global__ __launch_bounds__(kExtThreads, 2) void extend_rows_kernel(const ExtAr
     for (int kb = 0; kb < C::KB; ++kb)
 #pragma unroll
       for (int i = 0; i < 16; ++i) sc[kb][i] = 0.f;
+    // fragments are read KD products ahead, in this order (left to itself the compiler
+    // reads one or two ahead, and the products wait for LDS)
+    constexpr int KD = AHEAD, NKF = KS * C::KB;
+    bf16x8 kf[KD + 1];
+    auto kread = [&](int e) {
+      const int row = 32 * (e % C::KB) + col;
+      return *reinterpret_cast<const bf16x8 *>(kt + row * C::ROW + 16 * k_piece<D>(row, 2 * (e / C::KB) + half));
+    };
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks)
+    for (int e = 0; e < KD; ++e) kf[e] = kread(e);
 #pragma unroll
-      for (int kb = 0; kb < C::KB; ++kb) {
-        const int row = 32 * kb + col;
-        const bf16x8 kf = *reinterpret_cast<const bf16x8 *>(kt + row * C::ROW + 16 * k_piece<D>(row, 2 * ks + half));
-        sc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks], sc[kb], 0, 0, 0);
-      }
+    for (int e = 0; e < NKF; ++e) {
+      if (e + KD < NKF) kf[(e + KD) % (KD + 1)] = kread(e + KD);
+      if (RW == 4) __builtin_amdgcn_sched_barrier(0);
+      sc[e % C::KB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[e % (KD + 1)], qf[e / C::KB], sc[e % C::KB], 0, 0, 0);
+    }
     __builtin_amdgcn_s_setprio(0);
+    // the first fragments of V arrive during the softmax
+    constexpr int VD = AHEAD, NVF = 2 * C::KB * DB;
+    bf16x8 vf[VD + 1];
+    auto vread = [&](int e) { return v_frag(vt, e / (2 * DB), e / DB % 2, e % DB); };
+    if (RW == 4) {
+#pragma unroll
+      for (int e = 0; e < VD; ++e) vf[e] = vread(e);
+      __builtin_amdgcn_sched_barrier(0);
+    }
     // element i of block kb: key b0 + 32 kb + 8 (i / 4) + 4 half + i % 4
     const uint32_t k0 = b0 + 4 * half;
     const bool hide = b0 < ws.all_lo || b0 + C::KW > ws.all_hi;
@@ -309,19 +338,16 @@ __global__ __launch_bounds__(kExtThreads, 2) void extend_rows_kernel(const ExtAr
     if (RW == 1 && more) load_values();
     __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-    for (int kb = 0; kb < C::KB; ++kb)
+    for (int e = 0; e < NVF; ++e) {
+      if (e + VD < NVF) vf[(e + VD) % (VD + 1)] = vread(e + VD);
+      if (RW == 4) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-        for (int d = 0; d < DB; ++d) {
-          const bf16x8 vf = v_frag(vt, kb, ks, d);
-#pragma unroll
-          for (int part = 0; part < C::NP; ++part) {
-            const uint32_t *const w = &pw[part][kb][4 * ks];
-            o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, __builtin_bit_cast(bf16x8, u32x4e{w[0], w[1], w[2], w[3]}),
-                                                           o[d], 0, 0, 0);
-          }
-        }
+      for (int part = 0; part < C::NP; ++part) {
+        const uint32_t *const w = &pw[part][e / (2 * DB)][4 * (e / DB % 2)];
+        o[e % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+            vf[e % (VD + 1)], __builtin_bit_cast(bf16x8, u32x4e{w[0], w[1], w[2], w[3]}), o[e % DB], 0, 0, 0);
+      }
+    }
     __builtin_amdgcn_s_setprio(0);
   };
 
