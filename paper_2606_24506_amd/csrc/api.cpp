@@ -1944,7 +1944,7 @@ struct ExtItem {
 double choose_ranges(const Geom &g, int num_cus, uint64_t cap, std::vector<ExtItem> *items) {
   // us of a step of the kernel with its CUs full, and workgroups of a CU
   static constexpr struct { double us; int per_cu; } kCost[kXKinds] = {
-      {2.0, 8}, {1.4, 2}, {2.8, 2}, {2.7, 2}, {4.6, 2}, {5.0, 4}, {4.6, 2}, {2.6, 1}};
+      {2.0, 8}, {1.2, 2}, {2.5, 2}, {2.7, 2}, {4.6, 2}, {5.0, 4}, {4.6, 2}, {2.6, 1}};
   // a unit's start and end, another launch, and the way of partial rows
   constexpr double kUnit = 4.0, kLaunch = 5.0, kBytesPerUs = 3.0e6;
   double most = 1, base[kXKinds] = {}, all_units = 0, all_slots = 1e300;
