@@ -85,9 +85,10 @@ __global__ __launch_bounds__(kExtThreads) void extend_vec_kernel(const ExtArgs a
   const float lse = none ? -INFINITY : m + fast_log2(l);
   if (rq.all > 1) {
     const uint64_t pr = part_row(a, rq, x, un.split);
-#pragma unroll
-    for (int i = 0; i < E; ++i) a.ws_o[pr * (uint32_t)g.d_v + lane * E + i] = none ? 0.f : o[i] * inv;
     if (lane == 0) a.ws_l[pr] = lse;
+    if (none) return;  // (the join takes no sums of such a range)
+#pragma unroll
+    for (int i = 0; i < E; ++i) a.ws_o[pr * (uint32_t)g.d_v + lane * E + i] = o[i] * inv;
   } else {
     const uint64_t orow = x.tok * (uint32_t)g.hq + x.head;
 #pragma unroll
@@ -141,7 +142,7 @@ __global__ __launch_bounds__(kExtThreads) void ext_merge_kernel(const ExtMergeAr
     for (int u = 0; u < 4; ++u) {
       const float w = fast_exp2(e[u] - ref);
       sum += w;
-      if (w > 0.f) acc += w * v[u];  // (a range that saw nothing has nothing to add)
+      if (w > 0.f) acc += w * v[u];  // (a range that saw nothing has nothing to add, and wrote no sums)
     }
   }
 #pragma unroll

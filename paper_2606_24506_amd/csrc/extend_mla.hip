@@ -290,10 +290,11 @@ __global__ __launch_bounds__(64 * ExtMla::WAVES, 2) void extend_mla_kernel(const
   const float inv = none ? 0.f : 1.f / l, lse = none ? -INFINITY : m + fast_log2(l);
   if (rq.all > 1) {
     const uint64_t pr = part_row(a, rq, x, un.split);
+    if (quad == 0) a.ws_l[pr] = lse;
+    if (none) return;  // (the join takes no sums of such a range)
 #pragma unroll
     for (int d = 0; d < C::DB; ++d)
-      *reinterpret_cast<f32x4 *>(a.ws_o + pr * C::DV + 16 * d + 4 * quad) = none ? f32x4{0.f, 0.f, 0.f, 0.f} : o[d] * inv;
-    if (quad == 0) a.ws_l[pr] = lse;
+      *reinterpret_cast<f32x4 *>(a.ws_o + pr * C::DV + 16 * d + 4 * quad) = o[d] * inv;
   } else {
     const uint64_t orow = x.tok * (uint32_t)g.hq + x.head;
 #pragma unroll

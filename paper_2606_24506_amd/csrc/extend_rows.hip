@@ -90,10 +90,11 @@ CP_DEV void join_waves(const ExtArgs &a, const ExtReq &rq, const Unit &un, const
   }
   if (rq.all > 1) {
     const uint64_t pr = part_row(a, rq, y, un.split);
+    if (c0 == 0) a.ws_l[pr] = lse;
+    if (none) return;  // (the join takes no sums of such a range)
 #pragma unroll
     for (int c = 0; c < NC; c += 4)
       *reinterpret_cast<f32x4 *>(a.ws_o + pr * D + c0 + c) = f32x4{v[c], v[c + 1], v[c + 2], v[c + 3]};
-    if (c0 == 0) a.ws_l[pr] = lse;
   } else {
     const uint64_t orow = y.tok * (uint32_t)a.g.hq + y.head;
 #pragma unroll
@@ -462,14 +463,14 @@ __global__ __launch_bounds__(kExtThreads, 2) void extend_rows_kernel(const ExtAr
     const float inv = none ? 0.f : 1.f / l, lse = none ? -INFINITY : m + fast_log2(l);
     if (rq.all > 1) {
       const uint64_t pr = part_row(a, rq, x, un.split);
+      if (half == 0) a.ws_l[pr] = lse;
+      if (none) return;  // (the join takes no sums of such a range)
 #pragma unroll
       for (int d = 0; d < DB; ++d)
 #pragma unroll
-        for (int i = 0; i < 16; i += 4) {
-          const f32x4 w = {o[d][i] * inv, o[d][i + 1] * inv, o[d][i + 2] * inv, o[d][i + 3] * inv};
-          *reinterpret_cast<f32x4 *>(a.ws_o + pr * D + 32 * d + 2 * i + 4 * half) = none ? f32x4{0.f, 0.f, 0.f, 0.f} : w;
-        }
-      if (half == 0) a.ws_l[pr] = lse;
+        for (int i = 0; i < 16; i += 4)
+          *reinterpret_cast<f32x4 *>(a.ws_o + pr * D + 32 * d + 2 * i + 4 * half) =
+              f32x4{o[d][i] * inv, o[d][i + 1] * inv, o[d][i + 2] * inv, o[d][i + 3] * inv};
     } else {
       const uint64_t orow = x.tok * (uint32_t)g.hq + x.head;
 #pragma unroll
