@@ -93,7 +93,7 @@ struct ExtMergeArgs {
     uint32_t splits, pad;
   } req[kMaxReqPerLaunch];
 };
-static_assert(sizeof(ExtMergeArgs) <= 3072, "extend merge arguments too large");
+static_assert(sizeof(ExtMergeArgs) <= 3776, "extend merge arguments too large");
 
 // floor(2^32 / P), for page_divide on the device.
 inline uint32_t page_magic(int32_t page_tokens) {

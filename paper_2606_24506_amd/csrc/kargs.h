@@ -247,6 +247,6 @@ static_assert(sizeof(StackPushArgs) <= 3072, "stack push arguments too large");
 static_assert(sizeof(DecodeArgs) <= 3776, "decode kernel arguments too large");
 static_assert(sizeof(MergeArgs) <= 3072, "merge kernel arguments too large");
 static_assert(sizeof(AppendArgs) <= 3776, "append kernel arguments too large");
-static_assert(sizeof(PageCopyArgs) <= 3072, "page copy arguments too large");
+static_assert(sizeof(PageCopyArgs) <= 3776, "page copy arguments too large");
 
 }  // namespace cp

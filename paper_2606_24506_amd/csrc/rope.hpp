@@ -49,7 +49,7 @@ struct RopeArgs {
   RopePart part[kMaxRopeParts];
   int32_t item0[kMaxRopeParts + 1];  // first work item of each part among one token's
 };
-static_assert(sizeof(RopeArgs) <= 3072, "rope kernel arguments too large");
+static_assert(sizeof(RopeArgs) <= 3776, "rope kernel arguments too large");
 
 inline RopeK rope_k(const cp_rope &r, bool inverse) {
   return RopeK{r.dev_turns, r.magnitude, r.rot / 2, r.layout == CP_ROPE_INTERLEAVED, inverse};
