@@ -57,6 +57,12 @@ CP_DEV int v_piece(int row, int c) {
   return D == 128 ? c ^ (4 * (row & 3)) : c ^ (4 * ((row >> 1) & 1));
 }
 
+// What a probability has behind its leading 8 bits h, with its last bit set: an infinite V
+// that is seen times a part that is 0 would be NaN. (A floor of 1e-37 instead gave
+// hidden keys, and those that weigh less, that much of a large V. The last bit of 0 is
+// 2^-149, which the rounding to bf16 drops: what weighs nothing stays at nothing.)
+CP_DEV float low_part(float p, uint32_t h) { return __uint_as_float(__float_as_uint(p) | 1u) - __uint_as_float(h); }
+
 // Results of a tile of ROWS rows from its four waves' m, l and sums (parts: [wave][column]
 // [row] in LDS). A thread takes D ROWS / 256 columns of one row.
 template <int D, int ROWS>
@@ -331,9 +337,7 @@ __global__ __launch_bounds__(kExtThreads, 2) void extend_rows_kernel(const ExtAr
         // leading 8 bits, and the rest rounded: together 16 bits and a half step
         const uint32_t h0 = __float_as_uint(p0) & 0xFFFF0000u, h1 = __float_as_uint(p1) & 0xFFFF0000u;
         pw[0][i / 16][i % 16 / 2] = upper_halves(h0, h1);
-        // (kept above zero: an infinite V times 0 would be NaN)
-        pw[1][i / 16][i % 16 / 2] = pack_bf16x2(__builtin_fmaxf(p0 - __uint_as_float(h0), 1e-37f),
-                                                __builtin_fmaxf(p1 - __uint_as_float(h1), 1e-37f));
+        pw[1][i / 16][i % 16 / 2] = pack_bf16x2(low_part(p0, h0), low_part(p1, h1));
       }
     });
     if (RW == 1 && more) load_values();
@@ -663,9 +667,7 @@ __global__ __launch_bounds__(kExtThreads, 2) void extend_few_kernel(const ExtArg
         // leading 8 bits, and the rest rounded: together 16 bits and a half step
         const uint32_t h0 = __float_as_uint(p0) & 0xFFFF0000u, h1 = __float_as_uint(p1) & 0xFFFF0000u;
         pw[0][i / 2] = upper_halves(h0, h1);
-        // (kept above zero: an infinite V times 0 would be NaN)
-        pw[1][i / 2] = pack_bf16x2(__builtin_fmaxf(p0 - __uint_as_float(h0), 1e-37f),
-                                   __builtin_fmaxf(p1 - __uint_as_float(h1), 1e-37f));
+        pw[1][i / 2] = pack_bf16x2(low_part(p0, h0), low_part(p1, h1));
       });
 #pragma unroll
       for (int d = 0; d < C::DB; ++d) {
