@@ -638,7 +638,9 @@ typedef struct {
  *     out_h = sum_j softmax(s)_j V_j;  lse_h = ln sum_j exp(s_j).
  * A row that sees nothing (or whose scores are all -inf) gives out = 0 and
  * lse = -inf. What lies in positions that a row does not see does not reach
- * it, infinities and NaN included.
+ * it, infinities and NaN included. NaN in a V that a row sees gives NaN; an
+ * infinite one gives an infinite result, or NaN where its probability is below
+ * 2^-100 (which may be 0 in 32 bits).
  *   n_q  host, n entries, 0 <= n_q[i] <= context of request i.
  *   q    device, bf16, [sum n_q][n_q_heads][d_k] in call order; 16-byte
  *        aligned. out [sum n_q][n_q_heads][d_v] bf16 (8-byte aligned) and

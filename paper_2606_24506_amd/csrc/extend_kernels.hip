@@ -142,7 +142,8 @@ __global__ __launch_bounds__(kExtThreads) void ext_merge_kernel(const ExtMergeAr
     for (int u = 0; u < 4; ++u) {
       const float w = fast_exp2(e[u] - ref);
       sum += w;
-      if (w > 0.f) acc += w * v[u];  // (a range that saw nothing has nothing to add, and wrote no sums)
+      // (a range that saw nothing has nothing to add, and wrote no sums; those of weight 0 may be NaN)
+      if (e[u] != -INFINITY) acc += w * v[u];
     }
   }
 #pragma unroll

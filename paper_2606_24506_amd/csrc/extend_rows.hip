@@ -90,8 +90,8 @@ CP_DEV void join_waves(const ExtArgs &a, const ExtReq &rq, const Unit &un, const
   for (int c = 0; c < NC; ++c) {
     float acc = 0.f;
 #pragma unroll
-    for (int w = 0; w < 4; ++w)  // a wave that saw nothing of the row has nothing to add
-      if (f[w] > 0.f) acc += f[w] * parts[w * ROWS * D + (c0 + c) * ROWS + row];
+    for (int w = 0; w < 4; ++w)  // a wave that saw nothing of the row has nothing to add; sums of weight 0 may be NaN
+      if (stats[0][w][row] != -INFINITY) acc += f[w] * parts[w * ROWS * D + (c0 + c) * ROWS + row];
     v[c] = acc * inv;
   }
   if (rq.all > 1) {

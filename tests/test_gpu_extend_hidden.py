@@ -88,3 +88,30 @@ def test_large_values_in_sight_weigh_what_they_weigh(name, n_q, n):
     q, out, lse = run(sc, n_q, q=q)
     check(out, lse, attend(name, rows, q), rounds_to_16_bits(name, n_q), f"{name}")
     sc.close()
+
+
+@pytest.mark.parametrize("name", ["gqa8x2d128", "gqa6x2d64", "gqa4x2d256"])
+@pytest.mark.parametrize("n_q", [1, 6, 40])
+@pytest.mark.parametrize("n,low,splits", [(128, 32, 1), (600, 200, 3), (3000, 1500, 23)])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_special_values_in_sight_are_not_lost_in_joins(name, n_q, n, low, splits, bad):
+    """NaN in a V that a row sees gives NaN there, an infinite one no finite
+    result, also where all keys around it weigh nothing (their scores are 400
+    below the others) and their sums join those of the rest with weight 0."""
+    print(f"[case] extend lost {name} {n_q} {n} {splits} {bad}", flush=True)
+    sc = Scene(name, [n + n_q - 1], seed=42)
+    hq, hkv, dk, dv, row, scale = shape(name)
+    rows = sc.rows[0].clone()
+    q = sc.buffers(n_q)[0]
+    q[..., 0] = 16.0
+    for c in range(hkv):
+        rows[:low, c * dk] = -400 / (16.0 * scale)
+        rows[low:, c * dk] = 0
+    rows[20, hkv * dk + 5] = bad
+    replace(sc, rows)
+    _, out, _ = run(sc, n_q, q=q, num_splits=splits)
+    got = out[:, :hq // hkv, 5]
+    assert torch.isnan(got).all() if bad != bad else not torch.isfinite(got).any()
+    out[:, :hq // hkv, 5] = 0
+    assert torch.isfinite(out).all()
+    sc.close()
