@@ -25,7 +25,10 @@
  *     (all-or-nothing across a whole batch). A HIP failure after the checks
  *     (CP_EHIP from a copy or launch of an append or decode step) leaves
  *     the host tables updated as if the call had succeeded; the device
- *     state is then undefined and the pool should be closed.
+ *     state is then undefined and the pool should be closed. After such a
+ *     failure of cp_request_fork, cp_request_truncate or cp_attn_extend_step
+ *     the pool refuses work on its device memory (CP_ESTATE); requests can
+ *     still be closed and the pool destroyed.
  *   - Device-memory arguments are device pointers on the pool's device;
  *     host arguments are ordinary host pointers and are not retained after
  *     the call returns. Streams are hipStream_t passed as void* (NULL = the
@@ -492,7 +495,7 @@ cp_status cp_kv_gather(cp_pool *pool, int32_t req_id, int64_t start, int64_t n_t
  * the host has not read back, or where the model's stack must shrink.
  * Errors: CP_EINVAL (unknown id, another model, a destination that is not
  * empty, a prefix past the source or the reservation, a token in flight,
- * the same id twice), CP_EHIP. */
+ * the same id twice), CP_EHIP (if its launch failed, the pool is unusable). */
 cp_status cp_request_fork(cp_pool *pool, int32_t n, const int32_t *src_ids, const int32_t *dst_ids,
                           const int64_t *n_tok, void *hip_stream);
 
@@ -509,7 +512,7 @@ cp_status cp_request_fork(cp_pool *pool, int32_t n, const int32_t *src_ids, cons
  * is not there (nothing changed).
  * Errors: CP_EINVAL (unknown or duplicate id, a length out of range, a token
  * in flight), CP_ENOSPC, CP_ENOMEM (a virtual pool could not map chunks),
- * CP_EHIP. On a device_pages pool it may wait for the device as
+ * CP_EHIP (as for a fork). On a device_pages pool it may wait for the device as
  * cp_request_fork does. */
 cp_status cp_request_truncate(cp_pool *pool, int32_t n, const int32_t *ids, const int64_t *new_len,
                               void *hip_stream);
@@ -676,8 +679,8 @@ cp_status cp_attn_extend(cp_pool *pool, int32_t n, const int32_t *req_ids, const
  *   rows  device, bf16, [sum n_new][row_elems] in call order (one layer).
  * Errors: those of cp_kv_append and cp_attn_extend, plus CP_EINVAL for an
  * n_new that is not the tokens in flight. A refused call changes nothing;
- * after a HIP failure the tokens are placed and the cursors moved, and the
- * pool should be closed. */
+ * after a launch that failed the tokens are placed, the cursors moved, and the
+ * pool is unusable (CP_ESTATE). */
 cp_status cp_attn_extend_step(cp_pool *pool, int32_t n, const int32_t *req_ids, const int32_t *n_new,
                               const void *rows, const void *q, void *out, float *lse, void *hip_stream,
                               const cp_extend_opts *opts);

@@ -64,6 +64,17 @@ cp_status hip_fail(hipError_t e, const char *what) {
   return fail(CP_EHIP, "%s: %s", what, hipGetErrorString(e));
 }
 
+cp_status broken_pool() {
+  return fail(CP_ESTATE, "an earlier call's launch failed after the pool's tables had changed; destroy the pool");
+}
+
+// Calls that mark the pool unusable when their launch fails ask this first: an error
+// that another HIP call left behind would look like that launch's.
+cp_status earlier_error() {
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? CP_OK : hip_fail(e, "left behind by an earlier HIP call (nothing was done)");
+}
+
 // Makes the pool's device current for the duration of a call.
 struct DeviceGuard {
   int prev = -1;
@@ -120,7 +131,7 @@ struct cp_pool {
   // top, so these are the ones still there) and the page-table slots that
   // steps filled on the device and that it has not read back yet.
   bool dev_pages = false;
-  bool broken = false;  // a step's launch failed after its pops were booked
+  bool broken = false;  // a launch failed after the host's tables had changed: the device's are behind
   uint32_t *dev_stack = nullptr;
   int32_t *dev_top = nullptr;
   uint32_t *dev_pop = nullptr;
@@ -146,9 +157,13 @@ bool vmm_map(cp_pool *p, int32_t c) {
   void *va = p->dev_pool + (uint64_t)c * cb;
   if (p->vmm_handles.count(c)) return false;  // an earlier unmap of the slot failed
   hipMemGenericAllocationHandle_t h{};
-  if (hipMemCreate(&h, cb, &p->vmm_prop, 0) != hipSuccess) return false;
+  if (hipMemCreate(&h, cb, &p->vmm_prop, 0) != hipSuccess) {
+    (void)hipGetLastError();  // reported by the caller, and not by the next launch
+    return false;
+  }
   if (hipMemMap(va, cb, 0, h, 0) != hipSuccess) {
     (void)hipMemRelease(h);
+    (void)hipGetLastError();
     return false;
   }
   hipMemAccessDesc ad{};
@@ -157,6 +172,7 @@ bool vmm_map(cp_pool *p, int32_t c) {
   if (hipMemSetAccess(va, cb, &ad, 1) != hipSuccess) {
     (void)hipMemUnmap(va, cb);
     (void)hipMemRelease(h);
+    (void)hipGetLastError();
     return false;
   }
   p->vmm_handles[c] = h;
@@ -399,6 +415,7 @@ cp_status cp_pool_create(const cp_pool_desc *d, cp_pool **out) {
       he = hipMalloc((void **)&p->dev_pool, bytes);
       if (he != hipSuccess) {
         delete p;
+        (void)hipGetLastError();
         return fail(CP_ENOMEM, "hipMalloc of %llu pool bytes failed", (unsigned long long)bytes);
       }
       p->owns_pool = true;
@@ -431,6 +448,7 @@ cp_status cp_pool_create(const cp_pool_desc *d, cp_pool **out) {
     if (ok) ok = hipDeviceSynchronize() == hipSuccess;
     if (!ok) {
       cp_pool_destroy(p);
+      (void)hipGetLastError();
       return fail(CP_ENOMEM, "device allocation of pool metadata failed");
     }
   }
@@ -560,7 +578,7 @@ cp_status cp_request_fork(cp_pool *p, int32_t n, const int32_t *src, const int32
     cp_status rc = check_ids(p, n, dst);
     if (rc) return rc;
     if (n > 0 && !src) return fail(CP_EINVAL, "null src_ids");
-    if (p->broken) return fail(CP_ESTATE, "a failed decode step left the device page stacks out of step; destroy the pool");
+    if (p->broken) return broken_pool();
     const int32_t P = p->st.page_tokens();
     std::vector<int64_t> len((size_t)n), tails((size_t)p->st.n_models(), 0), shown((size_t)p->st.n_models(), 0);
     std::vector<int32_t> sorted(dst, dst + n);
@@ -583,6 +601,7 @@ cp_status cp_request_fork(cp_pool *p, int32_t n, const int32_t *src, const int32
       shown[(size_t)d.model] += (len[(size_t)i] + P - 1) / P * d.layers;
       if (len[(size_t)i] % P) tails[(size_t)d.model] += d.layers;
     }
+    if (!p->host_only && (rc = earlier_error())) return rc;
     rc = reconcile_pages(p);
     if (rc) return rc;
     std::vector<PageItem> items;
@@ -617,7 +636,9 @@ cp_status cp_request_fork(cp_pool *p, int32_t n, const int32_t *src, const int32
         models.push_back(d.model);
       }
     }
-    return launch_page_items(p, items, models, (hipStream_t)hip_stream);
+    rc = launch_page_items(p, items, models, (hipStream_t)hip_stream);
+    if (rc) p->broken = true;
+    return rc;
   });
 }
 
@@ -627,7 +648,7 @@ cp_status cp_request_truncate(cp_pool *p, int32_t n, const int32_t *ids, const i
     cp_status rc = check_ids(p, n, ids);
     if (rc) return rc;
     if (n > 0 && !new_len) return fail(CP_EINVAL, "null new_len");
-    if (p->broken) return fail(CP_ESTATE, "a failed decode step left the device page stacks out of step; destroy the pool");
+    if (p->broken) return broken_pool();
     bool any = false;
     for (int32_t i = 0; i < n; ++i) {
       const Request &r = p->st.req(ids[i]);
@@ -639,6 +660,7 @@ cp_status cp_request_truncate(cp_pool *p, int32_t n, const int32_t *ids, const i
       any = any || new_len[i] < r.ctx_len;
     }
     if (!any) return CP_OK;
+    if (!p->host_only && (rc = earlier_error())) return rc;
     rc = reconcile_pages(p);
     if (rc) return rc;
     std::vector<int64_t> more, pages;
@@ -678,7 +700,9 @@ cp_status cp_request_truncate(cp_pool *p, int32_t n, const int32_t *ids, const i
       }
     }
     for (int32_t i = 0; i < n; ++i) p->st.truncate(ids[i], new_len[i]);
-    return launch_page_items(p, items, models, (hipStream_t)hip_stream);
+    rc = launch_page_items(p, items, models, (hipStream_t)hip_stream);
+    if (rc) p->broken = true;
+    return rc;
   });
 }
 
@@ -868,7 +892,7 @@ cp_status append_impl(cp_pool *p, int32_t n, const int32_t *req_ids, const int32
   cp_status rc = check_ids(p, n, req_ids);
   if (rc) return rc;
   if (n > 0 && !n_new) return fail(CP_EINVAL, "null n_new");
-  if (p->broken) return fail(CP_ESTATE, "a failed decode step left the device page stacks out of step; destroy the pool");
+  if (p->broken) return broken_pool();
   // the page-table copies below must not overwrite entries a step popped
   rc = reconcile_pages(p);
   if (rc) return rc;
@@ -959,6 +983,7 @@ cp_status cp_kv_append_rope(cp_pool *p, int32_t n, const int32_t *req_ids, const
 cp_status cp_kv_gather(cp_pool *p, int32_t req_id, int64_t start, int64_t n_tok, void *dst, void *hip_stream) {
   if (!p) return fail(CP_EINVAL, "null pool");
   if (p->host_only) return fail(CP_ESTATE, "host-only pool has no device data");
+  if (p->broken) return broken_pool();
   if (!p->st.valid_open(req_id)) return fail(CP_EINVAL, "request %d is not open", req_id);
   const Request &r = p->st.req(req_id);
   if (start < 0 || n_tok < 0 || start + n_tok > r.ctx_len)
@@ -1102,7 +1127,10 @@ cp_status ensure_ws(cp_pool *p, uint64_t o_elems, uint64_t l_floats) {
       *buf = nullptr;
       *cap = 0;
     }
-    if (hipMalloc(&nb, c * sizeof(**buf)) != hipSuccess) return fail(CP_ENOMEM, "workspace allocation failed");
+    if (hipMalloc(&nb, c * sizeof(**buf)) != hipSuccess) {
+      (void)hipGetLastError();  // reported here, and not by the next launch
+      return fail(CP_ENOMEM, "workspace allocation failed");
+    }
     if (*buf) p->ws_retired.push_back(*buf);
     *buf = static_cast<std::remove_reference_t<decltype(*buf)>>(nb);
     *cap = c;
@@ -1132,7 +1160,7 @@ cp_status decode_prepare(cp_pool *p, int32_t n, const int32_t *req_ids, const vo
                          const cp_decode_opts *opts, cp_decode_opts *o_out, std::vector<GeomK> *gk_out) {
   if (!p) return fail(CP_EINVAL, "null pool");
   if (p->host_only) return fail(CP_ESTATE, "host-only pool cannot decode");
-  if (p->broken) return fail(CP_ESTATE, "a failed decode step left the device page stacks out of step; destroy the pool");
+  if (p->broken) return broken_pool();
   if (n < 1) return fail(CP_EINVAL, "decode needs at least one request");
   cp_status rc = check_ids(p, n, req_ids);
   if (rc) return rc;
@@ -2300,7 +2328,7 @@ cp_status cp_attn_extend(cp_pool *p, int32_t n, const int32_t *req_ids, const in
   return guarded([&]() -> cp_status {
     if (!p) return fail(CP_EINVAL, "null pool");
     if (p->host_only) return fail(CP_ESTATE, "host-only pool cannot attend");
-    if (p->broken) return fail(CP_ESTATE, "a failed decode step left the device page stacks out of step; destroy the pool");
+    if (p->broken) return broken_pool();
     cp_status rc = check_ids(p, n, req_ids);
     if (rc) return rc;
     if (n > 0 && !n_q) return fail(CP_EINVAL, "null n_q");
@@ -2322,7 +2350,7 @@ cp_status cp_attn_extend_step(cp_pool *p, int32_t n, const int32_t *req_ids, con
   return guarded([&]() -> cp_status {
     if (!p) return fail(CP_EINVAL, "null pool");
     if (p->host_only) return fail(CP_ESTATE, "host-only pool cannot attend");
-    if (p->broken) return fail(CP_ESTATE, "a failed decode step left the device page stacks out of step; destroy the pool");
+    if (p->broken) return broken_pool();
     cp_status rc = check_ids(p, n, req_ids);
     if (rc) return rc;
     if (n > 0 && !n_new) return fail(CP_EINVAL, "null n_new");
@@ -2355,6 +2383,8 @@ cp_status cp_attn_extend_step(cp_pool *p, int32_t n, const int32_t *req_ids, con
     if (rc) return rc;
     DeviceGuard g(p->device);
     rc = bind_extend_workspace(p, pl);
+    if (rc) return rc;
+    rc = earlier_error();
     if (rc) return rc;
     rc = reconcile_pages(p);  // the page-table copies below must not overwrite popped entries
     if (rc) return rc;
@@ -2394,6 +2424,7 @@ cp_status cp_attn_extend_step(cp_pool *p, int32_t n, const int32_t *req_ids, con
     if (rc == CP_OK) rc = launch_appends(p, items, rows, s, o.rope);
     if (rc == CP_OK) rc = run_extend(p, pl, q, out, lse, o, s);
     for (int32_t i = 0; i < n; ++i) p->st.advance(req_ids[i]);
+    if (rc) p->broken = true;  // rows or page-table entries are missing on the device
     return rc;
   });
 }

@@ -111,6 +111,7 @@ cp_status cp_rope_create(const cp_rope_desc *d, int32_t device, cp_rope **out) {
     const size_t bytes = r->turns.size() * sizeof(double);
     if (hipMalloc((void **)&r->dev_turns, bytes) != hipSuccess) {
       delete r;
+      (void)hipGetLastError();
       return fail(CP_ENOMEM, "allocation of the frequency table failed");
     }
     const hipError_t he = hipMemcpy(r->dev_turns, r->turns.data(), bytes, hipMemcpyHostToDevice);
