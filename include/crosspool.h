@@ -655,8 +655,8 @@ typedef struct {
  * requests of at most 32 rows (a row being a token and a query head of one KV
  * head); the vector kernel, which serves every other geometry, in fp32.
  * Requests that share leading pages (cp_request_fork) and stand next to each
- * other in the call may have those pages read once, by kernels for the rows
- * of all of them. Results depend on the logical KV, on which pages
+ * other in the call may have those pages read once, for the rows of all of
+ * them; a request's probabilities keep the parts that they have alone. Results depend on the logical KV, on which pages
  * requests share, and on the call, never on where pages are placed. The
  * cursor does not move. The call uses the pool's workspace, as the decode
  * calls do: it must not overlap with them on the GPU, and before a call is

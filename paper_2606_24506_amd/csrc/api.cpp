@@ -1949,6 +1949,17 @@ int32_t extend_kind(const Geom &g, int32_t path, int64_t n_q) {
   return g.kind == kMLA && g.latent == 512 && g.rope == 64 ? kXMla : kXVec;
 }
 
+// Does the kernel multiply probabilities in two bf16 parts?
+bool two_parts(int32_t kind) { return kind >= kXSome64 && kind <= kXFew128; }
+
+// The kernel of an item of several requests' query tokens, of which the first's own is
+// `alone`: a request keeps its precision beside others, and so requests of few rows
+// take tiles of 32 however many they are together.
+int32_t shared_kind(const Geom &g, int32_t path, int64_t tokens, int32_t alone) {
+  const int32_t kind = extend_kind(g, path, tokens);
+  return two_parts(alone) && !two_parts(kind) ? (g.head_dim == 64 ? kXSome64 : kXSome128) : kind;
+}
+
 // An item of a call (extend.h): its kernel, rows of all heads, row tiles per KV head,
 // steps of its longest tile, and the ranges that these are cut into.
 struct ExtItem {
@@ -2028,11 +2039,13 @@ double choose_ranges(const Geom &g, int num_cus, uint64_t cap, std::vector<ExtIt
 
 // Whole pages that request ids[i] of a call and those right behind it show alike from
 // the start on, and how many requests do (*count, 1 when it is not worth an
-// item): few rows each, which read their keys at the speed of memory, and at least
-// kShareTokens shared tokens.
+// item): few rows each, which read their keys at the speed of memory, alike in the
+// precision of their probabilities, and at least kShareTokens shared tokens.
 constexpr int64_t kShareTokens = 256, kShareRows = 128;
-int64_t shared_run(const cp_pool *p, int32_t n, const int32_t *ids, const int32_t *n_q, int32_t i, int32_t g,
+int64_t shared_run(const cp_pool *p, int32_t n, const int32_t *ids, const int32_t *n_q, int32_t i, const Geom &geom,
                    int32_t *count) {
+  const int32_t g = geom.g;
+  const bool parts = two_parts(extend_kind(geom, CP_PATH_AUTO, n_q[i]));
   const uint32_t *pt = p->st.pte_mirror();
   const int64_t P = p->st.page_tokens();
   const Request &a = p->st.req(ids[i]);
@@ -2042,6 +2055,7 @@ int64_t shared_run(const cp_pool *p, int32_t n, const int32_t *ids, const int32_
   for (int32_t k = i + 1; k < n && *count < kExtMaxReq; ++k) {
     const Request &b = p->st.req(ids[k]);
     if (n_q[k] < 1 || n_q[k] * (int64_t)g > kShareRows) break;
+    if (two_parts(extend_kind(geom, CP_PATH_AUTO, n_q[k])) != parts) break;
     const uint32_t *x = pt + a.plane_base(a.cursor), *y = pt + b.plane_base(b.cursor);
     const int64_t most = std::min(pages, b.ctx_len / P);
     int64_t same = 0;
@@ -2131,18 +2145,20 @@ cp_status plan_extend(cp_pool *p, int32_t n, const int32_t *ids, const int32_t *
     for (int32_t i = 0; look && i < n;) {
       int32_t count = 1;
       int64_t pages = 0;
-      if (n_q[i] > 0) pages = shared_run(p, n, ids, n_q, i, g.g, &count);
+      if (n_q[i] > 0) pages = shared_run(p, n, ids, n_q, i, g, &count);
       const int64_t keys = pages * p->st.page_tokens();
       if (count < 2) {
         if (n_q[i] > 0) apart.push_back(item_of(i, 1, 0, 0xFFFFFFFFll));
       } else {
-        apart.push_back(item_of(i, count, 0, keys));
+        int64_t tokens = 0;
+        for (int32_t k = i; k < i + count; ++k) tokens += n_q[k];
+        const int32_t kind = shared_kind(g, o.path, tokens, extend_kind(g, o.path, n_q[i]));
+        apart.push_back(item_of(i, count, 0, keys, kind));
         apart.back().shared = true;
-        const int32_t shared_kind = apart.back().kind;
         apart.back().group = groups;
         for (int32_t k = i; k < i + count; ++k) {
           // (by the same kernel, and so in the same launch)
-          apart.push_back(item_of(k, 1, keys, 0xFFFFFFFFll, shared_kind));
+          apart.push_back(item_of(k, 1, keys, 0xFFFFFFFFll, kind));
           apart.back().group = groups;
         }
         groups += 1;
