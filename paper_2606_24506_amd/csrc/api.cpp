@@ -2278,7 +2278,8 @@ void set_score_factors(ExtArgs *a, double scale) {
   double f = mul * cap;
   for (int k = 0; k < kTanhTerms; ++k, f *= mul * mul) {
     a->cap_k[k] = (float)(kTanh[k] * f);
-    if (!std::isfinite(a->cap_k[k])) a->cap_edge = 0.f;  // a tiny cap: never
+    // tiny and huge caps (from 7.6e4 on at head_dim 128): never, for want of range
+    if (!std::isnormal(a->cap_k[k])) a->cap_edge = 0.f;
   }
 }
 
