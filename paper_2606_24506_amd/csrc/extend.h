@@ -28,8 +28,8 @@ constexpr int32_t ext_tile_keys(int32_t kind) {
   return kind >= kXSome64 && kind <= kXFew128 ? 128 : kind == kXMla ? 32 : 64;
 }
 
-// tanh(x) = x + x sum_{k > 0} kTanh[k] x^2k, to 4e-8 of its value under kCapEdge: a
-// least-squares fit, reweighted towards its largest relative error.
+// tanh(x) = x + x sum_{k > 0} kTanh[k] x^2k, to 4.2e-8 of its value under kCapEdge (in
+// exact arithmetic): a least-squares fit, reweighted towards its largest relative error.
 constexpr int kTanhTerms = 4;
 constexpr float kTanh[kTanhTerms] = {1.f, -3.33326690e-01f, 1.32999740e-01f, -4.91567400e-02f};
 constexpr float kCapEdge = 0.35f;

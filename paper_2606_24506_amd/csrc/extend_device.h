@@ -47,9 +47,12 @@ CP_DEV uint32_t xcd_unit(uint32_t b, uint32_t n) {
   return x * per + min(x, rem) + b / 8;
 }
 
-// tanh to 2e-7 of its value. Under kCapEdge a polynomial in x^2 fitted to tanh(x) / x
-// (kTanh; 1 - 2 / (e^2x + 1) loses what the difference cancels, and scores far
-// under the cap are the usual case), above it the quotient.
+// tanh to 7e-7 of its value. Under kCapEdge a polynomial in x^2 fitted to tanh(x) / x
+// (kTanh, 2e-7 with its roundings; 1 - 2 / (e^2x + 1) loses what the difference cancels,
+// and scores far under the cap are the usual case), above it the quotient, which is
+// worst just above the edge: there e^2x = 2.0 is off by 2e-7 of itself (argument 8e-8,
+// exponential one last place, 1.2e-7), the quotient 0.66 by 3.1e-7 (2/3 of that, the
+// sum 6e-8, the reciprocal one last place), which is 6.2e-7 of the difference 0.34.
 CP_DEV float tanh_large(float x) {
   const float a = __builtin_fabsf(x);
   const float t = 1.f - 2.f * __builtin_amdgcn_rcpf(fast_exp2(a * (2.f * kLog2e)) + 1.f);
