@@ -9,6 +9,7 @@ built (``python -m paper_2606_24506_amd.build``); there is no fallback.
 """
 from __future__ import annotations
 
+import array
 import ctypes as C
 import os
 from typing import Optional, Sequence
@@ -222,30 +223,36 @@ def _check(rc: int):
         raise CrossPoolError(rc, LIB.cp_last_error().decode(errors="replace"))
 
 
+def _int_array(kind, code: str, xs):
+    """xs as a ctypes array of the kind; one of that kind passes as it is.
+    Numbers out of its range are refused (OverflowError)."""
+    if isinstance(xs, C.Array) and xs._type_ is kind:
+        return xs
+    return (kind * len(xs)).from_buffer(array.array(code, [int(x) for x in xs]))
+
+
 def i32_array(xs: Sequence[int]):
     """A host int32 array argument built once, for callers that repeat a
     call with the same request ids (it is passed as it is)."""
-    return (C.c_int32 * len(xs))(*[int(x) for x in xs])
+    return _int_array(C.c_int32, "i", list(xs))
 
 
 def i64_array(xs: Sequence[int]):
     """The same of int64, for lengths."""
-    return (C.c_int64 * len(xs))(*[int(x) for x in xs])
+    return _int_array(C.c_int64, "q", list(xs))
 
 
 def _i64_array(xs):
-    return xs if xs is None or isinstance(xs, C.Array) else i64_array(xs)
+    return None if xs is None else _int_array(C.c_int64, "q", xs)
 
 
 def _i32_array(xs: Sequence[int]):
     """A host int32 array argument: an array from i32_array passes as it is,
     a contiguous numpy int32 array passes its address (no copy), anything
-    else is copied into a ctypes array."""
-    if isinstance(xs, C.Array):
-        return xs
+    else (arrays of other integers too) is copied into a ctypes array."""
     if isinstance(xs, np.ndarray) and xs.dtype == np.int32 and xs.flags.c_contiguous:
         return xs.__array_interface__["data"][0]
-    return (C.c_int32 * len(xs))(*[int(x) for x in xs])
+    return _int_array(C.c_int32, "i", xs)
 
 
 def _ptr(t) -> Optional[int]:
