@@ -305,6 +305,17 @@ def cp_version() -> int:
     return int(LIB.cp_version())
 
 
+class _Known:
+    """What the checks of tensor arguments need of a pool: its device, and the
+    query heads of its models and open requests."""
+
+    def __init__(self, device: int):
+        self.device, self.models, self.requests = device, {}, {}
+
+
+_POOLS: dict = {}  # by handle
+
+
 def cp_pool_create(page_tokens: int = 64, pool_bytes: int = 0, chunk_bytes: int = 0, placement_seed: int = 0,
                    device: int = 0, device_mem=None, max_requests: int = 0, backing: int = 0,
                    max_workspace_bytes: int = 0, device_pages: int = 0) -> int:
@@ -312,11 +323,13 @@ def cp_pool_create(page_tokens: int = 64, pool_bytes: int = 0, chunk_bytes: int 
                      backing, max_workspace_bytes, device_pages)
     out = C.c_void_p()
     _check(LIB.cp_pool_create(C.byref(d), C.byref(out)))
+    _POOLS[out.value] = _Known(device)
     return out.value
 
 
 def cp_pool_destroy(pool: int) -> None:
     _check(LIB.cp_pool_destroy(pool))
+    _POOLS.pop(pool, None)
 
 
 def cp_pool_stats(pool: int) -> dict:
@@ -330,6 +343,8 @@ def cp_model_register(pool: int, kind: int, n_q_heads: int, n_kv_heads: int, hea
     m = cp_model_desc(kind, n_q_heads, n_kv_heads, head_dim, latent_dim, rope_dim, softmax_scale, 0, n_layers)
     mid = C.c_int32()
     _check(LIB.cp_model_register(pool, C.byref(m), C.byref(mid)))
+    if pool in _POOLS:
+        _POOLS[pool].models[mid.value] = n_q_heads
     return mid.value
 
 
@@ -342,6 +357,8 @@ def cp_model_info(pool: int, model_id: int) -> dict:
 def cp_request_open(pool: int, model_id: int, reserve_tokens: int) -> int:
     rid = C.c_int32()
     _check(LIB.cp_request_open(pool, model_id, reserve_tokens, C.byref(rid)))
+    if pool in _POOLS:
+        _POOLS[pool].requests[rid.value] = _POOLS[pool].models.get(model_id, 0)
     return rid.value
 
 
@@ -494,8 +511,9 @@ def cp_rope_apply(rope: int, parts, positions=None, first: int = 0, inverse: boo
     """parts: from rope_parts. positions: int32 device tensor (or address) with
     one entry per token, or None: first, first + 1, ..."""
     if hasattr(positions, "dtype") and (str(positions.dtype) != "torch.int32" or positions.numel() != parts.tokens or
-                                        not positions.is_cuda):
-        raise ValueError("positions holds one int32 per token, on the GPU")
+                                        not positions.is_cuda or
+                                        getattr(parts, "device", None) not in (None, positions.device.index)):
+        raise ValueError("positions holds one int32 per token, on the GPU of the tensors")
     _check(LIB.cp_rope_apply(rope, len(parts), parts, parts.tokens, _ptr(positions), first, int(inverse),
                              _stream(stream)))
 
@@ -512,12 +530,15 @@ def cp_kv_append_rope(pool: int, req_ids: Sequence[int], n_new: Sequence[int], r
                                  _stream(stream)))
 
 
-def _extend_opts(n, n_q, tensors, softcap, window, slopes, prefix, doc_begin, num_splits, path, rope):
+def _extend_opts(pool, req_ids, n_q, tensors, softcap, window, slopes, prefix, doc_begin, num_splits, path, rope):
+    n, known = len(req_ids), _POOLS.get(pool)
     for t in (*tensors, slopes, doc_begin):
-        if hasattr(t, "is_cuda") and not t.is_cuda:
-            raise ValueError("tensors of attention are on the GPU")
-    if hasattr(slopes, "dtype") and str(slopes.dtype) != "torch.float32":
-        raise ValueError("slopes holds one float32 per query head")
+        if hasattr(t, "is_cuda") and not (t.is_cuda and (known is None or t.device.index == known.device)):
+            raise ValueError("tensors of attention are on the GPU of the pool")
+    if hasattr(slopes, "dtype"):
+        heads = known.requests.get(int(req_ids[0]), 0) if known and n else 0
+        if str(slopes.dtype) != "torch.float32" or slopes.numel() < heads:
+            raise ValueError("slopes holds one float32 per query head")
     if hasattr(doc_begin, "dtype") and (str(doc_begin.dtype) != "torch.int32" or doc_begin.numel() != sum(n_q)):
         raise ValueError("doc_begin holds one int32 per query token")
     if prefix is not None:
@@ -537,7 +558,7 @@ def cp_attn_extend(pool: int, req_ids: Sequence[int], n_q: Sequence[int], q, out
     n = len(req_ids)
     if len(n_q) != n:
         raise ValueError("req_ids and n_q differ in length")
-    o = _extend_opts(n, n_q, (q, out, lse), softcap, window, slopes, prefix, doc_begin, num_splits, path, None)
+    o = _extend_opts(pool, req_ids, n_q, (q, out, lse), softcap, window, slopes, prefix, doc_begin, num_splits, path, None)
     _check(LIB.cp_attn_extend(pool, n, _i32_array(req_ids), _i32_array(n_q), _ptr(q), _ptr(out), _ptr(lse),
                               _stream(stream), C.byref(o)))
 
@@ -548,7 +569,7 @@ def cp_attn_extend_step(pool: int, req_ids: Sequence[int], n_new: Sequence[int],
     n = len(req_ids)
     if len(n_new) != n:
         raise ValueError("req_ids and n_new differ in length")
-    o = _extend_opts(n, n_new, (rows, q, out, lse), softcap, window, slopes, prefix, doc_begin, num_splits, path, rope)
+    o = _extend_opts(pool, req_ids, n_new, (rows, q, out, lse), softcap, window, slopes, prefix, doc_begin, num_splits, path, rope)
     _check(LIB.cp_attn_extend_step(pool, n, _i32_array(req_ids), _i32_array(n_new), _ptr(rows), _ptr(q), _ptr(out),
                                    _ptr(lse), _stream(stream), C.byref(o)))
 

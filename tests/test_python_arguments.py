@@ -42,3 +42,60 @@ def test_integers_out_of_range_are_refused():
     for r in (a, b, c):
         p.close(r)
     p.destroy()
+
+
+class Tensor:
+    """As much of a device tensor as the calls look at."""
+
+    is_cuda = True
+
+    def __init__(self, dtype, count, device=-1, contiguous=True):
+        self.dtype, self.count, self.contiguous = f"torch.{dtype}", count, contiguous
+        self.device = type("Device", (), dict(index=device))
+
+    def numel(self):
+        return self.count
+
+    def is_contiguous(self):
+        return self.contiguous
+
+    def data_ptr(self):
+        return 4096
+
+
+def test_tensors_of_attention_that_do_not_fit_are_refused():
+    p, (a, b, c) = host_pool()
+    two = p.open(p.register(**dict(ROW, n_q_heads=6)), 8)
+    for r, heads in ((a, 4), (two, 6)):
+        args = dict(q=Tensor("bfloat16", 1), out=Tensor("bfloat16", 1), lse=Tensor("float32", 1))
+        calls = (lambda **k: p.extend([r], [3], **{**args, **k}),
+                 lambda **k: p.extend_step([r], [3], Tensor("bfloat16", 1), **{**args, **k}))
+        good = dict(slopes=Tensor("float32", heads), doc_begin=Tensor("int32", 3))
+        for call in calls:
+            with pytest.raises(cpl.CrossPoolError) as e:  # all of it right, but no GPU
+                call(**good)
+            assert e.value.status == cpl.CP_ESTATE
+            for bad in (dict(slopes=Tensor("float32", heads - 1)), dict(slopes=Tensor("float64", heads)),
+                        dict(slopes=Tensor("float32", heads, contiguous=False)), dict(doc_begin=Tensor("int32", 2)),
+                        dict(doc_begin=Tensor("int64", 3)), dict(doc_begin=Tensor("int32", 3, contiguous=False)),
+                        dict(q=Tensor("bfloat16", 1, device=1)), dict(out=Tensor("bfloat16", 1, device=0)),
+                        dict(lse=Tensor("float32", 1, device=1)), dict(slopes=Tensor("float32", heads, device=1)),
+                        dict(doc_begin=Tensor("int32", 3, device=2)), dict(q=Tensor("bfloat16", 1, contiguous=False))):
+                with pytest.raises(ValueError):
+                    call(**{**good, **bad})
+    for r in (a, b, c, two):
+        p.close(r)
+    p.destroy()
+
+
+def test_positions_that_do_not_fit_are_refused():
+    rope = cpl.Rope(8, device=-1)
+    parts = (cpl.cp_rope_tensor * 1)(cpl.cp_rope_tensor(4096, 4096, 8, 8, 8, 8, 1, 8, 0, cpl.CP_ROPE_BF16))
+    parts.tokens, parts.device = 3, 0
+    with pytest.raises(cpl.CrossPoolError):
+        cpl.cp_rope_apply(rope.handle, parts, Tensor("int32", 3, device=0), stream=0)
+    for bad in (Tensor("int32", 3, device=1), Tensor("int32", 4, device=0), Tensor("int64", 3, device=0),
+                Tensor("int32", 3, device=0, contiguous=False)):
+        with pytest.raises(ValueError):
+            cpl.cp_rope_apply(rope.handle, parts, bad, stream=0)
+    rope.destroy()
