@@ -519,7 +519,11 @@ def cp_rope_apply(rope: int, parts, positions=None, first: int = 0, inverse: boo
 
 
 def _rope(rope) -> Optional[int]:
-    return rope.handle if isinstance(rope, Rope) else rope
+    if isinstance(rope, Rope):
+        if not rope.handle:
+            raise ValueError("the rotation is destroyed")
+        return rope.handle
+    return rope
 
 
 def cp_kv_append_rope(pool: int, req_ids: Sequence[int], n_new: Sequence[int], rows, rope, stream=None) -> None:
@@ -612,12 +616,12 @@ class Rope:
         self.handle = cp_rope_create(rot_dim, device, self._LAYOUT[layout], self._SCALING[scaling], **desc)
 
     def angles(self) -> np.ndarray:
-        return cp_rope_angles(self.handle, self.rot_dim)
+        return cp_rope_angles(_rope(self), self.rot_dim)
 
     def apply(self, parts, positions=None, first: int = 0, inverse: bool = False, stream=None) -> None:
         if parts.device not in (None, self.device):
             raise ValueError(f"the rotation is on device {self.device}, the tensors on {parts.device}")
-        cp_rope_apply(self.handle, parts, positions, first, inverse, stream)
+        cp_rope_apply(_rope(self), parts, positions, first, inverse, stream)
 
     def destroy(self) -> None:
         if self.handle:

@@ -99,3 +99,19 @@ def test_positions_that_do_not_fit_are_refused():
         with pytest.raises(ValueError):
             cpl.cp_rope_apply(rope.handle, parts, bad, stream=0)
     rope.destroy()
+
+
+def test_a_destroyed_rotation_is_not_no_rotation():
+    """(its handle, None, would store the rows as they are)"""
+    p, (a, b, c) = host_pool()
+    rope = cpl.Rope(8, device=-1)
+    rope.destroy()
+    rope.destroy()
+    for call in (lambda: p.extend_step([a], [3], 4096, 4096, 4096, 4096, 0, rope=rope),
+                 lambda: p.append_rope([a], [3], None, rope, 0), lambda: rope.angles(),
+                 lambda: rope.apply(cpl.rope_parts([]), stream=0)):
+        with pytest.raises(ValueError):
+            call()
+    for r in (a, b, c):
+        p.close(r)
+    p.destroy()
