@@ -569,8 +569,9 @@ typedef enum { CP_ROPE_BF16 = 0, CP_ROPE_F32 = 1 } cp_rope_dtype;
  * the last dimension contiguous. Elements [offset, offset + rot_dim) of each
  * head are rotated, the others copied. dst may be src (same strides), and
  * must not overlap it otherwise; distinct tokens and heads of dst must not
- * overlap (refused). Any alignment of whole elements works; 16-byte aligned rows are
- * faster. */
+ * overlap (refused). What one tensor of a call writes, no other of the call may read
+ * or write (refused where they begin at one address). Any alignment of whole
+ * elements works; 16-byte aligned rows are faster. */
 typedef struct {
   const void *src;
   void *dst;

@@ -169,6 +169,9 @@ cp_status cp_rope_apply(const cp_rope *r, int32_t n_tensors, const cp_rope_tenso
     if (x.src_token < 0 || x.src_head < 0 || x.dst_token < 0 || x.dst_head < 0)
       return fail(CP_EINVAL, "tensor %d: negative stride", i);
     if (n_tokens > 0 && (!x.src || !x.dst)) return fail(CP_EINVAL, "tensor %d: null pointer", i);
+    for (int32_t k = 0; k < i && n_tokens > 0; ++k)  // their workgroups run in no order
+      if (x.dst == t[k].dst || x.dst == t[k].src || x.src == t[k].dst)
+        return fail(CP_EINVAL, "tensors %d and %d: one writes where the other begins", k, i);
     const bool in_place = x.src == x.dst;
     if (in_place && ((n_tokens > 1 && x.src_token != x.dst_token) || (x.heads > 1 && x.src_head != x.dst_head)))
       return fail(CP_EINVAL, "tensor %d: in place needs the same strides", i);

@@ -115,3 +115,25 @@ def test_a_destroyed_rotation_is_not_no_rotation():
     for r in (a, b, c):
         p.close(r)
     p.destroy()
+
+
+def test_tensors_of_a_rotation_that_meet_are_refused():
+    rope = cpl.Rope(8, device=-1)
+
+    def status(*pairs, tokens=2):
+        parts = (cpl.cp_rope_tensor * len(pairs))(
+            *[cpl.cp_rope_tensor(s, d, 32, 8, 32, 8, 4, 8, 0, cpl.CP_ROPE_BF16) for s, d in pairs])
+        parts.tokens = tokens
+        with pytest.raises(cpl.CrossPoolError) as e:
+            cpl.cp_rope_apply(rope.handle, parts, stream=0)
+        return e.value.status
+
+    a, b, c, d = (1 << 20, 2 << 20, 3 << 20, 4 << 20)
+    for pairs in (((a, b), (c, b)), ((a, b), (b, c)), ((b, c), (a, b)), ((a, a), (a, b)), ((a, b), (a, a)),
+                  ((a, a), (a, a)), ((a, b), (c, d), (b, c))):
+        assert status(*pairs) == cpl.CP_EINVAL, pairs
+    # sources may be shared, and no tokens meet nowhere (a host-only rotation refuses all, last)
+    for pairs in (((a, b), (a, c)), ((a, a), (b, b)), ((a, b), (c, d))):
+        assert status(*pairs) == cpl.CP_ESTATE, pairs
+    assert status((a, a), (a, a), tokens=0) == cpl.CP_ESTATE
+    rope.destroy()
