@@ -143,8 +143,11 @@ typedef struct {
    * stack, with up to a chunk's worth of pages, before a step that would
    * empty it; pages in a stack count against their model's reservations.
    * The host copy of the popped entries is read back, waiting for the
-   * device, at the next cp_request_pages, cp_request_close or cp_kv_append;
-   * a close also returns stack pages no open reservation can still use.
+   * device, at the next cp_request_pages, cp_request_close, cp_kv_append,
+   * cp_kv_append_rope, cp_request_fork, cp_request_truncate or
+   * cp_attn_extend_step; a close also returns stack pages no open reservation
+   * can still use, and so do appends, chunk steps and forks whose new pages may
+   * be those (they then wait for the device too).
    * Results do not depend on this setting. A step may open at most 7168
    * pages of one model (requests times planes). */
   int32_t device_pages;
@@ -279,6 +282,7 @@ cp_status cp_request_pages(cp_pool *pool, int32_t req_id, int64_t first, int64_t
  * New pages come from the model's slab, or a fresh chunk of the shared
  *   budget; their page-table entries are written by the copy's launch, or
  *   (more than 352 of them) by a copy ahead of it.
+ * On a device_pages pool the call may wait for the device (cp_pool_desc).
  * Errors: CP_EINVAL (unknown or duplicate id, negative count, growth past
  *   the reservation, rows == NULL on a device pool), CP_EHIP. */
 cp_status cp_kv_append(cp_pool *pool, int32_t n, const int32_t *req_ids, const int32_t *n_new,
@@ -532,7 +536,9 @@ typedef enum {
   CP_ROPE_NTK = 2,    /* base * factor^(rot_dim / (rot_dim - 2)) as the base */
   /* by wavelength: r_i = orig_len f_i / (2 pi) is the number of turns over
    * the trained context and w = clamp((r_i - low_turns) / (high_turns -
-   * low_turns), 0, 1); f_i w + (f_i / factor) (1 - w) */
+   * low_turns), 0, 1); f_i w + (f_i / factor) (1 - w). (A ramp in the number of
+   * turns. Models that ramp in the pair's index i, between the pairs of
+   * high_turns and low_turns, need CP_ROPE_TABLE.) */
   CP_ROPE_PARTS = 3,
   CP_ROPE_TABLE = 4   /* table[i], rot_dim / 2 angles per position */
 } cp_rope_scaling;

@@ -2040,7 +2040,15 @@ double choose_ranges(const Geom &g, int num_cus, uint64_t cap, std::vector<ExtIt
 // Whole pages that request ids[i] of a call and those right behind it show alike from
 // the start on, and how many requests do (*count, 1 when it is not worth an
 // item): few rows each, which read their keys at the speed of memory, alike in the
-// precision of their probabilities, and at least kShareTokens shared tokens.
+// precision of their probabilities, and at least kShareTokens shared tokens. Whether
+// the item is used then, choose_ranges' estimates say. us a call, always shared and
+// never: below kShareTokens it never paid (GQA-32:8, 128 tokens, 8 branches 14.8 and
+// 9.4, 32 branches 19.0 and 10.2; MLA-16 24 and 15, 28 and 21); at 512 and 32 branches
+// GQA-32:8 21 and 23, MQA-32 19 and 21, MLA-16 31 and 24; at 16 K 52 and 155, 53 and 45,
+// 60 and 111. The estimates err for few branches of MLA-16 (2 K, 8 branches: shared, 30
+// instead of 20; 16 K, 4 branches 37 instead of 31) and short runs of MQA-32 (512, 32
+// branches: apart, 21 instead of 19). kShareRows bounds members: at 1,024 instead of
+// 128 no time changed.
 constexpr int64_t kShareTokens = 256, kShareRows = 128;
 int64_t shared_run(const cp_pool *p, int32_t n, const int32_t *ids, const int32_t *n_q, int32_t i, const Geom &geom,
                    int32_t *count) {
@@ -2060,7 +2068,8 @@ int64_t shared_run(const cp_pool *p, int32_t n, const int32_t *ids, const int32_
     const int64_t most = std::min(pages, b.ctx_len / P);
     int64_t same = 0;
     while (same < most && x[same] == y[same] && x[same] != kPendingPte) ++same;
-    // (a request that shares much less than those before starts the next run)
+    // (a request that shares much less than those before starts the next run: 16 branches
+    // of 8 K tokens and 1 K, GQA-32:8, take 23 us, and 34 as one run of 1 K; MLA-16 40, and 33)
     if (same * P < kShareTokens || 2 * same < pages) break;
     pages = same;
     *count += 1;

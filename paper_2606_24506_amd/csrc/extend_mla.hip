@@ -11,12 +11,17 @@ namespace cp {
 // 32 keys, a 36 KiB piece of LDS that serves K (576 wide) and V (its first 512
 // columns). Scores are transposed (S^T = K Q^T, 16x16x32 products: a lane holds
 // four of every 16 keys of its row) and, rounded, are the operand P^T of O^T =
-// V^T P^T in place. A fragment of 1 KiB feeds 16 rows, 16 cycles of a product,
-// and four SIMDs ask for twice what LDS gives, so the products run at half their
-// rate at most; with every CU full they reach 930 TFLOP/s (chunks of 2,048 over 16 K
-// keys), matrix cores 41% busy, LDS 42%, the vector unit 38%: a step's scores, softmax
-// and sums are a chain that two waves a SIMD cover in part. 32 rows a wave would
-// halve the reads, but their sums and queries do not fit in registers.
+// V^T P^T in place. A fragment of 1 KiB feeds 16 rows, 16 cycles of a product:
+// four SIMDs ask for the 256 bytes a cycle that LDS gives (544 KiB a step, 2,180 cycles
+// of LDS and as many of products). With every CU full (two requests of 16 K keys, the
+// last 2,048 tokens of each, 16 heads; warm) they reach 961 TFLOP/s, and 1,087 with 128
+// heads and 512 tokens; where half of the CUs run short contexts the matrix cores are
+// 41% busy, LDS 42%, the vector unit 38%: a step's scores, softmax and sums are a chain
+// that two waves a SIMD cover in part. 32 rows a wave would halve the reads, but
+// their sums and queries do not fit in registers.
+// Probabilities are rounded to one bf16 part (2.0e-3 from 64 bits instead of 1.7e-3):
+// with a second part, a second product for every fragment of V, prompts of 1,024 tokens
+// took 353 us instead of 285, and drafts of 5 tokens 58 instead of 50.
 //
 // KV goes from the pool to LDS directly, NBUF - 1 steps ahead, a load for a row's
 // latent part and one for eight rows' rotary parts. The lane for a 16-byte place of

@@ -22,12 +22,19 @@ namespace cp {
 // next step's keys go to LDS directly while this one's are worked on (through
 // registers, the loads' shuffles and LDS stores were a fifth of the vector unit's
 // work, and 40 registers). Bound by the vector unit (exponentials, cap) and the
-// matrix cores, which overlap only as far as two workgroups a CU take turns, and by
-// LDS, whose reads for 32 rows take as long as the products at their peak:
-// head_dim 128, chunks of 2,048 over 16 K keys, 886 TFLOP/s plain, 782 capped, 774
-// sloped (with loads through registers and no fragments read ahead 810, 726, 732; with
-// the first of these changed 847, 730, 718); head_dim 64 730, 563, 560 (636, 520, 549).
-// Steps of 32 keys and three workgroups a CU gained nothing (660 sloped; head_dim 64 595).
+// matrix cores, which overlap only as far as two workgroups a CU take turns; LDS reads
+// for 32 rows (1 KiB a product of 32 cycles, four SIMDs, at 256 bytes a cycle) take half
+// as long as the products. Two requests of 16 K keys, the last 2,048 tokens of each, 32
+// query heads over 8, the card warm: 936 TFLOP/s plain, 813 under a cap of 50, 797
+// sloped; 16 over 4 heads of head_dim 64 759, 576, 568. (From idle the clock is lower
+// for some 10 ms. Steps measured there: 886 plain, 782 capped, 774 sloped; with no
+// fragments read ahead 847, 730, 718; with loads through registers too 810, 726, 732.
+// Steps of 32 keys and three workgroups a CU: 660 sloped.) A cap of the scores' size
+// takes the tangent's other form: 555 under a cap of 2.
+// Probabilities are rounded to one bf16 part, off by at most 2^-8 of themselves, as the
+// outputs are: these are 2.0e-3 to 2.4e-3 from 64 bits instead of 1.6e-3 to 1.8e-3 (the
+// root of the mean square, of the values'). Two parts (RW = 1) took 1,304 us instead of 1,008 on capped prompts
+// of 16 K, 9 K and 4 K tokens, and 47 instead of 40 on packed documents of 700.
 // RW = 1: 32 rows, every wave with 32 keys of its own a step (few rows: bound
 // by reading KV); the waves' sums join at the end. Its loads pass through
 // registers, because a wave's keys are its own and no barrier is needed.
@@ -507,8 +514,8 @@ __global__ __launch_bounds__(kExtThreads, 2) void extend_rows_kernel(const ExtAr
 // keys and not 16, half of them of rows that are not there: the vector unit's
 // work for one row a tile halves, and so do the registers of queries and
 // sums: capped single tokens over 480 MB of KV take 85 us with the join (89 by RW = 1;
-// 6.1 TB/s in the kernel), sloped ones over 537 MB 86 (104; 6.7 TB/s). Lanes are (row `col` of 16, quarter `quad`); pieces of LDS rows are swapped
-// so that K reads (16 rows at one piece) and V reads (8 rows at two) meet no bank
+// 6.1 TB/s in the kernel), sloped ones over 537 MB 86 (104; 6.7 TB/s). Lanes are (row
+// `col` of 16, quarter `quad`); pieces of LDS rows are swapped so that K reads (16 rows at one piece) and V reads (8 rows at two) meet no bank
 // twice.
 template <int D>
 struct ExtFew {
