@@ -670,6 +670,11 @@ cp_status cp_request_truncate(cp_pool *p, int32_t n, const int32_t *ids, const i
       p->st.truncate_cost(n, ids, new_len, true, &more, &pages);
       if (!p->st.fits_budget(more)) return fail(CP_ENOSPC, "the pool page budget cannot take back the shared pages' place");
     }
+    for (int32_t m = 0; m < p->st.n_models(); ++m)
+      if (pages[(size_t)m] > p->st.free_slots(m)) {  // a chunk is taken only for copies that fill it
+        p->st.truncate_cost(n, ids, new_len, true, &more, &pages);
+        break;
+      }
     std::vector<PageItem> items;
     std::vector<int32_t> models;
     std::vector<PoolState::OwnPage> copies;

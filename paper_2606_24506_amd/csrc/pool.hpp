@@ -221,6 +221,8 @@ class PoolState {
   int64_t room_to_grow(int32_t model) const { return acct_[model].reserved - acct_[model].used + acct_[model].in_stack; }
   int64_t reserved(int32_t model) const { return acct_[model].reserved; }
   int64_t allocated(int32_t model) const { return acct_[model].used; }
+  // Free pages of the model's chunks.
+  int64_t free_slots(int32_t model) const { return acct_[model].held * models_[model].ppc - acct_[model].used; }
 
   const uint32_t *pte_mirror() const { return pte_.data(); }
   uint32_t *pte_mirror_mut() { return pte_.data(); }
