@@ -69,10 +69,11 @@ cp_status broken_pool() {
 }
 
 // Calls that mark the pool unusable when their launch fails ask this first: an error
-// that another HIP call left behind would look like that launch's.
+// that another HIP call left behind would look like that launch's. (That an event or
+// stream is not ready is none.)
 cp_status earlier_error() {
   const hipError_t e = hipGetLastError();
-  return e == hipSuccess ? CP_OK : hip_fail(e, "left behind by an earlier HIP call (nothing was done)");
+  return e == hipSuccess || e == hipErrorNotReady ? CP_OK : hip_fail(e, "left behind by an earlier HIP call (nothing was done)");
 }
 
 // Makes the pool's device current for the duration of a call.

@@ -17,7 +17,7 @@ int g_fail_in = 0;   // the n-th launch or asynchronous copy from now on fails (
 int g_last = 0;      // hipGetLastError
 int g_launches = 0;
 int g_no_memory = 0;  // device allocations fail
-constexpr int kLaunchFailure = 719, kInvalid = 1;
+constexpr int kLaunchFailure = 719;
 int step() {
   if (g_fail_in > 0 && --g_fail_in == 0) return g_last = kLaunchFailure;
   return 0;
@@ -27,7 +27,7 @@ int step() {
 extern "C" {
 void fake_fail_in(int n) { g_fail_in = n; }
 void fake_no_memory(int on) { g_no_memory = on; }
-void fake_leave_error() { g_last = kInvalid; }
+void fake_leave_error(int e) { g_last = e; }
 int fake_launches() { return g_launches; }
 
 hipError_t hipGetDeviceCount(int *n) { return *n = 1, 0; }

@@ -137,13 +137,17 @@ a, b = p.open(m, 40), p.open(m, 40)
 p.append([a], [12], at, 0)
 before = p.stats()
 for fn, args in ((p.fork, ([a], [b], None, 0)), (p.extend_step, ([a], [3], at, at, at, at, 0))):
-    fake.fake_leave_error()
+    fake.fake_leave_error(1)  # an invalid value
     assert status(fn, *args)[0] == cpl.CP_EHIP
     assert p.stats() == before and (p.ctx_len(a), p.ctx_len(b)) == (12, 0)
 p.fork([a], [b], None, 0)
-fake.fake_leave_error()
+fake.fake_leave_error(1)  # an invalid value
 assert status(p.truncate, [b], [6], 0)[0] == cpl.CP_EHIP
 assert p.ctx_len(b) == 12
+fake.fake_leave_error(600)  # an event that is not ready
+p.truncate([b], [6], 0)
+fake.fake_leave_error(600)
+p.extend_step([a], [3], at, at, at, at, 0)
 usable(p, [a, b])
 """,
 }
