@@ -692,6 +692,51 @@ cp_status cp_attn_extend_step(cp_pool *pool, int32_t n, const int32_t *req_ids, 
                               const void *rows, const void *q, void *out, float *lse, void *hip_stream,
                               const cp_extend_opts *opts);
 
+/* --------------------------------------------------------- drafted trees */
+
+#define CP_TREE_MAX_WORDS 128 /* trees of up to 4096 tokens */
+
+/* Trees of drafted tokens, each behind its request's context: tokens of one
+ * depth are alternatives for one position. Token t of a tree stands at position
+ * context-before-the-tree + depth[t]. */
+typedef struct {
+  /* Device, [sum of tokens][words]: bit u % 32 of word u / 32 of a token's row
+   * says that it sees token u of its own tree (its ancestors and itself, for a
+   * tree; any other set will do). Bits past the tree's tokens are ignored. */
+  const uint32_t *mask;
+  int32_t words; /* in [1, CP_TREE_MAX_WORDS]: trees of up to 32 * words tokens */
+  int32_t reserved0;
+  const int32_t *depth; /* device, one per token, in [0, its tree's tokens) (others count as the last of these) */
+} cp_tree;
+
+/* Masks and depths of n trees from the tokens' parents.
+ *   n_tok    host, n entries, 0 <= n_tok[i] <= 32 * words.
+ *   parents  device, [sum n_tok]: the number of each token's parent in its own
+ *            tree, less than its own; any other value (-1 is usual): a child of
+ *            the context's last token, depth 0.
+ *   mask     device, out, [sum n_tok][words]; depth: device, out, [sum n_tok].
+ * Errors: CP_EINVAL, CP_EHIP. */
+cp_status cp_tree_build(int32_t device, int32_t n, const int32_t *n_tok, const int32_t *parents, int32_t words,
+                        uint32_t *mask, int32_t *depth, void *hip_stream);
+
+/* cp_attn_extend of requests whose last n_q[i] tokens are such a tree: token t
+ * at position p = context - n_q[i] + depth[t] sees the context before the tree,
+ *     max(p - window + 1, doc_begin) <= j < context - n_q[i],
+ * and the tokens of the tree that its mask names (window and documents do not
+ * limit those); slopes multiply the distance of positions. opts->prefix must
+ * be NULL. Layouts, kernels, workspace and errors as there, plus CP_EINVAL for
+ * a tree that does not fit its mask. */
+cp_status cp_attn_tree(cp_pool *pool, int32_t n, const int32_t *req_ids, const int32_t *n_q, const void *q, void *out,
+                       float *lse, const cp_tree *tree, void *hip_stream, const cp_extend_opts *opts);
+
+/* cp_attn_extend_step of such trees: the drafted tokens' rows are placed one
+ * behind the other, in the order of the tree's numbers, and the same tokens
+ * attend as in cp_attn_tree; keys rotated by opts->rope are turned by their
+ * tokens' positions (by depth). */
+cp_status cp_attn_tree_step(cp_pool *pool, int32_t n, const int32_t *req_ids, const int32_t *n_new, const void *rows,
+                            const void *q, void *out, float *lse, const cp_tree *tree, void *hip_stream,
+                            const cp_extend_opts *opts);
+
 /* ---------------------------------------------------------------------
  * KV-cache planner (Section 3.1, "KV-cache Planner and Virtualizer",
  * Eq. 1-2): the pool budget for cp_pool_desc.pool_bytes, host only.

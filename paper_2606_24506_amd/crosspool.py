@@ -146,6 +146,15 @@ class cp_extend_opts(C.Structure):
     ]
 
 
+class cp_tree(C.Structure):
+    _fields_ = [
+        ("mask", C.c_void_p),
+        ("words", C.c_int32),
+        ("reserved0", C.c_int32),
+        ("depth", C.c_void_p),
+    ]
+
+
 class cp_plan_model(C.Structure):
     _fields_ = [("kappa_bytes", C.c_double), ("arrival_rate", C.c_double), ("n_samples", C.c_int64),
                 ("prompt_tokens", C.POINTER(C.c_int64)), ("output_tokens", C.POINTER(C.c_int64)),
@@ -206,6 +215,9 @@ def _load() -> C.CDLL:
         "cp_kv_append_rope": ([P, I32, VP, VP, VP, P, VP], I32),
         "cp_attn_extend": ([P, I32, VP, VP, VP, VP, VP, VP, C.POINTER(cp_extend_opts)], I32),
         "cp_attn_extend_step": ([P, I32, VP, VP, VP, VP, VP, VP, VP, C.POINTER(cp_extend_opts)], I32),
+        "cp_tree_build": ([I32, I32, VP, VP, I32, VP, VP, VP], I32),
+        "cp_attn_tree": ([P, I32, VP, VP, VP, VP, VP, C.POINTER(cp_tree), VP, C.POINTER(cp_extend_opts)], I32),
+        "cp_attn_tree_step": ([P, I32, VP, VP, VP, VP, VP, VP, C.POINTER(cp_tree), VP, C.POINTER(cp_extend_opts)], I32),
         "cp_plan_pool": ([C.POINTER(cp_plan_model), I32, C.POINTER(cp_plan_opts), C.POINTER(cp_plan_result)], I32),
     }
     for name, (args, res) in sig.items():
@@ -578,6 +590,57 @@ def cp_attn_extend_step(pool: int, req_ids: Sequence[int], n_new: Sequence[int],
                                    _ptr(lse), _stream(stream), C.byref(o)))
 
 
+def _tree(known, n_q, mask, depth):
+    """The record of a call's trees: mask int32 [tokens][words], depth int32
+    [tokens], on the GPU."""
+    total = sum(n_q)
+    if mask.dim() != 2 or mask.shape[0] != total or depth.numel() != total:
+        raise ValueError("mask is [tokens][words] and depth [tokens] of the call's trees")
+    for t in (mask, depth):
+        if str(t.dtype) != "torch.int32" or not t.is_cuda or (known is not None and t.device.index != known.device):
+            raise ValueError("mask and depth are int32, on the GPU of the pool")
+    return cp_tree(_ptr(mask), mask.shape[1], 0, _ptr(depth))
+
+
+def cp_tree_build(n_tok: Sequence[int], parents, mask, depth, stream=None) -> None:
+    """parents int32 [tokens of every tree]; mask int32 [tokens][words] and depth
+    int32 [tokens] are written. All on one GPU."""
+    total = sum(n_tok)
+    if parents.numel() != total or str(parents.dtype) != "torch.int32":
+        raise ValueError("parents holds one int32 per token")
+    if parents.device != mask.device:
+        raise ValueError("the tensors are on one GPU")
+    t = _tree(None, n_tok, mask, depth)
+    if depth.device != mask.device:
+        raise ValueError("the tensors are on one GPU")
+    _check(LIB.cp_tree_build(mask.device.index, len(n_tok), _i32_array(n_tok), _ptr(parents), t.words, t.mask, t.depth,
+                             _stream(stream)))
+
+
+def cp_attn_tree(pool: int, req_ids: Sequence[int], n_q: Sequence[int], q, out, lse, mask, depth, stream=None, *,
+                 softcap: float = 0.0, window: int = 0, slopes=None, doc_begin=None, num_splits: int = 0,
+                 path: int = CP_PATH_AUTO) -> None:
+    n = len(req_ids)
+    if len(n_q) != n:
+        raise ValueError("req_ids and n_q differ in length")
+    t = _tree(_POOLS.get(pool), n_q, mask, depth)
+    o = _extend_opts(pool, req_ids, n_q, (q, out, lse), softcap, window, slopes, None, doc_begin, num_splits, path, None)
+    _check(LIB.cp_attn_tree(pool, n, _i32_array(req_ids), _i32_array(n_q), _ptr(q), _ptr(out), _ptr(lse), C.byref(t),
+                            _stream(stream), C.byref(o)))
+
+
+def cp_attn_tree_step(pool: int, req_ids: Sequence[int], n_new: Sequence[int], rows, q, out, lse, mask, depth,
+                      stream=None, *, rope=None, softcap: float = 0.0, window: int = 0, slopes=None, doc_begin=None,
+                      num_splits: int = 0, path: int = CP_PATH_AUTO) -> None:
+    n = len(req_ids)
+    if len(n_new) != n:
+        raise ValueError("req_ids and n_new differ in length")
+    t = _tree(_POOLS.get(pool), n_new, mask, depth)
+    o = _extend_opts(pool, req_ids, n_new, (rows, q, out, lse), softcap, window, slopes, None, doc_begin, num_splits, path, rope)
+    _check(LIB.cp_attn_tree_step(pool, n, _i32_array(req_ids), _i32_array(n_new), _ptr(rows), _ptr(q), _ptr(out),
+                                 _ptr(lse), C.byref(t), _stream(stream), C.byref(o)))
+
+
 def cp_plan_pool(models, horizon_s: float, n_obs: int, quantile: float, seed: int, chunk_bytes: int = 2 << 20) -> dict:
     """models: sequence of dicts with kappa_bytes, arrival_rate and equal-length
     prompt_tokens / output_tokens / service_time_s sequences (trace records)."""
@@ -697,6 +760,12 @@ class Pool:
 
     def extend_step(self, req_ids, n_new, rows, q, out, lse, stream=None, **opts) -> None:
         cp_attn_extend_step(self.handle, req_ids, n_new, rows, q, out, lse, stream, **opts)
+
+    def tree(self, req_ids, n_q, q, out, lse, mask, depth, stream=None, **opts) -> None:
+        cp_attn_tree(self.handle, req_ids, n_q, q, out, lse, mask, depth, stream, **opts)
+
+    def tree_step(self, req_ids, n_new, rows, q, out, lse, mask, depth, stream=None, **opts) -> None:
+        cp_attn_tree_step(self.handle, req_ids, n_new, rows, q, out, lse, mask, depth, stream, **opts)
 
     def fork(self, src_ids, dst_ids, n_tok=None, stream=None) -> None:
         cp_request_fork(self.handle, src_ids, dst_ids, n_tok, stream)

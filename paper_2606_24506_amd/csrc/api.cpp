@@ -15,6 +15,7 @@
 #include "cost_line.hpp"
 #include "crosspool.h"
 #include "extend.h"
+#include "tree.h"
 #include "kargs.h"
 static_assert(cp::kNoAllocScratchBytes == CP_NOALLOC_WORKSPACE_BYTES, "the header states the fixed workspace size");
 #include "status.hpp"
@@ -36,6 +37,7 @@ hipError_t launch_merge(const MergeArgs &a, hipStream_t stream);
 hipError_t launch_extend(const ExtArgs &a, int32_t kind, hipStream_t stream);
 hipError_t launch_ext_merge(const ExtMergeArgs &a, uint32_t rows, uint32_t most_splits, hipStream_t stream);
 hipError_t launch_page_copy(const PageCopyArgs &a, hipStream_t stream);
+hipError_t launch_tree(const TreeArgs &a, hipStream_t stream);
 hipError_t launch_stack_push(const StackPushArgs &a, hipStream_t stream);
 hipError_t scratch_device_address(int device, void **out);
 }  // namespace cp
@@ -795,13 +797,14 @@ struct AppItem {
   uint64_t src_off;         // element offset of the first row in `rows`
   uint64_t ent = 0;         // new pages whose entries the launch carries:
   uint32_t n_ent = 0;       // their first index in the mirror, and how many
+  uint32_t tok0 = 0;        // the first row's place among the call's tokens
 };
 
 // Append launches for rows already accounted for in the host tables, in
 // groups of at most kMaxReqPerLaunch items and kMaxLaunchModels models; with
 // keys rotated on the way where a rotation is given.
 cp_status launch_appends(cp_pool *p, const std::vector<AppItem> &items, const void *rows, hipStream_t s,
-                         const cp_rope *rope = nullptr) {
+                         const cp_rope *rope = nullptr, const int32_t *depth = nullptr) {
   const int32_t P = p->st.page_tokens();
   size_t i = 0;
   while (i < items.size()) {
@@ -809,6 +812,7 @@ cp_status launch_appends(cp_pool *p, const std::vector<AppItem> &items, const vo
     a.pool = p->dev_pool;
     a.pte = p->dev_pte;
     a.rows = (const uint16_t *)rows;
+    a.depth = depth;
     int32_t nm = 0, model_map[16];
     for (int k = 0; k < 16; ++k) model_map[k] = -1;
     uint32_t blocks = 0;
@@ -828,6 +832,7 @@ cp_status launch_appends(cp_pool *p, const std::vector<AppItem> &items, const vo
         q.old_len = it.old_len;
         q.pte_base = it.pte_base;
         q.model = (uint16_t)mi;
+        q.tok0 = it.tok0;
         q.ent = kNoEnt;
         if (it.n_ent) {
           q.ent = (uint16_t)a.n_ent;
@@ -1944,13 +1949,20 @@ struct ExtPlan {
   uint64_t ws_rows = 0;  // partial rows
 };
 
+// What shapes a call's choice of kernels besides rows: the path, and trees with
+// capped or sloped scores, which have no tiles of 32 rows by 128 columns (extend_rows.hip).
+struct ExtHow {
+  int32_t path = CP_PATH_AUTO;
+  bool tree_any = false;
+};
+
 // The kernel of a request with n_q query tokens (extend.h).
-int32_t extend_kind(const Geom &g, int32_t path, int64_t n_q) {
-  if (path == CP_PATH_VALU) return kXVec;
+int32_t extend_kind(const Geom &g, const ExtHow &how, int64_t n_q) {
+  if (how.path == CP_PATH_VALU) return kXVec;
   if (g.kind == kGQA && (g.head_dim == 64 || g.head_dim == 128)) {
     const int64_t rows = n_q * g.g;
     if (g.head_dim == 64) return rows <= 16 ? kXFew64 : rows <= 32 ? kXSome64 : kXRows64;
-    return rows <= 16 ? kXFew128 : rows <= 32 ? kXSome128 : kXRows128;
+    return rows <= (how.tree_any ? 32 : 16) ? kXFew128 : rows <= 32 ? kXSome128 : kXRows128;
   }
   return g.kind == kMLA && g.latent == 512 && g.rope == 64 ? kXMla : kXVec;
 }
@@ -1961,9 +1973,10 @@ bool two_parts(int32_t kind) { return kind >= kXSome64 && kind <= kXFew128; }
 // The kernel of an item of several requests' query tokens, of which the first's own is
 // `alone`: a request keeps its precision beside others, and so requests of few rows
 // take tiles of 32 however many they are together.
-int32_t shared_kind(const Geom &g, int32_t path, int64_t tokens, int32_t alone) {
-  const int32_t kind = extend_kind(g, path, tokens);
-  return two_parts(alone) && !two_parts(kind) ? (g.head_dim == 64 ? kXSome64 : kXSome128) : kind;
+int32_t shared_kind(const Geom &g, const ExtHow &how, int64_t tokens, int32_t alone) {
+  const int32_t kind = extend_kind(g, how, tokens);
+  if (!two_parts(alone) || two_parts(kind)) return kind;
+  return g.head_dim == 64 ? kXSome64 : how.tree_any ? kXFew128 : kXSome128;
 }
 
 // An item of a call (extend.h): its kernel, rows of all heads, row tiles per KV head,
@@ -2057,9 +2070,9 @@ double choose_ranges(const Geom &g, int num_cus, uint64_t cap, std::vector<ExtIt
 // 128 no time changed.
 constexpr int64_t kShareTokens = 256, kShareRows = 128;
 int64_t shared_run(const cp_pool *p, int32_t n, const int32_t *ids, const int32_t *n_q, int32_t i, const Geom &geom,
-                   int32_t *count) {
+                   const ExtHow &how, int32_t *count) {
   const int32_t g = geom.g;
-  const bool parts = two_parts(extend_kind(geom, CP_PATH_AUTO, n_q[i]));
+  const bool parts = two_parts(extend_kind(geom, how, n_q[i]));
   const uint32_t *pt = p->st.pte_mirror();
   const int64_t P = p->st.page_tokens();
   const Request &a = p->st.req(ids[i]);
@@ -2069,7 +2082,7 @@ int64_t shared_run(const cp_pool *p, int32_t n, const int32_t *ids, const int32_
   for (int32_t k = i + 1; k < n && *count < kExtMaxReq; ++k) {
     const Request &b = p->st.req(ids[k]);
     if (n_q[k] < 1 || n_q[k] * (int64_t)g > kShareRows) break;
-    if (two_parts(extend_kind(geom, CP_PATH_AUTO, n_q[k])) != parts) break;
+    if (two_parts(extend_kind(geom, how, n_q[k])) != parts) break;
     const uint32_t *x = pt + a.plane_base(a.cursor), *y = pt + b.plane_base(b.cursor);
     const int64_t most = std::min(pages, b.ctx_len / P);
     int64_t same = 0;
@@ -2086,7 +2099,8 @@ int64_t shared_run(const cp_pool *p, int32_t n, const int32_t *ids, const int32_
 // Checks a call and plans it, at the contexts the requests will have with
 // extra[i] more tokens (NULL: none). Changes nothing.
 cp_status plan_extend(cp_pool *p, int32_t n, const int32_t *ids, const int32_t *n_q, const int32_t *extra,
-                      const void *q, const void *out, const float *lse, const cp_extend_opts &o, ExtPlan *pl) {
+                      const void *q, const void *out, const float *lse, const cp_extend_opts &o, const cp_tree *tree,
+                      ExtPlan *pl) {
   if (o.softcap != 0.f && !(o.softcap >= 1e-18f && o.softcap <= 1e18f))
     return fail(CP_EINVAL, "softcap must be 0 or in [1e-18, 1e18]");
   if (o.window < 0) return fail(CP_EINVAL, "window must be >= 0");
@@ -2111,6 +2125,18 @@ cp_status plan_extend(cp_pool *p, int32_t n, const int32_t *ids, const int32_t *
     return fail(CP_EINVAL, "q must be 16-byte aligned, out 8-byte, lse, slopes and doc_begin 4-byte");
   pl->geom = p->st.model(pl->model);
   const Geom &g = pl->geom;
+  if (tree) {
+    if (tree->words < 1 || tree->words > CP_TREE_MAX_WORDS)
+      return fail(CP_EINVAL, "tree words must be in [1, %d]", CP_TREE_MAX_WORDS);
+    if (o.prefix) return fail(CP_EINVAL, "trees take no prefix: every token sees the context before its tree");
+    if (total > 0 && (!tree->mask || !tree->depth)) return fail(CP_EINVAL, "null tree mask or depth");
+    if ((uintptr_t)tree->mask % 4 || (uintptr_t)tree->depth % 4)
+      return fail(CP_EINVAL, "tree mask and depth must be 4-byte aligned");
+    for (int32_t i = 0; i < n; ++i)
+      if (n_q[i] > 32 * tree->words)
+        return fail(CP_EINVAL, "a tree of %d tokens (request %d) does not fit %d words of mask", n_q[i], ids[i], tree->words);
+  }
+  const ExtHow how{o.path, tree && (o.slopes || o.softcap > 0.f)};
 
   std::vector<uint32_t> tok((size_t)n, 0u);
   for (int32_t i = 1; i < n; ++i) tok[(size_t)i] = tok[(size_t)i - 1] + (uint32_t)n_q[i - 1];
@@ -2129,7 +2155,7 @@ cp_status plan_extend(cp_pool *p, int32_t n, const int32_t *ids, const int32_t *
       lo = std::min(lo, o.window ? std::max<int64_t>(0, ctx - n_q[i] - o.window + 1) : 0);
       hi = std::max(hi, ctx);
     }
-    x.kind = kind >= 0 ? kind : extend_kind(g, o.path, tokens);
+    x.kind = kind >= 0 ? kind : extend_kind(g, how, tokens);
     const int64_t rows = ext_tile_rows(x.kind), keys = ext_tile_keys(x.kind);
     x.rows = tokens * g.hq;
     x.tiles = (tokens * g.g + rows - 1) / rows;
@@ -2160,14 +2186,14 @@ cp_status plan_extend(cp_pool *p, int32_t n, const int32_t *ids, const int32_t *
     for (int32_t i = 0; look && i < n;) {
       int32_t count = 1;
       int64_t pages = 0;
-      if (n_q[i] > 0) pages = shared_run(p, n, ids, n_q, i, g, &count);
+      if (n_q[i] > 0) pages = shared_run(p, n, ids, n_q, i, g, how, &count);
       const int64_t keys = pages * p->st.page_tokens();
       if (count < 2) {
         if (n_q[i] > 0) apart.push_back(item_of(i, 1, 0, 0xFFFFFFFFll));
       } else {
         int64_t tokens = 0;
         for (int32_t k = i; k < i + count; ++k) tokens += n_q[k];
-        const int32_t kind = shared_kind(g, o.path, tokens, extend_kind(g, o.path, n_q[i]));
+        const int32_t kind = shared_kind(g, how, tokens, extend_kind(g, how, n_q[i]));
         apart.push_back(item_of(i, count, 0, keys, kind));
         apart.back().shared = true;
         apart.back().group = groups;
@@ -2299,7 +2325,7 @@ void set_score_factors(ExtArgs *a, double scale) {
 }
 
 cp_status run_extend(cp_pool *p, const ExtPlan &pl, const void *q, void *out, float *lse, const cp_extend_opts &o,
-                     hipStream_t s) {
+                     const cp_tree *tree, hipStream_t s) {
   const Geom &g = pl.geom;
   const int32_t P = p->st.page_tokens();
   for (const ExtPlan::Launch &l : pl.launches) {
@@ -2319,6 +2345,11 @@ cp_status run_extend(cp_pool *p, const ExtPlan &pl, const void *q, void *out, fl
     a.page_magic = page_magic(P);
     a.n_req = (int32_t)l.req.size();
     a.n_units = (int32_t)l.units;
+    if (tree) {
+      a.tree_words = tree->words;
+      a.tree_mask = tree->mask;
+      a.tree_depth = tree->depth;
+    }
     a.g = geom_k(g, P);
     std::copy(l.req.begin(), l.req.end(), a.req);
     std::copy(l.member.begin(), l.member.end(), a.member);
@@ -2353,10 +2384,10 @@ cp_status bind_extend_workspace(cp_pool *p, const ExtPlan &pl) {
 
 }  // namespace
 
-extern "C" {
+namespace {
 
-cp_status cp_attn_extend(cp_pool *p, int32_t n, const int32_t *req_ids, const int32_t *n_q, const void *q, void *out,
-                         float *lse, void *hip_stream, const cp_extend_opts *opts) {
+cp_status extend_impl(cp_pool *p, int32_t n, const int32_t *req_ids, const int32_t *n_q, const void *q, void *out,
+                      float *lse, void *hip_stream, const cp_extend_opts *opts, const cp_tree *tree) {
   return guarded([&]() -> cp_status {
     if (!p) return fail(CP_EINVAL, "null pool");
     if (p->host_only) return fail(CP_ESTATE, "host-only pool cannot attend");
@@ -2366,19 +2397,20 @@ cp_status cp_attn_extend(cp_pool *p, int32_t n, const int32_t *req_ids, const in
     if (n > 0 && !n_q) return fail(CP_EINVAL, "null n_q");
     cp_extend_opts o{};
     if (opts) o = *opts;
-    if (o.rope) return fail(CP_EINVAL, "cp_attn_extend places no rows: opts.rope must be NULL");
+    if (o.rope) return fail(CP_EINVAL, "the call places no rows: opts.rope must be NULL");
     ExtPlan pl;
-    rc = plan_extend(p, n, req_ids, n_q, nullptr, q, out, lse, o, &pl);
+    rc = plan_extend(p, n, req_ids, n_q, nullptr, q, out, lse, o, tree, &pl);
     if (rc) return rc;
     DeviceGuard g(p->device);
     rc = bind_extend_workspace(p, pl);
     if (rc) return rc;
-    return run_extend(p, pl, q, out, lse, o, (hipStream_t)hip_stream);
+    return run_extend(p, pl, q, out, lse, o, tree, (hipStream_t)hip_stream);
   });
 }
 
-cp_status cp_attn_extend_step(cp_pool *p, int32_t n, const int32_t *req_ids, const int32_t *n_new, const void *rows,
-                              const void *q, void *out, float *lse, void *hip_stream, const cp_extend_opts *opts) {
+cp_status extend_step_impl(cp_pool *p, int32_t n, const int32_t *req_ids, const int32_t *n_new, const void *rows,
+                           const void *q, void *out, float *lse, void *hip_stream, const cp_extend_opts *opts,
+                           const cp_tree *tree) {
   return guarded([&]() -> cp_status {
     if (!p) return fail(CP_EINVAL, "null pool");
     if (p->host_only) return fail(CP_ESTATE, "host-only pool cannot attend");
@@ -2411,7 +2443,7 @@ cp_status cp_attn_extend_step(cp_pool *p, int32_t n, const int32_t *req_ids, con
     }
     if (any && !rows) return fail(CP_EINVAL, "null rows");
     ExtPlan pl;
-    rc = plan_extend(p, n, req_ids, n_new, placing.data(), q, out, lse, o, &pl);
+    rc = plan_extend(p, n, req_ids, n_new, placing.data(), q, out, lse, o, tree, &pl);
     if (rc) return rc;
     DeviceGuard g(p->device);
     rc = bind_extend_workspace(p, pl);
@@ -2444,7 +2476,7 @@ cp_status cp_attn_extend_step(cp_pool *p, int32_t n, const int32_t *req_ids, con
       }
       if (n_new[i] > 0) {
         items.push_back(AppItem{r.model, (uint32_t)n_new[i], (uint32_t)r.ctx_len, r.plane_base(r.cursor), src,
-                                r.plane_base(r.cursor) + (uint64_t)used, (uint32_t)(r.pages_used - used)});
+                                r.plane_base(r.cursor) + (uint64_t)used, (uint32_t)(r.pages_used - used), (uint32_t)(src / row_elems)});
         entries += (uint64_t)(r.pages_used - used);
         src += (uint64_t)n_new[i] * row_elems;
       }
@@ -2453,11 +2485,86 @@ cp_status cp_attn_extend_step(cp_pool *p, int32_t n, const int32_t *req_ids, con
       rc = push_ptes(p, lo, hi, s);
       for (AppItem &x : items) x.n_ent = 0;
     }
-    if (rc == CP_OK) rc = launch_appends(p, items, rows, s, o.rope);
-    if (rc == CP_OK) rc = run_extend(p, pl, q, out, lse, o, s);
+    if (rc == CP_OK) rc = launch_appends(p, items, rows, s, o.rope, tree ? tree->depth : nullptr);
+    if (rc == CP_OK) rc = run_extend(p, pl, q, out, lse, o, tree, s);
     for (int32_t i = 0; i < n; ++i) p->st.advance(req_ids[i]);
     if (rc) p->broken = true;  // rows or page-table entries are missing on the device
     return rc;
+  });
+}
+
+}  // namespace
+
+extern "C" {
+
+cp_status cp_attn_extend(cp_pool *p, int32_t n, const int32_t *req_ids, const int32_t *n_q, const void *q, void *out,
+                         float *lse, void *hip_stream, const cp_extend_opts *opts) {
+  return extend_impl(p, n, req_ids, n_q, q, out, lse, hip_stream, opts, nullptr);
+}
+
+cp_status cp_attn_extend_step(cp_pool *p, int32_t n, const int32_t *req_ids, const int32_t *n_new, const void *rows,
+                              const void *q, void *out, float *lse, void *hip_stream, const cp_extend_opts *opts) {
+  return extend_step_impl(p, n, req_ids, n_new, rows, q, out, lse, hip_stream, opts, nullptr);
+}
+
+cp_status cp_attn_tree(cp_pool *p, int32_t n, const int32_t *req_ids, const int32_t *n_q, const void *q, void *out,
+                       float *lse, const cp_tree *tree, void *hip_stream, const cp_extend_opts *opts) {
+  if (!tree) return fail(CP_EINVAL, "null tree");
+  return extend_impl(p, n, req_ids, n_q, q, out, lse, hip_stream, opts, tree);
+}
+
+cp_status cp_attn_tree_step(cp_pool *p, int32_t n, const int32_t *req_ids, const int32_t *n_new, const void *rows,
+                            const void *q, void *out, float *lse, const cp_tree *tree, void *hip_stream,
+                            const cp_extend_opts *opts) {
+  if (!tree) return fail(CP_EINVAL, "null tree");
+  return extend_step_impl(p, n, req_ids, n_new, rows, q, out, lse, hip_stream, opts, tree);
+}
+
+cp_status cp_tree_build(int32_t device, int32_t n, const int32_t *n_tok, const int32_t *parents, int32_t words,
+                        uint32_t *mask, int32_t *depth, void *hip_stream) {
+  return guarded([&]() -> cp_status {
+    if (n < 0 || (n > 0 && !n_tok)) return fail(CP_EINVAL, "negative count or null n_tok");
+    if (words < 1 || words > CP_TREE_MAX_WORDS) return fail(CP_EINVAL, "words must be in [1, %d]", CP_TREE_MAX_WORDS);
+    int64_t total = 0;
+    for (int32_t i = 0; i < n; ++i) {
+      if (n_tok[i] < 0 || n_tok[i] > 32 * words)
+        return fail(CP_EINVAL, "tree %d of %d tokens does not fit %d words of mask", i, n_tok[i], words);
+      total += n_tok[i];
+    }
+    if (total > 0x7FFFFFFF) return fail(CP_EINVAL, "too many tokens in one call");
+    if (total > 0 && (!parents || !mask || !depth)) return fail(CP_EINVAL, "null parents, mask or depth");
+    if ((uintptr_t)parents % 4 || (uintptr_t)mask % 4 || (uintptr_t)depth % 4)
+      return fail(CP_EINVAL, "parents, mask and depth must be 4-byte aligned");
+    const uint64_t at[3] = {(uint64_t)(uintptr_t)parents, (uint64_t)(uintptr_t)mask, (uint64_t)(uintptr_t)depth};
+    const uint64_t len[3] = {4ull * total, 4ull * total * words, 4ull * total};
+    for (int x = 0; x < 3; ++x)
+      for (int y = 0; y < x; ++y)
+        if (at[x] < at[y] + len[y] && at[y] < at[x] + len[x]) return fail(CP_EINVAL, "parents, mask and depth overlap");
+    int ndev = 0;
+    if (device < 0 || hipGetDeviceCount(&ndev) != hipSuccess || device >= ndev)
+      return fail(CP_EINVAL, "device %d not present", device);
+    DeviceGuard g(device);
+    TreeArgs a{};
+    a.parents = parents;
+    a.mask = mask;
+    a.depth = depth;
+    a.words = words;
+    uint32_t tok = 0;
+    for (int32_t i = 0; i < n; ++i) {
+      if (n_tok[i] == 0) continue;
+      TreeArgs::Req &r = a.req[a.n_req++];
+      r.tok0 = tok;
+      r.n = (uint32_t)n_tok[i];
+      r.block_begin = (uint32_t)a.n_blocks;
+      a.n_blocks += (n_tok[i] + kTreeThreads - 1) / kTreeThreads;
+      tok += r.n;
+      if (a.n_req < kMaxTreesPerLaunch) continue;
+      const hipError_t e = launch_tree(a, (hipStream_t)hip_stream);
+      if (e != hipSuccess) return hip_fail(e, "tree launch");
+      a.n_req = a.n_blocks = 0;
+    }
+    const hipError_t e = launch_tree(a, (hipStream_t)hip_stream);
+    return e == hipSuccess ? CP_OK : hip_fail(e, "tree launch");
   });
 }
 

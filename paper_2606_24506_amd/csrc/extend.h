@@ -75,6 +75,11 @@ struct ExtArgs {
   uint32_t window;
   uint32_t page_magic;  // page_divide
   int32_t n_req, n_units;
+  // Trees (NULL: the last tokens stand one behind the other): per query token which of
+  // its request's query tokens it sees, tree_words words, and its depth.
+  int32_t tree_words;
+  const uint32_t *tree_mask;
+  const int32_t *tree_depth;
   GeomK g;
   ExtReq req[kExtMaxReq];
   ExtMember member[kExtMaxReq];

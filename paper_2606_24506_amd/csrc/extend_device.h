@@ -5,6 +5,8 @@
 // a request is token r / g, head r % g. A work unit is a tile of consecutive rows
 // of one KV head over one range of keys. Row r at position p sees keys [lo, hi):
 //   hi = max(p + 1, prefix),  lo = max(p - window + 1, doc_begin, 0).
+// In a tree row r stands at p = base + depth, base = context - n_q, and sees keys
+// [min(lo, base), base) and those of the n_q behind that its mask names.
 // One pass over the keys keeps, per row, the running maximum m and sum l of
 // 2^(s - m) in fp32 (s: scores times log2 e) and the output sums; where a tile's
 // keys are cut into ranges, ext_merge_kernel joins their results.
@@ -68,8 +70,12 @@ CP_DEV float cap_tanh(float x) {
 
 // How a kernel's scores are formed (a kernel for each, for their registers
 // and instructions): products times a factor (left to the exponent's fma);
-// capped; capped or not, with slopes.
-enum : int { kModePlain = 0, kModeCap, kModeAny };
+// capped; capped or not, with slopes. The same with trees: products times a
+// factor, and anything else.
+enum : int { kModePlain = 0, kModeCap, kModeAny, kModeTree, kModeTreeAny };
+constexpr bool is_tree(int mode) { return mode >= kModeTree; }
+constexpr bool is_plain(int mode) { return mode == kModePlain || mode == kModeTree; }
+constexpr bool is_any(int mode) { return mode == kModeAny || mode == kModeTreeAny; }
 
 struct Unit {
   const ExtReq *rq;
@@ -90,7 +96,9 @@ struct Row {
   uint32_t pos, lo, hi;  // lo == hi: nothing
   uint32_t head;         // of all query heads
   uint64_t tok;          // query token of the call
+  uint32_t base;         // every key before it is behind the row: its own place + 1, or its tree's first
 };
+template <bool TREE>
 CP_DEV Row row_of(const ExtArgs &a, const ExtReq &rq, uint32_t kvh, uint32_t r) {
   const uint32_t g = (uint32_t)a.g.g, rows = rq.n_tok * g, rc = min(r, rows - 1);
   uint32_t t = rc / g, ctx = rq.ctx, n_q = rq.n_q, prefix = rq.prefix;
@@ -106,14 +114,66 @@ CP_DEV Row row_of(const ExtArgs &a, const ExtReq &rq, uint32_t kvh, uint32_t r) 
     t -= n_q;
   }
   x.pos = ctx - n_q + t;
-  x.hi = min(max(x.pos + 1, min(prefix, ctx)), rq.key_hi);
-  x.lo = max(a.window && x.pos >= a.window ? x.pos - a.window + 1 : 0u, rq.key_lo);
+  x.base = x.pos + 1;
+  if constexpr (TREE) {
+    x.base = ctx - n_q;
+    x.pos = x.base + min((uint32_t)a.tree_depth[x.tok], n_q - 1);
+    x.hi = min(ctx, rq.key_hi);
+  } else {
+    x.hi = min(max(x.pos + 1, min(prefix, ctx)), rq.key_hi);
+  }
+  x.lo = a.window && x.pos >= a.window ? x.pos - a.window + 1 : 0u;
   if (a.doc_begin) {
     const int32_t d = a.doc_begin[x.tok];
     if (d > 0) x.lo = max(x.lo, (uint32_t)d);
   }
+  if (TREE) x.lo = min(x.lo, x.base);
+  x.lo = max(x.lo, rq.key_lo);
   if (x.lo >= x.hi) x.lo = x.hi = 0;
   return x;  // rows past the last repeat it (their results are not stored)
+}
+
+// The tree of a row: its first key, its tokens, and the first of those in the call. (Looked
+// up afresh in the few steps that ask: kept through the loop they would cost registers
+// that the kernels have not.)
+struct Tree {
+  uint32_t base, n_q, tok0;
+};
+CP_DEV Tree tree_of(const ExtArgs &a, const ExtReq &rq, const Row &x) {
+  uint32_t t = (uint32_t)x.tok - rq.tok0, ctx = rq.ctx, n_q = rq.n_q;
+  asm volatile("" : "+v"(t));
+  for (uint32_t k = 0; k < rq.members; ++k) {
+    const ExtMember &m = a.member[rq.member0 + k];
+    ctx = m.ctx;
+    n_q = m.n_q;
+    if (t < n_q) break;
+    t -= n_q;
+  }
+  return Tree{ctx - n_q, n_q, (uint32_t)x.tok - t};
+}
+// Which of the N <= 64 keys from k0 on a row of a tree sees.
+template <int N>
+CP_DEV uint64_t tree_bits(const ExtArgs &a, const ExtReq &rq, const Row &x, uint32_t k0) {
+  const uint32_t base = tree_of(a, rq, x).base;
+  uint64_t b = ~0ull;
+  if (k0 + N > base) {
+    const uint32_t *const m = a.tree_mask + x.tok * (uint32_t)a.tree_words;
+    const uint32_t before = k0 < base ? base - k0 : 0u, first = k0 < base ? 0u : k0 - base;  // before < N
+    const uint32_t w = first / 32, sh = first % 32, n = (uint32_t)a.tree_words;
+    const uint32_t w0 = w < n ? m[w] : 0u, w1 = w + 1 < n ? m[w + 1] : 0u, w2 = w + 2 < n ? m[w + 2] : 0u;
+    b = (uint64_t)w0 | (uint64_t)w1 << 32;
+    if (sh) b = b >> sh | (uint64_t)w2 << (64 - sh);
+    if (before) b = b << before | ((1ull << before) - 1);
+  }
+  const uint32_t lo = x.lo > k0 ? min(x.lo - k0, 64u) : 0u, hi = x.hi > k0 ? min(x.hi - k0, 64u) : 0u;
+  if (hi < 64) b &= (1ull << hi) - 1;
+  return lo < 64 ? b >> lo << lo : 0;
+}
+// Where key j stands.
+CP_DEV uint32_t tree_pos(const ExtArgs &a, const Tree &t, uint32_t j) {
+  if (j < t.base) return j;
+  const uint32_t i = min(j - t.base, t.n_q - 1);  // (keys past the context are hidden)
+  return t.base + min((uint32_t)a.tree_depth[t.tok0 + i], t.n_q - 1);
 }
 
 // Stores of a row's result: NORMAL to the call's arrays, or a range's part.
@@ -139,9 +199,11 @@ CP_DEV bool all_small(const ExtArgs &a, const float (&s)[N]) {
 }
 
 // Scores of N keys of one row, from products to units of log2 e. Element i is
-// key k0 + at(i); behind: no key is past the position `pos` of any row of the wave.
+// key k0 + at(i); behind: no key is past the position of any row of the wave, or in its tree.
 template <int MODE, int N, class F>
-CP_DEV void shape_scores(const ExtArgs &a, float (&s)[N], float slope, uint32_t pos, uint32_t k0, bool behind, F at) {
+CP_DEV void shape_scores(const ExtArgs &a, const ExtReq &rq, float (&s)[N], float slope, const Row &x, uint32_t k0,
+                         bool behind, F at) {
+  const uint32_t pos = x.pos;
   if (MODE == kModeCap || a.softcap > 0.f) {
     if (all_small(a, s)) {
 #pragma unroll
@@ -154,15 +216,18 @@ CP_DEV void shape_scores(const ExtArgs &a, float (&s)[N], float slope, uint32_t 
 #pragma unroll
     for (int i = 0; i < N; ++i) s[i] *= a.score_mul;
   }
-  if constexpr (MODE == kModeAny) {
+  if constexpr (is_any(MODE)) {
     if (behind) {  // slope * (pos - key) in two steps
       const float far = (float)(pos - k0);
 #pragma unroll
       for (int i = 0; i < N; ++i) s[i] = __builtin_fmaf(-slope, far - (float)at(i), s[i]);
     } else {
+      Tree t{};
+      if (is_tree(MODE)) t = tree_of(a, rq, x);
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        const uint32_t key = k0 + at(i);
+        if (is_tree(MODE)) __builtin_amdgcn_sched_barrier(0);  // one load at once, for the registers
+        const uint32_t key = is_tree(MODE) ? tree_pos(a, t, k0 + at(i)) : k0 + at(i);
         s[i] = __builtin_fmaf(-slope, (float)(max(key, pos) - min(key, pos)), s[i]);
       }
     }
@@ -171,23 +236,23 @@ CP_DEV void shape_scores(const ExtArgs &a, float (&s)[N], float slope, uint32_t 
 
 // Scores of N keys of one row, with those out of sight made -inf, and their
 // maximum in units of log2 e. hide: some row of the wave does not see some of
-// the keys. Where it can, it leaves the products as they are (returns true), for
+// the keys; bits: of a tree, the row's tree_bits from k0 on. Where it can, it leaves the products as they are (returns true), for
 // weight() to scale or cap and take the reference off in one go.
-template <int MODE, int N, class F>
-CP_DEV bool scores_of(const ExtArgs &a, float (&s)[N], float slope, const Row &x, uint32_t k0, bool behind, bool hide,
-                      F at, float *top) {
-  bool raw = MODE == kModePlain || (MODE == kModeCap && !hide && all_small(a, s));
-  if (!raw) shape_scores<MODE, N>(a, s, slope, x.pos, k0, behind, at);
+template <int MODE, int N, class B, class F>
+CP_DEV bool scores_of(const ExtArgs &a, const ExtReq &rq, float (&s)[N], float slope, const Row &x, uint32_t k0,
+                      bool behind, bool hide, B bits, F at, float *top) {
+  bool raw = is_plain(MODE) || (MODE == kModeCap && !hide && all_small(a, s));
+  if (!raw) shape_scores<MODE, N>(a, rq, s, slope, x, k0, behind, at);
   if (hide) {
     const uint32_t lo = x.lo - k0, n = x.hi - x.lo;
 #pragma unroll
     for (int i = 0; i < N; ++i)
-      if ((uint32_t)at(i) - lo >= n) s[i] = -INFINITY;
+      if (is_tree(MODE) ? !(bits >> at(i) & 1) : (uint32_t)at(i) - lo >= n) s[i] = -INFINITY;
   }
   float t = s[0];
 #pragma unroll
   for (int i = 1; i < N; ++i) t = __builtin_fmaxf(t, s[i]);
-  if (MODE == kModePlain) t *= a.score_mul;
+  if (is_plain(MODE)) t *= a.score_mul;
   if (MODE == kModeCap && raw) t = small_cap(a, t, 0.f);
   *top = t;
   return raw;
@@ -196,7 +261,7 @@ CP_DEV bool scores_of(const ExtArgs &a, float (&s)[N], float slope, const Row &x
 // 2^(score - ref) of N elements in order: each(i, weight of i, weight of i + 1)
 template <int MODE, int N, class E>
 CP_DEV void weights(const ExtArgs &a, const float (&s)[N], bool raw, float ref, E each) {
-  if (MODE == kModePlain) {
+  if (is_plain(MODE)) {
 #pragma unroll
     for (int i = 0; i < N; i += 2)
       each(i, fast_exp2(__builtin_fmaf(s[i], a.score_mul, -ref)), fast_exp2(__builtin_fmaf(s[i + 1], a.score_mul, -ref)));
@@ -210,28 +275,29 @@ CP_DEV void weights(const ExtArgs &a, const float (&s)[N], bool raw, float ref, 
 }
 
 // Of some rows: the first key that any sees and the last plus one, the keys that
-// every one sees (a row that sees none: none), and their first position.
+// every one sees (a row that sees none: none), and the first key that is not behind
+// every one.
 struct Sight {
-  uint32_t lo, hi, all_lo, all_hi, pos;
+  uint32_t lo, hi, all_lo, all_hi, behind;
 };
 // Of a wave whose lanes with equal low bits (2 TOP values) hold one row.
-template <int TOP>
+template <int TOP, bool TREE>
 CP_DEV Sight wave_sight(const Row &x) {
   const bool some = x.lo < x.hi;
-  Sight s{some ? x.lo : 0xFFFFFFFFu, x.hi, x.lo, x.hi, x.pos};
+  Sight s{some ? x.lo : 0xFFFFFFFFu, x.hi, x.lo, TREE ? min(x.hi, x.base) : x.hi, x.base};
 #pragma unroll
   for (int o = TOP; o > 0; o >>= 1) {
     s.lo = min(s.lo, (uint32_t)__shfl_xor((int)s.lo, o, 64));
     s.hi = max(s.hi, (uint32_t)__shfl_xor((int)s.hi, o, 64));
     s.all_lo = max(s.all_lo, (uint32_t)__shfl_xor((int)s.all_lo, o, 64));
     s.all_hi = min(s.all_hi, (uint32_t)__shfl_xor((int)s.all_hi, o, 64));
-    s.pos = min(s.pos, (uint32_t)__shfl_xor((int)s.pos, o, 64));
+    s.behind = min(s.behind, (uint32_t)__shfl_xor((int)s.behind, o, 64));
   }
   s.lo = __builtin_amdgcn_readfirstlane(min(s.lo, s.hi));
   s.hi = __builtin_amdgcn_readfirstlane(s.hi);
   s.all_lo = __builtin_amdgcn_readfirstlane(s.all_lo);
   s.all_hi = __builtin_amdgcn_readfirstlane(s.all_hi);
-  s.pos = __builtin_amdgcn_readfirstlane(s.pos);
+  s.behind = __builtin_amdgcn_readfirstlane(s.behind);
   return s;
 }
 // Of a workgroup's waves (barriers inside).

@@ -25,7 +25,7 @@ __global__ __launch_bounds__(kExtThreads) void extend_vec_kernel(const ExtArgs a
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t r = un.tile * 4 + wave;
   if (r >= rq.n_tok * (uint32_t)g.g) return;  // no barrier below: waves are on their own
-  const Row x = row_of(a, rq, un.kvh, r);
+  const Row x = a.tree_mask ? row_of<true>(a, rq, un.kvh, r) : row_of<false>(a, rq, un.kvh, r);
   const uint32_t dk = (uint32_t)g.d_k, P = (uint32_t)g.page_tokens;
   float *const qw = qs + wave * dk;
   const uint16_t *const qrow = a.q + (x.tok * (uint32_t)g.hq + x.head) * dk;
@@ -41,7 +41,8 @@ __global__ __launch_bounds__(kExtThreads) void extend_vec_kernel(const ExtArgs a
   for (int i = 0; i < E; ++i) o[i] = 0.f;
   for (uint32_t k0 = b; k0 < e; k0 += 64) {
     const uint32_t key = k0 + lane;
-    const bool see = key < e;
+    bool see = key < e;
+    if (a.tree_mask && see && key >= x.base) see = tree_bits<1>(a, rq, x, key) & 1;
     float s = -INFINITY;
     uint64_t row = 0;
     if (see) {
@@ -61,7 +62,10 @@ __global__ __launch_bounds__(kExtThreads) void extend_vec_kernel(const ExtArgs a
       }
       s = acc * a.score_mul;
       if (a.softcap > 0.f) s = cap_tanh(s) * a.cap_mul;
-      if (a.slopes) s -= slope * (float)(max(x.pos, key) - min(x.pos, key));
+      if (a.slopes) {
+        const uint32_t at = a.tree_mask ? tree_pos(a, tree_of(a, rq, x), key) : key;
+        s -= slope * (float)(max(x.pos, at) - min(x.pos, at));
+      }
     }
     const float mn = fmaxf(m, wave_max(s)), base = mn == -INFINITY ? 0.f : mn;
     const float al = fast_exp2(m - base);
@@ -71,7 +75,9 @@ __global__ __launch_bounds__(kExtThreads) void extend_vec_kernel(const ExtArgs a
 #pragma unroll
     for (int i = 0; i < E; ++i) o[i] *= al;
     const uint32_t cnt = min(64u, e - k0);
+    const uint64_t seen = __builtin_amdgcn_ballot_w64(see);
     for (uint32_t j = 0; j < cnt; ++j) {
+      if (!(seen >> j & 1)) continue;  // of a tree
       const float pj = __shfl(p, (int)j, 64);
       const uint64_t rj = (uint64_t)(uint32_t)__shfl((int)(uint32_t)row, (int)j, 64) |
                           (uint64_t)(uint32_t)__shfl((int)(uint32_t)(row >> 32), (int)j, 64) << 32;

@@ -60,8 +60,8 @@ __global__ __launch_bounds__(64 * ExtMla::WAVES, 2) void extend_mla_kernel(const
 
   const uint32_t r = un.tile * 128 + 16 * wave + col;
   const bool busy = un.tile * 128 + 16 * wave < rows;  // else the wave only loads
-  const Row x = row_of(a, rq, un.kvh, r);
-  const Sight ws = wave_sight<8>(x);
+  const Row x = row_of<is_tree(MODE)>(a, rq, un.kvh, r);
+  const Sight ws = wave_sight<8, is_tree(MODE)>(x);
   const Sight gs = group_sight<C::WAVES>(ws, wave, lane, shared_u);
   const uint32_t first = gs.lo / C::KEYS, last = (gs.hi + C::KEYS - 1) / C::KEYS, steps = last - first;
   const uint32_t s0 = first + (uint32_t)((uint64_t)steps * un.split / rq.splits),
@@ -110,7 +110,7 @@ __global__ __launch_bounds__(64 * ExtMla::WAVES, 2) void extend_mla_kernel(const
 #pragma unroll
     for (int ks = 0; ks < C::KS; ++ks) qf[ks] = *reinterpret_cast<const bf16x8 *>(qrow + 32 * ks);
   }
-  const float slope = MODE == kModeAny && a.slopes ? a.slopes[x.head] * kLog2e : 0.f;
+  const float slope = is_any(MODE) && a.slopes ? a.slopes[x.head] * kLog2e : 0.f;
   // a wait the compiler sees: its own at the first use would drain the steps in flight
   __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);
 
@@ -213,7 +213,9 @@ __global__ __launch_bounds__(64 * ExtMla::WAVES, 2) void extend_mla_kernel(const
     __builtin_amdgcn_sched_barrier(0);
     auto &flat = reinterpret_cast<float(&)[8]>(sc);
     float t;
-    const bool raw = scores_of<MODE, 8>(a, flat, slope, x, k0, s * C::KEYS + C::KEYS <= ws.pos + 1, mix,
+    uint32_t bits = 0;
+    if (is_tree(MODE) && mix) bits = (uint32_t)(tree_bits<C::KEYS>(a, rq, x, s * C::KEYS) >> (4 * quad));
+    const bool raw = scores_of<MODE, 8>(a, rq, flat, slope, x, k0, s * C::KEYS + C::KEYS <= ws.behind, mix, bits,
                                         [](int i) { return 16 * (i / 4) + i % 4; }, &t);
     if (__builtin_amdgcn_ballot_w64(t > m + kLazy || (m == -INFINITY && t > m))) {
       const float mt = xor_max_16_32(t);
@@ -266,12 +268,14 @@ __global__ __launch_bounds__(64 * ExtMla::WAVES, 2) void extend_mla_kernel(const
       if (!busy) continue;
       const char *const tb = lds + ((s - s0) % C::NBUF) * C::TILE;
       const uint32_t k0 = s * C::KEYS + 4 * quad, lo = x.lo - k0, n = x.hi - x.lo;
+      const uint64_t bits = is_tree(MODE) ? tree_bits<C::KEYS>(a, rq, x, s * C::KEYS) >> (4 * quad) : ~0ull;
       const LaneIds vl = lane_ids();
       u32x4e seen;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const uint32_t e = 16 * (k / 2) + 2 * (k % 2);
-        seen[k] = (e - lo < n ? 0x3F80u : 0u) | (e + 1 - lo < n ? 0x3F800000u : 0u);
+        seen[k] = ((is_tree(MODE) ? bits >> e & 1 : e - lo < n) ? 0x3F80u : 0u) |
+                  ((is_tree(MODE) ? bits >> (e + 1) & 1 : e + 1 - lo < n) ? 0x3F800000u : 0u);
       }
 #pragma unroll
       for (int d = 0; d < C::DB; ++d)
@@ -315,7 +319,11 @@ namespace {
 template <bool NT>
 void launch_mla(const ExtArgs &a, hipStream_t stream) {
   const dim3 grid((uint32_t)a.n_units), block(64 * ExtMla::WAVES);
-  if (a.slopes)
+  if (a.tree_mask && (a.slopes || a.softcap > 0.f))
+    hipLaunchKernelGGL((extend_mla_kernel<kModeTreeAny, NT>), grid, block, 0, stream, a);
+  else if (a.tree_mask)
+    hipLaunchKernelGGL((extend_mla_kernel<kModeTree, NT>), grid, block, 0, stream, a);
+  else if (a.slopes)
     hipLaunchKernelGGL((extend_mla_kernel<kModeAny, NT>), grid, block, 0, stream, a);
   else if (a.softcap > 0.f)
     hipLaunchKernelGGL((extend_mla_kernel<kModeCap, NT>), grid, block, 0, stream, a);

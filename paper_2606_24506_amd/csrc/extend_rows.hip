@@ -2,6 +2,8 @@
 // 128, on the matrix cores.
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "extend_device.h"
 
 namespace cp {
@@ -50,6 +52,7 @@ struct ExtCfg {
   static constexpr int NL = KW / RPI;                 // 16-byte loads of K (and of V) of a thread (RW 1)
   static constexpr int KB = KW / 32;                  // blocks of 32 keys
   static constexpr int NP = RW == 4 ? 1 : 2;          // bf16 parts of a probability
+  using Bits = std::conditional_t<RW == 4, uint64_t, uint32_t>;  // a step's keys of a tree
   static constexpr int LDS = 2 * TILE * BUFS;
   static_assert(RW == 4 || LDS >= 4 * 32 * D * 4, "the join reuses the tiles");
 };
@@ -72,14 +75,14 @@ CP_DEV float low_part(float p, uint32_t h) { return __uint_as_float(__float_as_u
 
 // Results of a tile of ROWS rows from its four waves' m, l and sums (parts: [wave][column]
 // [row] in LDS). A thread takes D ROWS / 256 columns of one row.
-template <int D, int ROWS>
+template <int D, int ROWS, bool TREE>
 CP_DEV void join_waves(const ExtArgs &a, const ExtReq &rq, const Unit &un, const float *parts,
                        const float (&stats)[2][4][ROWS]) {
   constexpr int NC = D * ROWS / kExtThreads;
   const int row = threadIdx.x % ROWS, c0 = threadIdx.x / ROWS * NC;
   const uint32_t r = un.tile * ROWS + row;
   if (r >= rq.n_tok * (uint32_t)a.g.g) return;
-  const Row y = row_of(a, rq, un.kvh, r);
+  const Row y = row_of<TREE>(a, rq, un.kvh, r);
   float mt = stats[0][0][row];
 #pragma unroll
   for (int w = 1; w < 4; ++w) mt = __builtin_fmaxf(mt, stats[0][w][row]);
@@ -134,8 +137,8 @@ __global__ __launch_bounds__(kExtThreads, 2) void extend_rows_kernel(const ExtAr
 
   // ---- this lane's row, what its wave sees, and what the workgroup sees
   const uint32_t r = un.tile * (32 * RW) + (RW == 4 ? 32 * wave : 0) + col;
-  const Row x = row_of(a, rq, un.kvh, r);
-  const Sight ws = wave_sight<16>(x);
+  const Row x = row_of<is_tree(MODE)>(a, rq, un.kvh, r);
+  const Sight ws = wave_sight<16, is_tree(MODE)>(x);
   const Sight gs = RW == 4 ? group_sight<4>(ws, wave, lane, shared_u) : ws;
   // steps of the unit: whole steps from a multiple of KEYS on
   const uint32_t first = gs.lo / C::KEYS, last = (gs.hi + C::KEYS - 1) / C::KEYS, steps = last - first;
@@ -149,7 +152,7 @@ __global__ __launch_bounds__(kExtThreads, 2) void extend_rows_kernel(const ExtAr
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const bf16x8 *>(qrow + 16 * ks);
   }
-  const float slope = MODE == kModeAny && a.slopes ? a.slopes[x.head] * kLog2e : 0.f;
+  const float slope = is_any(MODE) && a.slopes ? a.slopes[x.head] * kLog2e : 0.f;
 
   float m = -INFINITY, l = 0.f;
   f32x16 o[DB];
@@ -322,7 +325,9 @@ __global__ __launch_bounds__(kExtThreads, 2) void extend_rows_kernel(const ExtAr
     const bool hide = b0 < ws.all_lo || b0 + C::KW > ws.all_hi;
     auto &flat = reinterpret_cast<float(&)[16 * C::KB]>(sc);
     float t;
-    const bool raw = scores_of<MODE, 16 * C::KB>(a, flat, slope, x, k0, b0 + C::KW <= ws.pos + 1, hide,
+    typename C::Bits bits = 0;
+    if (is_tree(MODE) && hide) bits = (typename C::Bits)(tree_bits<C::KW>(a, rq, x, b0) >> (4 * half));
+    const bool raw = scores_of<MODE, 16 * C::KB>(a, rq, flat, slope, x, k0, b0 + C::KW <= ws.behind, hide, bits,
                                                  [](int i) { return 32 * (i / 16) + 8 * (i % 16 / 4) + i % 4; }, &t);
     // the reference moves when some row's maximum passes it by 2^kLazy
     if (__builtin_amdgcn_ballot_w64(t > m + kLazy || (m == -INFINITY && t > m))) {
@@ -437,6 +442,7 @@ __global__ __launch_bounds__(kExtThreads, 2) void extend_rows_kernel(const ExtAr
       }
       __builtin_amdgcn_wave_barrier();
       const uint32_t k0 = base_of(s) + 4 * half, lo = x.lo - k0, n = x.hi - x.lo;
+      const uint64_t bits = is_tree(MODE) ? tree_bits<C::KW>(a, rq, x, base_of(s)) >> (4 * half) : ~0ull;
 #pragma unroll
       for (int d = 0; d < DB; ++d)
 #pragma unroll 1
@@ -452,7 +458,8 @@ __global__ __launch_bounds__(kExtThreads, 2) void extend_rows_kernel(const ExtAr
 #pragma unroll
               for (int k = 0; k < 4; ++k) {
                 const uint32_t e = 32 * kb + 16 * ks + 8 * (k / 2) + 2 * (k % 2);
-                seen[k] = (e - lo < n ? 0x3F80u : 0u) | (e + 1 - lo < n ? 0x3F800000u : 0u);
+                seen[k] = ((is_tree(MODE) ? bits >> e & 1 : e - lo < n) ? 0x3F80u : 0u) |
+                          ((is_tree(MODE) ? bits >> (e + 1) & 1 : e + 1 - lo < n) ? 0x3F800000u : 0u);
               }
               hit = __builtin_amdgcn_mfma_f32_32x32x16_bf16(special_ones(v_frag(vt, kb, ks, d), sign),
                                                             __builtin_bit_cast(bf16x8, seen), hit, 0, 0, 0);
@@ -505,7 +512,7 @@ __global__ __launch_bounds__(kExtThreads, 2) void extend_rows_kernel(const ExtAr
       stats[1][wave][col] = l;
     }
     __syncthreads();
-    join_waves<D, 32>(a, rq, un, reinterpret_cast<const float *>(lds), stats);
+    join_waves<D, 32, is_tree(MODE)>(a, rq, un, reinterpret_cast<const float *>(lds), stats);
   }
 }
 
@@ -543,8 +550,8 @@ __global__ __launch_bounds__(kExtThreads, 2) void extend_few_kernel(const ExtArg
   const int col = lane & 15, quad = lane >> 4;
   const uint32_t P = (uint32_t)g.page_tokens;
 
-  const Row x = row_of(a, rq, un.kvh, un.tile * 16 + col);
-  const Sight gs = wave_sight<8>(x);  // every wave has the same rows
+  const Row x = row_of<is_tree(MODE)>(a, rq, un.kvh, un.tile * 16 + col);
+  const Sight gs = wave_sight<8, is_tree(MODE)>(x);  // every wave has the same rows
   const uint32_t first = gs.lo / C::KEYS, last = (gs.hi + C::KEYS - 1) / C::KEYS, steps = last - first;
   const uint32_t s0 = first + (uint32_t)((uint64_t)steps * un.split / rq.splits),
                  s1 = first + (uint32_t)((uint64_t)steps * (un.split + 1) / rq.splits);
@@ -580,7 +587,7 @@ __global__ __launch_bounds__(kExtThreads, 2) void extend_few_kernel(const ExtArg
 #pragma unroll
     for (int ks = 0; ks < C::KS; ++ks) qf[ks] = *reinterpret_cast<const bf16x8 *>(qrow + 32 * ks);
   }
-  const float slope = MODE == kModeAny && a.slopes ? a.slopes[x.head] * kLog2e : 0.f;
+  const float slope = is_any(MODE) && a.slopes ? a.slopes[x.head] * kLog2e : 0.f;
   float m = -INFINITY, l = 0.f;
   f32x4 o[C::DB];
 #pragma unroll
@@ -655,7 +662,9 @@ __global__ __launch_bounds__(kExtThreads, 2) void extend_few_kernel(const ExtArg
         }
       auto &flat = reinterpret_cast<float(&)[8]>(sc);
       float t;
-      const bool raw = scores_of<MODE, 8>(a, flat, slope, x, k0, b0 + C::KW <= gs.pos + 1, mixed(s),
+      uint32_t bits = 0;
+      if (is_tree(MODE) && mixed(s)) bits = (uint32_t)(tree_bits<C::KW>(a, rq, x, b0) >> (4 * quad));
+      const bool raw = scores_of<MODE, 8>(a, rq, flat, slope, x, k0, b0 + C::KW <= gs.behind, mixed(s), bits,
                                           [](int i) { return 16 * (i / 4) + i % 4; }, &t);
       // the reference moves when some row's maximum passes it by 2^kLazy
       if (__builtin_amdgcn_ballot_w64(t > m + kLazy || (m == -INFINITY && t > m))) {
@@ -701,11 +710,13 @@ __global__ __launch_bounds__(kExtThreads, 2) void extend_few_kernel(const ExtArg
       store_v();
       __builtin_amdgcn_wave_barrier();
       const uint32_t k0 = base_of(s) + 4 * quad, lo = x.lo - k0, n = x.hi - x.lo;
+      const uint64_t bits = is_tree(MODE) ? tree_bits<C::KW>(a, rq, x, base_of(s)) >> (4 * quad) : ~0ull;
       u32x4e seen;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const uint32_t e = 16 * (k / 2) + 2 * (k % 2);
-        seen[k] = (e - lo < n ? 0x3F80u : 0u) | (e + 1 - lo < n ? 0x3F800000u : 0u);
+        seen[k] = ((is_tree(MODE) ? bits >> e & 1 : e - lo < n) ? 0x3F80u : 0u) |
+                  ((is_tree(MODE) ? bits >> (e + 1) & 1 : e + 1 - lo < n) ? 0x3F800000u : 0u);
       }
 #pragma unroll
       for (int d = 0; d < C::DB; ++d)
@@ -735,14 +746,20 @@ __global__ __launch_bounds__(kExtThreads, 2) void extend_few_kernel(const ExtArg
     stats[1][wave][col] = l;
   }
   __syncthreads();
-  join_waves<D, 16>(a, rq, un, reinterpret_cast<const float *>(lds), stats);
+  join_waves<D, 16, is_tree(MODE)>(a, rq, un, reinterpret_cast<const float *>(lds), stats);
 }
 
 namespace {
 template <int D, int RW>
 void launch_rows(const ExtArgs &a, hipStream_t stream) {
   const dim3 grid((uint32_t)a.n_units), block(kExtThreads);
-  if (a.slopes)
+  if (a.tree_mask && (a.slopes || a.softcap > 0.f)) {
+    // (no such tiles of 32 rows by 128 columns: 24 registers would spill, and the host takes tiles of 16)
+    if constexpr (D != 128 || RW != 1)
+      hipLaunchKernelGGL((extend_rows_kernel<D, RW, kModeTreeAny>), grid, block, 0, stream, a);
+  } else if (a.tree_mask)
+    hipLaunchKernelGGL((extend_rows_kernel<D, RW, kModeTree>), grid, block, 0, stream, a);
+  else if (a.slopes)
     hipLaunchKernelGGL((extend_rows_kernel<D, RW, kModeAny>), grid, block, 0, stream, a);
   else if (a.softcap > 0.f)
     hipLaunchKernelGGL((extend_rows_kernel<D, RW, kModeCap>), grid, block, 0, stream, a);
@@ -752,7 +769,11 @@ void launch_rows(const ExtArgs &a, hipStream_t stream) {
 template <int D>
 void launch_few(const ExtArgs &a, hipStream_t stream) {
   const dim3 grid((uint32_t)a.n_units), block(kExtThreads);
-  if (a.slopes)
+  if (a.tree_mask && (a.slopes || a.softcap > 0.f))
+    hipLaunchKernelGGL((extend_few_kernel<D, kModeTreeAny>), grid, block, 0, stream, a);
+  else if (a.tree_mask)
+    hipLaunchKernelGGL((extend_few_kernel<D, kModeTree>), grid, block, 0, stream, a);
+  else if (a.slopes)
     hipLaunchKernelGGL((extend_few_kernel<D, kModeAny>), grid, block, 0, stream, a);
   else if (a.softcap > 0.f)
     hipLaunchKernelGGL((extend_few_kernel<D, kModeCap>), grid, block, 0, stream, a);

@@ -177,7 +177,8 @@ __global__ __launch_bounds__(kCopyThreads) void kv_append_rope_kernel(const Appe
   const uint32_t pos0 = rq.old_len + row0;
   for (uint32_t i = threadIdx.x; i < nrows * pairs; i += kCopyThreads) {
     const uint32_t t = i / pairs;
-    turn[i] = rope_turn(rope, (int64_t)pos0 + t, (int32_t)(i - t * pairs));
+    const int64_t at = a.depth ? (int64_t)rq.old_len + a.depth[rq.tok0 + row0 + t] : (int64_t)pos0 + t;
+    turn[i] = rope_turn(rope, at, (int32_t)(i - t * pairs));
   }
   __syncthreads();
   const uint32_t nseg = (uint32_t)g.row_elems / 8, total = nrows * nseg;
