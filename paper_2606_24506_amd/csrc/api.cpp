@@ -1949,20 +1949,13 @@ struct ExtPlan {
   uint64_t ws_rows = 0;  // partial rows
 };
 
-// What shapes a call's choice of kernels besides rows: the path, and trees with
-// capped or sloped scores, which have no tiles of 32 rows by 128 columns (extend_rows.hip).
-struct ExtHow {
-  int32_t path = CP_PATH_AUTO;
-  bool tree_any = false;
-};
-
 // The kernel of a request with n_q query tokens (extend.h).
-int32_t extend_kind(const Geom &g, const ExtHow &how, int64_t n_q) {
-  if (how.path == CP_PATH_VALU) return kXVec;
+int32_t extend_kind(const Geom &g, int32_t path, int64_t n_q) {
+  if (path == CP_PATH_VALU) return kXVec;
   if (g.kind == kGQA && (g.head_dim == 64 || g.head_dim == 128)) {
     const int64_t rows = n_q * g.g;
     if (g.head_dim == 64) return rows <= 16 ? kXFew64 : rows <= 32 ? kXSome64 : kXRows64;
-    return rows <= (how.tree_any ? 32 : 16) ? kXFew128 : rows <= 32 ? kXSome128 : kXRows128;
+    return rows <= 16 ? kXFew128 : rows <= 32 ? kXSome128 : kXRows128;
   }
   return g.kind == kMLA && g.latent == 512 && g.rope == 64 ? kXMla : kXVec;
 }
@@ -1973,10 +1966,9 @@ bool two_parts(int32_t kind) { return kind >= kXSome64 && kind <= kXFew128; }
 // The kernel of an item of several requests' query tokens, of which the first's own is
 // `alone`: a request keeps its precision beside others, and so requests of few rows
 // take tiles of 32 however many they are together.
-int32_t shared_kind(const Geom &g, const ExtHow &how, int64_t tokens, int32_t alone) {
-  const int32_t kind = extend_kind(g, how, tokens);
-  if (!two_parts(alone) || two_parts(kind)) return kind;
-  return g.head_dim == 64 ? kXSome64 : how.tree_any ? kXFew128 : kXSome128;
+int32_t shared_kind(const Geom &g, int32_t path, int64_t tokens, int32_t alone) {
+  const int32_t kind = extend_kind(g, path, tokens);
+  return two_parts(alone) && !two_parts(kind) ? (g.head_dim == 64 ? kXSome64 : kXSome128) : kind;
 }
 
 // An item of a call (extend.h): its kernel, rows of all heads, row tiles per KV head,
@@ -2070,9 +2062,9 @@ double choose_ranges(const Geom &g, int num_cus, uint64_t cap, std::vector<ExtIt
 // 128 no time changed.
 constexpr int64_t kShareTokens = 256, kShareRows = 128;
 int64_t shared_run(const cp_pool *p, int32_t n, const int32_t *ids, const int32_t *n_q, int32_t i, const Geom &geom,
-                   const ExtHow &how, int32_t *count) {
+                   int32_t *count) {
   const int32_t g = geom.g;
-  const bool parts = two_parts(extend_kind(geom, how, n_q[i]));
+  const bool parts = two_parts(extend_kind(geom, CP_PATH_AUTO, n_q[i]));
   const uint32_t *pt = p->st.pte_mirror();
   const int64_t P = p->st.page_tokens();
   const Request &a = p->st.req(ids[i]);
@@ -2082,7 +2074,7 @@ int64_t shared_run(const cp_pool *p, int32_t n, const int32_t *ids, const int32_
   for (int32_t k = i + 1; k < n && *count < kExtMaxReq; ++k) {
     const Request &b = p->st.req(ids[k]);
     if (n_q[k] < 1 || n_q[k] * (int64_t)g > kShareRows) break;
-    if (two_parts(extend_kind(geom, how, n_q[k])) != parts) break;
+    if (two_parts(extend_kind(geom, CP_PATH_AUTO, n_q[k])) != parts) break;
     const uint32_t *x = pt + a.plane_base(a.cursor), *y = pt + b.plane_base(b.cursor);
     const int64_t most = std::min(pages, b.ctx_len / P);
     int64_t same = 0;
@@ -2136,7 +2128,6 @@ cp_status plan_extend(cp_pool *p, int32_t n, const int32_t *ids, const int32_t *
       if (n_q[i] > 32 * tree->words)
         return fail(CP_EINVAL, "a tree of %d tokens (request %d) does not fit %d words of mask", n_q[i], ids[i], tree->words);
   }
-  const ExtHow how{o.path, tree && (o.slopes || o.softcap > 0.f)};
 
   std::vector<uint32_t> tok((size_t)n, 0u);
   for (int32_t i = 1; i < n; ++i) tok[(size_t)i] = tok[(size_t)i - 1] + (uint32_t)n_q[i - 1];
@@ -2155,7 +2146,7 @@ cp_status plan_extend(cp_pool *p, int32_t n, const int32_t *ids, const int32_t *
       lo = std::min(lo, o.window ? std::max<int64_t>(0, ctx - n_q[i] - o.window + 1) : 0);
       hi = std::max(hi, ctx);
     }
-    x.kind = kind >= 0 ? kind : extend_kind(g, how, tokens);
+    x.kind = kind >= 0 ? kind : extend_kind(g, o.path, tokens);
     const int64_t rows = ext_tile_rows(x.kind), keys = ext_tile_keys(x.kind);
     x.rows = tokens * g.hq;
     x.tiles = (tokens * g.g + rows - 1) / rows;
@@ -2186,14 +2177,14 @@ cp_status plan_extend(cp_pool *p, int32_t n, const int32_t *ids, const int32_t *
     for (int32_t i = 0; look && i < n;) {
       int32_t count = 1;
       int64_t pages = 0;
-      if (n_q[i] > 0) pages = shared_run(p, n, ids, n_q, i, g, how, &count);
+      if (n_q[i] > 0) pages = shared_run(p, n, ids, n_q, i, g, &count);
       const int64_t keys = pages * p->st.page_tokens();
       if (count < 2) {
         if (n_q[i] > 0) apart.push_back(item_of(i, 1, 0, 0xFFFFFFFFll));
       } else {
         int64_t tokens = 0;
         for (int32_t k = i; k < i + count; ++k) tokens += n_q[k];
-        const int32_t kind = shared_kind(g, how, tokens, extend_kind(g, how, n_q[i]));
+        const int32_t kind = shared_kind(g, o.path, tokens, extend_kind(g, o.path, n_q[i]));
         apart.push_back(item_of(i, count, 0, keys, kind));
         apart.back().shared = true;
         apart.back().group = groups;

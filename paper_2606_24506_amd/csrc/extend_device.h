@@ -97,6 +97,7 @@ struct Row {
   uint32_t head;         // of all query heads
   uint64_t tok;          // query token of the call
   uint32_t base;         // every key before it is behind the row: its own place + 1, or its tree's first
+  uint32_t n_q, tok0;    // trees: their tokens, and the first of those in the call
 };
 template <bool TREE>
 CP_DEV Row row_of(const ExtArgs &a, const ExtReq &rq, uint32_t kvh, uint32_t r) {
@@ -117,6 +118,8 @@ CP_DEV Row row_of(const ExtArgs &a, const ExtReq &rq, uint32_t kvh, uint32_t r) 
   x.base = x.pos + 1;
   if constexpr (TREE) {
     x.base = ctx - n_q;
+    x.n_q = n_q;
+    x.tok0 = (uint32_t)x.tok - t;
     x.pos = x.base + min((uint32_t)a.tree_depth[x.tok], n_q - 1);
     x.hi = min(ctx, rq.key_hi);
   } else {
@@ -133,32 +136,23 @@ CP_DEV Row row_of(const ExtArgs &a, const ExtReq &rq, uint32_t kvh, uint32_t r) 
   return x;  // rows past the last repeat it (their results are not stored)
 }
 
-// The tree of a row: its first key, its tokens, and the first of those in the call. (Looked
-// up afresh in the few steps that ask: kept through the loop they would cost registers
-// that the kernels have not.)
-struct Tree {
-  uint32_t base, n_q, tok0;
-};
-CP_DEV Tree tree_of(const ExtArgs &a, const ExtReq &rq, const Row &x) {
-  uint32_t t = (uint32_t)x.tok - rq.tok0, ctx = rq.ctx, n_q = rq.n_q;
-  asm volatile("" : "+v"(t));
-  for (uint32_t k = 0; k < rq.members; ++k) {
-    const ExtMember &m = a.member[rq.member0 + k];
-    ctx = m.ctx;
-    n_q = m.n_q;
-    if (t < n_q) break;
-    t -= n_q;
-  }
-  return Tree{ctx - n_q, n_q, (uint32_t)x.tok - t};
+// A row of a tree, formed afresh in the few steps that ask: what is kept of it through the
+// loop costs registers that the kernels have not.
+CP_DEV Row tree_row(const ExtArgs &a, const ExtReq &rq, uint32_t kvh, uint32_t r) {
+  asm volatile("" : "+v"(r));
+  return row_of<true>(a, rq, kvh, r);
 }
-// Which of the N <= 64 keys from k0 on a row of a tree sees.
+struct RowAt {  // what tree_row takes
+  const ExtReq *rq;
+  uint32_t kvh, r;
+};
+// Which of the N <= 64 keys from k0 on it sees.
 template <int N>
-CP_DEV uint64_t tree_bits(const ExtArgs &a, const ExtReq &rq, const Row &x, uint32_t k0) {
-  const uint32_t base = tree_of(a, rq, x).base;
+CP_DEV uint64_t tree_bits(const ExtArgs &a, const Row &x, uint32_t k0) {
   uint64_t b = ~0ull;
-  if (k0 + N > base) {
+  if (k0 + N > x.base) {
     const uint32_t *const m = a.tree_mask + x.tok * (uint32_t)a.tree_words;
-    const uint32_t before = k0 < base ? base - k0 : 0u, first = k0 < base ? 0u : k0 - base;  // before < N
+    const uint32_t before = k0 < x.base ? x.base - k0 : 0u, first = k0 < x.base ? 0u : k0 - x.base;  // before < N
     const uint32_t w = first / 32, sh = first % 32, n = (uint32_t)a.tree_words;
     const uint32_t w0 = w < n ? m[w] : 0u, w1 = w + 1 < n ? m[w + 1] : 0u, w2 = w + 2 < n ? m[w + 2] : 0u;
     b = (uint64_t)w0 | (uint64_t)w1 << 32;
@@ -170,10 +164,10 @@ CP_DEV uint64_t tree_bits(const ExtArgs &a, const ExtReq &rq, const Row &x, uint
   return lo < 64 ? b >> lo << lo : 0;
 }
 // Where key j stands.
-CP_DEV uint32_t tree_pos(const ExtArgs &a, const Tree &t, uint32_t j) {
-  if (j < t.base) return j;
-  const uint32_t i = min(j - t.base, t.n_q - 1);  // (keys past the context are hidden)
-  return t.base + min((uint32_t)a.tree_depth[t.tok0 + i], t.n_q - 1);
+CP_DEV uint32_t tree_pos(const ExtArgs &a, const Row &x, uint32_t j) {
+  if (j < x.base) return j;
+  const uint32_t i = min(j - x.base, x.n_q - 1);  // (keys past the context are hidden)
+  return x.base + min((uint32_t)a.tree_depth[x.tok0 + i], x.n_q - 1);
 }
 
 // Stores of a row's result: NORMAL to the call's arrays, or a range's part.
@@ -201,7 +195,7 @@ CP_DEV bool all_small(const ExtArgs &a, const float (&s)[N]) {
 // Scores of N keys of one row, from products to units of log2 e. Element i is
 // key k0 + at(i); behind: no key is past the position of any row of the wave, or in its tree.
 template <int MODE, int N, class F>
-CP_DEV void shape_scores(const ExtArgs &a, const ExtReq &rq, float (&s)[N], float slope, const Row &x, uint32_t k0,
+CP_DEV void shape_scores(const ExtArgs &a, const RowAt &row, float (&s)[N], float slope, const Row &x, uint32_t k0,
                          bool behind, F at) {
   const uint32_t pos = x.pos;
   if (MODE == kModeCap || a.softcap > 0.f) {
@@ -222,8 +216,8 @@ CP_DEV void shape_scores(const ExtArgs &a, const ExtReq &rq, float (&s)[N], floa
 #pragma unroll
       for (int i = 0; i < N; ++i) s[i] = __builtin_fmaf(-slope, far - (float)at(i), s[i]);
     } else {
-      Tree t{};
-      if (is_tree(MODE)) t = tree_of(a, rq, x);
+      Row t{};
+      if (is_tree(MODE)) t = tree_row(a, *row.rq, row.kvh, row.r);
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         if (is_tree(MODE)) __builtin_amdgcn_sched_barrier(0);  // one load at once, for the registers
@@ -239,10 +233,10 @@ CP_DEV void shape_scores(const ExtArgs &a, const ExtReq &rq, float (&s)[N], floa
 // the keys; bits: of a tree, the row's tree_bits from k0 on. Where it can, it leaves the products as they are (returns true), for
 // weight() to scale or cap and take the reference off in one go.
 template <int MODE, int N, class B, class F>
-CP_DEV bool scores_of(const ExtArgs &a, const ExtReq &rq, float (&s)[N], float slope, const Row &x, uint32_t k0,
+CP_DEV bool scores_of(const ExtArgs &a, const RowAt &row, float (&s)[N], float slope, const Row &x, uint32_t k0,
                       bool behind, bool hide, B bits, F at, float *top) {
   bool raw = is_plain(MODE) || (MODE == kModeCap && !hide && all_small(a, s));
-  if (!raw) shape_scores<MODE, N>(a, rq, s, slope, x, k0, behind, at);
+  if (!raw) shape_scores<MODE, N>(a, row, s, slope, x, k0, behind, at);
   if (hide) {
     const uint32_t lo = x.lo - k0, n = x.hi - x.lo;
 #pragma unroll

@@ -42,7 +42,7 @@ __global__ __launch_bounds__(kExtThreads) void extend_vec_kernel(const ExtArgs a
   for (uint32_t k0 = b; k0 < e; k0 += 64) {
     const uint32_t key = k0 + lane;
     bool see = key < e;
-    if (a.tree_mask && see && key >= x.base) see = tree_bits<1>(a, rq, x, key) & 1;
+    if (a.tree_mask && see && key >= x.base) see = tree_bits<1>(a, x, key) & 1;
     float s = -INFINITY;
     uint64_t row = 0;
     if (see) {
@@ -63,7 +63,7 @@ __global__ __launch_bounds__(kExtThreads) void extend_vec_kernel(const ExtArgs a
       s = acc * a.score_mul;
       if (a.softcap > 0.f) s = cap_tanh(s) * a.cap_mul;
       if (a.slopes) {
-        const uint32_t at = a.tree_mask ? tree_pos(a, tree_of(a, rq, x), key) : key;
+        const uint32_t at = a.tree_mask ? tree_pos(a, x, key) : key;
         s -= slope * (float)(max(x.pos, at) - min(x.pos, at));
       }
     }

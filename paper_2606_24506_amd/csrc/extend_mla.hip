@@ -59,6 +59,7 @@ __global__ __launch_bounds__(64 * ExtMla::WAVES, 2) void extend_mla_kernel(const
   const uint32_t P = (uint32_t)g.page_tokens, rows = rq.n_tok * (uint32_t)g.g;
 
   const uint32_t r = un.tile * 128 + 16 * wave + col;
+  auto row_now = [&] { return un.tile * 128 + 16 * wave + (uint32_t)lane_ids().col; };
   const bool busy = un.tile * 128 + 16 * wave < rows;  // else the wave only loads
   const Row x = row_of<is_tree(MODE)>(a, rq, un.kvh, r);
   const Sight ws = wave_sight<8, is_tree(MODE)>(x);
@@ -205,7 +206,7 @@ __global__ __launch_bounds__(64 * ExtMla::WAVES, 2) void extend_mla_kernel(const
     }
     if (!busy) continue;
     // the first fragments of V arrive during the softmax
-    constexpr int VD = 4;
+    constexpr int VD = MODE == kModeTreeAny ? 2 : 4;  // (with 4 a query fragment would spill)
     bf16x8 vf[VD + 1];
     const LaneIds vl = lane_ids();
 #pragma unroll
@@ -214,8 +215,8 @@ __global__ __launch_bounds__(64 * ExtMla::WAVES, 2) void extend_mla_kernel(const
     auto &flat = reinterpret_cast<float(&)[8]>(sc);
     float t;
     uint32_t bits = 0;
-    if (is_tree(MODE) && mix) bits = (uint32_t)(tree_bits<C::KEYS>(a, rq, x, s * C::KEYS) >> (4 * quad));
-    const bool raw = scores_of<MODE, 8>(a, rq, flat, slope, x, k0, s * C::KEYS + C::KEYS <= ws.behind, mix, bits,
+    if (is_tree(MODE) && mix) bits = (uint32_t)(tree_bits<C::KEYS>(a, tree_row(a, rq, un.kvh, row_now()), s * C::KEYS) >> (4 * quad));
+    const bool raw = scores_of<MODE, 8>(a, RowAt{&rq, un.kvh, row_now()}, flat, slope, x, k0, s * C::KEYS + C::KEYS <= ws.behind, mix, bits,
                                         [](int i) { return 16 * (i / 4) + i % 4; }, &t);
     if (__builtin_amdgcn_ballot_w64(t > m + kLazy || (m == -INFINITY && t > m))) {
       const float mt = xor_max_16_32(t);
@@ -268,7 +269,7 @@ __global__ __launch_bounds__(64 * ExtMla::WAVES, 2) void extend_mla_kernel(const
       if (!busy) continue;
       const char *const tb = lds + ((s - s0) % C::NBUF) * C::TILE;
       const uint32_t k0 = s * C::KEYS + 4 * quad, lo = x.lo - k0, n = x.hi - x.lo;
-      const uint64_t bits = is_tree(MODE) ? tree_bits<C::KEYS>(a, rq, x, s * C::KEYS) >> (4 * quad) : ~0ull;
+      const uint64_t bits = is_tree(MODE) ? tree_bits<C::KEYS>(a, tree_row(a, rq, un.kvh, row_now()), s * C::KEYS) >> (4 * quad) : ~0ull;
       const LaneIds vl = lane_ids();
       u32x4e seen;
 #pragma unroll

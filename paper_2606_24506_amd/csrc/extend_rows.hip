@@ -138,6 +138,7 @@ __global__ __launch_bounds__(kExtThreads, 2) void extend_rows_kernel(const ExtAr
   // ---- this lane's row, what its wave sees, and what the workgroup sees
   const uint32_t r = un.tile * (32 * RW) + (RW == 4 ? 32 * wave : 0) + col;
   const Row x = row_of<is_tree(MODE)>(a, rq, un.kvh, r);
+  const RowAt at_row{&rq, un.kvh, r};
   const Sight ws = wave_sight<16, is_tree(MODE)>(x);
   const Sight gs = RW == 4 ? group_sight<4>(ws, wave, lane, shared_u) : ws;
   // steps of the unit: whole steps from a multiple of KEYS on
@@ -326,8 +327,8 @@ __global__ __launch_bounds__(kExtThreads, 2) void extend_rows_kernel(const ExtAr
     auto &flat = reinterpret_cast<float(&)[16 * C::KB]>(sc);
     float t;
     typename C::Bits bits = 0;
-    if (is_tree(MODE) && hide) bits = (typename C::Bits)(tree_bits<C::KW>(a, rq, x, b0) >> (4 * half));
-    const bool raw = scores_of<MODE, 16 * C::KB>(a, rq, flat, slope, x, k0, b0 + C::KW <= ws.behind, hide, bits,
+    if (is_tree(MODE) && hide) bits = (typename C::Bits)(tree_bits<C::KW>(a, tree_row(a, rq, un.kvh, at_row.r), b0) >> (4 * half));
+    const bool raw = scores_of<MODE, 16 * C::KB>(a, at_row, flat, slope, x, k0, b0 + C::KW <= ws.behind, hide, bits,
                                                  [](int i) { return 32 * (i / 16) + 8 * (i % 16 / 4) + i % 4; }, &t);
     // the reference moves when some row's maximum passes it by 2^kLazy
     if (__builtin_amdgcn_ballot_w64(t > m + kLazy || (m == -INFINITY && t > m))) {
@@ -442,7 +443,7 @@ __global__ __launch_bounds__(kExtThreads, 2) void extend_rows_kernel(const ExtAr
       }
       __builtin_amdgcn_wave_barrier();
       const uint32_t k0 = base_of(s) + 4 * half, lo = x.lo - k0, n = x.hi - x.lo;
-      const uint64_t bits = is_tree(MODE) ? tree_bits<C::KW>(a, rq, x, base_of(s)) >> (4 * half) : ~0ull;
+      const uint64_t bits = is_tree(MODE) ? tree_bits<C::KW>(a, tree_row(a, rq, un.kvh, at_row.r), base_of(s)) >> (4 * half) : ~0ull;
 #pragma unroll
       for (int d = 0; d < DB; ++d)
 #pragma unroll 1
@@ -551,6 +552,7 @@ __global__ __launch_bounds__(kExtThreads, 2) void extend_few_kernel(const ExtArg
   const uint32_t P = (uint32_t)g.page_tokens;
 
   const Row x = row_of<is_tree(MODE)>(a, rq, un.kvh, un.tile * 16 + col);
+  const RowAt at_row{&rq, un.kvh, un.tile * 16 + col};
   const Sight gs = wave_sight<8, is_tree(MODE)>(x);  // every wave has the same rows
   const uint32_t first = gs.lo / C::KEYS, last = (gs.hi + C::KEYS - 1) / C::KEYS, steps = last - first;
   const uint32_t s0 = first + (uint32_t)((uint64_t)steps * un.split / rq.splits),
@@ -663,8 +665,8 @@ __global__ __launch_bounds__(kExtThreads, 2) void extend_few_kernel(const ExtArg
       auto &flat = reinterpret_cast<float(&)[8]>(sc);
       float t;
       uint32_t bits = 0;
-      if (is_tree(MODE) && mixed(s)) bits = (uint32_t)(tree_bits<C::KW>(a, rq, x, b0) >> (4 * quad));
-      const bool raw = scores_of<MODE, 8>(a, rq, flat, slope, x, k0, b0 + C::KW <= gs.behind, mixed(s), bits,
+      if (is_tree(MODE) && mixed(s)) bits = (uint32_t)(tree_bits<C::KW>(a, tree_row(a, rq, un.kvh, at_row.r), b0) >> (4 * quad));
+      const bool raw = scores_of<MODE, 8>(a, at_row, flat, slope, x, k0, b0 + C::KW <= gs.behind, mixed(s), bits,
                                           [](int i) { return 16 * (i / 4) + i % 4; }, &t);
       // the reference moves when some row's maximum passes it by 2^kLazy
       if (__builtin_amdgcn_ballot_w64(t > m + kLazy || (m == -INFINITY && t > m))) {
@@ -710,7 +712,7 @@ __global__ __launch_bounds__(kExtThreads, 2) void extend_few_kernel(const ExtArg
       store_v();
       __builtin_amdgcn_wave_barrier();
       const uint32_t k0 = base_of(s) + 4 * quad, lo = x.lo - k0, n = x.hi - x.lo;
-      const uint64_t bits = is_tree(MODE) ? tree_bits<C::KW>(a, rq, x, base_of(s)) >> (4 * quad) : ~0ull;
+      const uint64_t bits = is_tree(MODE) ? tree_bits<C::KW>(a, tree_row(a, rq, un.kvh, at_row.r), base_of(s)) >> (4 * quad) : ~0ull;
       u32x4e seen;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
@@ -753,11 +755,9 @@ namespace {
 template <int D, int RW>
 void launch_rows(const ExtArgs &a, hipStream_t stream) {
   const dim3 grid((uint32_t)a.n_units), block(kExtThreads);
-  if (a.tree_mask && (a.slopes || a.softcap > 0.f)) {
-    // (no such tiles of 32 rows by 128 columns: 24 registers would spill, and the host takes tiles of 16)
-    if constexpr (D != 128 || RW != 1)
-      hipLaunchKernelGGL((extend_rows_kernel<D, RW, kModeTreeAny>), grid, block, 0, stream, a);
-  } else if (a.tree_mask)
+  if (a.tree_mask && (a.slopes || a.softcap > 0.f))
+    hipLaunchKernelGGL((extend_rows_kernel<D, RW, kModeTreeAny>), grid, block, 0, stream, a);
+  else if (a.tree_mask)
     hipLaunchKernelGGL((extend_rows_kernel<D, RW, kModeTree>), grid, block, 0, stream, a);
   else if (a.slopes)
     hipLaunchKernelGGL((extend_rows_kernel<D, RW, kModeAny>), grid, block, 0, stream, a);
