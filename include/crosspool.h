@@ -737,6 +737,44 @@ cp_status cp_attn_tree_step(cp_pool *pool, int32_t n, const int32_t *req_ids, co
                             const void *q, void *out, float *lse, const cp_tree *tree, void *hip_stream,
                             const cp_extend_opts *opts);
 
+/* ------------------------------------- what a request keeps of its tokens */
+
+/* Four-byte numbers kept per cached token of a request, in device memory: token
+ * j of KV head h in layer l is element l * layer + h * head + j (strides in
+ * elements; rows of heads and layers must not overlap). */
+typedef struct {
+  void *data;    /* 4-byte aligned */
+  int64_t len;   /* elements of one row: at least the tokens of the request */
+  int64_t head;  /* from one KV head's row to the next's, >= len (one KV head: ignored) */
+  int64_t layer; /* from one layer's rows to the next's, behind its last row (one layer: ignored) */
+} cp_token_rows;
+
+/* The weight that queries give to each cached token, which says what a cache
+ * can do without: for every KV head h and token j of each request, in one layer,
+ *     sum[h][j] = decay * old[h][j] + sum over t, q of e^(s_j - lse[t][q]),
+ * t being the last n_q[i] tokens of the request's context, as far as they see
+ * j, and q the query heads of h; scores s, masks and positions as in
+ * cp_attn_extend, and lse what that call (or a decode) gave for the same
+ * queries and options. Rows whose lse is -inf give nothing; NaN in an lse gives NaN
+ * to what its row sees. Sums are held in 32 bits, added in an order that the
+ * call's arguments decide.
+ *   n_q    host, 0 <= n_q[i] <= context (0: the old sums decay).
+ *   q, lse device, as in cp_attn_extend.
+ *   layer  whose KV is read (and whose rows of old and sum are); the context is
+ *          the committed tokens, and those in flight where the layer's step has
+ *          placed them.
+ *   old    host array of n records of floats, or NULL: no sums so far. Not read
+ *          where decay is 0.
+ *   sum    host array of n records of floats, written for the request's tokens,
+ *          elements behind them left as they are. May be the same as old, entry by
+ *          entry; must not overlap otherwise.
+ *   opts   may be NULL; num_splits: most parts that the rows of a key are cut into.
+ * Uses the pool's workspace like cp_attn_extend. Errors: CP_EINVAL, CP_ESTATE
+ * (host-only pool), CP_ENOMEM (workspace), CP_EHIP. */
+cp_status cp_attn_weights(cp_pool *pool, int32_t n, const int32_t *req_ids, const int32_t *n_q, const void *q,
+                          const float *lse, int32_t layer, float decay, const cp_token_rows *old,
+                          const cp_token_rows *sum, void *hip_stream, const cp_extend_opts *opts);
+
 /* ---------------------------------------------------------------------
  * KV-cache planner (Section 3.1, "KV-cache Planner and Virtualizer",
  * Eq. 1-2): the pool budget for cp_pool_desc.pool_bytes, host only.

@@ -25,7 +25,8 @@ KERNEL_FLAGS = ["-mllvm", "-amdgpu-mfma-vgpr-form"]
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function", f"-I{os.path.join(ROOT, 'include')}", f"-I{CSRC}"]
 
 SOURCES = ["api.cpp", "pool.cpp", "planner.cpp", "rope.cpp", "kernels.hip", "wide_kernels.hip", "rope_kernels.hip",
-           "extend_kernels.hip", "extend_rows.hip", "extend_mla.hip", "tree_kernels.hip"]
+           "extend_kernels.hip", "extend_rows.hip", "extend_mla.hip", "tree_kernels.hip",
+           "weigh_kernels.hip"]
 
 
 def _run(cmd):

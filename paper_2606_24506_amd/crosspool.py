@@ -155,6 +155,15 @@ class cp_tree(C.Structure):
     ]
 
 
+class cp_token_rows(C.Structure):
+    _fields_ = [
+        ("data", C.c_void_p),
+        ("len", C.c_int64),
+        ("head", C.c_int64),
+        ("layer", C.c_int64),
+    ]
+
+
 class cp_plan_model(C.Structure):
     _fields_ = [("kappa_bytes", C.c_double), ("arrival_rate", C.c_double), ("n_samples", C.c_int64),
                 ("prompt_tokens", C.POINTER(C.c_int64)), ("output_tokens", C.POINTER(C.c_int64)),
@@ -218,6 +227,7 @@ def _load() -> C.CDLL:
         "cp_tree_build": ([I32, I32, VP, VP, I32, VP, VP, VP], I32),
         "cp_attn_tree": ([P, I32, VP, VP, VP, VP, VP, C.POINTER(cp_tree), VP, C.POINTER(cp_extend_opts)], I32),
         "cp_attn_tree_step": ([P, I32, VP, VP, VP, VP, VP, VP, C.POINTER(cp_tree), VP, C.POINTER(cp_extend_opts)], I32),
+        "cp_attn_weights": ([P, I32, VP, VP, VP, VP, I32, C.c_float, VP, VP, VP, C.POINTER(cp_extend_opts)], I32),
         "cp_plan_pool": ([C.POINTER(cp_plan_model), I32, C.POINTER(cp_plan_opts), C.POINTER(cp_plan_result)], I32),
     }
     for name, (args, res) in sig.items():
@@ -323,6 +333,7 @@ class _Known:
 
     def __init__(self, device: int):
         self.device, self.models, self.requests = device, {}, {}
+        self.kv, self.shapes = {}, {}  # (layers, KV heads) of models and open requests
 
 
 _POOLS: dict = {}  # by handle
@@ -357,6 +368,7 @@ def cp_model_register(pool: int, kind: int, n_q_heads: int, n_kv_heads: int, hea
     _check(LIB.cp_model_register(pool, C.byref(m), C.byref(mid)))
     if pool in _POOLS:
         _POOLS[pool].models[mid.value] = n_q_heads
+        _POOLS[pool].kv[mid.value] = (max(1, n_layers), n_kv_heads)
     return mid.value
 
 
@@ -371,6 +383,7 @@ def cp_request_open(pool: int, model_id: int, reserve_tokens: int) -> int:
     _check(LIB.cp_request_open(pool, model_id, reserve_tokens, C.byref(rid)))
     if pool in _POOLS:
         _POOLS[pool].requests[rid.value] = _POOLS[pool].models.get(model_id, 0)
+        _POOLS[pool].shapes[rid.value] = _POOLS[pool].kv.get(model_id)
     return rid.value
 
 
@@ -641,6 +654,62 @@ def cp_attn_tree_step(pool: int, req_ids: Sequence[int], n_new: Sequence[int], r
                                  _ptr(lse), C.byref(t), _stream(stream), C.byref(o)))
 
 
+def token_rows(tensors):
+    """The records of what a call's requests keep per token, built once for
+    callers that repeat a call: one tensor per request, [KV heads][tokens] or
+    [layers][KV heads][tokens], float32 (sums) or int32 (token numbers), the last
+    dimension contiguous."""
+    tensors = list(tensors)
+    arr = (cp_token_rows * len(tensors))()
+    for i, t in enumerate(tensors):
+        if t.dim() not in (2, 3) or (t.shape[-1] > 1 and t.stride(-1) != 1):
+            raise ValueError("rows are [KV heads][tokens] or [layers][KV heads][tokens], tokens contiguous")
+        if str(t.dtype) not in ("torch.float32", "torch.int32") or t.dtype != tensors[0].dtype:
+            raise ValueError("rows are float32 or int32")
+        if not t.is_cuda or t.device != tensors[0].device:
+            raise ValueError("rows are on one GPU")
+        arr[i] = cp_token_rows(t.data_ptr(), t.shape[-1], t.stride(-2), t.stride(0) if t.dim() == 3 else 0)
+    arr.keep = tensors
+    arr.heads = [(t.shape[0] if t.dim() == 3 else 1, t.shape[-2]) for t in tensors]
+    arr.floats = not tensors or str(tensors[0].dtype) == "torch.float32"
+    arr.device = tensors[0].device.index if tensors else None
+    return arr
+
+
+def _rows_arg(pool, req_ids, rows, floats: bool):
+    """Records of token_rows (or tensors), one per request of the call and as many
+    rows as its model has KV heads and layers."""
+    if rows is None:
+        return None
+    if not isinstance(rows, C.Array):
+        rows = token_rows(rows)
+    known = _POOLS.get(pool)
+    if len(rows) != len(req_ids):
+        raise ValueError("one record of rows per request")
+    if rows.floats != floats:
+        raise ValueError("sums are float32, token numbers int32")
+    if known is not None:
+        if rows.device not in (None, known.device):
+            raise ValueError("rows are on the GPU of the pool")
+        for r, (layers, heads) in zip(req_ids, rows.heads):
+            if known.shapes.get(int(r), (layers, heads)) != (layers, heads):
+                raise ValueError("rows for every layer and KV head of the request's model")
+    return rows
+
+
+def cp_attn_weights(pool: int, req_ids: Sequence[int], n_q: Sequence[int], q, lse, new, stream=None, *, old=None,
+                    decay: float = 1.0, layer: int = 0, softcap: float = 0.0, window: int = 0, slopes=None, prefix=None,
+                    doc_begin=None, num_splits: int = 0, path: int = CP_PATH_AUTO) -> None:
+    """new (written) and old: token_rows of the requests' sums, or their tensors."""
+    n = len(req_ids)
+    if len(n_q) != n:
+        raise ValueError("req_ids and n_q differ in length")
+    o = _extend_opts(pool, req_ids, n_q, (q, lse), softcap, window, slopes, prefix, doc_begin, num_splits, path, None)
+    new, old = _rows_arg(pool, req_ids, new, True), _rows_arg(pool, req_ids, old, True)
+    _check(LIB.cp_attn_weights(pool, n, _i32_array(req_ids), _i32_array(n_q), _ptr(q), _ptr(lse), layer, decay, old, new,
+                               _stream(stream), C.byref(o)))
+
+
 def cp_plan_pool(models, horizon_s: float, n_obs: int, quantile: float, seed: int, chunk_bytes: int = 2 << 20) -> dict:
     """models: sequence of dicts with kappa_bytes, arrival_rate and equal-length
     prompt_tokens / output_tokens / service_time_s sequences (trace records)."""
@@ -766,6 +835,9 @@ class Pool:
 
     def tree_step(self, req_ids, n_new, rows, q, out, lse, mask, depth, stream=None, **opts) -> None:
         cp_attn_tree_step(self.handle, req_ids, n_new, rows, q, out, lse, mask, depth, stream, **opts)
+
+    def weights(self, req_ids, n_q, q, lse, new, stream=None, **opts) -> None:
+        cp_attn_weights(self.handle, req_ids, n_q, q, lse, new, stream, **opts)
 
     def fork(self, src_ids, dst_ids, n_tok=None, stream=None) -> None:
         cp_request_fork(self.handle, src_ids, dst_ids, n_tok, stream)

@@ -16,6 +16,7 @@
 #include "crosspool.h"
 #include "extend.h"
 #include "tree.h"
+#include "weigh.h"
 #include "kargs.h"
 static_assert(cp::kNoAllocScratchBytes == CP_NOALLOC_WORKSPACE_BYTES, "the header states the fixed workspace size");
 #include "status.hpp"
@@ -38,6 +39,8 @@ hipError_t launch_extend(const ExtArgs &a, int32_t kind, hipStream_t stream);
 hipError_t launch_ext_merge(const ExtMergeArgs &a, uint32_t rows, uint32_t most_splits, hipStream_t stream);
 hipError_t launch_page_copy(const PageCopyArgs &a, hipStream_t stream);
 hipError_t launch_tree(const TreeArgs &a, hipStream_t stream);
+hipError_t launch_weigh(const WeighArgs &a, int32_t kind, hipStream_t stream);
+hipError_t launch_weigh_join(const WeighJoinArgs &a, hipStream_t stream);
 hipError_t launch_stack_push(const StackPushArgs &a, hipStream_t stream);
 hipError_t scratch_device_address(int device, void **out);
 }  // namespace cp
@@ -2297,7 +2300,8 @@ cp_status plan_extend(cp_pool *p, int32_t n, const int32_t *ids, const int32_t *
 }
 
 // The factors of the scores (extend.h), formed in 64 bits.
-void set_score_factors(ExtArgs *a, double scale) {
+template <class Args>
+void set_score_factors(Args *a, double scale) {
   const double log2e = 1.4426950408889634;
   if (!(a->softcap > 0.f)) {
     a->score_mul = (float)(scale * log2e);
@@ -2556,6 +2560,242 @@ cp_status cp_tree_build(int32_t device, int32_t n, const int32_t *n_tok, const i
     }
     const hipError_t e = launch_tree(a, (hipStream_t)hip_stream);
     return e == hipSuccess ? CP_OK : hip_fail(e, "tree launch");
+  });
+}
+
+}  // extern "C"
+
+// ------------------------------------------- weights given to cached tokens
+
+namespace {
+
+// Checks the rows that a call's requests keep of something per token (cp_token_rows):
+// room for len[i] tokens of every KV head and layer, rows that do not overlap.
+cp_status check_token_rows(const char *what, int32_t n, const cp_token_rows *rows, const int64_t *len, int32_t hkv,
+                           int32_t layers, bool written) {
+  std::vector<std::pair<uint64_t, uint64_t>> spans;
+  for (int32_t i = 0; i < n; ++i) {
+    const cp_token_rows &r = rows[i];
+    if (len[i] == 0) continue;
+    if (!r.data || (uintptr_t)r.data % 4) return fail(CP_EINVAL, "%s of entry %d: null or not 4-byte aligned", what, i);
+    if (r.len < len[i])
+      return fail(CP_EINVAL, "%s of entry %d hold %lld tokens, %lld are needed", what, i, (long long)r.len, (long long)len[i]);
+    const int64_t heads = (hkv - 1) * r.head + r.len;
+    if (r.len > (int64_t)1 << 40 || (hkv > 1 && (r.head < r.len || r.head > (int64_t)1 << 40)) ||
+        (layers > 1 && (r.layer < (hkv > 1 ? heads : r.len) || r.layer > (int64_t)1 << 48)))
+      return fail(CP_EINVAL, "%s of entry %d: rows of heads or layers overlap", what, i);
+    const uint64_t at = (uint64_t)(uintptr_t)r.data;
+    spans.emplace_back(at, at + 4 * (uint64_t)((layers > 1 ? (layers - 1) * r.layer : 0) + (hkv > 1 ? (hkv - 1) * r.head : 0) +
+                                               r.len));
+  }
+  if (!written) return CP_OK;
+  std::sort(spans.begin(), spans.end());
+  for (size_t i = 1; i < spans.size(); ++i)
+    if (spans[i].first < spans[i - 1].second) return fail(CP_EINVAL, "%s of two entries overlap", what);
+  return CP_OK;
+}
+
+// Rows read (in) and written (out) by one call are the same, entry by entry, or apart.
+cp_status check_rows_apart(int32_t n, const cp_token_rows *in, const cp_token_rows *out, const int64_t *len, int32_t hkv,
+                           int32_t layers) {
+  struct Span {
+    uint64_t lo, hi;
+    int32_t i;
+    bool out;
+  };
+  std::vector<Span> all;
+  for (int32_t i = 0; i < n; ++i) {
+    if (len[i] == 0) continue;
+    for (int k = 0; k < 2; ++k) {
+      const cp_token_rows &r = k ? out[i] : in[i];
+      const uint64_t at = (uint64_t)(uintptr_t)r.data;
+      all.push_back(Span{at, at + 4 * (uint64_t)((layers > 1 ? (layers - 1) * r.layer : 0) +
+                                                 (hkv > 1 ? (hkv - 1) * r.head : 0) + r.len), i, k == 1});
+    }
+  }
+  std::sort(all.begin(), all.end(), [](const Span &x, const Span &y) { return x.lo < y.lo; });
+  for (size_t k = 0; k < all.size(); ++k)
+    for (size_t j = k + 1; j < all.size() && all[j].lo < all[k].hi; ++j) {
+      const Span &x = all[k], &y = all[j];
+      if (x.out == y.out) continue;
+      const int32_t i = x.i;
+      const bool same = i == y.i && in[i].data == out[i].data && (hkv == 1 || in[i].head == out[i].head) &&
+                        (layers == 1 || in[i].layer == out[i].layer);
+      if (!same) return fail(CP_EINVAL, "rows that the call reads and writes overlap without being the same (entry %d)", i);
+    }
+  return CP_OK;
+}
+
+// The kernel of a request with `rows` rows per KV head (weigh.h).
+int32_t weigh_kind(const Geom &g, int32_t path, int64_t rows) {
+  if (path == CP_PATH_VALU) return kWVec;
+  const bool few = rows >= 1 && rows <= 16;
+  if (g.kind == kGQA && g.head_dim == 64) return few ? kWFew64 : kWRows64;
+  if (g.kind == kGQA && g.head_dim == 128) return few ? kWFew128 : kWRows128;
+  if (g.kind == kMLA && g.latent == 512 && g.rope == 64) return few ? kWFewMla : kWRowsMla;
+  return kWVec;
+}
+
+struct WeighPlan {
+  struct Launch {
+    int32_t kind = 0;
+    std::vector<WeighReq> req;
+    uint32_t units = 0;
+  };
+  std::vector<Launch> launches;
+  std::vector<WeighJoinArgs::Req> joins;
+  uint64_t ws = 0;  // partial sums
+};
+
+}  // namespace
+
+extern "C" {
+
+cp_status cp_attn_weights(cp_pool *p, int32_t n, const int32_t *req_ids, const int32_t *n_q, const void *q,
+                          const float *lse, int32_t layer, float decay, const cp_token_rows *old,
+                          const cp_token_rows *sum, void *hip_stream, const cp_extend_opts *opts) {
+  return guarded([&]() -> cp_status {
+    if (!p) return fail(CP_EINVAL, "null pool");
+    if (p->host_only) return fail(CP_ESTATE, "host-only pool cannot attend");
+    if (p->broken) return broken_pool();
+    cp_status rc = check_ids(p, n, req_ids);
+    if (rc) return rc;
+    if (n < 1) return fail(CP_EINVAL, "weights need at least one request");
+    if (!n_q || !sum) return fail(CP_EINVAL, "null n_q or sum");
+    cp_extend_opts o{};
+    if (opts) o = *opts;
+    if (o.softcap != 0.f && !(o.softcap >= 1e-18f && o.softcap <= 1e18f))
+      return fail(CP_EINVAL, "softcap must be 0 or in [1e-18, 1e18]");
+    if (o.window < 0) return fail(CP_EINVAL, "window must be >= 0");
+    if (o.num_splits < 0) return fail(CP_EINVAL, "num_splits must be >= 0");
+    if (o.path != CP_PATH_AUTO && o.path != CP_PATH_VALU) return fail(CP_EINVAL, "path must be automatic or vector");
+    if (o.rope) return fail(CP_EINVAL, "the call places no rows: opts.rope must be NULL");
+    if (!(decay >= 0.f && decay <= 1.f)) return fail(CP_EINVAL, "decay must be in [0, 1]");
+    const int32_t model = p->st.req(req_ids[0]).model;
+    const Geom &g = p->st.model(model);
+    if (layer < 0 || layer >= g.layers) return fail(CP_EINVAL, "layer %d of a model of %d", layer, g.layers);
+    std::vector<int64_t> ctx((size_t)n);
+    std::vector<uint32_t> tok((size_t)n, 0u);
+    int64_t total = 0;
+    for (int32_t i = 0; i < n; ++i) {
+      const Request &r = p->st.req(req_ids[i]);
+      if (r.model != model) return fail(CP_EINVAL, "the requests of a call belong to one model");
+      // tokens in flight are there in the layers that their steps have passed
+      ctx[(size_t)i] = r.ctx_len + (layer < r.cursor ? r.inflight : 0);
+      if (n_q[i] < 0 || n_q[i] > ctx[(size_t)i])
+        return fail(CP_EINVAL, "request %d has a context of %lld tokens, not %d to ask for", req_ids[i],
+                    (long long)ctx[(size_t)i], n_q[i]);
+      if (o.prefix && o.prefix[i] < 0) return fail(CP_EINVAL, "negative prefix for request %d", req_ids[i]);
+      tok[(size_t)i] = (uint32_t)total;
+      total += n_q[i];
+      if (total > 0x7FFFFFFF || (int64_t)n_q[i] * g.g > 0x7FFFFFFF) return fail(CP_EINVAL, "too many query rows in one call");
+    }
+    if (total > 0 && (!q || !lse)) return fail(CP_EINVAL, "null q or lse");
+    if ((uintptr_t)q % 16 || (uintptr_t)lse % 4 || (uintptr_t)o.slopes % 4 || (uintptr_t)o.doc_begin % 4)
+      return fail(CP_EINVAL, "q must be 16-byte aligned, lse, slopes and doc_begin 4-byte");
+    if (decay == 0.f) old = nullptr;  // what it holds is not read
+    if ((rc = check_token_rows("sum", n, sum, ctx.data(), g.hkv, g.layers, true))) return rc;
+    if (old && (rc = check_token_rows("old", n, old, ctx.data(), g.hkv, g.layers, false))) return rc;
+    if (old && (rc = check_rows_apart(n, old, sum, ctx.data(), g.hkv, g.layers))) return rc;
+
+    // Rows of a tile of keys are cut where the tiles alone leave workgroups idle: about
+    // kWeighUnits a launch, none of fewer than kWeighLeast blocks of rows.
+    constexpr double kWeighUnits = 1024;
+    constexpr int64_t kWeighLeast = 4;
+    auto rows_of = [&](int32_t i) { return (int64_t)n_q[i] * g.g; };
+    double work = 0;  // blocks of rows, of all tiles
+    for (int32_t i = 0; i < n; ++i) {
+      if (ctx[(size_t)i] == 0) continue;
+      const double tiles = (double)((ctx[(size_t)i] + weigh_tile_keys(weigh_kind(g, o.path, rows_of(i))) - 1) /
+                                    weigh_tile_keys(weigh_kind(g, o.path, rows_of(i))));
+      work += tiles * g.hkv * (double)((rows_of(i) + kWeighBlock - 1) / kWeighBlock);
+    }
+    const int64_t per = std::max<int64_t>(kWeighLeast, (int64_t)std::ceil(work / kWeighUnits));
+    WeighPlan pl;
+    for (int32_t kind = 0; kind < kWKinds; ++kind)
+      for (int32_t i = 0; i < n; ++i) {
+        const int64_t c = ctx[(size_t)i];
+        if (c == 0 || weigh_kind(g, o.path, rows_of(i)) != kind) continue;
+        const int64_t keys = weigh_tile_keys(kind), tiles = (c + keys - 1) / keys;
+        const int64_t blocks = (rows_of(i) + kWeighBlock - 1) / kWeighBlock;
+        const bool few = kind >= kWFew64 && kind <= kWFewMla;
+        int64_t splits = few || blocks == 0 ? 1 : o.num_splits ? std::min<int64_t>(o.num_splits, blocks) : (blocks + per - 1) / per;
+        splits = std::min<int64_t>(splits, 64);
+        if (p->ws_limit && pool_ws_bytes(0, (pl.ws + (uint64_t)(splits * c * g.hkv))) > p->ws_limit) splits = 1;
+        const int64_t u = (tiles * g.hkv * splits + 7) / 8 * 8;
+        if (u > kMaxExtUnits) return fail(CP_EINVAL, "too long a context of request %d in one call", req_ids[i]);
+        if (pl.launches.empty() || pl.launches.back().kind != kind || (int)pl.launches.back().req.size() == kWeighMaxReq ||
+            pl.launches.back().units + u > kMaxExtUnits) {
+          pl.launches.emplace_back();
+          pl.launches.back().kind = kind;
+        }
+        WeighPlan::Launch &l = pl.launches.back();
+        const Request &r = p->st.req(req_ids[i]);
+        WeighReq e{};
+        e.old = old ? (const float *)old[i].data + (int64_t)layer * old[i].layer : nullptr;
+        e.sum = (float *)sum[i].data + (int64_t)layer * sum[i].layer;
+        e.old_head = old ? old[i].head : 0;
+        e.sum_head = sum[i].head;
+        e.unit_begin = l.units;
+        e.pte_base = r.plane_base(layer);
+        e.ctx = (uint32_t)c;
+        e.n_q = (uint32_t)n_q[i];
+        e.prefix = o.prefix ? (uint32_t)o.prefix[i] : 0u;
+        e.tok0 = tok[(size_t)i];
+        e.tiles = (uint32_t)tiles;
+        e.splits = (uint32_t)splits;
+        if (splits > 1) {
+          e.ws = pl.ws;
+          pl.ws += (uint64_t)(splits * c * g.hkv);
+          pl.joins.push_back(WeighJoinArgs::Req{e.old, e.sum, e.old_head, e.sum_head, e.ws, 0u, e.ctx, e.splits, 0u});
+        }
+        l.req.push_back(e);
+        l.units += (uint32_t)u;
+      }
+    DeviceGuard guard(p->device);
+    if (pl.ws && (rc = ensure_ws(p, 0, pl.ws))) return rc;
+    const hipStream_t s = (hipStream_t)hip_stream;
+    const int32_t P = p->st.page_tokens();
+    for (const WeighPlan::Launch &l : pl.launches) {
+      WeighArgs a{};
+      a.pool = p->dev_pool;
+      a.pte = p->dev_pte;
+      a.q = (const uint16_t *)q;
+      a.lse = lse;
+      a.ws = p->ws_l;
+      a.slopes = o.slopes;
+      a.doc_begin = o.doc_begin;
+      a.decay = decay;
+      a.softcap = o.softcap;
+      set_score_factors(&a, g.scale);
+      a.window = (uint32_t)o.window;
+      a.page_magic = page_magic(P);
+      a.g_magic = page_magic(g.g);
+      a.n_req = (int32_t)l.req.size();
+      a.n_units = (int32_t)l.units;
+      a.g = geom_k(g, P);
+      std::copy(l.req.begin(), l.req.end(), a.req);
+      const hipError_t e = launch_weigh(a, l.kind, s);
+      if (e != hipSuccess) return hip_fail(e, "weights launch");
+    }
+    for (size_t i = 0; i < pl.joins.size();) {
+      WeighJoinArgs m{};
+      m.ws = p->ws_l;
+      m.decay = decay;
+      m.hkv = g.hkv;
+      for (; i < pl.joins.size() && m.n_req < kWeighMaxReq; ++i) {
+        const int64_t blocks = ((int64_t)pl.joins[i].ctx * g.hkv + kWeighThreads - 1) / kWeighThreads;
+        if (m.n_req > 0 && m.n_blocks + blocks > kMaxExtUnits) break;
+        if (blocks > 1 << 23) return fail(CP_EINVAL, "too long a context in one call");
+        WeighJoinArgs::Req &x = m.req[m.n_req++];
+        x = pl.joins[i];
+        x.block_begin = (uint32_t)m.n_blocks;
+        m.n_blocks += (int32_t)blocks;
+      }
+      const hipError_t e = launch_weigh_join(m, s);
+      if (e != hipSuccess) return hip_fail(e, "weights join launch");
+    }
+    return CP_OK;
   });
 }
 

@@ -177,15 +177,16 @@ CP_DEV uint64_t part_row(const ExtArgs &a, const ExtReq &rq, const Row &x, uint3
 
 // product * sum_k cap_k product^2k: the capped score, in units of log2 e, of a
 // product under cap_edge. less: subtracted in the last step.
-CP_DEV float small_cap(const ExtArgs &a, float s, float less) {
+template <class A>
+CP_DEV float small_cap(const A &a, float s, float less) {
   const float y = s * s;
   float p = a.cap_k[kTanhTerms - 1];
 #pragma unroll
   for (int k = kTanhTerms - 2; k >= 0; --k) p = __builtin_fmaf(p, y, a.cap_k[k]);
   return __builtin_fmaf(s, p, -less);
 }
-template <int N>
-CP_DEV bool all_small(const ExtArgs &a, const float (&s)[N]) {
+template <int N, class A>
+CP_DEV bool all_small(const A &a, const float (&s)[N]) {
   float big = 0.f;
 #pragma unroll
   for (int i = 0; i < N; ++i) big = __builtin_fmaxf(big, __builtin_fabsf(s[i]));
@@ -194,8 +195,8 @@ CP_DEV bool all_small(const ExtArgs &a, const float (&s)[N]) {
 
 // Scores of N keys of one row, from products to units of log2 e. Element i is
 // key k0 + at(i); behind: no key is past the position of any row of the wave, or in its tree.
-template <int MODE, int N, class F>
-CP_DEV void shape_scores(const ExtArgs &a, const RowAt &row, float (&s)[N], float slope, const Row &x, uint32_t k0,
+template <int MODE, int N, class A, class F>
+CP_DEV void shape_scores(const A &a, const RowAt &row, float (&s)[N], float slope, const Row &x, uint32_t k0,
                          bool behind, F at) {
   const uint32_t pos = x.pos;
   if (MODE == kModeCap || a.softcap > 0.f) {
@@ -217,11 +218,12 @@ CP_DEV void shape_scores(const ExtArgs &a, const RowAt &row, float (&s)[N], floa
       for (int i = 0; i < N; ++i) s[i] = __builtin_fmaf(-slope, far - (float)at(i), s[i]);
     } else {
       Row t{};
-      if (is_tree(MODE)) t = tree_row(a, *row.rq, row.kvh, row.r);
+      if constexpr (is_tree(MODE)) t = tree_row(a, *row.rq, row.kvh, row.r);
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         if (is_tree(MODE)) __builtin_amdgcn_sched_barrier(0);  // one load at once, for the registers
-        const uint32_t key = is_tree(MODE) ? tree_pos(a, t, k0 + at(i)) : k0 + at(i);
+        uint32_t key = k0 + at(i);
+        if constexpr (is_tree(MODE)) key = tree_pos(a, t, key);
         s[i] = __builtin_fmaf(-slope, (float)(max(key, pos) - min(key, pos)), s[i]);
       }
     }
@@ -232,8 +234,8 @@ CP_DEV void shape_scores(const ExtArgs &a, const RowAt &row, float (&s)[N], floa
 // maximum in units of log2 e. hide: some row of the wave does not see some of
 // the keys; bits: of a tree, the row's tree_bits from k0 on. Where it can, it leaves the products as they are (returns true), for
 // weight() to scale or cap and take the reference off in one go.
-template <int MODE, int N, class B, class F>
-CP_DEV bool scores_of(const ExtArgs &a, const RowAt &row, float (&s)[N], float slope, const Row &x, uint32_t k0,
+template <int MODE, int N, class A, class B, class F>
+CP_DEV bool scores_of(const A &a, const RowAt &row, float (&s)[N], float slope, const Row &x, uint32_t k0,
                       bool behind, bool hide, B bits, F at, float *top) {
   bool raw = is_plain(MODE) || (MODE == kModeCap && !hide && all_small(a, s));
   if (!raw) shape_scores<MODE, N>(a, row, s, slope, x, k0, behind, at);
@@ -253,8 +255,8 @@ CP_DEV bool scores_of(const ExtArgs &a, const RowAt &row, float (&s)[N], float s
 }
 
 // 2^(score - ref) of N elements in order: each(i, weight of i, weight of i + 1)
-template <int MODE, int N, class E>
-CP_DEV void weights(const ExtArgs &a, const float (&s)[N], bool raw, float ref, E each) {
+template <int MODE, int N, class A, class E>
+CP_DEV void weights(const A &a, const float (&s)[N], bool raw, float ref, E each) {
   if (is_plain(MODE)) {
 #pragma unroll
     for (int i = 0; i < N; i += 2)

@@ -84,3 +84,29 @@ def attend_tree(name, rows, q, sees, depth, softcap=0.0, window=0, slopes=None, 
             out[i, h] = w @ v[idx]
             mag[i, h] = w @ v[idx].abs()
     return out, lse, mag
+
+
+def given(name, rows, q, lse, softcap=0.0, window=0, slopes=None, prefix=0, doc_begin=None):
+    """The weight that the queries of the rows' last tokens give to each row, per KV
+    head, in 64 bits: e^(s - lse) of what they see."""
+    hq, hkv, _, _, _, scale = shape(name)
+    n, t = rows.shape[0], q.shape[0]
+    q, lse = q.double().cpu(), lse.double().cpu()
+    pos = torch.arange(n - t, n)[:, None]
+    j = torch.arange(n)[None]
+    see = j < torch.maximum(pos + 1, torch.tensor(min(prefix, n)))
+    if window:
+        see &= j > pos - window
+    if doc_begin is not None:
+        see &= j >= doc_begin.cpu().long()[:, None]
+    out = torch.zeros(hkv, n, dtype=torch.float64)
+    for h in range(hq):
+        k, _ = heads_of(name, rows, h)
+        s = (q[:, h] @ k.t()) * scale
+        if softcap:
+            s = softcap * torch.tanh(s / softcap)
+        if slopes is not None:
+            s = s - float(slopes[h]) * (pos - j).abs().double()
+        w = torch.where(see & (lse[:, h] != -math.inf)[:, None], torch.exp(s - lse[:, h, None]), 0.0)
+        out[h // (hq // hkv)] += w.sum(0)
+    return out
