@@ -251,6 +251,12 @@ cp_status cp_request_close(cp_pool *pool, int32_t req_id);
  * layer's decode step). */
 cp_status cp_request_len(cp_pool *pool, int32_t req_id, int64_t *ctx_len);
 
+/* The position of the request's next token: its committed tokens, and those
+ * evicted from it (cp_kv_evict; cutting it to no token at all, by cp_request_truncate
+ * or cp_request_keep, starts again at 0). cp_kv_append_rope and the steps with a rotation turn new
+ * keys by it. */
+cp_status cp_request_position(cp_pool *pool, int32_t req_id, int64_t *position);
+
 /* The request's layer cursor (Section 3.2): the layer its next decode step
  * reads, in [0, n_layers), and how many new tokens are in flight (placed at
  * the first layer's step, committed after the last layer's; at most 1 but
@@ -774,6 +780,62 @@ typedef struct {
 cp_status cp_attn_weights(cp_pool *pool, int32_t n, const int32_t *req_ids, const int32_t *n_q, const void *q,
                           const float *lse, int32_t layer, float decay, const cp_token_rows *old,
                           const cp_token_rows *sum, void *hip_stream, const cp_extend_opts *opts);
+
+/* ------------------------------------------------ keeping some of the tokens */
+
+/* Of each request's tokens from first[i] on, keep those given and drop the
+ * rest, in every layer; the kept ones stand behind one another then, from
+ * first[i] on, and the request has first[i] + n_keep[i] tokens. For the path of
+ * a drafted tree that was accepted: its tokens are at the positions that their
+ * depths gave them.
+ *   first   host, n entries in [0, committed tokens].
+ *   n_keep  host, n entries, >= 0.
+ *   keep    host, the requests' lists in call order: token numbers counted from
+ *           first[i], rising, less than the tokens from there on.
+ * Rows move on hip_stream; later calls must be ordered after work already
+ * enqueued on the requests, as those on the same stream are. Pages that
+ * another request shows too are replaced where rows move, and the last one;
+ * pages behind the new end go back to the pool. The reservation stays.
+ * Errors: CP_EINVAL (unknown or duplicate id, a token in flight, lists that do
+ * not rise or fit), CP_ENOSPC (the budget cannot hold the replaced shared pages
+ * beside their replacements, and what giving up shared pages owes the
+ * reservation: nothing changed), CP_ENOMEM (a virtual pool could not map
+ * chunks), CP_EHIP (if a launch failed, the pool is unusable). May wait for the
+ * device as cp_request_fork does. */
+cp_status cp_request_keep(cp_pool *pool, int32_t n, const int32_t *req_ids, const int64_t *first, const int32_t *n_keep,
+                          const int32_t *keep, void *hip_stream);
+
+typedef struct {
+  int32_t first, last; /* tokens at the start and at the end that stay whatever their weight */
+  /* Host array of n records of floats, or NULL: the weights of the tokens that stayed, in
+   * their new places; elements from there to the request's old length become 0. May be
+   * the same as weights, entry by entry; must not overlap otherwise. */
+  const cp_token_rows *new_weights;
+  /* Host array of n records of int32, or NULL: the numbers that the tokens which
+   * stayed had before, rising. */
+  const cp_token_rows *kept;
+} cp_evict_opts;
+
+/* Cut each request to its n_keep[i] tokens of most weight: in every layer and
+ * KV head by itself, the first and last ones of cp_evict_opts and, of those
+ * between, the ones with the largest weights (equal weights: those that come
+ * first; NaN weighs less than anything). What stays stays in its order, and the
+ * request has n_keep[i] tokens then, of other numbers in each layer and KV head;
+ * a request of no more tokens is left as it is. Attention of its queries goes on
+ * over what is left; window, slopes, documents and prefixes count the
+ * tokens held. New tokens' keys are rotated by the position
+ * that they would have had (cp_request_position).
+ *   n_keep   host, n entries, >= 0; first + last at most that where tokens go.
+ *   weights  host array of n records of floats (cp_attn_weights makes such sums).
+ *   opts     may be NULL: none kept anyway.
+ * All requests of a call belong to one model. Pages shared with other requests
+ * are replaced, not written, and freed by their last user; otherwise rows move
+ * in place. Uses the pool's workspace (4 bytes for each kept token of a layer
+ * and KV head where opts->kept is NULL, and for each page); must not overlap
+ * with calls that do on the GPU. Ordering, errors and waits as in
+ * cp_request_keep, plus CP_ESTATE (host-only pool) and CP_ENOMEM (workspace). */
+cp_status cp_kv_evict(cp_pool *pool, int32_t n, const int32_t *req_ids, const int64_t *n_keep,
+                      const cp_token_rows *weights, const cp_evict_opts *opts, void *hip_stream);
 
 /* ---------------------------------------------------------------------
  * KV-cache planner (Section 3.1, "KV-cache Planner and Virtualizer",

@@ -26,7 +26,7 @@ COMMON = ["-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function", f"-I{os
 
 SOURCES = ["api.cpp", "pool.cpp", "planner.cpp", "rope.cpp", "kernels.hip", "wide_kernels.hip", "rope_kernels.hip",
            "extend_kernels.hip", "extend_rows.hip", "extend_mla.hip", "tree_kernels.hip",
-           "weigh_kernels.hip"]
+           "weigh_kernels.hip", "compact_kernels.hip"]
 
 
 def _run(cmd):

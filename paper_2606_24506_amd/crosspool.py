@@ -164,6 +164,15 @@ class cp_token_rows(C.Structure):
     ]
 
 
+class cp_evict_opts(C.Structure):
+    _fields_ = [
+        ("first", C.c_int32),
+        ("last", C.c_int32),
+        ("new_weights", C.c_void_p),
+        ("kept", C.c_void_p),
+    ]
+
+
 class cp_plan_model(C.Structure):
     _fields_ = [("kappa_bytes", C.c_double), ("arrival_rate", C.c_double), ("n_samples", C.c_int64),
                 ("prompt_tokens", C.POINTER(C.c_int64)), ("output_tokens", C.POINTER(C.c_int64)),
@@ -228,6 +237,9 @@ def _load() -> C.CDLL:
         "cp_attn_tree": ([P, I32, VP, VP, VP, VP, VP, C.POINTER(cp_tree), VP, C.POINTER(cp_extend_opts)], I32),
         "cp_attn_tree_step": ([P, I32, VP, VP, VP, VP, VP, VP, C.POINTER(cp_tree), VP, C.POINTER(cp_extend_opts)], I32),
         "cp_attn_weights": ([P, I32, VP, VP, VP, VP, I32, C.c_float, VP, VP, VP, C.POINTER(cp_extend_opts)], I32),
+        "cp_request_position": ([P, I32, C.POINTER(I64)], I32),
+        "cp_request_keep": ([P, I32, VP, VP, VP, VP, VP], I32),
+        "cp_kv_evict": ([P, I32, VP, VP, VP, C.POINTER(cp_evict_opts), VP], I32),
         "cp_plan_pool": ([C.POINTER(cp_plan_model), I32, C.POINTER(cp_plan_opts), C.POINTER(cp_plan_result)], I32),
     }
     for name, (args, res) in sig.items():
@@ -710,6 +722,36 @@ def cp_attn_weights(pool: int, req_ids: Sequence[int], n_q: Sequence[int], q, ls
                                _stream(stream), C.byref(o)))
 
 
+def cp_request_position(pool: int, req_id: int) -> int:
+    n = C.c_int64()
+    _check(LIB.cp_request_position(pool, req_id, C.byref(n)))
+    return n.value
+
+
+def cp_request_keep(pool: int, req_ids: Sequence[int], first: Sequence[int], n_keep: Sequence[int], keep: Sequence[int],
+                    stream=None) -> None:
+    """keep: the requests' lists one behind the other, n_keep[i] entries each."""
+    n = len(req_ids)
+    if len(first) != n or len(n_keep) != n:
+        raise ValueError("req_ids, first and n_keep differ in length")
+    if len(keep) != sum(n_keep):
+        raise ValueError("keep holds n_keep entries of each request")
+    _check(LIB.cp_request_keep(pool, n, _i32_array(req_ids), _i64_array(first), _i32_array(n_keep), _i32_array(keep),
+                               _stream(stream)))
+
+
+def cp_kv_evict(pool: int, req_ids: Sequence[int], n_keep: Sequence[int], weights, stream=None, *, new=None, kept=None,
+                first: int = 0, last: int = 0) -> None:
+    """weights, new (float32) and kept (int32): token_rows, or their tensors."""
+    n = len(req_ids)
+    if len(n_keep) != n:
+        raise ValueError("req_ids and n_keep differ in length")
+    weights, new = _rows_arg(pool, req_ids, weights, True), _rows_arg(pool, req_ids, new, True)
+    kept = _rows_arg(pool, req_ids, kept, False)
+    o = cp_evict_opts(first, last, None if new is None else C.addressof(new), None if kept is None else C.addressof(kept))
+    _check(LIB.cp_kv_evict(pool, n, _i32_array(req_ids), _i64_array(n_keep), weights, C.byref(o), _stream(stream)))
+
+
 def cp_plan_pool(models, horizon_s: float, n_obs: int, quantile: float, seed: int, chunk_bytes: int = 2 << 20) -> dict:
     """models: sequence of dicts with kappa_bytes, arrival_rate and equal-length
     prompt_tokens / output_tokens / service_time_s sequences (trace records)."""
@@ -838,6 +880,15 @@ class Pool:
 
     def weights(self, req_ids, n_q, q, lse, new, stream=None, **opts) -> None:
         cp_attn_weights(self.handle, req_ids, n_q, q, lse, new, stream, **opts)
+
+    def keep(self, req_ids, first, n_keep, keep, stream=None) -> None:
+        cp_request_keep(self.handle, req_ids, first, n_keep, keep, stream)
+
+    def evict(self, req_ids, n_keep, weights, stream=None, **opts) -> None:
+        cp_kv_evict(self.handle, req_ids, n_keep, weights, stream, **opts)
+
+    def position(self, req_id: int) -> int:
+        return cp_request_position(self.handle, req_id)
 
     def fork(self, src_ids, dst_ids, n_tok=None, stream=None) -> None:
         cp_request_fork(self.handle, src_ids, dst_ids, n_tok, stream)

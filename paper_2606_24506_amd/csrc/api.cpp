@@ -17,6 +17,7 @@
 #include "extend.h"
 #include "tree.h"
 #include "weigh.h"
+#include "compact.h"
 #include "kargs.h"
 static_assert(cp::kNoAllocScratchBytes == CP_NOALLOC_WORKSPACE_BYTES, "the header states the fixed workspace size");
 #include "status.hpp"
@@ -41,6 +42,8 @@ hipError_t launch_page_copy(const PageCopyArgs &a, hipStream_t stream);
 hipError_t launch_tree(const TreeArgs &a, hipStream_t stream);
 hipError_t launch_weigh(const WeighArgs &a, int32_t kind, hipStream_t stream);
 hipError_t launch_weigh_join(const WeighJoinArgs &a, hipStream_t stream);
+hipError_t launch_evict_select(const EvictArgs &a, hipStream_t stream);
+hipError_t launch_moves(const MoveArgs &a, int how, hipStream_t stream);
 hipError_t launch_stack_push(const StackPushArgs &a, hipStream_t stream);
 hipError_t scratch_device_address(int device, void **out);
 }  // namespace cp
@@ -724,6 +727,13 @@ cp_status cp_request_len(cp_pool *p, int32_t req_id, int64_t *ctx_len) {
   return CP_OK;
 }
 
+cp_status cp_request_position(cp_pool *p, int32_t req_id, int64_t *position) {
+  if (!p || !position) return fail(CP_EINVAL, "null argument");
+  if (!p->st.valid_open(req_id)) return fail(CP_EINVAL, "request %d is not open", req_id);
+  *position = p->st.req(req_id).ctx_len + p->st.req(req_id).dropped;
+  return CP_OK;
+}
+
 cp_status cp_request_cursor(cp_pool *p, int32_t req_id, int32_t *layer, int32_t *in_flight) {
   if (!p || !layer || !in_flight) return fail(CP_EINVAL, "null argument");
   if (!p->st.valid_open(req_id)) return fail(CP_EINVAL, "request %d is not open", req_id);
@@ -800,7 +810,7 @@ struct AppItem {
   uint64_t src_off;         // element offset of the first row in `rows`
   uint64_t ent = 0;         // new pages whose entries the launch carries:
   uint32_t n_ent = 0;       // their first index in the mirror, and how many
-  uint32_t tok0 = 0;        // the first row's place among the call's tokens
+  uint32_t dropped = 0;     // tokens evicted from the request
 };
 
 // Append launches for rows already accounted for in the host tables, in
@@ -835,7 +845,7 @@ cp_status launch_appends(cp_pool *p, const std::vector<AppItem> &items, const vo
         q.old_len = it.old_len;
         q.pte_base = it.pte_base;
         q.model = (uint16_t)mi;
-        q.tok0 = it.tok0;
+        q.dropped = it.dropped;
         q.ent = kNoEnt;
         if (it.n_ent) {
           q.ent = (uint16_t)a.n_ent;
@@ -956,7 +966,7 @@ cp_status append_impl(cp_pool *p, int32_t n, const int32_t *req_ids, const int32
     }
     for (int32_t l = 0; l < r.layers && n_new[i] > 0; ++l) {
       items.push_back(AppItem{r.model, (uint32_t)n_new[i], old_len, r.plane_base(l), src,
-                              r.plane_base(l) + (uint64_t)used, (uint32_t)(r.pages_used - used)});
+                              r.plane_base(l) + (uint64_t)used, (uint32_t)(r.pages_used - used), (uint32_t)r.dropped});
       entries += (uint64_t)(r.pages_used - used);
       src += (uint64_t)n_new[i] * row_elems;
     }
@@ -2471,7 +2481,8 @@ cp_status extend_step_impl(cp_pool *p, int32_t n, const int32_t *req_ids, const 
       }
       if (n_new[i] > 0) {
         items.push_back(AppItem{r.model, (uint32_t)n_new[i], (uint32_t)r.ctx_len, r.plane_base(r.cursor), src,
-                                r.plane_base(r.cursor) + (uint64_t)used, (uint32_t)(r.pages_used - used), (uint32_t)(src / row_elems)});
+                                r.plane_base(r.cursor) + (uint64_t)used, (uint32_t)(r.pages_used - used),
+                                (uint32_t)r.dropped});
         entries += (uint64_t)(r.pages_used - used);
         src += (uint64_t)n_new[i] * row_elems;
       }
@@ -2569,59 +2580,46 @@ cp_status cp_tree_build(int32_t device, int32_t n, const int32_t *n_tok, const i
 
 namespace {
 
-// Checks the rows that a call's requests keep of something per token (cp_token_rows):
-// room for len[i] tokens of every KV head and layer, rows that do not overlap.
-cp_status check_token_rows(const char *what, int32_t n, const cp_token_rows *rows, const int64_t *len, int32_t hkv,
-                           int32_t layers, bool written) {
-  std::vector<std::pair<uint64_t, uint64_t>> spans;
+// What a call's requests keep per token (cp_token_rows): the memory of each entry.
+struct RowSpan {
+  uint64_t lo, hi;
+  int32_t kind, entry;  // kind: an argument of the call
+  const cp_token_rows *rows;
+};
+
+// Checks one argument: room for len[i] tokens of every KV head and layer, rows that do not
+// overlap. Appends the entries' spans.
+cp_status check_token_rows(const char *what, int32_t kind, int32_t n, const cp_token_rows *rows, const int64_t *len,
+                           int32_t hkv, int32_t layers, std::vector<RowSpan> *spans) {
   for (int32_t i = 0; i < n; ++i) {
     const cp_token_rows &r = rows[i];
     if (len[i] == 0) continue;
     if (!r.data || (uintptr_t)r.data % 4) return fail(CP_EINVAL, "%s of entry %d: null or not 4-byte aligned", what, i);
-    if (r.len < len[i])
+    if (r.len < len[i] || r.len > (int64_t)1 << 40)
       return fail(CP_EINVAL, "%s of entry %d hold %lld tokens, %lld are needed", what, i, (long long)r.len, (long long)len[i]);
-    const int64_t heads = (hkv - 1) * r.head + r.len;
-    if (r.len > (int64_t)1 << 40 || (hkv > 1 && (r.head < r.len || r.head > (int64_t)1 << 40)) ||
-        (layers > 1 && (r.layer < (hkv > 1 ? heads : r.len) || r.layer > (int64_t)1 << 48)))
-      return fail(CP_EINVAL, "%s of entry %d: rows of heads or layers overlap", what, i);
+    if (hkv > 1 && (r.head < r.len || r.head > (int64_t)1 << 40))
+      return fail(CP_EINVAL, "%s of entry %d: rows of heads overlap", what, i);
+    const int64_t one = (hkv > 1 ? (hkv - 1) * r.head : 0) + r.len;  // a layer's
+    if (layers > 1 && (r.layer < one || r.layer > (int64_t)1 << 48))
+      return fail(CP_EINVAL, "%s of entry %d: rows of layers overlap", what, i);
     const uint64_t at = (uint64_t)(uintptr_t)r.data;
-    spans.emplace_back(at, at + 4 * (uint64_t)((layers > 1 ? (layers - 1) * r.layer : 0) + (hkv > 1 ? (hkv - 1) * r.head : 0) +
-                                               r.len));
+    spans->push_back(RowSpan{at, at + 4 * (uint64_t)((layers > 1 ? (layers - 1) * r.layer : 0) + one), kind, i, &r});
   }
-  if (!written) return CP_OK;
-  std::sort(spans.begin(), spans.end());
-  for (size_t i = 1; i < spans.size(); ++i)
-    if (spans[i].first < spans[i - 1].second) return fail(CP_EINVAL, "%s of two entries overlap", what);
   return CP_OK;
 }
 
-// Rows read (in) and written (out) by one call are the same, entry by entry, or apart.
-cp_status check_rows_apart(int32_t n, const cp_token_rows *in, const cp_token_rows *out, const int64_t *len, int32_t hkv,
-                           int32_t layers) {
-  struct Span {
-    uint64_t lo, hi;
-    int32_t i;
-    bool out;
-  };
-  std::vector<Span> all;
-  for (int32_t i = 0; i < n; ++i) {
-    if (len[i] == 0) continue;
-    for (int k = 0; k < 2; ++k) {
-      const cp_token_rows &r = k ? out[i] : in[i];
-      const uint64_t at = (uint64_t)(uintptr_t)r.data;
-      all.push_back(Span{at, at + 4 * (uint64_t)((layers > 1 ? (layers - 1) * r.layer : 0) +
-                                                 (hkv > 1 ? (hkv - 1) * r.head : 0) + r.len), i, k == 1});
-    }
-  }
-  std::sort(all.begin(), all.end(), [](const Span &x, const Span &y) { return x.lo < y.lo; });
-  for (size_t k = 0; k < all.size(); ++k)
-    for (size_t j = k + 1; j < all.size() && all[j].lo < all[k].hi; ++j) {
-      const Span &x = all[k], &y = all[j];
-      if (x.out == y.out) continue;
-      const int32_t i = x.i;
-      const bool same = i == y.i && in[i].data == out[i].data && (hkv == 1 || in[i].head == out[i].head) &&
-                        (layers == 1 || in[i].layer == out[i].layer);
-      if (!same) return fail(CP_EINVAL, "rows that the call reads and writes overlap without being the same (entry %d)", i);
+// Arguments 0 are read, those of other kinds written. What is written overlaps nothing, but
+// that an entry of argument 1 may be the same as its entry of argument 0.
+cp_status check_rows_apart(std::vector<RowSpan> *spans, int32_t hkv, int32_t layers) {
+  std::sort(spans->begin(), spans->end(), [](const RowSpan &x, const RowSpan &y) { return x.lo < y.lo; });
+  for (size_t k = 0; k < spans->size(); ++k)
+    for (size_t j = k + 1; j < spans->size() && (*spans)[j].lo < (*spans)[k].hi; ++j) {
+      const RowSpan &x = (*spans)[k], &y = (*spans)[j];
+      if (x.kind == 0 && y.kind == 0) continue;
+      const bool same = x.kind + y.kind == 1 && x.entry == y.entry && x.lo == y.lo &&
+                        (hkv == 1 || x.rows->head == y.rows->head) && (layers == 1 || x.rows->layer == y.rows->layer);
+      if (!same)
+        return fail(CP_EINVAL, "rows per token of entries %d and %d overlap without being the same", x.entry, y.entry);
     }
   return CP_OK;
 }
@@ -2694,9 +2692,10 @@ cp_status cp_attn_weights(cp_pool *p, int32_t n, const int32_t *req_ids, const i
     if ((uintptr_t)q % 16 || (uintptr_t)lse % 4 || (uintptr_t)o.slopes % 4 || (uintptr_t)o.doc_begin % 4)
       return fail(CP_EINVAL, "q must be 16-byte aligned, lse, slopes and doc_begin 4-byte");
     if (decay == 0.f) old = nullptr;  // what it holds is not read
-    if ((rc = check_token_rows("sum", n, sum, ctx.data(), g.hkv, g.layers, true))) return rc;
-    if (old && (rc = check_token_rows("old", n, old, ctx.data(), g.hkv, g.layers, false))) return rc;
-    if (old && (rc = check_rows_apart(n, old, sum, ctx.data(), g.hkv, g.layers))) return rc;
+    std::vector<RowSpan> spans;
+    if (old && (rc = check_token_rows("old", 0, n, old, ctx.data(), g.hkv, g.layers, &spans))) return rc;
+    if ((rc = check_token_rows("sum", 1, n, sum, ctx.data(), g.hkv, g.layers, &spans))) return rc;
+    if ((rc = check_rows_apart(&spans, g.hkv, g.layers))) return rc;
 
     // Rows of a tile of keys are cut where the tiles alone leave workgroups idle: about
     // kWeighUnits a launch, none of fewer than kWeighLeast blocks of rows.
@@ -2796,6 +2795,354 @@ cp_status cp_attn_weights(cp_pool *p, int32_t n, const int32_t *req_ids, const i
       if (e != hipSuccess) return hip_fail(e, "weights join launch");
     }
     return CP_OK;
+  });
+}
+
+}  // extern "C"
+
+// ------------------------------------------------ keeping some of the tokens
+
+namespace {
+
+// Requests that are cut to new_len[i] tokens, of which those from from[i] on may be written:
+// the checks of the budget, and room for pages of their own. Nothing has changed but chunks
+// taken, on success.
+cp_status prepare_cut(cp_pool *p, int32_t n, const int32_t *ids, const int64_t *from, const int64_t *new_len) {
+  std::vector<int64_t> more, pages;
+  p->st.cut_cost(n, ids, from, new_len, &more, &pages);
+  if (!p->st.fits_budget(more)) return fail(CP_ENOSPC, "the pool page budget cannot take pages in the place of shared ones");
+  std::vector<int32_t> carved;
+  for (int32_t m = 0; m < p->st.n_models(); ++m) {
+    const int64_t slots = p->st.virt() && more[(size_t)m] ? p->st.reserved(m) + more[(size_t)m] - p->st.allocated(m)
+                                                          : pages[(size_t)m];
+    if (!p->st.ensure_slots(m, slots, &carved)) {
+      p->st.release_empty(carved);
+      return fail(CP_ENOMEM, "could not map physical memory for %lld pages of model %d", (long long)slots, m);
+    }
+  }
+  return CP_OK;
+}
+
+// The columns of a model's row that one workgroup of the moves takes.
+uint32_t column_blocks(const Geom &g, int cols) { return (uint32_t)((g.row_elems / 8 + cols - 1) / cols); }
+
+struct MoveItem {
+  MoveReq rq;
+  int32_t model;
+};
+
+// Launches moves, in order; lists of cp_request_keep travel in the arguments (how 0), a
+// longer one in parts, one behind the other.
+cp_status run_moves(cp_pool *p, const std::vector<MoveItem> &items, int how, const int32_t *lists, hipStream_t s) {
+  size_t i = 0;
+  uint32_t done = 0;  // of item i
+  while (i < items.size()) {
+    MoveArgs a{};
+    a.pool = p->dev_pool;
+    a.pte = p->dev_pte;
+    int32_t nm = 0, model_map[16];
+    for (int k = 0; k < 16; ++k) model_map[k] = -1;
+    uint32_t ents = 0;
+    int64_t blocks = 0;
+    while (i < items.size() && a.n_req < kMaxMoveReq) {
+      const MoveItem &it = items[i];
+      const Geom &g = p->st.model(it.model);
+      int32_t mi = model_map[it.model];
+      if (mi < 0 && nm == kMaxLaunchModels) break;
+      MoveReq x = it.rq;
+      x.k0 += done;
+      bool part = false;
+      if (how == 0) {
+        if (ents == (uint32_t)kMoveEntMax) break;
+        const uint32_t k = std::min(x.n - x.k0, (uint32_t)kMoveEntMax - ents);
+        part = k < x.n - x.k0;
+        for (uint32_t e = 0; e < k; ++e) a.ent[ents + e] = (uint32_t)lists[it.rq.ent0 + done + e];
+        x.ent0 = ents;
+        x.n = x.k0 + k;
+        ents += k;
+        done = part ? done + k : 0;
+        x.per_layer = column_blocks(g, kKeepCols);
+      } else if (how == 1) {
+        x.per_layer = column_blocks(g, kMoveCols);
+      } else {
+        const uint64_t total = (uint64_t)(x.n - x.k0) * (uint64_t)(g.row_elems / 8), per = kApartThreads * kApartUnroll;
+        x.per_layer = (uint32_t)((total + per - 1) / per);
+      }
+      const int64_t add = (int64_t)x.per_layer * g.layers;
+      if (blocks > 0 && blocks + add > kMaxExtUnits) break;  // (a launch has less than 2^32 threads)
+      if (mi < 0) {
+        mi = model_map[it.model] = nm;
+        a.geom[nm++] = geom_k(g, p->st.page_tokens());
+      }
+      x.model = (uint32_t)mi;
+      x.block_begin = (uint32_t)blocks;
+      blocks += add;
+      a.req[a.n_req++] = x;
+      if (part) break;  // its rest must come behind it
+      ++i;
+    }
+    a.n_blocks = (int32_t)blocks;
+    const hipError_t e = launch_moves(a, how, s);
+    if (e != hipSuccess) return hip_fail(e, "row moves launch");
+  }
+  return CP_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+cp_status cp_request_keep(cp_pool *p, int32_t n, const int32_t *ids, const int64_t *first, const int32_t *n_keep,
+                          const int32_t *keep, void *hip_stream) {
+  return guarded([&]() -> cp_status {
+    if (!p) return fail(CP_EINVAL, "null pool");
+    cp_status rc = check_ids(p, n, ids);
+    if (rc) return rc;
+    if (n > 0 && (!first || !n_keep)) return fail(CP_EINVAL, "null first or n_keep");
+    if (p->broken) return broken_pool();
+    std::vector<int64_t> from((size_t)n), len((size_t)n);
+    bool any = false;
+    int64_t at = 0;
+    for (int32_t i = 0; i < n; ++i) {
+      const Request &r = p->st.req(ids[i]);
+      if (r.cursor != 0 || r.inflight)
+        return fail(CP_EINVAL, "request %d has a token in flight; finish its decode steps first", ids[i]);
+      if (first[i] < 0 || first[i] > r.ctx_len)
+        return fail(CP_EINVAL, "request %d has %lld tokens, no token %lld", ids[i], (long long)r.ctx_len, (long long)first[i]);
+      if (n_keep[i] < 0 || n_keep[i] > r.ctx_len - first[i])
+        return fail(CP_EINVAL, "%d tokens of request %d, which has %lld from %lld on", n_keep[i], ids[i],
+                    (long long)(r.ctx_len - first[i]), (long long)first[i]);
+      if (n_keep[i] > 0 && !keep) return fail(CP_EINVAL, "null keep");
+      const int32_t *const l = keep + at;
+      int32_t stay = 0;  // those that are where they belong
+      for (int32_t k = 0; k < n_keep[i]; ++k) {
+        if (l[k] < 0 || l[k] >= r.ctx_len - first[i] || (k > 0 && l[k] <= l[k - 1]))
+          return fail(CP_EINVAL, "kept tokens of request %d must rise, and be some of its %lld from %lld on", ids[i],
+                      (long long)(r.ctx_len - first[i]), (long long)first[i]);
+        stay += l[k] == k;
+      }
+      len[(size_t)i] = first[i] + n_keep[i];
+      from[(size_t)i] = first[i] + stay;
+      any = any || len[(size_t)i] < r.ctx_len;
+      at += n_keep[i];
+    }
+    if (!any) return CP_OK;
+    if (!p->host_only && (rc = earlier_error())) return rc;
+    if ((rc = reconcile_pages(p))) return rc;
+    if ((rc = prepare_cut(p, n, ids, from.data(), len.data()))) return rc;
+    // (what the host must allocate comes before any change)
+    const int32_t P = p->st.page_tokens();
+    std::vector<PageItem> items;
+    std::vector<int32_t> models;
+    std::vector<MoveItem> moves;
+    std::vector<std::vector<PoolState::OwnPage>> copies((size_t)n);
+    size_t most = 0;
+    for (int32_t i = 0; i < n; ++i) {
+      const size_t k = (size_t)(p->st.req(ids[i]).layers * ((len[(size_t)i] + P - 1) / P - std::min(len[(size_t)i], from[(size_t)i]) / P));
+      copies[(size_t)i].reserve(k);
+      most += k;
+    }
+    items.reserve(most);
+    models.reserve(most);
+    moves.reserve((size_t)n);
+    for (int32_t i = 0; i < n; ++i) {
+      const Request &r = p->st.req(ids[i]);
+      p->st.cut_own(ids[i], from[(size_t)i], len[(size_t)i], &copies[(size_t)i]);
+      for (const PoolState::OwnPage &c : copies[(size_t)i]) {
+        const int64_t page = (int64_t)(c.slot - r.pte_base) % r.plane;
+        items.push_back(PageItem{c.slot, c.slot, 0u, (uint32_t)std::min<int64_t>(P, r.ctx_len - page * P), c.from, c.to, 0u, 0u});
+        models.push_back(r.model);
+      }
+    }
+    at = 0;
+    for (int32_t i = 0; i < n; ++i) {
+      const Request &r = p->st.req(ids[i]);
+      const uint32_t stay = (uint32_t)(from[(size_t)i] - first[i]);
+      if (from[(size_t)i] < len[(size_t)i] && !p->host_only) {
+        MoveItem m{};
+        m.model = r.model;
+        m.rq.src = p->dev_pte + r.pte_base;
+        m.rq.src_plane = m.rq.dst_plane = (uint32_t)r.plane;
+        m.rq.dst_base = r.pte_base;
+        m.rq.first = (uint32_t)first[i];
+        m.rq.k0 = stay;
+        m.rq.n = (uint32_t)n_keep[i];
+        m.rq.rows = (uint32_t)(r.ctx_len - first[i]);
+        m.rq.ent0 = (uint32_t)(at + stay);
+        moves.push_back(m);
+      }
+      at += n_keep[i];
+    }
+    for (int32_t i = 0; i < n; ++i) p->st.cut_give_up(p->st.req(ids[i]).model, copies[(size_t)i]);
+    for (int32_t i = 0; i < n; ++i) p->st.truncate(ids[i], len[(size_t)i]);
+    if (p->host_only) return CP_OK;
+    DeviceGuard g(p->device);
+    rc = launch_page_items(p, items, models, (hipStream_t)hip_stream);
+    if (rc == CP_OK) rc = run_moves(p, moves, 0, keep, (hipStream_t)hip_stream);
+    if (rc) p->broken = true;
+    return rc;
+  });
+}
+
+cp_status cp_kv_evict(cp_pool *p, int32_t n, const int32_t *ids, const int64_t *n_keep, const cp_token_rows *weights,
+                      const cp_evict_opts *opts, void *hip_stream) {
+  return guarded([&]() -> cp_status {
+    if (!p) return fail(CP_EINVAL, "null pool");
+    if (p->host_only) return fail(CP_ESTATE, "host-only pool has no rows to choose from");
+    cp_status rc = check_ids(p, n, ids);
+    if (rc) return rc;
+    if (n > 0 && (!n_keep || !weights)) return fail(CP_EINVAL, "null n_keep or weights");
+    if (p->broken) return broken_pool();
+    if (n == 0) return CP_OK;
+    cp_evict_opts o{};
+    if (opts) o = *opts;
+    if (o.first < 0 || o.last < 0) return fail(CP_EINVAL, "first and last must be >= 0");
+    const int32_t P = p->st.page_tokens(), model = p->st.req(ids[0]).model;
+    const Geom &g = p->st.model(model);
+    std::vector<int64_t> held((size_t)n), len((size_t)n), from((size_t)n);
+    uint64_t lists = 0, tabs = 0;  // 32-bit words
+    for (int32_t i = 0; i < n; ++i) {
+      const Request &r = p->st.req(ids[i]);
+      if (r.model != model) return fail(CP_EINVAL, "the requests of a call belong to one model");
+      if (r.cursor != 0 || r.inflight)
+        return fail(CP_EINVAL, "request %d has a token in flight; finish its decode steps first", ids[i]);
+      held[(size_t)i] = r.ctx_len;
+      len[(size_t)i] = std::min(n_keep[i], r.ctx_len);
+      if (n_keep[i] < 0) return fail(CP_EINVAL, "negative n_keep for request %d", ids[i]);
+      if (n_keep[i] < r.ctx_len && (int64_t)o.first + o.last > n_keep[i])
+        return fail(CP_EINVAL, "request %d: %d first and %d last tokens are more than the %lld to keep", ids[i], o.first, o.last,
+                    (long long)n_keep[i]);
+      if (r.dropped + r.ctx_len > 0xFFFFFFF0ll) return fail(CP_EINVAL, "request %d: positions out of range", ids[i]);
+      from[(size_t)i] = len[(size_t)i] < r.ctx_len ? std::min<int64_t>(o.first, len[(size_t)i]) : r.ctx_len;
+      lists += (uint64_t)(len[(size_t)i] * g.layers * g.hkv);
+      tabs += (uint64_t)(r.pages_used * g.layers);
+    }
+    std::vector<RowSpan> spans;
+    if ((rc = check_token_rows("weights", 0, n, weights, held.data(), g.hkv, g.layers, &spans))) return rc;
+    if (o.new_weights && (rc = check_token_rows("new_weights", 1, n, o.new_weights, held.data(), g.hkv, g.layers, &spans)))
+      return rc;
+    if (o.kept && (rc = check_token_rows("kept", 2, n, o.kept, len.data(), g.hkv, g.layers, &spans))) return rc;
+    if ((rc = check_rows_apart(&spans, g.hkv, g.layers))) return rc;
+    if ((rc = earlier_error())) return rc;
+    if ((rc = reconcile_pages(p))) return rc;
+    DeviceGuard guard(p->device);
+    if ((rc = ensure_ws(p, 0, (o.kept ? 0 : lists) + tabs))) return rc;
+    if ((rc = prepare_cut(p, n, ids, from.data(), len.data()))) return rc;
+    // (what the host must allocate comes before any change)
+    std::vector<std::vector<PoolState::OwnPage>> copies((size_t)n);
+    std::vector<EvictReq> req((size_t)n);
+    std::vector<MoveItem> place, apart;
+    std::vector<uint32_t> ent;
+    size_t most = 0;
+    for (int32_t i = 0; i < n; ++i) {
+      const size_t k = (size_t)(g.layers * std::max<int64_t>(0, (len[(size_t)i] + P - 1) / P - from[(size_t)i] / P));
+      copies[(size_t)i].reserve(k);
+      most += k;
+    }
+    ent.reserve(most);
+    place.reserve((size_t)n);
+    apart.reserve((size_t)n);
+    uint32_t *ws = (uint32_t *)p->ws_l;
+    uint64_t lo = UINT64_MAX, hi = 0;
+    for (int32_t i = 0; i < n; ++i) {
+      const Request &r = p->st.req(ids[i]);
+      const bool cut = len[(size_t)i] < r.ctx_len;
+      EvictReq &e = req[(size_t)i];
+      e.old = (const float *)weights[i].data;
+      e.old_head = weights[i].head;
+      e.old_layer = weights[i].layer;
+      if (o.new_weights) {
+        e.sum = (float *)o.new_weights[i].data;
+        e.sum_head = o.new_weights[i].head;
+        e.sum_layer = o.new_weights[i].layer;
+      }
+      if (o.kept) {
+        e.list = (int32_t *)o.kept[i].data;
+        e.list_head = o.kept[i].head;
+        e.list_layer = o.kept[i].layer;
+      } else {
+        e.list = (int32_t *)ws;
+        e.list_head = len[(size_t)i];
+        e.list_layer = len[(size_t)i] * g.hkv;
+        ws += len[(size_t)i] * g.hkv * g.layers;
+      }
+      e.n = (uint32_t)r.ctx_len;
+      e.keep = (uint32_t)len[(size_t)i];
+      e.first = cut ? (uint32_t)o.first : 0u;
+      e.last = cut ? (uint32_t)o.last : 0u;
+      e.layers = (uint32_t)g.layers;
+      e.hkv = (uint32_t)g.hkv;
+      e.pte_base = r.pte_base;
+      e.plane = (uint32_t)r.plane;
+      e.tab_n = (uint32_t)r.pages_used;
+      e.ent = kNoWs;
+      if (!cut) continue;
+      p->st.cut_own(ids[i], from[(size_t)i], len[(size_t)i], &copies[(size_t)i]);
+      MoveItem m{};
+      m.model = model;
+      m.rq.list = e.list;
+      m.rq.list_head = e.list_head;
+      m.rq.list_layer = e.list_layer;
+      m.rq.src = p->dev_pte + r.pte_base;
+      m.rq.src_plane = m.rq.dst_plane = (uint32_t)r.plane;
+      m.rq.dst_base = r.pte_base;
+      m.rq.k0 = (uint32_t)from[(size_t)i];
+      m.rq.n = e.keep;
+      m.rq.rows = e.n;
+      const int64_t page0 = from[(size_t)i] / P, pages = (len[(size_t)i] + P - 1) / P - page0;
+      if (!copies[(size_t)i].empty()) {
+        e.tab = ws;
+        ws += r.pages_used * g.layers;
+        e.page0 = (uint32_t)page0;
+        e.pages = (uint32_t)pages;
+        m.rq.src = e.tab;
+        m.rq.src_plane = e.tab_n;
+        // rows that stay where they are in a replaced page move too
+        m.rq.k0 = (uint32_t)(page0 * P);
+        lo = std::min<uint64_t>(lo, r.pte_base + (uint64_t)page0);
+        hi = std::max<uint64_t>(hi, r.plane_base(r.layers - 1) + (uint64_t)(page0 + pages));
+      }
+      if (m.rq.k0 >= m.rq.n) continue;
+      ((int64_t)copies[(size_t)i].size() == pages * g.layers ? apart : place).push_back(m);
+    }
+    for (int32_t i = 0; i < n; ++i) p->st.cut_give_up(model, copies[(size_t)i]);
+    for (int32_t i = 0; i < n; ++i) {
+      const int64_t dropped = p->st.req(ids[i]).dropped + held[(size_t)i] - len[(size_t)i];
+      p->st.truncate(ids[i], len[(size_t)i]);
+      p->st.set_dropped(ids[i], dropped);
+    }
+    const hipStream_t s = (hipStream_t)hip_stream;
+    // the choice; new entries travel with it where they fit, and by a copy behind it otherwise
+    const bool carried = most <= (size_t)kEvictEntMax;
+    rc = CP_OK;
+    for (int32_t i = 0; i < n && rc == CP_OK;) {
+      EvictArgs a{};
+      a.pte = p->dev_pte;
+      uint32_t ents = 0;
+      int64_t blocks = 0;
+      for (; i < n && a.n_req < kEvictMaxReq; ++i) {
+        EvictReq &e = req[(size_t)i];
+        if (e.keep == 0 && !e.sum) continue;
+        const int64_t add = (int64_t)e.layers * e.hkv;
+        if (blocks > 0 && blocks + add > kMaxExtUnits / 4) break;
+        if (e.tab && carried) {
+          e.ent = ents;
+          for (uint32_t l = 0; l < e.layers; ++l, ents += e.pages)
+            std::copy_n(p->st.pte_mirror() + e.pte_base + (uint64_t)l * e.plane + e.page0, e.pages, a.ent + ents);
+        }
+        e.block_begin = (uint32_t)blocks;
+        blocks += add;
+        a.req[a.n_req++] = e;
+      }
+      a.n_blocks = (int32_t)blocks;
+      const hipError_t err = launch_evict_select(a, s);
+      if (err != hipSuccess) rc = hip_fail(err, "eviction launch");
+    }
+    if (rc == CP_OK && !carried) rc = push_ptes(p, lo, hi, s);
+    if (rc == CP_OK) rc = run_moves(p, place, 1, nullptr, s);
+    if (rc == CP_OK) rc = run_moves(p, apart, 2, nullptr, s);
+    if (rc) p->broken = true;
+    return rc;
   });
 }
 

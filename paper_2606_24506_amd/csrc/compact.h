@@ -1,0 +1,65 @@
+// Requests that keep some of their tokens (cp_request_keep, cp_kv_evict): launch records
+// shared by the host (api.cpp) and the kernels (compact_kernels.hip).
+#pragma once
+
+#include <stdint.h>
+
+#include "kargs.h"
+
+namespace cp {
+
+constexpr int kMaxMoveReq = 28;    // requests of one launch
+constexpr int kMoveEntMax = 288;   // kept tokens that one launch of cp_request_keep carries
+constexpr int kEvictMaxReq = 14;
+constexpr int kEvictEntMax = 448;  // new page-table entries that one launch of the choice carries
+constexpr int kSelectThreads = 1024;
+constexpr int kKeepThreads = 256, kKeepCols = 16, kKeepUnroll = 4;     // cp_request_keep
+constexpr int kMoveThreads = 1024, kMoveCols = 8, kMoveUnroll = 8;     // evictions in place
+constexpr int kApartThreads = 256, kApartUnroll = 4;                   // ... into pages of their own
+
+// Rows of one request, in every layer: row first + k becomes what row first + list[k] was,
+// k0 <= k < n.
+struct MoveReq {
+  const uint32_t *src;  // page-table entries of the rows read, and from layer to layer
+  const int32_t *list;  // NULL: MoveArgs::ent
+  int64_t list_head, list_layer;
+  uint32_t src_plane;
+  uint32_t dst_base, dst_plane;  // entries of the pages written, in MoveArgs::pte
+  uint32_t first, k0, n, rows;   // rows: tokens of the request before (list entries are less)
+  uint32_t ent0;                 // list == NULL: its entries from k0 on
+  uint32_t block_begin, per_layer;  // workgroups of one layer
+  uint32_t model, pad;
+};
+struct MoveArgs {
+  uint8_t *pool;
+  const uint32_t *pte;
+  int32_t n_req, n_blocks;
+  GeomK geom[kMaxLaunchModels];
+  MoveReq req[kMaxMoveReq];
+  uint32_t ent[kMoveEntMax];
+};
+static_assert(sizeof(MoveReq) == 80, "move record");
+
+// One request of the choice: per layer and KV head the `keep` tokens of `n` that stay.
+struct EvictReq {
+  const float *old;
+  float *sum;     // NULL: the sums stay as they are
+  int32_t *list;  // out, [layer][head][keep] by these strides
+  int64_t old_head, old_layer, sum_head, sum_layer, list_head, list_layer;
+  uint32_t *tab;  // entries as they were, [layer][tab_n], of requests whose pages are replaced (NULL: none)
+  uint32_t n, keep;
+  uint32_t first, last;  // kept anyway
+  uint32_t block_begin, layers, hkv, tab_n;
+  uint32_t pte_base, plane;  // of the request in the page table
+  uint32_t page0, pages;     // entries replaced: pages [page0, page0 + pages) of every layer
+  uint32_t ent, pad;         // ... whose new ones are EvictArgs::ent[ent + layer * pages ...] (kNoWs: written later)
+};
+struct EvictArgs {
+  uint32_t *pte;
+  int32_t n_req, n_blocks;
+  EvictReq req[kEvictMaxReq];
+  uint32_t ent[kEvictEntMax];
+};
+static_assert(sizeof(MoveArgs) <= 3776 && sizeof(EvictArgs) <= 3776, "compaction kernel arguments too large");
+
+}  // namespace cp

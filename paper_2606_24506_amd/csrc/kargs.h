@@ -183,7 +183,7 @@ struct AppReq {
   uint32_t pte_base;
   uint16_t model;
   uint16_t ent;  // index in AppendArgs::ent of its first new page's entry (kNoEnt: in the page table)
-  uint32_t tok0;  // its first row among AppendArgs::depth
+  uint32_t dropped;  // tokens evicted from it: a row's position, for rotated keys, is that much further
 };
 constexpr uint16_t kNoEnt = 0xFFFFu;
 // New page-table entries one append launch carries; appends that open more
@@ -194,7 +194,8 @@ struct AppendArgs {
   uint8_t *pool;
   uint32_t *pte;  // written only where a new page's entry comes with the launch
   const uint16_t *rows;
-  const int32_t *depth;  // rows of drafted trees, keys rotated: their depths (NULL: one behind the other)
+  const int32_t *depth;  // rows of drafted trees, keys rotated: their depths, one for
+                         // each row of `rows` (NULL: the rows stand one behind the other)
   int32_t n_req, n_blocks, n_ent, pad1;
   GeomK geom[kMaxLaunchModels];
   AppReq req[kMaxReqPerLaunch];

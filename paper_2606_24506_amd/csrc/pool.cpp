@@ -521,6 +521,7 @@ void PoolState::fork(int32_t src, int32_t dst, int64_t n_tok) {
   }
   d.pages_used = whole + tail;
   d.ctx_len = n_tok;
+  d.dropped = s.dropped;
   acct_[d.model].reserved -= whole * d.layers;
 }
 
@@ -544,6 +545,41 @@ void PoolState::truncate(int32_t id, int64_t new_len) {
     acct_[r.model].reserved += drop - free_pages(pte_.data() + r.plane_base(l) + keep, drop);
   r.pages_used = keep;
   r.ctx_len = new_len;
+  if (new_len == 0) r.dropped = 0;
+}
+
+void PoolState::cut_cost(int32_t n, const int32_t *ids, const int64_t *from, const int64_t *new_len,
+                         std::vector<int64_t> *reserved, std::vector<int64_t> *pages) const {
+  reserved->assign(models_.size(), 0);
+  pages->assign(models_.size(), 0);
+  for (int32_t i = 0; i < n; ++i) {
+    const Request &r = reqs_[ids[i]];
+    const int64_t keep = ceil_div(new_len[i], P_);
+    for (int32_t l = 0; l < r.layers; ++l) {
+      const uint32_t *pt = pte_.data() + r.plane_base(l);
+      for (int64_t k = std::min(from[i] / P_, keep); k < r.pages_used; ++k) {
+        if (!sharers(pt[k])) continue;
+        (*reserved)[(size_t)r.model] += 1;
+        (*pages)[(size_t)r.model] += k < keep;
+      }
+    }
+  }
+}
+
+void PoolState::cut_own(int32_t id, int64_t from, int64_t new_len, std::vector<OwnPage> *copies) {
+  const Request &r = reqs_[id];
+  const int64_t keep = ceil_div(new_len, P_);
+  for (int32_t l = 0; l < r.layers; ++l)
+    for (int64_t k = from / P_; k < keep; ++k) {
+      const uint32_t slot = r.plane_base(l) + (uint32_t)k, old = pte_[slot];
+      if (!sharers(old)) continue;
+      alloc_pages(r.model, 1, &pte_[slot]);
+      copies->push_back(OwnPage{slot, old, pte_[slot]});
+    }
+}
+
+void PoolState::cut_give_up(int32_t model, const std::vector<OwnPage> &copies) {
+  for (const OwnPage &c : copies) acct_[model].reserved += 1 - free_pages(&c.from, 1);
 }
 
 void PoolState::truncate_cost(int32_t n, const int32_t *ids, const int64_t *new_len, bool exact,

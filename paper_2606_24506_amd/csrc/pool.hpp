@@ -60,6 +60,7 @@ struct Request {
   int64_t reserve_pages = 0;  // all planes
   int64_t plane = 0;          // page-table entries per plane
   int64_t pages_used = 0;     // per plane
+  int64_t dropped = 0;        // tokens evicted: the next token stands at ctx_len + dropped (0 again once truncated to nothing)
   uint32_t pte_base = 0;
   int32_t layers = 1;
   int32_t cursor = 0;
@@ -213,6 +214,18 @@ class PoolState {
   // page that the call's requests share among themselves counts for each).
   void truncate_cost(int32_t n, const int32_t *ids, const int64_t *new_len, bool exact,
                      std::vector<int64_t> *reserved, std::vector<int64_t> *pages) const;
+  // Cutting requests to some of their tokens, whose rows move to the front: pages from
+  // from[i] / P to the new last one are written, and those that had another user when the
+  // call began are replaced (other requests of the call read them too). First, for all of
+  // a call's: pages of their own (after ensure_slots); appends one record for each. Then
+  // the old pages are given up, and each request truncated.
+  // cut_cost: what this adds to each model's `reserved` at most, before anything is given
+  // up, and the pages it allocates.
+  void cut_cost(int32_t n, const int32_t *ids, const int64_t *from, const int64_t *new_len,
+                std::vector<int64_t> *reserved, std::vector<int64_t> *pages) const;
+  void cut_own(int32_t id, int64_t from, int64_t new_len, std::vector<OwnPage> *copies);
+  void cut_give_up(int32_t model, const std::vector<OwnPage> &copies);
+  void set_dropped(int32_t id, int64_t n) { reqs_[id].dropped = n; }
   // Would the budget hold every reservation with these additions (per model)?
   bool fits_budget(const std::vector<int64_t> &extra) const;
   // Users of a page beyond its first.

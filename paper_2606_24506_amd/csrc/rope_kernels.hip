@@ -175,9 +175,11 @@ __global__ __launch_bounds__(kCopyThreads) void kv_append_rope_kernel(const Appe
   };
   const uint32_t pairs = (uint32_t)rope.pairs, rot = 2 * pairs;
   const uint32_t pos0 = rq.old_len + row0;
+  const int64_t first = (int64_t)rq.old_len + rq.dropped;
+  const int32_t *const depth = a.depth ? a.depth + rq.src_off / (uint32_t)g.row_elems + row0 : nullptr;
   for (uint32_t i = threadIdx.x; i < nrows * pairs; i += kCopyThreads) {
     const uint32_t t = i / pairs;
-    const int64_t at = a.depth ? (int64_t)rq.old_len + a.depth[rq.tok0 + row0 + t] : (int64_t)pos0 + t;
+    const int64_t at = first + (depth ? (int64_t)depth[t] : (int64_t)row0 + t);
     turn[i] = rope_turn(rope, at, (int32_t)(i - t * pairs));
   }
   __syncthreads();

@@ -110,3 +110,29 @@ def given(name, rows, q, lse, softcap=0.0, window=0, slopes=None, prefix=0, doc_
         w = torch.where(see & (lse[:, h] != -math.inf)[:, None], torch.exp(s - lse[:, h, None]), 0.0)
         out[h // (hq // hkv)] += w.sum(0)
     return out
+
+
+def heaviest(w, keep, first, last):
+    """Numbers of the tokens of one row of weights that stay, rising."""
+    n = len(w)
+    if keep >= n:
+        return list(range(n))
+    middle = [(x != x, -x if x == x else 0.0, t) for t, x in enumerate(w)][first:n - last]  # NaN behind -inf
+    chosen = sorted(middle)[:keep - first - last]
+    return list(range(first)) + sorted(c[2] for c in chosen) + list(range(n - last, n))
+
+
+def kept_rows(name, rows, kept):
+    """rows [layers][n][row] cut to kept [layers][KV heads][keep]."""
+    _, hkv, dk, dv, row, _ = shape(name)
+    out = torch.zeros(rows.shape[0], len(kept[0][0]), row, dtype=rows.dtype)
+    rows = rows.cpu()
+    for l in range(rows.shape[0]):
+        for h in range(hkv):
+            idx = torch.tensor(kept[l][h], dtype=torch.int64)
+            if GEOMS[name]["kind"] == cpl.CP_KIND_MLA:
+                out[l] = rows[l][idx]
+            else:
+                for part in (h, hkv + h):
+                    out[l][:, part * dk:(part + 1) * dk] = rows[l][idx][:, part * dk:(part + 1) * dk]
+    return out
