@@ -2840,6 +2840,7 @@ cp_status run_moves(cp_pool *p, const std::vector<MoveItem> &items, int how, con
     MoveArgs a{};
     a.pool = p->dev_pool;
     a.pte = p->dev_pte;
+    a.page_magic = page_magic(p->st.page_tokens());
     int32_t nm = 0, model_map[16];
     for (int k = 0; k < 16; ++k) model_map[k] = -1;
     uint32_t ents = 0;
@@ -2865,8 +2866,8 @@ cp_status run_moves(cp_pool *p, const std::vector<MoveItem> &items, int how, con
       } else if (how == 1) {
         x.per_layer = column_blocks(g, kMoveCols);
       } else {
-        const uint64_t total = (uint64_t)(x.n - x.k0) * (uint64_t)(g.row_elems / 8), per = kApartThreads * kApartUnroll;
-        x.per_layer = (uint32_t)((total + per - 1) / per);
+        const uint32_t rows = apart_rows((uint32_t)g.row_elems / 8);
+        x.per_layer = (x.n - x.k0 + rows - 1) / rows;
       }
       const int64_t add = (int64_t)x.per_layer * g.layers;
       if (blocks > 0 && blocks + add > kMaxExtUnits) break;  // (a launch has less than 2^32 threads)

@@ -16,6 +16,11 @@ constexpr int kSelectThreads = 1024;
 constexpr int kKeepThreads = 256, kKeepCols = 16, kKeepUnroll = 4;     // cp_request_keep
 constexpr int kMoveThreads = 1024, kMoveCols = 8, kMoveUnroll = 8;     // evictions in place
 constexpr int kApartThreads = 256, kApartUnroll = 4;                   // ... into pages of their own
+// Rows of a workgroup of those (segs: 16-byte pieces of a row).
+constexpr uint32_t apart_rows(uint32_t segs) {
+  const uint32_t r = (uint32_t)(kApartThreads * kApartUnroll) / segs;
+  return r < 1 ? 1 : r;
+}
 
 // Rows of one request, in every layer: row first + k becomes what row first + list[k] was,
 // k0 <= k < n.
@@ -34,6 +39,7 @@ struct MoveArgs {
   uint8_t *pool;
   const uint32_t *pte;
   int32_t n_req, n_blocks;
+  uint32_t page_magic, pad;
   GeomK geom[kMaxLaunchModels];
   MoveReq req[kMaxMoveReq];
   uint32_t ent[kMoveEntMax];

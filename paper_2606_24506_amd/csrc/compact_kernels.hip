@@ -4,6 +4,7 @@
 
 #include "compact.h"
 #include "decode_mfma.h"
+#include "extend_device.h"
 #include "device_common.h"
 
 namespace cp {
@@ -32,13 +33,15 @@ struct Cut {
 
 }  // namespace
 
-// A workgroup per layer and KV head. The k-th largest of the middle's sums is found by
-// counting: each pass spreads the numbers between the smallest and the largest that are
-// still possible over 2,048 counters (in the order of floats, which spreads sums of any
-// scale) and keeps the counter that holds the k-th; after at most three passes it holds one
-// value. Then every wave takes a piece of the row in order and writes the numbers that
-// stay, in their order. The row is read again in each pass: from L2, as fast as LDS would
-// give it, and of any length. Bound by those passes of one workgroup.
+// A workgroup per layer and KV head, a wave for every piece of the row. The k-th largest of
+// the middle's sums is found by counting: each pass spreads the numbers between the
+// smallest and the largest that are still possible over 2,048 counters (in the order of
+// floats, which spreads sums of any scale) and keeps the counter that holds the k-th; after
+// at most three passes it holds one value. Then every wave writes the numbers of its piece
+// that stay, in their order.
+// R > 0: the row in registers, R numbers a thread (rows of up to 1,024 R); 0: read again in
+// each pass, eight loads in flight. Bound by the passes of one workgroup.
+template <int R>
 __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(const EvictArgs a) {
   __shared__ uint32_t hist[kBins];
   __shared__ uint32_t part[2][kSelWaves];
@@ -48,6 +51,40 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(const Evic
   const uint32_t b = blockIdx.x - rq.block_begin, layer = b / rq.hkv, head = b - layer * rq.hkv;
   const uint32_t tid = threadIdx.x;
   const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const float *const w = rq.old + (int64_t)layer * rq.old_layer + (int64_t)head * rq.old_head;
+  int32_t *const list = rq.list + (int64_t)layer * rq.list_layer + (int64_t)head * rq.list_head;
+  const uint32_t m0 = rq.first, m1 = rq.n - rq.last, m = m1 - m0, need0 = rq.keep - rq.first - rq.last;
+  // this wave's piece of the middle
+  const uint32_t each = ((m + kSelWaves - 1) / kSelWaves + 63) / 64 * 64;
+  const uint32_t s0 = min(m1, m0 + wave * each), s1 = min(m1, s0 + each);
+  uint32_t key[R > 0 ? R : 1];
+  if constexpr (R > 0) {
+    float x[R];
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+      const uint32_t i = s0 + 64 * j + lane;
+      x[j] = i < s1 ? w[i] : 0.f;
+    }
+#pragma unroll
+    for (int j = 0; j < R; ++j) key[j] = order_key(x[j]);
+  }
+  // f(number, its key, is it one?), in order; whole waves
+  auto each_of = [&](auto f) {
+    if constexpr (R > 0) {
+#pragma unroll
+      for (int j = 0; j < R; ++j)
+        if (s0 + 64 * j < s1) f(s0 + 64 * j + lane, key[j], s0 + 64 * j + lane < s1);
+    } else {
+      for (uint32_t i0 = s0; i0 < s1; i0 += 64 * 8) {
+        float x[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = w[min(i0 + 64 * j + lane, s1 - 1)];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (i0 + 64 * j < s1) f(i0 + 64 * j + lane, order_key(x[j]), i0 + 64 * j + lane < s1);
+      }
+    }
+  };
 
   // ---- the entries of pages that are replaced, as they were, and their new ones
   if (head == 0 && rq.tab) {
@@ -58,17 +95,12 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(const Evic
       for (uint32_t i = tid; i < rq.pages; i += kSelectThreads) pte[rq.page0 + i] = a.ent[rq.ent + layer * rq.pages + i];
   }
 
-  const float *const w = rq.old + (int64_t)layer * rq.old_layer + (int64_t)head * rq.old_head;
-  int32_t *const list = rq.list + (int64_t)layer * rq.list_layer + (int64_t)head * rq.list_head;
-  const uint32_t m0 = rq.first, m1 = rq.n - rq.last, need0 = rq.keep - rq.first - rq.last;
-
   // ---- smallest and largest
   uint32_t lo = 0xFFFFFFFFu, hi = 0;
-  for (uint32_t i = m0 + tid; i < m1; i += kSelectThreads) {
-    const uint32_t k = order_key(w[i]);
-    lo = min(lo, k);
-    hi = max(hi, k);
-  }
+  each_of([&](uint32_t, uint32_t k, bool is) {
+    lo = min(lo, is ? k : 0xFFFFFFFFu);
+    hi = max(hi, is ? k : 0u);
+  });
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) {
     lo = min(lo, (uint32_t)__shfl_xor((int)lo, o, 64));
@@ -85,17 +117,15 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(const Evic
     hi = max(hi, part[1][i]);
   }
   Cut cut{hi, need0};  // (nothing to find where none, or all, of the middle stay)
-  if (need0 == m1 - m0) cut = Cut{0, need0};
-  if (need0 > 0 && need0 < m1 - m0) {
+  if (need0 == m) cut = Cut{0, need0};
+  if (need0 > 0 && need0 < m) {
     uint32_t need = need0;
     while (lo < hi) {
       const int bits = 32 - __builtin_clz(hi - lo), s = bits > 11 ? bits - 11 : 0;
       for (uint32_t i = tid; i < kBins; i += kSelectThreads) hist[i] = 0;
       __syncthreads();
-      for (uint32_t i0 = m0; i0 < m1; i0 += kSelectThreads) {
-        const uint32_t i = i0 + tid;
-        const uint32_t k = i < m1 ? order_key(w[i]) : 0u;
-        const bool in = i < m1 && k >= lo && k <= hi;
+      each_of([&](uint32_t, uint32_t k, bool is) {
+        const bool in = is && k >= lo && k <= hi;
         const uint32_t bin = (k - lo) >> s;
         // (many equal numbers: one addition for those of the wave's first)
         const uint64_t some = __builtin_amdgcn_ballot_w64(in);
@@ -105,7 +135,7 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(const Evic
           if (lane == __builtin_ctzll(some)) atomicAdd(&hist[lead], (uint32_t)__builtin_popcountll(same));
           if (in && bin != lead) atomicAdd(&hist[bin], 1u);
         }
-      }
+      });
       __syncthreads();
       // counters from the largest down: a thread has two
       const uint32_t h0 = hist[kBins - 1 - 2 * tid], h1 = hist[kBins - 2 - 2 * tid];
@@ -141,17 +171,12 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(const Evic
     cut = Cut{lo, need};
   }
 
-  // ---- the numbers that stay, in order: pieces of the middle, one for each wave
-  const uint32_t m = m1 - m0, each = ((m + kSelWaves - 1) / kSelWaves + 63) / 64 * 64;
-  const uint32_t s0 = min(m1, m0 + wave * each), s1 = min(m1, s0 + each);
+  // ---- the numbers that stay, in order
   uint32_t above = 0, equal = 0;
-  for (uint32_t i0 = s0; i0 < s1; i0 += 64) {
-    const uint32_t i = i0 + lane;
-    const uint32_t k = i < s1 ? order_key(w[i]) : 0u;
-    above += (uint32_t)__builtin_popcountll(__builtin_amdgcn_ballot_w64(i < s1 && k > cut.key));
-    equal += (uint32_t)__builtin_popcountll(__builtin_amdgcn_ballot_w64(i < s1 && k == cut.key));
-  }
-  if (need0 == 0) above = 0;
+  each_of([&](uint32_t, uint32_t k, bool is) {
+    above += (uint32_t)__builtin_popcountll(__builtin_amdgcn_ballot_w64(is && k > cut.key));
+    equal += (uint32_t)__builtin_popcountll(__builtin_amdgcn_ballot_w64(is && k == cut.key));
+  });
   __syncthreads();
   if (lane == 0) {
     part[0][wave] = above;
@@ -166,16 +191,14 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(const Evic
   at += min(eq, cut.equal);
   const uint64_t below = (1ull << lane) - 1;
   if (need0 > 0)
-    for (uint32_t i0 = s0; i0 < s1; i0 += 64) {
-      const uint32_t i = i0 + lane;
-      const uint32_t k = i < s1 ? order_key(w[i]) : 0u;
-      const uint64_t be = __builtin_amdgcn_ballot_w64(i < s1 && k == cut.key);
-      const bool take = i < s1 && (k > cut.key || (k == cut.key && eq + (uint32_t)__builtin_popcountll(be & below) < cut.equal));
+    each_of([&](uint32_t i, uint32_t k, bool is) {
+      const uint64_t be = __builtin_amdgcn_ballot_w64(is && k == cut.key);
+      const bool take = is && (k > cut.key || (k == cut.key && eq + (uint32_t)__builtin_popcountll(be & below) < cut.equal));
       const uint64_t bt = __builtin_amdgcn_ballot_w64(take);
       if (take) list[at + (uint32_t)__builtin_popcountll(bt & below)] = (int32_t)i;
       at += (uint32_t)__builtin_popcountll(bt);
       eq += (uint32_t)__builtin_popcountll(be);
-    }
+    });
   for (uint32_t i = tid; i < rq.first; i += kSelectThreads) list[i] = (int32_t)i;
   for (uint32_t i = tid; i < rq.last; i += kSelectThreads) list[rq.keep - rq.last + i] = (int32_t)(rq.n - rq.last + i);
 
@@ -187,11 +210,11 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(const Evic
   __syncthreads();
   for (uint32_t c = 0; c < rq.keep; c += U * kSelectThreads) {
     float v[U];
+    int32_t from[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const uint32_t k = c + u * kSelectThreads + tid;
-      v[u] = k < rq.keep ? w[list[k]] : 0.f;
-    }
+    for (int u = 0; u < U; ++u) from[u] = list[min(c + u * kSelectThreads + tid, rq.keep - 1)];
+#pragma unroll
+    for (int u = 0; u < U; ++u) v[u] = w[from[u]];
     __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);
     __syncthreads();
 #pragma unroll
@@ -206,16 +229,26 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(const Evic
 
 // ------------------------------------------------------------------- moves
 
-// A 16-byte column of a row: which KV head's list it goes by.
-CP_DEV uint32_t column_head(const GeomK &g, uint32_t seg) {
-  return g.kind == 0 ? 0u : seg * 8 / (uint32_t)g.d_k % (uint32_t)g.hkv;
+namespace {
+// A 16-byte column of a row: which KV head's list it goes by, and the bytes from its page
+// to it in slot 0 and from slot to slot.
+struct Column {
+  uint32_t head, step;
+  uint64_t at;
+};
+CP_DEV Column column_of(const GeomK &g, uint32_t seg) {
+  if (g.kind == 0) return Column{0u, (uint32_t)g.d_k * 2, 16ull * seg};
+  const uint32_t per = (uint32_t)g.d_k / 8, part = seg / per, hkv = (uint32_t)g.hkv, v = part >= hkv;
+  const uint32_t h = part - v * hkv;
+  return Column{h, (uint32_t)g.d_k * 2, (uint64_t)(2 * h + v) * (uint32_t)g.page_tokens * ((uint32_t)g.d_k * 2) + 16 * (seg - part * per)};
 }
+}  // namespace
 
 // Rows in place: a workgroup owns COLS columns of 16 bytes of one layer and takes the rows
 // that stay in order, THREADS / COLS * UNROLL at once: all are read before any is written,
 // and those of later steps lie behind what this one writes (list entries rise: entry k is at
-// least k). So no workgroup waits for another. Bound by the round trips of a step where
-// there are few workgroups.
+// least k). So no workgroup waits for another. Bound by the round trips of a step (list,
+// page table, row), each asked for by all of a thread's rows at once.
 template <int THREADS, int COLS, int UNROLL>
 __global__ __launch_bounds__(THREADS) void move_kernel(const MoveArgs a) {
   constexpr uint32_t RPI = THREADS / COLS;
@@ -225,64 +258,92 @@ __global__ __launch_bounds__(THREADS) void move_kernel(const MoveArgs a) {
   const uint32_t b = blockIdx.x - rq.block_begin, layer = b / rq.per_layer, P = (uint32_t)g.page_tokens;
   const uint32_t seg = (b - layer * rq.per_layer) * COLS + threadIdx.x % COLS, row = threadIdx.x / COLS;
   const bool mine = seg < (uint32_t)g.row_elems / 8;
-  const int32_t *const list =
-      rq.list ? rq.list + (int64_t)layer * rq.list_layer + (int64_t)column_head(g, mine ? seg : 0u) * rq.list_head : nullptr;
+  const Column c = column_of(g, mine ? seg : 0u);
+  const int32_t *const list = rq.list ? rq.list + (int64_t)layer * rq.list_layer + (int64_t)c.head * rq.list_head
+                                      : reinterpret_cast<const int32_t *>(a.ent) + rq.ent0 - rq.k0;
   const uint32_t *const src = rq.src + (uint64_t)layer * rq.src_plane, *const dst = a.pte + rq.dst_base + layer * rq.dst_plane;
 #pragma unroll 1
   for (uint32_t base = rq.k0; base < rq.n; base += RPI * UNROLL) {
+    uint32_t from[UNROLL], to[UNROLL], fs[UNROLL], ts[UNROLL];
     u32x4m v[UNROLL];
-    uint64_t to[UNROLL];
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u) {  // (threads without a row repeat the last one)
+      const uint32_t k = min(base + u * RPI + row, rq.n - 1);
+      from[u] = rq.first + min((uint32_t)list[k], rq.rows - 1);
+      to[u] = rq.first + k;
+    }
     bool moves[UNROLL];
 #pragma unroll
     for (int u = 0; u < UNROLL; ++u) {
-      const uint32_t k = base + u * RPI + row;
-      moves[u] = mine && k < rq.n;
-      if (!moves[u]) continue;
-      const uint32_t s = rq.first + min(list ? (uint32_t)list[k] : a.ent[rq.ent0 + (k - rq.k0)], rq.rows - 1);
-      const uint32_t d = rq.first + k, sp = src[s / P], dp = dst[d / P];
-      moves[u] = s != d || sp != dp;
-      to[u] = ((uint64_t)dp << 8) + row_seg_offset(g, d % P, seg);
-      if (moves[u]) v[u] = *reinterpret_cast<const u32x4m *>(a.pool + ((uint64_t)sp << 8) + row_seg_offset(g, s % P, seg));
+      moves[u] = from[u] != to[u];
+      from[u] = src[page_divide(from[u], P, a.page_magic, &fs[u])];
+      to[u] = dst[page_divide(to[u], P, a.page_magic, &ts[u])];
+    }
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u) {
+      moves[u] = (moves[u] || from[u] != to[u]) && mine && base + u * RPI + row < rq.n;
+      v[u] = *reinterpret_cast<const u32x4m *>(a.pool + ((uint64_t)from[u] << 8) + c.at + (uint64_t)fs[u] * c.step);
     }
     __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);
     __syncthreads();
 #pragma unroll
     for (int u = 0; u < UNROLL; ++u)
-      if (moves[u]) *reinterpret_cast<u32x4m *>(a.pool + to[u]) = v[u];
+      if (moves[u]) *reinterpret_cast<u32x4m *>(a.pool + ((uint64_t)to[u] << 8) + c.at + (uint64_t)ts[u] * c.step) = v[u];
   }
 }
 
-// Rows that go to pages which nothing of the call reads: in any order.
+// Rows that go to pages which nothing of the call reads: in any order, 16 KiB or a row a
+// workgroup.
 __global__ __launch_bounds__(kApartThreads) void move_apart_kernel(const MoveArgs a) {
+  constexpr int U = kApartUnroll;
   const int r = sorted_search(a.n_req, blockIdx.x, [&](int i) { return a.req[i].block_begin; });
   const MoveReq &rq = a.req[r];
   const GeomK &g = a.geom[rq.model];
   const uint32_t b = blockIdx.x - rq.block_begin, layer = b / rq.per_layer, P = (uint32_t)g.page_tokens;
-  const uint32_t nseg = (uint32_t)g.row_elems / 8;
-  const uint64_t i0 = (uint64_t)(b - layer * rq.per_layer) * (kApartThreads * kApartUnroll) + threadIdx.x,
-                 total = (uint64_t)(rq.n - rq.k0) * nseg;
+  const uint32_t nseg = (uint32_t)g.row_elems / 8, R = apart_rows(nseg);
+  const uint32_t d0 = rq.k0 + (b - layer * rq.per_layer) * R, total = min(R, rq.n - d0) * nseg;
+  const int32_t *const lists = rq.list + (int64_t)layer * rq.list_layer;
   const uint32_t *const src = rq.src + (uint64_t)layer * rq.src_plane, *const dst = a.pte + rq.dst_base + layer * rq.dst_plane;
-  u32x4m v[kApartUnroll];
-  uint64_t to[kApartUnroll];
+  for (uint32_t i0 = threadIdx.x; i0 < total; i0 += U * kApartThreads) {
+    uint32_t from[U], to[U], ts[U];
+    uint64_t at[U];
+    u32x4m v[U];
 #pragma unroll
-  for (int u = 0; u < kApartUnroll; ++u) {
-    const uint64_t i = i0 + u * kApartThreads;
-    if (i >= total) continue;
-    const uint32_t row = (uint32_t)(i / nseg), seg = (uint32_t)(i - (uint64_t)row * nseg), d = rq.k0 + row;
-    const int32_t *const list = rq.list + (int64_t)layer * rq.list_layer + (int64_t)column_head(g, seg) * rq.list_head;
-    const uint32_t s = min((uint32_t)list[d], rq.rows - 1);
-    to[u] = ((uint64_t)dst[d / P] << 8) + row_seg_offset(g, d % P, seg);
-    v[u] = __builtin_nontemporal_load(
-        reinterpret_cast<const u32x4m *>(a.pool + ((uint64_t)src[s / P] << 8) + row_seg_offset(g, s % P, seg)));
+    for (int u = 0; u < U; ++u) {  // (threads without a piece repeat the last one)
+      const uint32_t i = min(i0 + u * kApartThreads, total - 1), row = i / nseg, d = d0 + row;
+      const Column c = column_of(g, i - row * nseg);
+      at[u] = c.at;
+      from[u] = min((uint32_t)lists[(int64_t)c.head * rq.list_head + d], rq.rows - 1);
+      to[u] = dst[page_divide(d, P, a.page_magic, &ts[u])];
+    }
+    const uint32_t step = (uint32_t)g.d_k * 2;
+    uint32_t fs[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) from[u] = src[page_divide(from[u], P, a.page_magic, &fs[u])];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      v[u] = __builtin_nontemporal_load(
+          reinterpret_cast<const u32x4m *>(a.pool + ((uint64_t)from[u] << 8) + at[u] + (uint64_t)fs[u] * step));
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (i0 + u * kApartThreads < total)
+        *reinterpret_cast<u32x4m *>(a.pool + ((uint64_t)to[u] << 8) + at[u] + (uint64_t)ts[u] * step) = v[u];
   }
-#pragma unroll
-  for (int u = 0; u < kApartUnroll; ++u)
-    if (i0 + u * kApartThreads < total) *reinterpret_cast<u32x4m *>(a.pool + to[u]) = v[u];
 }
 
 hipError_t launch_evict_select(const EvictArgs &a, hipStream_t stream) {
   if (a.n_blocks <= 0) return hipSuccess;
-  hipLaunchKernelGGL(evict_select_kernel, dim3((uint32_t)a.n_blocks), dim3(kSelectThreads), 0, stream, a);
+  uint32_t most = 0;
+  for (int i = 0; i < a.n_req; ++i) most = a.req[i].n > most ? a.req[i].n : most;
+  const dim3 grid((uint32_t)a.n_blocks), block(kSelectThreads);
+  if (most <= 4 * kSelectThreads)
+    hipLaunchKernelGGL(evict_select_kernel<4>, grid, block, 0, stream, a);
+  else if (most <= 16 * kSelectThreads)
+    hipLaunchKernelGGL(evict_select_kernel<16>, grid, block, 0, stream, a);
+  else if (most <= 64 * kSelectThreads)
+    hipLaunchKernelGGL(evict_select_kernel<64>, grid, block, 0, stream, a);
+  else
+    hipLaunchKernelGGL(evict_select_kernel<0>, grid, block, 0, stream, a);
   return hipGetLastError();
 }
 

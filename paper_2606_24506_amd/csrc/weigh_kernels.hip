@@ -32,25 +32,43 @@ struct WeighRow {
   Row x;
   float ref, slope;
 };
-CP_DEV WeighRow weigh_row(const WeighArgs &a, const WeighReq &rq, uint32_t kvh, uint32_t r) {
-  const uint32_t g = (uint32_t)a.g.g, rows = rq.n_q * g;
+// What of a row comes from memory: asked for a block ahead, looked at a block later.
+struct RowLoads {
+  float lse, slope;
+  int32_t doc;
+};
+struct RowAddr {
+  uint32_t t;     // query token of the request
+  uint64_t tok;   // ... of the call
+  uint32_t head;  // of all query heads
+};
+CP_DEV RowAddr row_addr(const WeighArgs &a, const WeighReq &rq, uint32_t kvh, uint32_t r) {
   uint32_t j;
-  const uint32_t t = page_divide(min(r, rows - 1), g, a.g_magic, &j);
+  RowAddr x;
+  x.t = page_divide(min(r, rq.n_q * (uint32_t)a.g.g - 1), (uint32_t)a.g.g, a.g_magic, &j);
+  x.tok = (uint64_t)rq.tok0 + x.t;
+  x.head = kvh * (uint32_t)a.g.g + j;
+  return x;
+}
+CP_DEV RowLoads row_loads(const WeighArgs &a, const RowAddr &x) {
+  RowLoads l;
+  l.lse = a.lse[x.tok * (uint32_t)a.g.hq + x.head];
+  l.doc = a.doc_begin ? a.doc_begin[x.tok] : 0;
+  l.slope = a.slopes ? a.slopes[x.head] : 0.f;
+  return l;
+}
+CP_DEV WeighRow weigh_row(const WeighArgs &a, const WeighReq &rq, const RowAddr &at, const RowLoads &l, uint32_t r) {
   WeighRow w;
-  w.x.tok = (uint64_t)rq.tok0 + t;
-  w.x.head = kvh * g + j;
-  w.x.pos = rq.ctx - rq.n_q + t;
+  w.x.tok = at.tok;
+  w.x.head = at.head;
+  w.x.pos = rq.ctx - rq.n_q + at.t;
   w.x.hi = max(w.x.pos + 1, min(rq.prefix, rq.ctx));
   w.x.lo = a.window && w.x.pos >= a.window ? w.x.pos - a.window + 1 : 0u;
-  if (a.doc_begin) {
-    const int32_t d = a.doc_begin[w.x.tok];
-    if (d > 0) w.x.lo = max(w.x.lo, (uint32_t)d);
-  }
-  const float lse = a.lse[w.x.tok * (uint32_t)a.g.hq + w.x.head];
-  w.ref = lse * kLog2e;
-  w.slope = a.slopes ? a.slopes[w.x.head] * kLog2e : 0.f;
+  if (l.doc > 0) w.x.lo = max(w.x.lo, (uint32_t)l.doc);
+  w.ref = l.lse * kLog2e;
+  w.slope = l.slope * kLog2e;
   // rows past the last, and those that saw nothing, give nothing
-  if (r >= rows || w.x.lo >= w.x.hi || lse == -INFINITY) {
+  if (r >= rq.n_q * (uint32_t)a.g.g || w.x.lo >= w.x.hi || l.lse == -INFINITY) {
     w.x.lo = w.x.hi = 0;
     w.ref = 0.f;
   }
@@ -126,7 +144,8 @@ __global__ __launch_bounds__(kWeighThreads) void weigh_few_kernel(const WeighArg
     at[n] = a.pte[rq.pte_base + pg];
   }
   bf16x8 qf[KS];
-  const WeighRow w = weigh_row(a, rq, un.kvh, col);
+  const RowAddr ra = row_addr(a, rq, un.kvh, col);
+  const WeighRow w = weigh_row(a, rq, ra, row_loads(a, ra), col);
   {
     const uint16_t *const qrow = a.q + (w.x.tok * (uint32_t)a.g.hq + w.x.head) * DK + 8 * quad;
 #pragma unroll
@@ -194,8 +213,6 @@ __global__ __launch_bounds__(kWeighThreads, DK == 576 && MODE != kModePlain ? 1 
   using C = WeighCfg<DK>;
   constexpr int KB = C::KB, KS = C::KS, NE = 16 * KB;
   __shared__ __attribute__((aligned(16))) char lds[2 * C::TILE];
-  __shared__ f32x4 meta[2][kWeighBlock];  // of a row: reference, and lo, hi, position as bits
-  __shared__ float slopes[2][kWeighBlock];
   const WeighUnit un = weigh_unit(a);
   if (un.none) return;
   const WeighReq &rq = *un.rq;
@@ -203,7 +220,6 @@ __global__ __launch_bounds__(kWeighThreads, DK == 576 && MODE != kModePlain ? 1 
   const int col = lane & 31, half = lane >> 5;
   const uint32_t P = (uint32_t)a.g.page_tokens, t0 = un.tile * C::KEYS, b0 = t0 + wave * C::KW;
   const Blocks bl = weigh_blocks(a, rq, t0, min(t0 + C::KEYS, rq.ctx), un.split);
-  const uint32_t rows = rq.n_q * (uint32_t)a.g.g;
 
   // ---- K: lane holds key 32 kb + col, dims 16 ks + 8 half .. + 7
   bf16x8 kf[KB][KS];
@@ -221,11 +237,9 @@ __global__ __launch_bounds__(kWeighThreads, DK == 576 && MODE != kModePlain ? 1 
   }
 
   // ---- a block's queries go to LDS directly; rows past the last repeat it
-  auto row_addr = [&](uint32_t r) {
-    uint32_t j;
-    const uint32_t t = page_divide(min(r, rows - 1), (uint32_t)a.g.g, a.g_magic, &j);
-    return (uint64_t)(uintptr_t)a.q +
-           (((uint64_t)rq.tok0 + t) * (uint32_t)a.g.hq + un.kvh * (uint32_t)a.g.g + j) * (2ull * DK);
+  auto query = [&](uint32_t r) {
+    const RowAddr x = row_addr(a, rq, un.kvh, r);
+    return (uint64_t)(uintptr_t)a.q + (x.tok * (uint32_t)a.g.hq + x.head) * (2ull * DK);
   };
   auto issue = [&](uint32_t blk, int buf) {
     const uint32_t to = lds_addr(lds) + buf * C::TILE;
@@ -233,45 +247,36 @@ __global__ __launch_bounds__(kWeighThreads, DK == 576 && MODE != kModePlain ? 1 
 #pragma unroll
     for (int i = 0; i < N; ++i) {  // a wave's instruction: RPI rows
       const int row0 = (wave * N + i) * RPI, row = row0 + lane / CPR;
-      lane_load_lds<false>(row_addr(blk * kWeighBlock + row) + 16 * C::lat_piece(row, lane % CPR), to + row0 * C::LAT);
+      lane_load_lds<false>(query(blk * kWeighBlock + row) + 16 * C::lat_piece(row, lane % CPR), to + row0 * C::LAT);
     }
     if constexpr (C::ROT > 0) {
       const int row = 8 * wave + lane / 8;
-      lane_load_lds<false>(row_addr(blk * kWeighBlock + row) + C::LAT + 16 * C::rot_piece(row, lane % 8),
+      lane_load_lds<false>(query(blk * kWeighBlock + row) + C::LAT + 16 * C::rot_piece(row, lane % 8),
                            to + kWeighBlock * C::LAT + 8 * wave * C::ROT);
     }
   };
-  auto put_meta = [&](const WeighRow &w, int buf) {
-    meta[buf][threadIdx.x] = f32x4{w.ref, __uint_as_float(w.x.lo), __uint_as_float(w.x.hi), __uint_as_float(w.x.pos)};
-    if (MODE == kModeAny) slopes[buf][threadIdx.x] = w.slope;
-  };
-
   float acc[NE];
 #pragma unroll
   for (int i = 0; i < NE; ++i) acc[i] = 0.f;
 
-  WeighRow w{};
+  auto loads = [&](uint32_t blk) { return row_loads(a, row_addr(a, rq, un.kvh, blk * kWeighBlock + col)); };
+  RowLoads next{};
+  if (bl.from < bl.to) next = loads(bl.from);
   // a wait the compiler sees for K: its own would drain blocks in flight
   __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);
-  if (bl.from < bl.to) {
-    if (threadIdx.x < kWeighBlock) put_meta(weigh_row(a, rq, un.kvh, bl.from * kWeighBlock + threadIdx.x), 0);
-    issue(bl.from, 0);
-  }
+  if (bl.from < bl.to) issue(bl.from, 0);
 #pragma unroll 1
   for (uint32_t blk = bl.from; blk < bl.to; ++blk) {
     const int buf = (blk - bl.from) & 1;
-    const bool more = blk + 1 < bl.to;
+    const uint32_t r = blk * kWeighBlock + col;
+    const WeighRow w = weigh_row(a, rq, row_addr(a, rq, un.kvh, r), next, r);
+    const Row &x = w.x;
     wait_vm<0>();
     __syncthreads();  // this block is there for every wave; the one before is done with
-    if (more) {
-      if (threadIdx.x < kWeighBlock) w = weigh_row(a, rq, un.kvh, (blk + 1) * kWeighBlock + threadIdx.x);
+    if (blk + 1 < bl.to) {
+      next = loads(blk + 1);
       issue(blk + 1, buf ^ 1);
     }
-    const f32x4 m = meta[buf][col];
-    Row x{};
-    x.lo = __float_as_uint(m[1]);
-    x.hi = __float_as_uint(m[2]);
-    x.pos = __float_as_uint(m[3]);
     if (__builtin_amdgcn_ballot_w64(x.lo < b0 + C::KW && x.hi > b0)) {
       const char *const qt = lds + buf * C::TILE;
       f32x16 sc[KB];
@@ -292,16 +297,14 @@ __global__ __launch_bounds__(kWeighThreads, DK == 576 && MODE != kModePlain ? 1 
       auto &flat = reinterpret_cast<float(&)[NE]>(sc);
       const bool hide = __builtin_amdgcn_ballot_w64(x.lo > b0 || x.hi < b0 + C::KW) != 0;
       const bool behind = MODE == kModeAny && __builtin_amdgcn_ballot_w64(x.pos + 1 < b0 + C::KW) == 0;
-      const float slope = MODE == kModeAny ? slopes[buf][col] : 0.f;
       float top;
       auto key_of = [](int i) { return 32 * (i / 16) + 8 * (i % 16 / 4) + i % 4; };
-      const bool raw = scores_of<MODE, NE>(a, RowAt{}, flat, slope, x, b0 + 4 * half, behind, hide, 0u, key_of, &top);
-      weights<MODE, NE>(a, flat, raw, nan_row(flat, m[0], x, b0 + 4 * half, key_of), [&](int i, float p0, float p1) {
+      const bool raw = scores_of<MODE, NE>(a, RowAt{}, flat, w.slope, x, b0 + 4 * half, behind, hide, 0u, key_of, &top);
+      weights<MODE, NE>(a, flat, raw, nan_row(flat, w.ref, x, b0 + 4 * half, key_of), [&](int i, float p0, float p1) {
         acc[i] += p0;
         acc[i + 1] += p1;
       });
     }
-    if (more && threadIdx.x < kWeighBlock) put_meta(w, buf ^ 1);
   }
 
   // ---- the lanes' sums of a key: 32 lanes of one half
@@ -344,7 +347,10 @@ __global__ __launch_bounds__(kWeighThreads) void weigh_vec_kernel(const WeighArg
   const uint32_t r1 = min(bl.to * kWeighBlock, rows);
   for (uint32_t r0 = bl.from * kWeighBlock; r0 < r1; r0 += R) {
     __syncthreads();
-    if (threadIdx.x < R) ws[threadIdx.x] = weigh_row(a, rq, un.kvh, r0 + threadIdx.x);
+    if (threadIdx.x < R) {
+      const RowAddr ra = row_addr(a, rq, un.kvh, r0 + threadIdx.x);
+      ws[threadIdx.x] = weigh_row(a, rq, ra, row_loads(a, ra), r0 + threadIdx.x);
+    }
     for (uint32_t i = threadIdx.x; i < R * dk; i += kWeighThreads) {
       uint32_t j;
       const uint32_t row = i / dk, t = page_divide(min(r0 + row, rows - 1), g, a.g_magic, &j);
