@@ -2634,6 +2634,7 @@ int32_t weigh_kind(const Geom &g, int32_t path, int64_t rows) {
   return kWVec;
 }
 
+constexpr int64_t kWeighMaxParts = 64;
 struct WeighPlan {
   struct Launch {
     int32_t kind = 0;
@@ -2697,29 +2698,49 @@ cp_status cp_attn_weights(cp_pool *p, int32_t n, const int32_t *req_ids, const i
     if ((rc = check_token_rows("sum", 1, n, sum, ctx.data(), g.hkv, g.layers, &spans))) return rc;
     if ((rc = check_rows_apart(&spans, g.hkv, g.layers))) return rc;
 
-    // Rows of a tile of keys are cut where the tiles alone leave workgroups idle: about
-    // kWeighUnits a launch, none of fewer than kWeighLeast blocks of rows.
-    constexpr double kWeighUnits = 1024;
-    constexpr int64_t kWeighLeast = 4;
+    // Rows of a tile of keys are cut into parts where the tiles alone leave workgroups idle
+    // or the longest runs alone at the end: of parts of 2^k blocks of rows those with the
+    // shortest estimate, whole turns of the workgroups that run at once and, past two of
+    // them, half a turn more.
     auto rows_of = [&](int32_t i) { return (int64_t)n_q[i] * g.g; };
-    double work = 0;  // blocks of rows, of all tiles
-    for (int32_t i = 0; i < n; ++i) {
-      if (ctx[(size_t)i] == 0) continue;
-      const double tiles = (double)((ctx[(size_t)i] + weigh_tile_keys(weigh_kind(g, o.path, rows_of(i))) - 1) /
-                                    weigh_tile_keys(weigh_kind(g, o.path, rows_of(i))));
-      work += tiles * g.hkv * (double)((rows_of(i) + kWeighBlock - 1) / kWeighBlock);
+    auto blocks_of = [&](int32_t i) { return (rows_of(i) + kWeighBlock - 1) / kWeighBlock; };
+    int64_t per = INT64_MAX;
+    double best = 1e300;
+    for (int64_t k = 2; k <= 1 << 20; k *= 2) {
+      // us of a block, and workgroups of a CU at once, by kernel
+      static constexpr struct { double us; int per_cu; } kCost[kWKinds] = {
+          {20, 4}, {4, 5}, {4, 6}, {4, 3}, {2.6, 3}, {3.7, 3}, {5.0, 1}};
+      constexpr double kUnit = 4.0;  // a unit's start and end
+      double t = 0, most = 0;
+      for (int kind = 0; kind < kWKinds; ++kind) {
+        double units = 0, longest = 0;
+        for (int32_t i = 0; i < n; ++i) {
+          if (ctx[(size_t)i] == 0 || weigh_kind(g, o.path, rows_of(i)) != kind) continue;
+          const int64_t tiles = (ctx[(size_t)i] + weigh_tile_keys(kind) - 1) / weigh_tile_keys(kind);
+          const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(kWeighMaxParts, (blocks_of(i) + k - 1) / k));
+          units += (double)(tiles * g.hkv * parts);
+          longest = std::max(longest, (double)((blocks_of(i) + parts - 1) / parts));
+          most = std::max(most, (double)blocks_of(i));
+        }
+        const double turns = units / ((double)p->num_cus * kCost[kind].per_cu);
+        t += (turns <= 2 ? std::ceil(turns) : turns + 0.5) * (kUnit + longest * kCost[kind].us);
+      }
+      if (t < best) {
+        best = t;
+        per = k;
+      }
+      if ((double)k >= most) break;
     }
-    const int64_t per = std::max<int64_t>(kWeighLeast, (int64_t)std::ceil(work / kWeighUnits));
     WeighPlan pl;
     for (int32_t kind = 0; kind < kWKinds; ++kind)
       for (int32_t i = 0; i < n; ++i) {
         const int64_t c = ctx[(size_t)i];
         if (c == 0 || weigh_kind(g, o.path, rows_of(i)) != kind) continue;
         const int64_t keys = weigh_tile_keys(kind), tiles = (c + keys - 1) / keys;
-        const int64_t blocks = (rows_of(i) + kWeighBlock - 1) / kWeighBlock;
+        const int64_t blocks = blocks_of(i);
         const bool few = kind >= kWFew64 && kind <= kWFewMla;
         int64_t splits = few || blocks == 0 ? 1 : o.num_splits ? std::min<int64_t>(o.num_splits, blocks) : (blocks + per - 1) / per;
-        splits = std::min<int64_t>(splits, 64);
+        splits = std::min<int64_t>(splits, kWeighMaxParts);
         if (p->ws_limit && pool_ws_bytes(0, (pl.ws + (uint64_t)(splits * c * g.hkv))) > p->ws_limit) splits = 1;
         const int64_t u = (tiles * g.hkv * splits + 7) / 8 * 8;
         if (u > kMaxExtUnits) return fail(CP_EINVAL, "too long a context of request %d in one call", req_ids[i]);

@@ -63,17 +63,22 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(const Evic
 #pragma unroll
     for (int j = 0; j < R; ++j) {
       const uint32_t i = s0 + 64 * j + lane;
-      x[j] = i < s1 ? w[i] : 0.f;
+      x[j] = i < s1 ? w[i] : __builtin_nanf("");
     }
 #pragma unroll
     for (int j = 0; j < R; ++j) key[j] = order_key(x[j]);
   }
-  // f(number, its key, is it one?), in order; whole waves
+  // f(the number of the first lane's, keys), in order; whole waves. Lanes behind the last
+  // number of a piece have a key of 0, as NaN has.
   auto each_of = [&](auto f) {
     if constexpr (R > 0) {
+      constexpr int G = R < 8 ? R : 8;
 #pragma unroll
-      for (int j = 0; j < R; ++j)
-        if (s0 + 64 * j < s1) f(s0 + 64 * j + lane, key[j], s0 + 64 * j + lane < s1);
+      for (int j0 = 0; j0 < R; j0 += G)
+        if (s0 + 64 * j0 < s1) {
+#pragma unroll
+          for (int j = j0; j < j0 + G; ++j) f(s0 + 64 * j, key[j]);
+        }
     } else {
       for (uint32_t i0 = s0; i0 < s1; i0 += 64 * 8) {
         float x[8];
@@ -81,7 +86,7 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(const Evic
         for (int j = 0; j < 8; ++j) x[j] = w[min(i0 + 64 * j + lane, s1 - 1)];
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-          if (i0 + 64 * j < s1) f(i0 + 64 * j + lane, order_key(x[j]), i0 + 64 * j + lane < s1);
+          if (i0 + 64 * j < s1) f(i0 + 64 * j, i0 + 64 * j + lane < s1 ? order_key(x[j]) : 0u);
       }
     }
   };
@@ -96,10 +101,10 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(const Evic
   }
 
   // ---- smallest and largest
-  uint32_t lo = 0xFFFFFFFFu, hi = 0;
-  each_of([&](uint32_t, uint32_t k, bool is) {
-    lo = min(lo, is ? k : 0xFFFFFFFFu);
-    hi = max(hi, is ? k : 0u);
+  uint32_t lo = 0xFFFFFFFFu, hi = 0;  // (a smallest of 0, where a lane has no number, costs width and nothing else)
+  each_of([&](uint32_t i0, uint32_t k) {
+    lo = min(lo, i0 + lane < s1 ? k : 0xFFFFFFFFu);
+    hi = max(hi, k);
   });
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) {
@@ -124,18 +129,14 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(const Evic
       const int bits = 32 - __builtin_clz(hi - lo), s = bits > 11 ? bits - 11 : 0;
       for (uint32_t i = tid; i < kBins; i += kSelectThreads) hist[i] = 0;
       __syncthreads();
-      each_of([&](uint32_t, uint32_t k, bool is) {
-        const bool in = is && k >= lo && k <= hi;
-        const uint32_t bin = (k - lo) >> s;
-        // (many equal numbers: one addition for those of the wave's first)
-        const uint64_t some = __builtin_amdgcn_ballot_w64(in);
-        if (some) {
-          const uint32_t lead = (uint32_t)__builtin_amdgcn_readlane((int)bin, __builtin_ctzll(some));
-          const uint64_t same = __builtin_amdgcn_ballot_w64(in && bin == lead);
-          if (lane == __builtin_ctzll(some)) atomicAdd(&hist[lead], (uint32_t)__builtin_popcountll(same));
-          if (in && bin != lead) atomicAdd(&hist[bin], 1u);
-        }
+      // (as many may be the smallest, tokens that nothing looked at: counted by the wave)
+      uint32_t least = 0;
+      each_of([&](uint32_t i0, uint32_t k) {
+        const uint32_t off = k - lo;
+        least += (uint32_t)__builtin_popcountll(__builtin_amdgcn_ballot_w64(off == 0 && (lo > 0 || i0 + lane < s1)));
+        if (off - 1 < hi - lo) atomicAdd(&hist[off >> s], 1u);
       });
+      if (lane == 0 && least) atomicAdd(&hist[0], least);
       __syncthreads();
       // counters from the largest down: a thread has two
       const uint32_t h0 = hist[kBins - 1 - 2 * tid], h1 = hist[kBins - 2 - 2 * tid];
@@ -173,9 +174,9 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(const Evic
 
   // ---- the numbers that stay, in order
   uint32_t above = 0, equal = 0;
-  each_of([&](uint32_t, uint32_t k, bool is) {
-    above += (uint32_t)__builtin_popcountll(__builtin_amdgcn_ballot_w64(is && k > cut.key));
-    equal += (uint32_t)__builtin_popcountll(__builtin_amdgcn_ballot_w64(is && k == cut.key));
+  each_of([&](uint32_t i0, uint32_t k) {
+    above += (uint32_t)__builtin_popcountll(__builtin_amdgcn_ballot_w64(k > cut.key));
+    if (cut.equal) equal += (uint32_t)__builtin_popcountll(__builtin_amdgcn_ballot_w64(k == cut.key && i0 + lane < s1));
   });
   __syncthreads();
   if (lane == 0) {
@@ -189,15 +190,22 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(const Evic
     eq += part[1][i];
   }
   at += min(eq, cut.equal);
-  const uint64_t below = (1ull << lane) - 1;
+  auto below = [](uint64_t mask) {
+    return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0u));
+  };
   if (need0 > 0)
-    each_of([&](uint32_t i, uint32_t k, bool is) {
-      const uint64_t be = __builtin_amdgcn_ballot_w64(is && k == cut.key);
-      const bool take = is && (k > cut.key || (k == cut.key && eq + (uint32_t)__builtin_popcountll(be & below) < cut.equal));
+    each_of([&](uint32_t i0, uint32_t k) {
+      bool take = k > cut.key;
+      if (eq < cut.equal) {  // (the first of those that are equal, whatever wave has them)
+        const bool same = k == cut.key && i0 + lane < s1;
+        const uint64_t be = __builtin_amdgcn_ballot_w64(same);
+        take = take || (same && eq + below(be) < cut.equal);
+        eq += (uint32_t)__builtin_popcountll(be);
+      }
       const uint64_t bt = __builtin_amdgcn_ballot_w64(take);
-      if (take) list[at + (uint32_t)__builtin_popcountll(bt & below)] = (int32_t)i;
+      const uint32_t to = at + below(bt);
+      if (take && to < rq.keep - rq.last) list[to] = (int32_t)(i0 + lane);  // (always, unless the sums change meanwhile)
       at += (uint32_t)__builtin_popcountll(bt);
-      eq += (uint32_t)__builtin_popcountll(be);
     });
   for (uint32_t i = tid; i < rq.first; i += kSelectThreads) list[i] = (int32_t)i;
   for (uint32_t i = tid; i < rq.last; i += kSelectThreads) list[rq.keep - rq.last + i] = (int32_t)(rq.n - rq.last + i);

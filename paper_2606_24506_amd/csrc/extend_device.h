@@ -348,6 +348,11 @@ CP_DEV void lane_load_lds(uint64_t addr, uint32_t lds_base) {
   else
     asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(addr), "s"(lds_base) : "memory", "m0");
 }
+// Four bytes a lane, every lane with an address of its own, to LDS at lds_base + 4 lane.
+CP_DEV void dword_load_lds(uint64_t addr, uint32_t lds_base) {
+  lds_base = __builtin_amdgcn_readfirstlane(lds_base);
+  asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dword %0, off" ::"v"(addr), "s"(lds_base) : "memory", "m0");
+}
 #pragma clang diagnostic pop
 
 CP_DEV float other_half(float x) {

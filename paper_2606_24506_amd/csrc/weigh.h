@@ -13,15 +13,15 @@ namespace cp {
 // query head of one KV head).
 //   kWVec   vector: one thread per key, any geometry.
 //   kWFew*  matrix cores, at most 16 rows: bound by reading K.
-//   kWRows* matrix cores, keys in registers, blocks of 32 rows streamed past them.
+//   kWRows* matrix cores, keys in registers, blocks of rows streamed past them.
 // 64 and 128: GQA / MHA of that head_dim; Mla: latent 512 and rotary part 64.
 enum : int32_t { kWVec = 0, kWFew64, kWFew128, kWFewMla, kWRows64, kWRows128, kWRowsMla, kWKinds };
 
 constexpr int kWeighThreads = 256;
-constexpr int kWeighBlock = 32;  // rows of a block
+constexpr int kWeighBlock = 64;  // rows of a block
 // Keys of a workgroup.
 constexpr int32_t weigh_tile_keys(int32_t kind) {
-  return kind == kWFew64 ? 512 : kind == kWFewMla || kind == kWRowsMla ? 128 : 256;
+  return kind == kWFew64 ? 512 : kind == kWFewMla ? 128 : 256;
 }
 
 struct WeighReq {

@@ -190,137 +190,294 @@ __global__ __launch_bounds__(kWeighThreads) void weigh_few_kernel(const WeighArg
 
 // --------------------------------------------------------------- many rows
 
-// K in registers (32 or 64 keys of a wave, the 32x32x16 products' first operand), queries
-// streamed past them through LDS in blocks of 32 rows, one block ahead. Scores are
-// transposed as in the attention kernels: a lane holds one row's scores, and adds their
-// exponentials to sums of its own, one for every key; the lanes' sums meet at the end.
+// K in registers (the products' first operand), queries and their log-sum-exp streamed past
+// them through LDS, a ring of four steps of 64 rows (MLA 32). Scores are transposed as in the attention kernels: a
+// lane holds one row's scores, and adds their exponentials to sums of its own, one for
+// every key; the lanes' sums meet at the end.
+// head_dim 64 and 128: 64 keys a wave, turns of 32 rows by 32x32x16 products. A score costs
+// a multiply-add, an exponential and an addition, 16 cycles a wave for 64 of them, and its
+// products 16 too (head_dim 128): plain scores are one turn behind their products, so that
+// the vector unit and the matrix cores work at once (the compiler left to itself starts the
+// exponentials when the products are done), and whatever else the vector unit does in a
+// turn counts: rows' places are formed once and moved on block by block, and masks looked
+// at only where some row of the block does not see some key.
+// MLA: 32 keys a wave, 144 registers, turns of 16 rows by 16x16x32 products, whose few
+// scores leave registers to read fragments ahead. LDS bounds it with the matrix cores: a
+// fragment of 1 KiB feeds 32 cycles of products.
 template <int DK>
 struct WeighCfg {
-  static constexpr int KB = DK == 576 ? 1 : 2;   // blocks of 32 keys of a wave
-  static constexpr int KW = 32 * KB, WAVES = kWeighThreads / 64, KEYS = KW * WAVES;
-  static constexpr int KS = DK / 16;
-  static constexpr int LAT = DK == 576 ? 1024 : 2 * DK;  // bytes of a row in LDS (latent part), and behind all of those
-  static constexpr int ROT = DK == 576 ? 128 : 0;        // ... of its rotary part
-  static constexpr int TILE = kWeighBlock * (LAT + ROT);
+  static constexpr bool MLA = DK == 576;
+  static constexpr int KB = MLA ? 2 : 4;           // blocks of 16 keys of a wave
+  static constexpr int RT = 16;                    // rows of a turn, and keys of a block
+  static constexpr int THREADS = MLA ? 512 : 256, WAVES = THREADS / 64;
+  static constexpr int KW = RT * KB, KEYS = KW * WAVES;
+  static constexpr int KD = 32;                    // dims of a product
+  static constexpr int KS = DK / KD;
+  static constexpr int EB = 4;                     // scores of a lane and block
+  static constexpr int LAT = MLA ? 1024 : 2 * DK;  // bytes of a row in LDS (latent part), and behind all of those
+  static constexpr int ROT = MLA ? 128 : 0;        // ... of its rotary part
+  static constexpr int STEP = MLA ? 32 : 64, TURNS = STEP / RT;  // rows between two barriers
+  static constexpr int TILE = STEP * (LAT + ROT) + 256;          // bytes of a step: queries, and 64 log-sum-exps
+  static constexpr int RING = DK == 128 ? 3 : 4;  // (three workgroups a CU)
   // pieces of 16 bytes, swapped by the row so that 16 rows at one piece meet no bank twice
   static CP_DEV int lat_piece(int row, int c) { return LAT == 128 ? c ^ ((row >> 1) & 7) : c ^ (row & 15); }
   static CP_DEV int rot_piece(int row, int c) { return c ^ ((row >> 1) & 7); }
 };
 
-// (capped and sloped scores beside 144 registers of an MLA key: one wave a SIMD, or they spill)
 template <int DK, int MODE>
-__global__ __launch_bounds__(kWeighThreads, DK == 576 && MODE != kModePlain ? 1 : 2) void weigh_rows_kernel(const WeighArgs a) {
+__global__ __launch_bounds__(WeighCfg<DK>::THREADS, DK == 576 ? 2 : 3) void weigh_rows_kernel(const WeighArgs a) {
   using C = WeighCfg<DK>;
-  constexpr int KB = C::KB, KS = C::KS, NE = 16 * KB;
-  __shared__ __attribute__((aligned(16))) char lds[2 * C::TILE];
+  typedef float scores_t __attribute__((ext_vector_type(C::EB)));
+  constexpr int KB = C::KB, KS = C::KS, NE = C::EB * KB, TURNS = C::TURNS, STEP = C::STEP;
+  constexpr bool BEHIND = MODE == kModePlain && !C::MLA;  // exponentials a turn behind
+  __shared__ __attribute__((aligned(16))) char lds[C::RING * C::TILE];
   const WeighUnit un = weigh_unit(a);
   if (un.none) return;
   const WeighReq &rq = *un.rq;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int col = lane & 31, half = lane >> 5;
-  const uint32_t P = (uint32_t)a.g.page_tokens, t0 = un.tile * C::KEYS, b0 = t0 + wave * C::KW;
+  const int col = lane % C::RT, part = lane / C::RT;  // row of a turn; which dims, and keys
+  const uint32_t P = (uint32_t)a.g.page_tokens, g = (uint32_t)a.g.g, hq = (uint32_t)a.g.hq;
+  const uint32_t t0 = un.tile * C::KEYS, b0 = t0 + wave * C::KW;
   const Blocks bl = weigh_blocks(a, rq, t0, min(t0 + C::KEYS, rq.ctx), un.split);
+  // steps of rows (a block's last may lie past the last row)
+  const uint32_t from = bl.from * (kWeighBlock / STEP), to = min(bl.to * (kWeighBlock / STEP), (rq.n_q * g + STEP - 1) / STEP);
 
-  // ---- K: lane holds key 32 kb + col, dims 16 ks + 8 half .. + 7
+  // ---- K: lane holds key RT kb + col, dims KD ks + 8 part .. + 7
   bf16x8 kf[KB][KS];
-  if (bl.from < bl.to) {
-    const uint8_t *const head = a.pool + (DK == 576 ? 0ull : (uint64_t)un.kvh * (4ull * P * DK)) + 16 * half;
+  if (from < to) {
+    const uint8_t *const head = a.pool + (C::MLA ? 0ull : (uint64_t)un.kvh * (4ull * P * DK)) + 16 * part;
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
       uint32_t slot;
-      const uint32_t pg = page_divide(min(b0 + 32 * kb + col, rq.ctx - 1), P, a.page_magic, &slot);
+      const uint32_t pg = page_divide(min(b0 + C::RT * kb + col, rq.ctx - 1), P, a.page_magic, &slot);
       const u32x4e *const k = reinterpret_cast<const u32x4e *>(head + ((uint64_t)a.pte[rq.pte_base + pg] << 8) +
                                                               (uint64_t)slot * (2 * DK));
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) kf[kb][ks] = __builtin_bit_cast(bf16x8, __builtin_nontemporal_load(k + 2 * ks));
+      for (int ks = 0; ks < KS; ++ks)
+        kf[kb][ks] = __builtin_bit_cast(bf16x8, k[ks * (C::KD / 8)]);
     }
   }
 
-  // ---- a block's queries go to LDS directly; rows past the last repeat it
-  auto query = [&](uint32_t r) {
-    const RowAddr x = row_addr(a, rq, un.kvh, r);
-    return (uint64_t)(uintptr_t)a.q + (x.tok * (uint32_t)a.g.hq + x.head) * (2ull * DK);
+  // ---- places of rows. Row r of a step is `off(r)` rows of the call's queries behind the
+  // step's first where steps end with tokens or a token's heads are all of one KV head's;
+  // otherwise, and in the last step, each is looked up (rows past the last repeat it).
+  const uint32_t last_full = rq.n_q * g / STEP;  // steps from here on are not whole
+  const bool even = a.g.hkv == 1 || STEP % g == 0;
+  auto off = [&](uint32_t row) {
+    if (a.g.hkv == 1) return row;
+    uint32_t j;
+    const uint32_t t = page_divide(row, g, a.g_magic, &j);
+    return t * hq + j;
   };
-  auto issue = [&](uint32_t blk, int buf) {
-    const uint32_t to = lds_addr(lds) + buf * C::TILE;
-    constexpr int CPR = C::LAT / 16, RPI = CPR >= 64 ? 1 : 64 / CPR, N = kWeighBlock / RPI / C::WAVES;
+  auto first_row = [&](uint32_t st) {  // of the call's queries
+    return a.g.hkv == 1 ? (uint64_t)rq.tok0 * hq + (uint64_t)st * STEP
+                        : ((uint64_t)rq.tok0 + (uint64_t)st * (STEP / g)) * hq + un.kvh * g;
+  };
+  // a step's queries and log-sum-exps go to LDS directly: N instructions of RPI rows for each
+  // wave, MLA's rotary parts by the first waves, and the same 64 numbers by every wave (one
+  // count of loads in flight for all)
+  constexpr int CPR = C::LAT / 16, RPI = CPR >= 64 ? 1 : 64 / CPR, N = STEP / RPI / C::WAVES;
+  constexpr int ROTW = C::ROT > 0 ? STEP / 8 : 0;  // waves with an instruction of eight rotary rows
+  constexpr int NO = C::MLA ? 1 : N;  // (MLA: a wave's latent rows, one an instruction, follow each other)
+  uint32_t qoff[NO], roff = 0, loff;  // bytes from the step's first row to this lane's pieces; rows, to its own
 #pragma unroll
-    for (int i = 0; i < N; ++i) {  // a wave's instruction: RPI rows
+  for (int i = 0; i < NO; ++i) {
+    const int row = (wave * N + i) * RPI + lane / CPR;
+    qoff[i] = off(row) * (2 * DK) + (C::MLA ? 0 : 16 * C::lat_piece(row, lane % CPR));
+  }
+  if (C::MLA) {
+    const int row = (8 * wave + lane / 8) % STEP;
+    roff = off(row) * (2 * DK) + C::LAT + 16 * C::rot_piece(row, lane % 8);
+  }
+  loff = off(lane % STEP);
+  auto issue = [&](uint32_t st) {
+    const uint32_t tile = lds_addr(lds) + (st - from) % C::RING * C::TILE;
+    const bool whole = even && st < last_full;
+    const uint64_t base = (uint64_t)(uintptr_t)a.q + first_row(st) * (2ull * DK);
+    auto place = [&](uint32_t row) {
+      const RowAddr x = row_addr(a, rq, un.kvh, st * STEP + row);
+      return x.tok * hq + x.head;
+    };
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
       const int row0 = (wave * N + i) * RPI, row = row0 + lane / CPR;
-      lane_load_lds<false>(query(blk * kWeighBlock + row) + 16 * C::lat_piece(row, lane % CPR), to + row0 * C::LAT);
+      if (whole && C::MLA)
+        row_load_lds<false>(base + (uint64_t)(row0 * (2 * DK)), 16u * C::lat_piece(row0, lane), tile + row0 * C::LAT);
+      else if (whole)
+        row_load_lds<false>(base, qoff[C::MLA ? 0 : i], tile + row0 * C::LAT);
+      else
+        lane_load_lds<false>((uint64_t)(uintptr_t)a.q + place(row) * (2ull * DK) + 16 * C::lat_piece(row, lane % CPR),
+                             tile + row0 * C::LAT);
     }
-    if constexpr (C::ROT > 0) {
+    if (wave < ROTW) {
       const int row = 8 * wave + lane / 8;
-      lane_load_lds<false>(query(blk * kWeighBlock + row) + C::LAT + 16 * C::rot_piece(row, lane % 8),
-                           to + kWeighBlock * C::LAT + 8 * wave * C::ROT);
+      if (whole)
+        row_load_lds<false>(base, roff, tile + STEP * C::LAT + 8 * wave * C::ROT);
+      else
+        lane_load_lds<false>((uint64_t)(uintptr_t)a.q + place(row) * (2ull * DK) + C::LAT + 16 * C::rot_piece(row, lane % 8),
+                             tile + STEP * C::LAT + 8 * wave * C::ROT);
     }
+    dword_load_lds((uint64_t)(uintptr_t)a.lse + 4 * (whole ? first_row(st) + loff : place(lane % STEP)),
+                   tile + STEP * (C::LAT + C::ROT));
   };
+
   float acc[NE];
 #pragma unroll
   for (int i = 0; i < NE; ++i) acc[i] = 0.f;
+  // element i: key b0 + 4 part + key_of(i)
+  auto key_of = [](int i) { return 16 * (i / 4) + i % 4; };
 
-  auto loads = [&](uint32_t blk) { return row_loads(a, row_addr(a, rq, un.kvh, blk * kWeighBlock + col)); };
-  RowLoads next{};
-  if (bl.from < bl.to) next = loads(bl.from);
-  // a wait the compiler sees for K: its own would drain blocks in flight
-  __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);
-  if (bl.from < bl.to) issue(bl.from, 0);
-#pragma unroll 1
-  for (uint32_t blk = bl.from; blk < bl.to; ++blk) {
-    const int buf = (blk - bl.from) & 1;
-    const uint32_t r = blk * kWeighBlock + col;
-    const WeighRow w = weigh_row(a, rq, row_addr(a, rq, un.kvh, r), next, r);
-    const Row &x = w.x;
-    wait_vm<0>();
-    __syncthreads();  // this block is there for every wave; the one before is done with
-    if (blk + 1 < bl.to) {
-      next = loads(blk + 1);
-      issue(blk + 1, buf ^ 1);
-    }
-    if (__builtin_amdgcn_ballot_w64(x.lo < b0 + C::KW && x.hi > b0)) {
-      const char *const qt = lds + buf * C::TILE;
-      f32x16 sc[KB];
+  // Does every row of a step see every key of this wave (documents aside)?
+  auto all_seen = [&](uint32_t st) {
+    uint32_t rest;
+    const uint32_t r0 = st * STEP, base = rq.ctx - rq.n_q;
+    const uint32_t p0 = base + page_divide(r0, g, a.g_magic, &rest), p1 = base + page_divide(r0 + STEP - 1, g, a.g_magic, &rest);
+    return st < last_full && !a.doc_begin && b0 + C::KW <= max(p0 + 1, min(rq.prefix, rq.ctx)) &&
+           (a.window == 0 || p1 < b0 + a.window);
+  };
+  // fragments of a turn's queries: row `col`, dims KD ks + 8 part
+  auto q_frag = [&](const char *qt, int turn, int ks) {
+    const int row = C::RT * turn + col, c = ks * (C::KD / 8) + part;
+    return *reinterpret_cast<const bf16x8 *>(
+        C::MLA && ks * (C::KD / 8) >= 64 ? qt + STEP * C::LAT + row * C::ROT + 16 * C::rot_piece(row, c - 64)
+                                         : qt + row * C::LAT + 16 * C::lat_piece(row, c));
+  };
+  // products of a turn; after(e) follows the e-th of KS KB
+  auto products = [&](const char *qt, int turn, scores_t (&sc)[KB], auto after) {
+    constexpr int AHEAD = C::MLA ? 4 : 1;
+    bf16x8 qf[AHEAD + 1];
 #pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
+    for (int ks = 0; ks < AHEAD; ++ks) qf[ks] = q_frag(qt, turn, ks);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) sc[kb][i] = 0.f;
+    for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        const int c = 2 * ks + half;
-        const char *const at = DK == 576 && ks >= 32 ? qt + kWeighBlock * C::LAT + col * C::ROT + 16 * C::rot_piece(col, c - 64)
-                                                     : qt + col * C::LAT + 16 * C::lat_piece(col, c);
-        const bf16x8 qf = *reinterpret_cast<const bf16x8 *>(at);
+      for (int i = 0; i < C::EB; ++i) sc[kb][i] = 0.f;
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb) sc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[kb][ks], qf, sc[kb], 0, 0, 0);
+    for (int ks = 0; ks < KS; ++ks) {
+      if (ks + AHEAD < KS) qf[(ks + AHEAD) % (AHEAD + 1)] = q_frag(qt, turn, ks + AHEAD);
+      if (C::MLA) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) {
+        sc[kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[kb][ks], qf[ks % (AHEAD + 1)], sc[kb], 0, 0, 0);
+        after(ks * KB + kb);
       }
-      // element i of block kb: key b0 + 32 kb + 8 (i / 4) + 4 half + i % 4
-      auto &flat = reinterpret_cast<float(&)[NE]>(sc);
-      const bool hide = __builtin_amdgcn_ballot_w64(x.lo > b0 || x.hi < b0 + C::KW) != 0;
-      const bool behind = MODE == kModeAny && __builtin_amdgcn_ballot_w64(x.pos + 1 < b0 + C::KW) == 0;
-      float top;
-      auto key_of = [](int i) { return 32 * (i / 16) + 8 * (i % 16 / 4) + i % 4; };
-      const bool raw = scores_of<MODE, NE>(a, RowAt{}, flat, w.slope, x, b0 + 4 * half, behind, hide, 0u, key_of, &top);
-      weights<MODE, NE>(a, flat, raw, nan_row(flat, w.ref, x, b0 + 4 * half, key_of), [&](int i, float p0, float p1) {
-        acc[i] += p0;
-        acc[i + 1] += p1;
-      });
+    }
+  };
+  // Scores in the form that their exponentials take, those out of sight -inf, and the
+  // reference that comes off. easy: every row sees every key, and has a log-sum-exp.
+  auto shape = [&](scores_t (&sc)[KB], uint32_t st, int turn, float lse, bool easy, bool *raw) {
+    auto &flat = reinterpret_cast<float(&)[NE]>(sc);
+    float top;
+    if (__builtin_expect(easy && MODE == kModePlain, 1)) {
+      *raw = true;
+      return lse * kLog2e;
+    }
+    const uint32_t r = st * STEP + C::RT * turn + col;
+    const RowAddr at = row_addr(a, rq, un.kvh, r);
+    RowLoads l;
+    l.lse = lse;
+    l.doc = a.doc_begin ? a.doc_begin[at.tok] : 0;
+    l.slope = MODE == kModeAny && a.slopes ? a.slopes[at.head] : 0.f;
+    const WeighRow w = weigh_row(a, rq, at, l, r);
+    const bool hide = !easy && __builtin_amdgcn_ballot_w64(w.x.lo > b0 || w.x.hi < b0 + C::KW) != 0;
+    const bool behind = MODE == kModeAny && __builtin_amdgcn_ballot_w64(w.x.pos + 1 < b0 + C::KW) == 0;
+    *raw = scores_of<MODE, NE>(a, RowAt{}, flat, w.slope, w.x, b0 + 4 * part, behind, hide, 0u, key_of, &top);
+    return nan_row(flat, w.ref, w.x, b0 + 4 * part, key_of);
+  };
+
+  for (uint32_t st = from; st < to && st < from + C::RING - 1; ++st) issue(st);
+  // K is there from here on: the compiler's own waits, inside the loop, would drain blocks in flight
+#pragma unroll
+  for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(kf[kb][ks]));
+  scores_t held[2][KB];  // BEHIND: a turn's scores, and those of the one before
+  float held_ref = 0.f;
+  if (BEHIND) {
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int i = 0; i < C::EB; ++i) held[1][kb][i] = -INFINITY;
+  }
+  static_assert(TURNS % 2 == 0, "turns alternate");
+#pragma unroll 1
+  for (uint32_t st = from; st < to; ++st) {
+    // own loads of this step have landed once at most the later steps' remain
+    constexpr int L = N + 1, LATER = C::RING - 2;
+    if (to - st <= LATER) wait_vm<0>();
+    else if (wave < ROTW) wait_vm<LATER * (L + 1)>();
+    else wait_vm<LATER * L>();
+    __syncthreads();  // this step is there for every wave; the one before is done with
+    if (st + C::RING - 1 < to) issue(st + C::RING - 1);
+    const char *const qt = lds + (st - from) % C::RING * C::TILE;
+    const float *const lse_of = reinterpret_cast<const float *>(qt + STEP * (C::LAT + C::ROT)) + col;
+    float lse[TURNS];
+    bool none = false;
+#pragma unroll
+    for (int t = 0; t < TURNS; ++t) {
+      lse[t] = lse_of[C::RT * t];
+      none = none || !(lse[t] > -INFINITY);
+    }
+    const bool easy = all_seen(st) && __builtin_amdgcn_ballot_w64(none) == 0;
+    if constexpr (BEHIND) {
+#pragma unroll
+      for (int t = 0; t < TURNS; ++t) {
+        constexpr int EACH = NE / (KS * KB);
+        bool raw;
+        auto &prev = reinterpret_cast<float(&)[NE]>(held[(t & 1) ^ 1]);
+        float p[EACH] = {};
+        __builtin_amdgcn_sched_barrier(0);
+        // an exponential's sum is taken a product later, when it is there
+        products(qt, t, held[t & 1], [&](int e) {
+#pragma unroll
+          for (int i = 0; i < EACH; ++i) {
+            if (e > 0) {
+              acc[(e - 1) * EACH + i] += p[i];
+              asm volatile("" : "+v"(acc[(e - 1) * EACH + i]));  // here, and not where the loop ends
+            }
+            p[i] = fast_exp2(__builtin_fmaf(prev[e * EACH + i], a.score_mul, -held_ref));
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        });
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) acc[NE - EACH + i] += p[i];
+        held_ref = shape(held[t & 1], st, t, lse[t], easy, &raw);
+      }
+    } else {
+#pragma unroll 1
+      for (int t = 0; t < TURNS; ++t) {
+        bool raw;
+        scores_t sc[KB];
+        float mine = lse[0];
+#pragma unroll
+        for (int u = 1; u < TURNS; ++u) mine = t == u ? lse[u] : mine;
+        products(qt, t, sc, [](int) {});
+        const float ref = shape(sc, st, t, mine, easy, &raw);
+        weights<MODE, NE>(a, reinterpret_cast<float(&)[NE]>(sc), raw, ref, [&](int i, float p0, float p1) {
+          acc[i] += p0;
+          acc[i + 1] += p1;
+        });
+      }
     }
   }
+  if constexpr (BEHIND) {
+    auto &prev = reinterpret_cast<float(&)[NE]>(held[1]);
+#pragma unroll
+    for (int i = 0; i < NE; ++i) acc[i] += fast_exp2(__builtin_fmaf(prev[i], a.score_mul, -held_ref));
+  }
 
-  // ---- the lanes' sums of a key: 32 lanes of one half
+  // ---- the lanes' sums of a key: the RT lanes of one part
 #pragma unroll
   for (int kb = 0; kb < KB; ++kb) {
     float mine = 0.f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      float s = row_sum_16(acc[16 * kb + i]);
-      const auto o = __builtin_amdgcn_permlane16_swap(__float_as_uint(s), __float_as_uint(s), false, false);
-      s = __uint_as_float(o[0]) + __uint_as_float(o[1]);
+    for (int i = 0; i < C::EB; ++i) {
+      const float s = row_sum_16(acc[C::EB * kb + i]);
       mine = (col & 15) == i ? s : mine;
     }
     const int i = col & 15;
-    const uint32_t key = b0 + 32 * kb + 8 * (i / 4) + 4 * half + i % 4;
-    if (col < 16 && key < rq.ctx) put_sum(a, rq, un.kvh, un.split, key, mine);
+    const uint32_t key = b0 + 4 * part + key_of(C::EB * kb + (i < C::EB ? i : 0));
+    if (col < C::EB && key < rq.ctx) put_sum(a, rq, un.kvh, un.split, key, mine);
   }
 }
 
@@ -409,12 +566,13 @@ void launch_matrix(const WeighArgs &a, hipStream_t stream) {
     else
       hipLaunchKernelGGL((weigh_few_kernel<DK, kModePlain>), grid, block, 0, stream, a);
   } else {
+    const dim3 wide(WeighCfg<DK>::THREADS);
     if (a.slopes)
-      hipLaunchKernelGGL((weigh_rows_kernel<DK, kModeAny>), grid, block, 0, stream, a);
+      hipLaunchKernelGGL((weigh_rows_kernel<DK, kModeAny>), grid, wide, 0, stream, a);
     else if (a.softcap > 0.f)
-      hipLaunchKernelGGL((weigh_rows_kernel<DK, kModeCap>), grid, block, 0, stream, a);
+      hipLaunchKernelGGL((weigh_rows_kernel<DK, kModeCap>), grid, wide, 0, stream, a);
     else
-      hipLaunchKernelGGL((weigh_rows_kernel<DK, kModePlain>), grid, block, 0, stream, a);
+      hipLaunchKernelGGL((weigh_rows_kernel<DK, kModePlain>), grid, wide, 0, stream, a);
   }
 }
 }  // namespace
