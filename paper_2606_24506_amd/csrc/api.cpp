@@ -37,7 +37,7 @@ int matrix_streams(int variant);
 int matrix_step_tokens(int variant, int hkv);
 hipError_t launch_merge(const MergeArgs &a, hipStream_t stream);
 hipError_t launch_extend(const ExtArgs &a, int32_t kind, hipStream_t stream);
-hipError_t launch_ext_merge(const ExtMergeArgs &a, uint32_t rows, uint32_t most_splits, hipStream_t stream);
+hipError_t launch_ext_merge(const ExtMergeArgs &a, uint32_t rows, uint32_t most_splits, bool few_lanes, hipStream_t stream);
 hipError_t launch_page_copy(const PageCopyArgs &a, hipStream_t stream);
 hipError_t launch_tree(const TreeArgs &a, hipStream_t stream);
 hipError_t launch_weigh(const WeighArgs &a, int32_t kind, hipStream_t stream);
@@ -2376,7 +2376,7 @@ cp_status run_extend(cp_pool *p, const ExtPlan &pl, const void *q, void *out, fl
       rows += x.rows;
       most = std::max(most, x.splits);
     }
-    const hipError_t e = launch_ext_merge(m, rows, most, s);
+    const hipError_t e = launch_ext_merge(m, rows, most, tree != nullptr, s);
     if (e != hipSuccess) return hip_fail(e, "extend join launch");
   }
   return CP_OK;
@@ -2698,46 +2698,54 @@ cp_status cp_attn_weights(cp_pool *p, int32_t n, const int32_t *req_ids, const i
     if ((rc = check_token_rows("sum", 1, n, sum, ctx.data(), g.hkv, g.layers, &spans))) return rc;
     if ((rc = check_rows_apart(&spans, g.hkv, g.layers))) return rc;
 
-    // Rows of a tile of keys are cut into parts where the tiles alone leave workgroups idle
-    // or the longest runs alone at the end: of parts of 2^k blocks of rows those with the
+    // Rows of a tile of keys are cut into parts where the tiles alone leave workgroups idle,
+    // or the longest would run alone at the end: of parts of k blocks of rows those with the
     // shortest estimate, whole turns of the workgroups that run at once and, past two of
-    // them, half a turn more.
-    auto rows_of = [&](int32_t i) { return (int64_t)n_q[i] * g.g; };
-    auto blocks_of = [&](int32_t i) { return (rows_of(i) + kWeighBlock - 1) / kWeighBlock; };
-    int64_t per = INT64_MAX;
+    // them, half a turn more. (Two prompts of 8 K and 5 K, 5,000 tokens of each, 32 heads over
+    // 8: uncut 705 us, in 4 parts 400, in 16 366, in 64 465; 64 tokens of four contexts of
+    // 22 K in all, MLA-16: uncut 86, in 2 parts 53, in 3 67.)
+    struct Work {
+      int32_t kind;
+      int64_t tiles, blocks;
+    };
+    std::vector<Work> jobs((size_t)n);
+    int64_t per = INT64_MAX, most = 0;
+    for (int32_t i = 0; i < n; ++i) {
+      const int64_t rows = (int64_t)n_q[i] * g.g;
+      Work &w = jobs[(size_t)i];
+      w.kind = weigh_kind(g, o.path, rows);
+      w.tiles = (ctx[(size_t)i] + weigh_tile_keys(w.kind) - 1) / weigh_tile_keys(w.kind);
+      w.blocks = (rows + kWeighBlock - 1) / kWeighBlock;
+      if (rows > 16) most = std::max(most, w.blocks);
+    }
     double best = 1e300;
-    for (int64_t k = 2; k <= 1 << 20; k *= 2) {
+    for (int64_t k = 2; most > 2; k = std::max(k + 1, k * 5 / 4)) {
       // us of a block, and workgroups of a CU at once, by kernel
       static constexpr struct { double us; int per_cu; } kCost[kWKinds] = {
           {20, 4}, {4, 5}, {4, 6}, {4, 3}, {2.6, 3}, {3.7, 3}, {5.0, 1}};
       constexpr double kUnit = 4.0;  // a unit's start and end
-      double t = 0, most = 0;
+      double t = 0, units[kWKinds] = {}, longest[kWKinds] = {};
+      for (const Work &w : jobs) {
+        const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(kWeighMaxParts, (w.blocks + k - 1) / k));
+        units[w.kind] += (double)(w.tiles * g.hkv * parts);
+        longest[w.kind] = std::max(longest[w.kind], (double)((w.blocks + parts - 1) / parts));
+      }
       for (int kind = 0; kind < kWKinds; ++kind) {
-        double units = 0, longest = 0;
-        for (int32_t i = 0; i < n; ++i) {
-          if (ctx[(size_t)i] == 0 || weigh_kind(g, o.path, rows_of(i)) != kind) continue;
-          const int64_t tiles = (ctx[(size_t)i] + weigh_tile_keys(kind) - 1) / weigh_tile_keys(kind);
-          const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(kWeighMaxParts, (blocks_of(i) + k - 1) / k));
-          units += (double)(tiles * g.hkv * parts);
-          longest = std::max(longest, (double)((blocks_of(i) + parts - 1) / parts));
-          most = std::max(most, (double)blocks_of(i));
-        }
-        const double turns = units / ((double)p->num_cus * kCost[kind].per_cu);
-        t += (turns <= 2 ? std::ceil(turns) : turns + 0.5) * (kUnit + longest * kCost[kind].us);
+        const double turns = units[kind] / ((double)p->num_cus * kCost[kind].per_cu);
+        t += (turns <= 2 ? std::ceil(turns) : turns + 0.5) * (kUnit + longest[kind] * kCost[kind].us);
       }
       if (t < best) {
         best = t;
         per = k;
       }
-      if ((double)k >= most) break;
+      if (k >= most) break;
     }
     WeighPlan pl;
     for (int32_t kind = 0; kind < kWKinds; ++kind)
       for (int32_t i = 0; i < n; ++i) {
         const int64_t c = ctx[(size_t)i];
-        if (c == 0 || weigh_kind(g, o.path, rows_of(i)) != kind) continue;
-        const int64_t keys = weigh_tile_keys(kind), tiles = (c + keys - 1) / keys;
-        const int64_t blocks = blocks_of(i);
+        if (c == 0 || jobs[(size_t)i].kind != kind) continue;
+        const int64_t tiles = jobs[(size_t)i].tiles, blocks = jobs[(size_t)i].blocks;
         const bool few = kind >= kWFew64 && kind <= kWFewMla;
         int64_t splits = few || blocks == 0 ? 1 : o.num_splits ? std::min<int64_t>(o.num_splits, blocks) : (blocks + per - 1) / per;
         splits = std::min<int64_t>(splits, kWeighMaxParts);

@@ -17,12 +17,13 @@ namespace {
 
 constexpr int kSelWaves = kSelectThreads / 64;
 constexpr int kBins = 2048;
+constexpr uint32_t kCands = 2048;  // numbers still possible that fit LDS
 
-// Numbers in the order of floats: NaN below all, -0 as 0.
+// Numbers in the order of floats, from 1 on: NaN (1) below all, -0 as 0. 0 is no number.
 CP_DEV uint32_t order_key(float f) {
-  const uint32_t u = __float_as_uint(f + 0.f);
-  if ((u & 0x7FFFFFFFu) > 0x7F800000u) return 0u;
-  return u & 0x80000000u ? ~u : u | 0x80000000u;
+  const float x = f + 0.f;
+  const uint32_t u = __float_as_uint(x), k = u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+  return x == x ? k : 1u;
 }
 
 // The threshold of the k heaviest: all above `above` are among them, and the first `equal`
@@ -45,7 +46,8 @@ template <int R>
 __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(const EvictArgs a) {
   __shared__ uint32_t hist[kBins];
   __shared__ uint32_t part[2][kSelWaves];
-  __shared__ uint32_t found[4];  // lo, hi, still needed, exact
+  __shared__ uint32_t found[5];  // lo, hi, still needed, as many in the counter; candidates
+  __shared__ uint32_t cand[kCands];
   const int r = sorted_search(a.n_req, blockIdx.x, [&](int i) { return a.req[i].block_begin; });
   const EvictReq &rq = a.req[r];
   const uint32_t b = blockIdx.x - rq.block_begin, layer = b / rq.hkv, head = b - layer * rq.hkv;
@@ -60,16 +62,15 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(const Evic
   uint32_t key[R > 0 ? R : 1];
   if constexpr (R > 0) {
     float x[R];
+    if (s0 < s1) {
 #pragma unroll
-    for (int j = 0; j < R; ++j) {
-      const uint32_t i = s0 + 64 * j + lane;
-      x[j] = i < s1 ? w[i] : __builtin_nanf("");
+      for (int j = 0; j < R; ++j) x[j] = w[min(s0 + 64 * j + lane, s1 - 1)];
     }
 #pragma unroll
-    for (int j = 0; j < R; ++j) key[j] = order_key(x[j]);
+    for (int j = 0; j < R; ++j) key[j] = s0 + 64 * j + lane < s1 ? order_key(x[j]) : 0u;
   }
   // f(the number of the first lane's, keys), in order; whole waves. Lanes behind the last
-  // number of a piece have a key of 0, as NaN has.
+  // number of a piece have a key of 0.
   auto each_of = [&](auto f) {
     if constexpr (R > 0) {
       constexpr int G = R < 8 ? R : 8;
@@ -101,9 +102,9 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(const Evic
   }
 
   // ---- smallest and largest
-  uint32_t lo = 0xFFFFFFFFu, hi = 0;  // (a smallest of 0, where a lane has no number, costs width and nothing else)
-  each_of([&](uint32_t i0, uint32_t k) {
-    lo = min(lo, i0 + lane < s1 ? k : 0xFFFFFFFFu);
+  uint32_t lo = 0xFFFFFFFFu, hi = 0;  // lo: less 1, so that a key of 0 is no smallest
+  each_of([&](uint32_t, uint32_t k) {
+    lo = min(lo, k - 1);
     hi = max(hi, k);
   });
 #pragma unroll
@@ -121,22 +122,29 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(const Evic
     lo = min(lo, part[0][i]);
     hi = max(hi, part[1][i]);
   }
-  Cut cut{hi, need0};  // (nothing to find where none, or all, of the middle stay)
-  if (need0 == m) cut = Cut{0, need0};
+  lo = __builtin_amdgcn_readfirstlane(lo + 1);
+  hi = __builtin_amdgcn_readfirstlane(hi);
+  Cut cut{need0 == m ? 0u : hi, 0u};  // (nothing to find where none, or all, of the middle stay)
   if (need0 > 0 && need0 < m) {
     uint32_t need = need0;
+    bool few = false;  // the numbers still possible are `cand`, n_cand of them
     while (lo < hi) {
       const int bits = 32 - __builtin_clz(hi - lo), s = bits > 11 ? bits - 11 : 0;
       for (uint32_t i = tid; i < kBins; i += kSelectThreads) hist[i] = 0;
       __syncthreads();
       // (as many may be the smallest, tokens that nothing looked at: counted by the wave)
-      uint32_t least = 0;
-      each_of([&](uint32_t i0, uint32_t k) {
-        const uint32_t off = k - lo;
-        least += (uint32_t)__builtin_popcountll(__builtin_amdgcn_ballot_w64(off == 0 && (lo > 0 || i0 + lane < s1)));
-        if (off - 1 < hi - lo) atomicAdd(&hist[off >> s], 1u);
-      });
-      if (lane == 0 && least) atomicAdd(&hist[0], least);
+      if (few) {
+        for (uint32_t i = tid; i < found[4]; i += kSelectThreads)
+          if (cand[i] - lo <= hi - lo) atomicAdd(&hist[(cand[i] - lo) >> s], 1u);
+      } else {
+        uint32_t least = 0;
+        each_of([&](uint32_t, uint32_t k) {
+          const uint32_t off = k - lo;
+          least += (uint32_t)__builtin_popcountll(__builtin_amdgcn_ballot_w64(off == 0));
+          if (off - 1 < hi - lo) atomicAdd(&hist[off >> s], 1u);
+        });
+        if (lane == 0 && least) atomicAdd(&hist[0], least);
+      }
       __syncthreads();
       // counters from the largest down: a thread has two
       const uint32_t h0 = hist[kBins - 1 - 2 * tid], h1 = hist[kBins - 2 - 2 * tid];
@@ -157,15 +165,23 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(const Evic
         found[0] = nlo;
         found[1] = min(hi, nlo + ((1u << s) - 1u));
         found[2] = left;
-        found[3] = left == (first ? h0 : h1);  // every number of the counter is among them
+        found[3] = first ? h0 : h1;
       }
       __syncthreads();
-      lo = found[0];
-      hi = found[1];
-      need = found[2];
-      if (found[3] && lo > 0) {
+      lo = __builtin_amdgcn_readfirstlane(found[0]);
+      hi = __builtin_amdgcn_readfirstlane(found[1]);
+      need = __builtin_amdgcn_readfirstlane(found[2]);
+      const uint32_t in_bin = __builtin_amdgcn_readfirstlane(found[3]);
+      if (need == in_bin) {  // every number of the counter is among them
         lo = hi = lo - 1;
         need = 0;
+      } else if (!few && lo < hi && in_bin <= kCands) {  // those of the counter, in any order
+        if (tid == 0) found[4] = 0;
+        __syncthreads();
+        each_of([&](uint32_t, uint32_t k) {
+          if (k - lo <= hi - lo) cand[atomicAdd(&found[4], 1u) % kCands] = k;
+        });
+        few = true;
       }
       __syncthreads();
     }
@@ -174,9 +190,9 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(const Evic
 
   // ---- the numbers that stay, in order
   uint32_t above = 0, equal = 0;
-  each_of([&](uint32_t i0, uint32_t k) {
+  each_of([&](uint32_t, uint32_t k) {
     above += (uint32_t)__builtin_popcountll(__builtin_amdgcn_ballot_w64(k > cut.key));
-    if (cut.equal) equal += (uint32_t)__builtin_popcountll(__builtin_amdgcn_ballot_w64(k == cut.key && i0 + lane < s1));
+    if (cut.equal) equal += (uint32_t)__builtin_popcountll(__builtin_amdgcn_ballot_w64(k == cut.key));
   });
   __syncthreads();
   if (lane == 0) {
@@ -189,23 +205,25 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(const Evic
     at += part[0][i];
     eq += part[1][i];
   }
-  at += min(eq, cut.equal);
+  at = __builtin_amdgcn_readfirstlane(at + min(eq, cut.equal));
+  eq = __builtin_amdgcn_readfirstlane(eq);
+  const uint32_t end = rq.keep - rq.last;
   auto below = [](uint64_t mask) {
     return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0u));
   };
-  if (need0 > 0)
-    each_of([&](uint32_t i0, uint32_t k) {
-      bool take = k > cut.key;
-      if (eq < cut.equal) {  // (the first of those that are equal, whatever wave has them)
-        const bool same = k == cut.key && i0 + lane < s1;
-        const uint64_t be = __builtin_amdgcn_ballot_w64(same);
-        take = take || (same && eq + below(be) < cut.equal);
-        eq += (uint32_t)__builtin_popcountll(be);
-      }
-      const uint64_t bt = __builtin_amdgcn_ballot_w64(take);
-      const uint32_t to = at + below(bt);
-      if (take && to < rq.keep - rq.last) list[to] = (int32_t)(i0 + lane);  // (always, unless the sums change meanwhile)
-      at += (uint32_t)__builtin_popcountll(bt);
+  auto put = [&](uint32_t i0, bool take) {
+    const uint64_t bt = __builtin_amdgcn_ballot_w64(take);
+    const uint32_t to = at + below(bt);
+    if (take && to < end) list[to] = (int32_t)(i0 + lane);  // (always, unless the sums change meanwhile)
+    at += (uint32_t)__builtin_popcountll(bt);
+  };
+  if (need0 > 0 && cut.equal == 0)
+    each_of([&](uint32_t i0, uint32_t k) { put(i0, k > cut.key); });
+  else if (need0 > 0)
+    each_of([&](uint32_t i0, uint32_t k) {  // the first of those that are equal, whatever wave has them
+      const uint64_t be = __builtin_amdgcn_ballot_w64(k == cut.key);
+      put(i0, k > cut.key || (k == cut.key && eq + below(be) < cut.equal));
+      eq += (uint32_t)__builtin_popcountll(be);
     });
   for (uint32_t i = tid; i < rq.first; i += kSelectThreads) list[i] = (int32_t)i;
   for (uint32_t i = tid; i < rq.last; i += kSelectThreads) list[rq.keep - rq.last + i] = (int32_t)(rq.n - rq.last + i);

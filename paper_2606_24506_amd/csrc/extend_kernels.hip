@@ -203,12 +203,17 @@ hipError_t launch_extend(const ExtArgs &a, int32_t kind, hipStream_t stream) {
   return hipGetLastError();
 }
 
-hipError_t launch_ext_merge(const ExtMergeArgs &in, uint32_t rows, uint32_t most_splits, hipStream_t stream) {
+// few_lanes (trees): no more lanes of a row than it takes to fill the card, kJoinThreads
+// threads in all: their sums' way through LDS costs more than a row's own chain then.
+constexpr uint64_t kJoinThreads = 1 << 19;
+hipError_t launch_ext_merge(const ExtMergeArgs &in, uint32_t rows, uint32_t most_splits, bool few_lanes, hipStream_t stream) {
   if (rows == 0) return hipSuccess;
   ExtMergeArgs a = in;
   const int dv4 = a.d_v / 4;
   a.lanes = 1;
-  while (a.lanes * 2 * dv4 <= kExtThreads && (uint32_t)a.lanes < most_splits) a.lanes *= 2;
+  while (a.lanes * 2 * dv4 <= kExtThreads && (uint32_t)a.lanes < most_splits &&
+         (!few_lanes || (uint64_t)rows * (uint64_t)(dv4 * a.lanes) < kJoinThreads))
+    a.lanes *= 2;
   const uint32_t per = (uint32_t)(kExtThreads / (dv4 * a.lanes));
   hipLaunchKernelGGL(ext_merge_kernel, dim3((rows + per - 1) / per), dim3(kExtThreads), 0, stream, a);
   return hipGetLastError();
