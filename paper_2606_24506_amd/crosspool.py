@@ -615,6 +615,17 @@ def cp_attn_extend_step(pool: int, req_ids: Sequence[int], n_new: Sequence[int],
                                    _ptr(lse), _stream(stream), C.byref(o)))
 
 
+_DTYPES: dict = {}
+
+
+def _dtype(t) -> str:
+    """The name of a tensor's type (each looked up once: str() takes a microsecond)."""
+    name = _DTYPES.get(t.dtype)
+    if name is None:
+        name = _DTYPES[t.dtype] = str(t.dtype)
+    return name
+
+
 def _tree(known, n_q, mask, depth):
     """The record of a call's trees: mask int32 [tokens][words], depth int32
     [tokens], on the GPU."""
@@ -622,7 +633,7 @@ def _tree(known, n_q, mask, depth):
     if mask.dim() != 2 or mask.shape[0] != total or depth.numel() != total:
         raise ValueError("mask is [tokens][words] and depth [tokens] of the call's trees")
     for t in (mask, depth):
-        if str(t.dtype) != "torch.int32" or not t.is_cuda or (known is not None and t.device.index != known.device):
+        if _dtype(t) != "torch.int32" or not t.is_cuda or (known is not None and t.device.index != known.device):
             raise ValueError("mask and depth are int32, on the GPU of the pool")
     return cp_tree(_ptr(mask), mask.shape[1], 0, _ptr(depth))
 
@@ -631,14 +642,13 @@ def cp_tree_build(n_tok: Sequence[int], parents, mask, depth, stream=None) -> No
     """parents int32 [tokens of every tree]; mask int32 [tokens][words] and depth
     int32 [tokens] are written. All on one GPU."""
     total = sum(n_tok)
-    if parents.numel() != total or str(parents.dtype) != "torch.int32":
+    if parents.numel() != total or _dtype(parents) != "torch.int32":
         raise ValueError("parents holds one int32 per token")
-    if parents.device != mask.device:
-        raise ValueError("the tensors are on one GPU")
     t = _tree(None, n_tok, mask, depth)
-    if depth.device != mask.device:
+    device = mask.device
+    if parents.device != device or depth.device != device:
         raise ValueError("the tensors are on one GPU")
-    _check(LIB.cp_tree_build(mask.device.index, len(n_tok), _i32_array(n_tok), _ptr(parents), t.words, t.mask, t.depth,
+    _check(LIB.cp_tree_build(device.index, len(n_tok), _i32_array(n_tok), _ptr(parents), t.words, t.mask, t.depth,
                              _stream(stream)))
 
 
@@ -682,7 +692,7 @@ def token_rows(tensors):
             raise ValueError("rows are on one GPU")
         arr[i] = cp_token_rows(t.data_ptr(), t.shape[-1], t.stride(-2), t.stride(0) if t.dim() == 3 else 0)
     arr.keep = tensors
-    arr.heads = [(t.shape[0] if t.dim() == 3 else 1, t.shape[-2]) for t in tensors]
+    arr.shapes = {(t.shape[0] if t.dim() == 3 else 1, t.shape[-2]) for t in tensors}  # (layers, KV heads)
     arr.floats = not tensors or str(tensors[0].dtype) == "torch.float32"
     arr.device = tensors[0].device.index if tensors else None
     return arr
@@ -703,9 +713,10 @@ def _rows_arg(pool, req_ids, rows, floats: bool):
     if known is not None:
         if rows.device not in (None, known.device):
             raise ValueError("rows are on the GPU of the pool")
-        for r, (layers, heads) in zip(req_ids, rows.heads):
-            if known.shapes.get(int(r), (layers, heads)) != (layers, heads):
-                raise ValueError("rows for every layer and KV head of the request's model")
+        # (the requests of a call are of one model, or the call is refused)
+        shape = known.shapes.get(int(req_ids[0])) if len(req_ids) else None
+        if shape is not None and rows.shapes - {shape}:
+            raise ValueError("rows for every layer and KV head of the requests' model")
     return rows
 
 

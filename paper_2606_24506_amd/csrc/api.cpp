@@ -2838,7 +2838,10 @@ namespace {
 // taken, on success.
 cp_status prepare_cut(cp_pool *p, int32_t n, const int32_t *ids, const int64_t *from, const int64_t *new_len) {
   std::vector<int64_t> more, pages;
-  p->st.cut_cost(n, ids, from, new_len, &more, &pages);
+  p->st.cut_cost(n, ids, from, new_len, p->st.virt(), &more, &pages);
+  bool exact = p->st.virt();  // (the bound first; a chunk is taken only for pages that fill it)
+  for (int32_t m = 0; m < p->st.n_models() && !exact; ++m) exact = pages[(size_t)m] > p->st.free_slots(m);
+  if (!p->st.virt() && (exact || !p->st.fits_budget(more))) p->st.cut_cost(n, ids, from, new_len, true, &more, &pages);
   if (!p->st.fits_budget(more)) return fail(CP_ENOSPC, "the pool page budget cannot take pages in the place of shared ones");
   std::vector<int32_t> carved;
   for (int32_t m = 0; m < p->st.n_models(); ++m) {
@@ -2972,6 +2975,8 @@ cp_status cp_request_keep(cp_pool *p, int32_t n, const int32_t *ids, const int64
       copies[(size_t)i].reserve(k);
       most += k;
     }
+    std::vector<uint32_t> olds;
+    olds.reserve(most);
     items.reserve(most);
     models.reserve(most);
     moves.reserve((size_t)n);
@@ -3003,7 +3008,7 @@ cp_status cp_request_keep(cp_pool *p, int32_t n, const int32_t *ids, const int64
       }
       at += n_keep[i];
     }
-    for (int32_t i = 0; i < n; ++i) p->st.cut_give_up(p->st.req(ids[i]).model, copies[(size_t)i]);
+    for (int32_t i = 0; i < n; ++i) p->st.cut_give_up(p->st.req(ids[i]).model, copies[(size_t)i], &olds);
     for (int32_t i = 0; i < n; ++i) p->st.truncate(ids[i], len[(size_t)i]);
     if (p->host_only) return CP_OK;
     DeviceGuard g(p->device);
@@ -3062,14 +3067,14 @@ cp_status cp_kv_evict(cp_pool *p, int32_t n, const int32_t *ids, const int64_t *
     std::vector<std::vector<PoolState::OwnPage>> copies((size_t)n);
     std::vector<EvictReq> req((size_t)n);
     std::vector<MoveItem> place, apart;
-    std::vector<uint32_t> ent;
     size_t most = 0;
     for (int32_t i = 0; i < n; ++i) {
       const size_t k = (size_t)(g.layers * std::max<int64_t>(0, (len[(size_t)i] + P - 1) / P - from[(size_t)i] / P));
       copies[(size_t)i].reserve(k);
       most += k;
     }
-    ent.reserve(most);
+    std::vector<uint32_t> olds;
+    olds.reserve(most);
     place.reserve((size_t)n);
     apart.reserve((size_t)n);
     uint32_t *ws = (uint32_t *)p->ws_l;
@@ -3135,7 +3140,7 @@ cp_status cp_kv_evict(cp_pool *p, int32_t n, const int32_t *ids, const int64_t *
       if (m.rq.k0 >= m.rq.n) continue;
       ((int64_t)copies[(size_t)i].size() == pages * g.layers ? apart : place).push_back(m);
     }
-    for (int32_t i = 0; i < n; ++i) p->st.cut_give_up(model, copies[(size_t)i]);
+    for (int32_t i = 0; i < n; ++i) p->st.cut_give_up(model, copies[(size_t)i], &olds);
     for (int32_t i = 0; i < n; ++i) {
       const int64_t dropped = p->st.req(ids[i]).dropped + held[(size_t)i] - len[(size_t)i];
       p->st.truncate(ids[i], len[(size_t)i]);

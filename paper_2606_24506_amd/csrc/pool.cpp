@@ -548,38 +548,49 @@ void PoolState::truncate(int32_t id, int64_t new_len) {
   if (new_len == 0) r.dropped = 0;
 }
 
-void PoolState::cut_cost(int32_t n, const int32_t *ids, const int64_t *from, const int64_t *new_len,
+void PoolState::cut_cost(int32_t n, const int32_t *ids, const int64_t *from, const int64_t *new_len, bool exact,
                          std::vector<int64_t> *reserved, std::vector<int64_t> *pages) const {
   reserved->assign(models_.size(), 0);
   pages->assign(models_.size(), 0);
   for (int32_t i = 0; i < n; ++i) {
     const Request &r = reqs_[ids[i]];
-    const int64_t keep = ceil_div(new_len[i], P_);
-    for (int32_t l = 0; l < r.layers; ++l) {
-      const uint32_t *pt = pte_.data() + r.plane_base(l);
-      for (int64_t k = std::min(from[i] / P_, keep); k < r.pages_used; ++k) {
-        if (!sharers(pt[k])) continue;
-        (*reserved)[(size_t)r.model] += 1;
-        (*pages)[(size_t)r.model] += k < keep;
-      }
+    const int64_t keep = ceil_div(new_len[i], P_), k0 = std::min(from[i] / P_, keep);
+    int64_t &more = (*reserved)[(size_t)r.model], &own = (*pages)[(size_t)r.model];
+    if (!exact) {
+      more += (r.pages_used - k0) * r.layers;
+      own += (keep - k0) * r.layers;
+      continue;
     }
+    for (int32_t l = 0; l < r.layers; ++l)
+      each_shared(pte_.data() + r.plane_base(l) + k0, r.pages_used - k0, [&](int64_t k) {
+        more += 1;
+        own += k < keep - k0;
+      });
   }
 }
 
 void PoolState::cut_own(int32_t id, int64_t from, int64_t new_len, std::vector<OwnPage> *copies) {
   const Request &r = reqs_[id];
-  const int64_t keep = ceil_div(new_len, P_);
-  for (int32_t l = 0; l < r.layers; ++l)
-    for (int64_t k = from / P_; k < keep; ++k) {
-      const uint32_t slot = r.plane_base(l) + (uint32_t)k, old = pte_[slot];
-      if (!sharers(old)) continue;
-      alloc_pages(r.model, 1, &pte_[slot]);
-      copies->push_back(OwnPage{slot, old, pte_[slot]});
-    }
+  const int64_t keep = ceil_div(new_len, P_), k0 = std::min(from / P_, keep);
+  const size_t first = copies->size();
+  for (int32_t l = 0; l < r.layers; ++l) {
+    const uint32_t slot = r.plane_base(l) + (uint32_t)k0;
+    each_shared(pte_.data() + slot, keep - k0,
+                [&](int64_t k) { copies->push_back(OwnPage{slot + (uint32_t)k, pte_[slot + (uint64_t)k], 0u}); });
+  }
+  // (pages in a row take theirs at once)
+  for (size_t i = first; i < copies->size();) {
+    size_t j = i + 1;
+    while (j < copies->size() && (*copies)[j].slot == (*copies)[j - 1].slot + 1) ++j;
+    alloc_pages(r.model, (int64_t)(j - i), &pte_[(*copies)[i].slot]);
+    for (; i < j; ++i) (*copies)[i].to = pte_[(*copies)[i].slot];
+  }
 }
 
-void PoolState::cut_give_up(int32_t model, const std::vector<OwnPage> &copies) {
-  for (const OwnPage &c : copies) acct_[model].reserved += 1 - free_pages(&c.from, 1);
+void PoolState::cut_give_up(int32_t model, const std::vector<OwnPage> &copies, std::vector<uint32_t> *scratch) {
+  scratch->clear();
+  for (const OwnPage &c : copies) scratch->push_back(c.from);
+  acct_[model].reserved += (int64_t)copies.size() - free_pages(scratch->data(), (int64_t)scratch->size());
 }
 
 void PoolState::truncate_cost(int32_t n, const int32_t *ids, const int64_t *new_len, bool exact,

@@ -220,11 +220,12 @@ class PoolState {
   // a call's: pages of their own (after ensure_slots); appends one record for each. Then
   // the old pages are given up, and each request truncated.
   // cut_cost: what this adds to each model's `reserved` at most, before anything is given
-  // up, and the pages it allocates.
-  void cut_cost(int32_t n, const int32_t *ids, const int64_t *from, const int64_t *new_len,
+  // up, and the pages it allocates; not exact: at most that (as if every page were shared).
+  void cut_cost(int32_t n, const int32_t *ids, const int64_t *from, const int64_t *new_len, bool exact,
                 std::vector<int64_t> *reserved, std::vector<int64_t> *pages) const;
   void cut_own(int32_t id, int64_t from, int64_t new_len, std::vector<OwnPage> *copies);
-  void cut_give_up(int32_t model, const std::vector<OwnPage> &copies);
+  // (*scratch: room for as many entries as copies)
+  void cut_give_up(int32_t model, const std::vector<OwnPage> &copies, std::vector<uint32_t> *scratch);
   void set_dropped(int32_t id, int64_t n) { reqs_[id].dropped = n; }
   // Would the budget hold every reservation with these additions (per model)?
   bool fits_budget(const std::vector<int64_t> &extra) const;
@@ -280,6 +281,19 @@ class PoolState {
   // Takes a user from pages in order; those without another are freed (a
   // chunk goes back when its last page does). Returns how many were.
   int64_t free_pages(const uint32_t *ptes, int64_t n);
+  // f(i) for those of n pages of one model that have users beyond the first, in order; a
+  // chunk is looked up once for the pages in a row that lie in it.
+  template <class F>
+  void each_shared(const uint32_t *ptes, int64_t n, F f) const {
+    const uint32_t chunk256 = (uint32_t)(chunk_bytes_ >> 8);
+    for (int64_t i = 0; i < n;) {
+      const uint32_t c = ptes[i] / chunk256, lo = c * chunk256;
+      const Chunk &ch = chunks_[c];
+      const uint32_t page256 = (uint32_t)((uint64_t)models_[ch.model].page_bytes >> 8);
+      for (; i < n && ptes[i] >= lo && ptes[i] - lo < chunk256; ++i)
+        if (!ch.more.empty() && ch.more[(ptes[i] - lo) / page256]) f(i);
+    }
+  }
   void grow_planes(Request &r, int64_t new_len, uint64_t *first, uint64_t *count);
 
   int32_t P_ = 64;
