@@ -2709,7 +2709,7 @@ cp_status cp_attn_weights(cp_pool *p, int32_t n, const int32_t *req_ids, const i
       int64_t tiles, blocks;
     };
     std::vector<Work> jobs((size_t)n);
-    int64_t per = INT64_MAX, most = 0;
+    int64_t per = 1, most = 0;
     for (int32_t i = 0; i < n; ++i) {
       const int64_t rows = (int64_t)n_q[i] * g.g;
       Work &w = jobs[(size_t)i];
@@ -2718,6 +2718,7 @@ cp_status cp_attn_weights(cp_pool *p, int32_t n, const int32_t *req_ids, const i
       w.blocks = (rows + kWeighBlock - 1) / kWeighBlock;
       if (rows > 16) most = std::max(most, w.blocks);
     }
+    per = std::max(per, most);  // (two blocks are not cut)
     double best = 1e300;
     for (int64_t k = 2; most > 2; k = std::max(k + 1, k * 5 / 4)) {
       // us of a block, and workgroups of a CU at once, by kernel
@@ -2773,6 +2774,8 @@ cp_status cp_attn_weights(cp_pool *p, int32_t n, const int32_t *req_ids, const i
         e.tiles = (uint32_t)tiles;
         e.splits = (uint32_t)splits;
         if (splits > 1) {
+          if (c * g.hkv > (int64_t)kMaxExtUnits * kWeighThreads)
+            return fail(CP_EINVAL, "too long a context of request %d in one call", req_ids[i]);
           e.ws = pl.ws;
           pl.ws += (uint64_t)(splits * c * g.hkv);
           pl.joins.push_back(WeighJoinArgs::Req{e.old, e.sum, e.old_head, e.sum_head, e.ws, 0u, e.ctx, e.splits, 0u});
@@ -2814,7 +2817,6 @@ cp_status cp_attn_weights(cp_pool *p, int32_t n, const int32_t *req_ids, const i
       for (; i < pl.joins.size() && m.n_req < kWeighMaxReq; ++i) {
         const int64_t blocks = ((int64_t)pl.joins[i].ctx * g.hkv + kWeighThreads - 1) / kWeighThreads;
         if (m.n_req > 0 && m.n_blocks + blocks > kMaxExtUnits) break;
-        if (blocks > 1 << 23) return fail(CP_EINVAL, "too long a context in one call");
         WeighJoinArgs::Req &x = m.req[m.n_req++];
         x = pl.joins[i];
         x.block_begin = (uint32_t)m.n_blocks;
