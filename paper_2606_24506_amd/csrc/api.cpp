@@ -2588,9 +2588,9 @@ struct RowSpan {
 };
 
 // Checks one argument: room for len[i] tokens of every KV head and layer, rows that do not
-// overlap. Appends the entries' spans.
+// overlap. Appends the spans of the entries (of one layer, or of all: -1).
 cp_status check_token_rows(const char *what, int32_t kind, int32_t n, const cp_token_rows *rows, const int64_t *len,
-                           int32_t hkv, int32_t layers, std::vector<RowSpan> *spans) {
+                           int32_t hkv, int32_t layers, int32_t layer, std::vector<RowSpan> *spans) {
   for (int32_t i = 0; i < n; ++i) {
     const cp_token_rows &r = rows[i];
     if (len[i] == 0) continue;
@@ -2602,10 +2602,27 @@ cp_status check_token_rows(const char *what, int32_t kind, int32_t n, const cp_t
     const int64_t one = (hkv > 1 ? (hkv - 1) * r.head : 0) + r.len;  // a layer's
     if (layers > 1 && (r.layer < one || r.layer > (int64_t)1 << 48))
       return fail(CP_EINVAL, "%s of entry %d: rows of layers overlap", what, i);
-    const uint64_t at = (uint64_t)(uintptr_t)r.data;
-    spans->push_back(RowSpan{at, at + 4 * (uint64_t)((layers > 1 ? (layers - 1) * r.layer : 0) + one), kind, i, &r});
+    const uint64_t at = (uint64_t)(uintptr_t)r.data + (layer > 0 ? 4 * (uint64_t)(layer * r.layer) : 0);
+    const int32_t n_layers = layer < 0 ? layers : 1;
+    spans->push_back(RowSpan{at, at + 4 * (uint64_t)((n_layers > 1 ? (n_layers - 1) * r.layer : 0) + one), kind, i, &r});
   }
   return CP_OK;
+}
+
+// Do rows of x and y, each in rising places, meet? (Slices of one tensor may lie between
+// one another's rows.)
+bool rows_meet(const RowSpan &x, const RowSpan &y, int32_t hkv, int32_t layers) {
+  auto row = [&](const RowSpan &s, int64_t i) {
+    return s.lo + 4 * (uint64_t)((layers > 1 ? i / hkv * s.rows->layer : 0) + (hkv > 1 ? i % hkv * s.rows->head : 0));
+  };
+  const int64_t n = (int64_t)hkv * layers;
+  for (int64_t i = 0, j = 0; i < n && j < n;) {
+    const uint64_t a = row(x, i), b = row(y, j);
+    if (a < b + 4 * (uint64_t)y.rows->len && b < a + 4 * (uint64_t)x.rows->len) return true;
+    if (a < b) ++i;
+    else ++j;
+  }
+  return false;
 }
 
 // Arguments 0 are read, those of other kinds written. What is written overlaps nothing, but
@@ -2618,7 +2635,7 @@ cp_status check_rows_apart(std::vector<RowSpan> *spans, int32_t hkv, int32_t lay
       if (x.kind == 0 && y.kind == 0) continue;
       const bool same = x.kind + y.kind == 1 && x.entry == y.entry && x.lo == y.lo &&
                         (hkv == 1 || x.rows->head == y.rows->head) && (layers == 1 || x.rows->layer == y.rows->layer);
-      if (!same)
+      if (!same && rows_meet(x, y, hkv, layers))
         return fail(CP_EINVAL, "rows per token of entries %d and %d overlap without being the same", x.entry, y.entry);
     }
   return CP_OK;
@@ -2694,9 +2711,9 @@ cp_status cp_attn_weights(cp_pool *p, int32_t n, const int32_t *req_ids, const i
       return fail(CP_EINVAL, "q must be 16-byte aligned, lse, slopes and doc_begin 4-byte");
     if (decay == 0.f) old = nullptr;  // what it holds is not read
     std::vector<RowSpan> spans;
-    if (old && (rc = check_token_rows("old", 0, n, old, ctx.data(), g.hkv, g.layers, &spans))) return rc;
-    if ((rc = check_token_rows("sum", 1, n, sum, ctx.data(), g.hkv, g.layers, &spans))) return rc;
-    if ((rc = check_rows_apart(&spans, g.hkv, g.layers))) return rc;
+    if (old && (rc = check_token_rows("old", 0, n, old, ctx.data(), g.hkv, g.layers, layer, &spans))) return rc;
+    if ((rc = check_token_rows("sum", 1, n, sum, ctx.data(), g.hkv, g.layers, layer, &spans))) return rc;
+    if ((rc = check_rows_apart(&spans, g.hkv, 1))) return rc;
 
     // Rows of a tile of keys are cut into parts where the tiles alone leave workgroups idle,
     // or the longest would run alone at the end: of parts of k blocks of rows those with the
@@ -3055,10 +3072,10 @@ cp_status cp_kv_evict(cp_pool *p, int32_t n, const int32_t *ids, const int64_t *
       tabs += (uint64_t)(r.pages_used * g.layers);
     }
     std::vector<RowSpan> spans;
-    if ((rc = check_token_rows("weights", 0, n, weights, held.data(), g.hkv, g.layers, &spans))) return rc;
-    if (o.new_weights && (rc = check_token_rows("new_weights", 1, n, o.new_weights, held.data(), g.hkv, g.layers, &spans)))
+    if ((rc = check_token_rows("weights", 0, n, weights, held.data(), g.hkv, g.layers, -1, &spans))) return rc;
+    if (o.new_weights && (rc = check_token_rows("new_weights", 1, n, o.new_weights, held.data(), g.hkv, g.layers, -1, &spans)))
       return rc;
-    if (o.kept && (rc = check_token_rows("kept", 2, n, o.kept, len.data(), g.hkv, g.layers, &spans))) return rc;
+    if (o.kept && (rc = check_token_rows("kept", 2, n, o.kept, len.data(), g.hkv, g.layers, -1, &spans))) return rc;
     if ((rc = check_rows_apart(&spans, g.hkv, g.layers))) return rc;
     if ((rc = earlier_error())) return rc;
     if ((rc = reconcile_pages(p))) return rc;
