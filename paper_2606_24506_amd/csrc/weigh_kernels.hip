@@ -156,7 +156,7 @@ __global__ __launch_bounds__(kWeighThreads) void weigh_few_kernel(const WeighArg
   for (int n = 0; n < NB; ++n) {
     const u32x4e *const k = reinterpret_cast<const u32x4e *>(head + ((uint64_t)at[n] << 8) + (uint64_t)slot[n] * (2 * DK));
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) kf[n][ks] = __builtin_nontemporal_load(k + 4 * ks);
+    for (int ks = 0; ks < KS; ++ks) kf[n][ks] = k[4 * ks];
   }
 #pragma unroll
   for (int n = 0; n < NB; ++n) {

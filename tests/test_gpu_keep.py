@@ -301,3 +301,101 @@ def test_a_run_of_them_together(name, rot):
     assert sc.pool.ctx_len(sc.ids[1]) < positions[1]
     rope.destroy()
     sc.close()
+
+
+@pytest.mark.parametrize("name", ["gqa8x2d128", "mla16"])
+def test_rows_that_lie_between_one_anothers(name):
+    """One tensor for every request's numbers, requests inside layers: sums, choice and
+    numbers as with tensors of their own."""
+    print(f"[case] interleaved {name}", flush=True)
+    layers, n, lens = 3, 3, [200, 77, 131]
+    sc = Scene(name, lens, seed=8, layers=layers, room=10)
+    forks = [sc.pool.open(sc.model, m + 10) for m in lens]
+    sc.pool.fork(sc.ids, forks)
+    q, _, lse = sc.buffers(30 * n)
+    lse.fill_(3.0)
+    t = max(lens)
+    one, apart = torch.full((layers, n, sc.hkv, t), 7.0, device="cuda"), []
+    slices = [one[:, i, :, :m] for i, m in enumerate(lens)]
+    apart = [torch.full((layers, sc.hkv, m), 7.0, device="cuda") for m in lens]
+    for layer in range(layers):
+        sc.pool.weights(sc.ids, [30] * n, q, lse, slices, layer=layer)
+        sc.pool.weights(sc.ids, [30] * n, q, lse, apart, layer=layer)
+        sc.pool.weights(sc.ids, [30] * n, q, lse, slices, old=slices, decay=0.5, layer=layer)
+        sc.pool.weights(sc.ids, [30] * n, q, lse, apart, old=apart, decay=0.5, layer=layer)
+    for x, y in zip(slices, apart):
+        assert torch.equal(x, y) and (y != 7).all()
+    keep = [60, 77, 20]
+    numbers = torch.full((layers, n, sc.hkv, t), -1, dtype=torch.int32, device="cuda")
+    lists = [numbers[:, i, :, :k] for i, k in enumerate(keep)]
+    own = [torch.full((layers, sc.hkv, k), -1, dtype=torch.int32, device="cuda") for k in keep]
+    sc.pool.evict(sc.ids, keep, slices, new=slices, kept=lists, first=4, last=9)
+    sc.pool.evict(forks, keep, apart, new=apart, kept=own, first=4, last=9)
+    for i, (a, b, k) in enumerate(zip(sc.ids, forks, keep)):
+        assert torch.equal(slices[i], apart[i]) and torch.equal(lists[i], own[i])
+        assert torch.equal(sc.held(a, k, layers), sc.held(b, k, layers))
+        assert (one[:, i, :, lens[i]:] == 7).all() and (numbers[:, i, :, k:] == -1).all()
+    sc.ids += forks
+    sc.close()
+
+
+def test_two_graphs_of_sums_share_a_workspace():
+    """Parts of rows in the pool's workspace: replays in turn, with an eager call between."""
+    print("[case] two graphs", flush=True)
+    sc = Scene("gqa8x2d128", [3000, 700], seed=9)
+    sets = []
+    stream = torch.cuda.Stream()
+    for k, splits in ((300, 5), (64, 3)):
+        q, _, lse = sc.buffers(2 * k)
+        lse.fill_(2.0 + splits)
+        new = [torch.zeros(sc.hkv, m, device="cuda") for m in (3000, 700)]
+        call = lambda new=new, q=q, lse=lse, k=k, splits=splits: sc.pool.weights(sc.ids, [k, k], q, lse, new, num_splits=splits)
+        with torch.cuda.stream(stream):
+            call()
+        stream.synchronize()
+        want = [x.clone() for x in new]
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=stream):
+            call()
+        sets.append((g, call, new, want))
+    for turn in range(4):
+        for g, call, new, want in sets:
+            for x in new:
+                x.fill_(-1.0)
+            if turn == 2:
+                call()
+                for x, y in zip(new, want):
+                    assert torch.equal(x, y)
+                    x.fill_(-1.0)
+            g.replay()
+            torch.cuda.synchronize()
+            for x, y in zip(new, want):
+                assert torch.equal(x, y), turn
+    sc.close()
+
+
+def test_a_stream_of_their_own():
+    """Sums, an eviction and kept tokens one behind the other on a side stream."""
+    print("[case] side stream", flush=True)
+    sc = Scene("gqa8x2d128", [2500], seed=10, room=50)
+    b = sc.pool.open(sc.model, 2600)
+    sc.pool.fork(sc.ids, [b])
+    torch.cuda.synchronize()
+    side, out = torch.cuda.Stream(), []
+    q, _, lse = sc.buffers(40)
+    lse.fill_(4.0)
+    for rid, stream in ((sc.ids[0], torch.cuda.current_stream()), (b, side)):
+        new = torch.zeros(1, sc.hkv, 2500, device="cuda")
+        torch.cuda.synchronize()
+        with torch.cuda.stream(stream):
+            if stream is side:
+                torch.cuda._sleep(2_000_000)
+            sc.pool.weights([rid], [40], q, lse, [new])
+            sc.pool.evict([rid], [900], [new], new=[new], first=5, last=40)
+            sc.pool.keep([rid], [800], [30], list(range(0, 90, 3)))
+            rows = sc.held(rid, 830)
+        torch.cuda.synchronize()
+        out.append((new, rows))
+    assert torch.equal(out[0][0], out[1][0]) and torch.equal(out[0][1], out[1][1])
+    sc.ids.append(b)
+    sc.close()
