@@ -123,12 +123,27 @@ CP_DEV float row_sum_16(float x) {
 
 // --------------------------------------------------------------- few rows
 
-// At most 16 rows: S^T = K Q^T by 16x16x32 products, K from the pool straight to the
-// operand's registers (a lane holds 16 bytes of one key's row), all of a wave's keys asked
-// for at once. A lane has four keys of one row; the rows' sum is over 16 lanes.
+// At most 16 rows: S^T = K Q^T by 16x16x32 products, a lane holding 16 bytes of one key's row
+// of the first operand. All of a wave's keys are asked for at once. Rows of 256 bytes come in
+// loads of 1 KiB that follow each other in memory, kept in no cache, and each block of 16 is
+// turned into operands through LDS of the wave's own, without a barrier; others are loaded as
+// operands, every line by two loads. A lane then has four keys of one row; the rows' sum is
+// over 16 lanes. Bound by reading K: 8 requests of 32 K tokens, 8 heads of 128, 90 us (6.0 TB/s;
+// loaded as operands 104, those uncached 111); heads of 64, 128 K tokens 213 (5.0 TB/s, turned
+// 215); latent, 32 of 32 K 235 (5.1 TB/s; uncached 283, turned 295: fewer waves).
+template <int DK>
+struct FewCfg {
+  static constexpr int NB = weigh_tile_keys(DK == 128 ? kWFew128 : DK == 64 ? kWFew64 : kWFewMla) / 64;  // blocks of a wave
+  static constexpr int ROW = 2 * DK, LOADS = 16 * ROW / 1024;
+  static constexpr bool TURN = DK == 128;
+  static_assert(!TURN || ROW == 256, "sixteen pieces of 16 bytes a row");
+};
+
 template <int DK, int MODE>
 __global__ __launch_bounds__(kWeighThreads) void weigh_few_kernel(const WeighArgs a) {
-  constexpr int KS = DK / 32, NB = DK == 128 ? 4 : DK == 64 ? 8 : 2;  // blocks of 16 keys of a wave
+  using C = FewCfg<DK>;
+  constexpr int KS = DK / 32, NB = C::NB;
+  __shared__ __attribute__((aligned(16))) char lds[C::TURN ? 4 * 16 * C::ROW : 16];
   const WeighUnit un = weigh_unit(a);
   if (un.none) return;
   const WeighReq &rq = *un.rq;
@@ -136,7 +151,6 @@ __global__ __launch_bounds__(kWeighThreads) void weigh_few_kernel(const WeighArg
   const int col = lane & 15, quad = lane >> 4;
   const uint32_t P = (uint32_t)a.g.page_tokens, b0 = (un.tile * 4 + wave) * (16 * NB);
   if (b0 >= rq.ctx) return;  // (no barrier below)
-  const uint8_t *const head = a.pool + (DK == 576 ? 0ull : (uint64_t)un.kvh * (4ull * P * DK)) + 16 * quad;
   uint32_t at[NB], slot[NB];
 #pragma unroll
   for (int n = 0; n < NB; ++n) {  // keys past the context: the last one (their sums are not stored)
@@ -151,17 +165,39 @@ __global__ __launch_bounds__(kWeighThreads) void weigh_few_kernel(const WeighArg
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const bf16x8 *>(qrow + 32 * ks);
   }
-  u32x4e kf[NB][KS];
+  const uint8_t *const head = a.pool + (DK == 576 ? 0ull : (uint64_t)un.kvh * (4ull * P * DK));
+  u32x4e kf[NB][C::LOADS];
 #pragma unroll
   for (int n = 0; n < NB; ++n) {
-    const u32x4e *const k = reinterpret_cast<const u32x4e *>(head + ((uint64_t)at[n] << 8) + (uint64_t)slot[n] * (2 * DK));
+    const uint64_t row_at = (uint64_t)(uintptr_t)head + ((uint64_t)at[n] << 8) + (uint64_t)slot[n] * C::ROW;  // of key `col`
+    const int lo = (int)(uint32_t)row_at, hi = (int)(uint32_t)(row_at >> 32);
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) kf[n][ks] = k[4 * ks];
+    for (int i = 0; i < C::LOADS; ++i) {
+      if (C::TURN) {  // row 4 i + quad, piece col
+        const int key = 4 * (4 * i + quad);
+        const uint64_t from = (uint64_t)(uint32_t)__builtin_amdgcn_ds_bpermute(key, hi) << 32 |
+                              (uint32_t)__builtin_amdgcn_ds_bpermute(key, lo);
+        kf[n][i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4e *>(from) + col);
+      } else {
+        kf[n][i] = reinterpret_cast<const u32x4e *>(row_at)[4 * i + quad];
+      }
+    }
   }
+  char *const mine = lds + wave * (16 * C::ROW);
 #pragma unroll
   for (int n = 0; n < NB; ++n) {
     const uint32_t k0 = b0 + 16 * n;
     if (k0 >= rq.ctx) return;
+    if constexpr (C::TURN) {  // (pieces swapped by the row: 16 rows at one piece meet no bank twice)
+#pragma unroll
+      for (int i = 0; i < C::LOADS; ++i)
+        *reinterpret_cast<u32x4e *>(mine + (4 * i + quad) * C::ROW + 16 * (col ^ (4 * i + quad))) = kf[n][i];
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+        kf[n][ks] = *reinterpret_cast<const u32x4e *>(mine + col * C::ROW + 16 * ((4 * ks + quad) ^ col));
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
     f32x4 sc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks)
@@ -190,20 +226,25 @@ __global__ __launch_bounds__(kWeighThreads) void weigh_few_kernel(const WeighArg
 
 // --------------------------------------------------------------- many rows
 
-// K in registers (the products' first operand), queries and their log-sum-exp streamed past
-// them through LDS, a ring of four steps of 64 rows (MLA 32). Scores are transposed as in the attention kernels: a
-// lane holds one row's scores, and adds their exponentials to sums of its own, one for
-// every key; the lanes' sums meet at the end.
-// head_dim 64 and 128: 64 keys a wave, turns of 32 rows by 32x32x16 products. A score costs
-// a multiply-add, an exponential and an addition, 16 cycles a wave for 64 of them, and its
-// products 16 too (head_dim 128): plain scores are one turn behind their products, so that
-// the vector unit and the matrix cores work at once (the compiler left to itself starts the
-// exponentials when the products are done), and whatever else the vector unit does in a
-// turn counts: rows' places are formed once and moved on block by block, and masks looked
-// at only where some row of the block does not see some key.
-// MLA: 32 keys a wave, 144 registers, turns of 16 rows by 16x16x32 products, whose few
-// scores leave registers to read fragments ahead. LDS bounds it with the matrix cores: a
-// fragment of 1 KiB feeds 32 cycles of products.
+// K in registers (the products' first operand), queries and their log-sum-exps streamed past
+// them through LDS, a ring of steps of 64 rows (MLA 32). Scores are transposed as in the
+// attention kernels: a lane holds one row's scores, and adds their exponentials to sums of its
+// own, one for every key; the lanes' sums meet at the end. Turns of 16 rows, 16x16x32 products.
+// head_dim 64 and 128: 64 keys a wave, three workgroups a CU (LDS: a ring of three steps for
+// 128). A score costs a multiply-add, an exponential and an addition, 16 cycles a wave for 64
+// of them, and its products 16 too (head_dim 128): plain scores are one turn behind their
+// products, so that the vector unit and the matrix cores work at once (the compiler left to
+// itself starts the exponentials when the products are done), and masks are looked at only
+// where some row of a step does not see some key. Bound by the products with the vector work
+// in their shadow: the last 5,000 tokens of 8 K and of 5 K, 32 heads over 8, 364 to 385 us, 0.9
+// PFLOP/s where a large library product reaches 1.39; without the exponentials 320, without
+// the products 190, without new queries 350. 32 rows by 32x32x16 products took 655 us where
+// these take 450; an inner loop without a moved register, its turns apart from those with a
+// mask, took as long.
+// MLA: 32 keys a wave, 144 registers, whose few scores leave registers to read fragments
+// ahead. LDS bounds it with the matrix cores: a fragment of 1 KiB feeds 32 cycles of products.
+// 64 rows past 256 keys take 5 us (0.97 PFLOP/s with every CU full); 64 tokens of four contexts
+// of 22 K in all, 16 heads, 41 us, of which a third goes to 174 units on 256 CUs.
 template <int DK>
 struct WeighCfg {
   static constexpr bool MLA = DK == 576;
@@ -484,7 +525,8 @@ __global__ __launch_bounds__(WeighCfg<DK>::THREADS, DK == 576 ? 2 : 3) void weig
 // ------------------------------------------------------------ vector path
 
 // A thread per key, eight rows at a time from LDS, for every geometry. Bound by the vector
-// unit and each thread's own row reads; it serves the geometries without a matrix kernel.
+// unit and each thread's own row reads (a block of 64 rows takes 20 us and more); it serves the
+// geometries without a matrix kernel.
 __global__ __launch_bounds__(kWeighThreads) void weigh_vec_kernel(const WeighArgs a) {
   constexpr int R = 8;
   extern __shared__ float qs[];  // [R][d_k]
@@ -541,7 +583,8 @@ __global__ __launch_bounds__(kWeighThreads) void weigh_vec_kernel(const WeighArg
 
 // ------------------------------------------------------------------- join
 
-// The parts of keys whose rows were cut, in order. A thread per KV head and key.
+// The parts of keys whose rows were cut, in order. A thread per KV head and key. Bound by its
+// launch (13 K tokens of 8 heads in 8 parts: 5 us).
 __global__ __launch_bounds__(kWeighThreads) void weigh_join_kernel(const WeighJoinArgs a) {
   const int r = sorted_search(a.n_req, blockIdx.x, [&](int i) { return a.req[i].block_begin; });
   const WeighJoinArgs::Req &rq = a.req[r];
