@@ -179,7 +179,7 @@ __global__ __launch_bounds__(kCopyThreads) void kv_append_rope_kernel(const Appe
   const int32_t *const depth = a.depth ? a.depth + rq.src_off / (uint32_t)g.row_elems + row0 : nullptr;
   for (uint32_t i = threadIdx.x; i < nrows * pairs; i += kCopyThreads) {
     const uint32_t t = i / pairs;
-    const int64_t at = first + (depth ? (int64_t)depth[t] : (int64_t)row0 + t);
+    const int64_t at = first + (depth ? min((uint32_t)depth[t], rq.n_new - 1) : row0 + t);
     turn[i] = rope_turn(rope, at, (int32_t)(i - t * pairs));
   }
   __syncthreads();

@@ -274,6 +274,30 @@ def test_steps_place_rows_turned_by_depth(name, layout, rot):
     sc.close()
 
 
+def test_depths_out_of_range_count_as_the_last():
+    """Positions of queries and of rotated keys, and distances of keys, alike."""
+    print("[case] depths out of range", flush=True)
+    n, k = 90, 7
+    rope = cpl.Rope(64, layout="half")
+    slopes = torch.linspace(0.5, 0.01, 16, device="cuda")
+    mask, depth = device_tree([[-1, 0, 0, 1, 1, 2, 2]])
+    for at, bad in ((3, -1), (5, 1000), (0, -(2 ** 31)), (6, 2 ** 31 - 1)):
+        held = []
+        for value in (bad, k - 1):
+            sc = Scene("gqa8x2d128", [n], seed=12, room=20)
+            new = sc.normal(k, sc.row, sigma=0.7)
+            q, out, lse = sc.buffers(k)
+            d = depth.clone()
+            d[at] = value
+            sc.pool.tree_step(sc.ids, [k], new, q, out, lse, mask, d, rope=rope, slopes=slopes[:sc.hq])
+            held.append((out, lse, sc.held(sc.ids[0], n + k)))
+            torch.cuda.synchronize()
+            sc.close()
+        for x, y in zip(*held):
+            assert torch.equal(x, y)
+    rope.destroy()
+
+
 def test_many_requests_take_several_launches():
     lens = [40 + (37 * i) % 90 for i in range(100)]
     sc = Scene("gqa6x2d64", lens, seed=12)
