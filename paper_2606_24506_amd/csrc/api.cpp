@@ -2914,8 +2914,8 @@ cp_status run_moves(cp_pool *p, const std::vector<MoveItem> &items, int how, con
         ents += k;
         done = part ? done + k : 0;
         x.per_layer = column_blocks(g, kKeepCols);
-      } else if (how == 1) {
-        x.per_layer = column_blocks(g, kMoveCols);
+      } else if (how != 2) {
+        x.per_layer = column_blocks(g, how == 1 ? kMoveCols : kMoveFewCols);
       } else {
         const uint32_t rows = apart_rows((uint32_t)g.row_elems / 8);
         x.per_layer = (x.n - x.k0 + rows - 1) / rows;
@@ -3193,7 +3193,8 @@ cp_status cp_kv_evict(cp_pool *p, int32_t n, const int32_t *ids, const int64_t *
       if (err != hipSuccess) rc = hip_fail(err, "eviction launch");
     }
     if (rc == CP_OK && !carried) rc = push_ptes(p, lo, hi, s);
-    if (rc == CP_OK) rc = run_moves(p, place, 1, nullptr, s);
+    const int64_t wide = (int64_t)place.size() * column_blocks(g, kMoveCols) * g.layers;
+    if (rc == CP_OK) rc = run_moves(p, place, 4 * wide <= p->num_cus ? 3 : 1, nullptr, s);
     if (rc == CP_OK) rc = run_moves(p, apart, 2, nullptr, s);
     if (rc) p->broken = true;
     return rc;

@@ -15,6 +15,9 @@ constexpr int kEvictEntMax = 448;  // new page-table entries that one launch of 
 constexpr int kSelectThreads = 1024;
 constexpr int kKeepThreads = 256, kKeepCols = 16, kKeepUnroll = 4;     // cp_request_keep
 constexpr int kMoveThreads = 1024, kMoveCols = 8, kMoveUnroll = 8;     // evictions in place
+// ... where workgroups of kMoveCols columns are at most a quarter of the card's CUs (64 of them
+// 11.7 us, with half of the columns 10.0; 36 11.4 and 9.0; but 192 26 and 28, 224 26 and 32)
+constexpr int kMoveFewCols = 4;
 constexpr int kApartThreads = 256, kApartUnroll = 4;                   // ... into pages of their own
 // Rows of a workgroup of those (segs: 16-byte pieces of a row).
 constexpr uint32_t apart_rows(uint32_t segs) {

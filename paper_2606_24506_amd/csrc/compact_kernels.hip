@@ -277,7 +277,8 @@ CP_DEV Column column_of(const GeomK &g, uint32_t seg) {
 // and those of later steps lie behind what this one writes (list entries rise: entry k is at
 // least k). So no workgroup waits for another. Bound by the round trips of a step (list,
 // page table, row), each asked for by all of a thread's rows at once: 2,048 of 16 K and 1,125
-// of 9 K tokens, 8 heads of 128, 12 us (13 MB read and written; 142 with one row in flight);
+// of 9 K tokens, 8 heads of 128, 10 us (13 MB read and written; 142 with one row in flight),
+// half of four 4 K contexts in 16 layers 205 (5.2 TB/s);
 // accepted paths of 4 requests 3 us, 31 with the lists' loads in a row.
 template <int THREADS, int COLS, int UNROLL>
 __global__ __launch_bounds__(THREADS) void move_kernel(const MoveArgs a) {
@@ -377,7 +378,7 @@ hipError_t launch_evict_select(const EvictArgs &a, hipStream_t stream) {
   return hipGetLastError();
 }
 
-// how: 0 short lists in the arguments, 1 in place, 2 apart
+// how: 0 short lists in the arguments, 1 in place, 2 apart, 3 in place with few workgroups
 hipError_t launch_moves(const MoveArgs &a, int how, hipStream_t stream) {
   if (a.n_blocks <= 0) return hipSuccess;
   const dim3 grid((uint32_t)a.n_blocks);
@@ -385,6 +386,8 @@ hipError_t launch_moves(const MoveArgs &a, int how, hipStream_t stream) {
     hipLaunchKernelGGL((move_kernel<kKeepThreads, kKeepCols, kKeepUnroll>), grid, dim3(kKeepThreads), 0, stream, a);
   else if (how == 1)
     hipLaunchKernelGGL((move_kernel<kMoveThreads, kMoveCols, kMoveUnroll>), grid, dim3(kMoveThreads), 0, stream, a);
+  else if (how == 3)
+    hipLaunchKernelGGL((move_kernel<kMoveThreads, kMoveFewCols, kMoveUnroll>), grid, dim3(kMoveThreads), 0, stream, a);
   else
     hipLaunchKernelGGL(move_apart_kernel, grid, dim3(kApartThreads), 0, stream, a);
   return hipGetLastError();
