@@ -274,6 +274,30 @@ def test_steps_place_rows_turned_by_depth(name, layout, rot):
     sc.close()
 
 
+def test_steps_of_requests_without_a_tree():
+    """Their cursors move on, and the others' trees are as alone."""
+    print("[case] tree step, some without", flush=True)
+    lens, sizes = [20, 64, 33], [0, 6, 0]
+    held = []
+    mask, depth = device_tree([make_tree(6, 2)])
+    for some in ([0, 1, 2], [1]):
+        sc = Scene("gqa8x2d128", lens, seed=13, room=20, layers=2)
+        for layer in range(2):
+            sc.gen.manual_seed(50 + layer)
+            new = sc.normal(6, sc.row, sigma=0.7)
+            q, out, lse = sc.buffers(6)
+            sc.pool.tree_step([sc.ids[i] for i in some], [sizes[i] for i in some], new, q, out, lse, mask, depth)
+            held.append((out, lse))
+            want = (1, 0) if layer == 0 else (0, 0)
+            assert all(sc.pool.cursor(sc.ids[i]) == want for i in some if i != 1)
+        assert [sc.pool.ctx_len(i) for i in sc.ids] == [20, 70, 33]
+        held.append((sc.held(sc.ids[1], 70, layers=2),) * 2)
+        torch.cuda.synchronize()
+        sc.close()
+    for x, y in zip(held[:3], held[3:]):
+        assert torch.equal(x[0], y[0]) and torch.equal(x[1], y[1])
+
+
 def test_depths_out_of_range_count_as_the_last():
     """Positions of queries and of rotated keys, and distances of keys, alike."""
     print("[case] depths out of range", flush=True)
