@@ -2903,16 +2903,10 @@ cp_status run_moves(cp_pool *p, const std::vector<MoveItem> &items, int how, con
       if (mi < 0 && nm == kMaxLaunchModels) break;
       MoveReq x = it.rq;
       x.k0 += done;
-      bool part = false;
+      uint32_t listed = x.n - x.k0;  // entries that travel with this launch (how 0)
       if (how == 0) {
         if (ents == (uint32_t)kMoveEntMax) break;
-        const uint32_t k = std::min(x.n - x.k0, (uint32_t)kMoveEntMax - ents);
-        part = k < x.n - x.k0;
-        for (uint32_t e = 0; e < k; ++e) a.ent[ents + e] = (uint32_t)lists[it.rq.ent0 + done + e];
-        x.ent0 = ents;
-        x.n = x.k0 + k;
-        ents += k;
-        done = part ? done + k : 0;
+        listed = std::min(listed, (uint32_t)kMoveEntMax - ents);
         x.per_layer = column_blocks(g, kKeepCols);
       } else if (how != 2) {
         x.per_layer = column_blocks(g, how == 1 ? kMoveCols : kMoveFewCols);
@@ -2922,6 +2916,14 @@ cp_status run_moves(cp_pool *p, const std::vector<MoveItem> &items, int how, con
       }
       const int64_t add = (int64_t)x.per_layer * g.layers;
       if (blocks > 0 && blocks + add > kMaxExtUnits) break;  // (a launch has less than 2^32 threads)
+      const bool part = listed < x.n - x.k0;
+      if (how == 0) {
+        for (uint32_t e = 0; e < listed; ++e) a.ent[ents + e] = (uint32_t)lists[it.rq.ent0 + done + e];
+        x.ent0 = ents;
+        x.n = x.k0 + listed;
+        ents += listed;
+        done = part ? done + listed : 0;
+      }
       if (mi < 0) {
         mi = model_map[it.model] = nm;
         a.geom[nm++] = geom_k(g, p->st.page_tokens());
