@@ -666,7 +666,7 @@ cp_status cp_request_truncate(cp_pool *p, int32_t n, const int32_t *ids, const i
                     (long long)new_len[i]);
       if (r.cursor != 0 || r.inflight)
         return fail(CP_EINVAL, "request %d has a token in flight; finish its decode steps first", ids[i]);
-      any = any || new_len[i] < r.ctx_len;
+      any = any || new_len[i] < r.ctx_len || (new_len[i] == 0 && r.dropped);  // (its position starts again)
     }
     if (!any) return CP_OK;
     if (!p->host_only && (rc = earlier_error())) return rc;
@@ -2977,7 +2977,7 @@ cp_status cp_request_keep(cp_pool *p, int32_t n, const int32_t *ids, const int64
       }
       len[(size_t)i] = first[i] + n_keep[i];
       from[(size_t)i] = first[i] + stay;
-      any = any || len[(size_t)i] < r.ctx_len;
+      any = any || len[(size_t)i] < r.ctx_len || (len[(size_t)i] == 0 && r.dropped);  // (its position starts again)
       at += n_keep[i];
     }
     if (!any) return CP_OK;

@@ -50,3 +50,53 @@ for r in ids:
     p.close(r)
 p.destroy()
 """, queued)
+
+
+EMPTIED = """
+p, m = heads_pool()
+a, b, c = p.open(m, 64), p.open(m, 64), p.open(m, 64)
+W = lambda n: rows(rec(n))
+def emptied(r, n):  # of n tokens by an eviction
+    p.append([r], [n], at, 0)
+    assert LIB.cp_kv_evict(p.handle, 1, I32(r), I64(0), W(n), None, None) == cpl.CP_OK
+    assert (p.ctx_len(r), p.position(r)) == (0, n)
+"""
+
+
+@pytest.mark.parametrize("cut, of_b, of_c", [
+    ("p.truncate([a], [0], 0)", 10, 5), ("p.keep([a], [0], [0], [], 0)", 10, 5),
+    ("p.truncate([b, a], [9, 0], 0)", 9, 5), ("p.keep([b, a], [9, 0], [0, 0], [], 0)", 9, 5),
+    ("p.truncate([b, a], [10, 0], 0)", 10, 5), ("p.keep([b, a], [0, 0], [10, 0], range(10), 0)", 10, 5),
+    ("p.truncate([a, c], [0, 0], 0)", 10, 0), ("p.keep([c, a], [0, 0], [0, 0], [], 0)", 10, 0)])
+def test_a_request_cut_to_nothing_starts_at_0(cut, of_b, of_c, queued):
+    """... also one that an eviction had left nothing of, alone and in company: new keys are
+    turned by their places from 0 on."""
+    run(MORE + EMPTIED + f"""
+p.append([b], [10], at, 0)
+emptied(a, 20)
+emptied(c, 5)
+{cut}
+assert (p.ctx_len(a), p.position(a)) == (0, 0)
+assert (p.position(b), p.ctx_len(b), p.position(c), p.ctx_len(c)) == ({of_b}, {of_b}, {of_c}, 0)
+p.append([a], [7], at, 0)
+assert p.position(a) == 7
+usable(p, [b, a, c])
+""", queued)
+
+
+def test_an_evicted_request_keeps_its_position_otherwise(queued):
+    run(MORE + EMPTIED + """
+emptied(a, 20)
+p.truncate([b], [0], 0)
+p.keep([], [], [], [], 0)
+p.truncate([], [], 0)
+assert (p.ctx_len(a), p.position(a)) == (0, 20)
+p.append([a], [7], at, 0)
+assert p.position(a) == 27
+p.truncate([a], [3], 0)
+assert p.position(a) == 23
+p.keep([a], [0], [2], [0, 2], 0)
+assert p.position(a) == 22
+p.append([b], [10], at, 0)
+usable(p, [b, a, c])
+""", queued)
