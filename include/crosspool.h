@@ -36,8 +36,10 @@
  *   - Calls that enqueue GPU work (append, decode, gather) return once the
  *     work is enqueued; host-side metadata (context lengths, page tables) is
  *     already updated at return, so append-then-decode on one stream is
- *     ordered. Launch failures return CP_EHIP; device faults surface at the
- *     caller's next synchronisation.
+ *     ordered. (Page-table entries of many new pages are copied from memory of
+ *     the pool's, which goes round: a call may wait for the copies of calls
+ *     long before it.) Launch failures return CP_EHIP; device faults surface
+ *     at the caller's next synchronisation.
  *   - A pool is not thread-safe: the caller serialises calls on one pool.
  *     Decode calls on one pool must not overlap on the GPU (one stream, or
  *     the caller orders streams), because they share the pool's workspace.

@@ -100,3 +100,120 @@ assert p.position(a) == 22
 p.append([b], [10], at, 0)
 usable(p, [b, a, c])
 """, queued)
+
+
+STAGED = """
+p = cpl.Pool(page_tokens=P, pool_bytes=64 << 20, chunk_bytes=1 << 16, device=0)
+m = p.register(cpl.CP_KIND_GQA, 2 * HKV, HKV, head_dim=64, n_layers=LAYERS)
+def evict(r, n, keep):
+    w = (ctypes.c_float * (n * HKV * LAYERS))()
+    x = rows(cp_token_rows(ctypes.addressof(w), n, n, n * HKV))
+    assert LIB.cp_kv_evict(p.handle, 1, I32(r), I64(keep), x, None, None) == cpl.CP_OK
+fake.late_copies(1)
+"""
+CLOSE = """
+for r in ids:
+    p.close(r)
+p.destroy()
+"""
+REWRITES = {
+    "a prompt that a fork keeps is evicted, its entries being on the way": """
+ids = a, b = [p.open(m, 4000) for _ in range(2)]
+p.append([a], [4000], at, 0)
+p.fork([a], [b], None, 0)
+evict(a, 4000, 1600)
+""",
+    "branches evicted twice": """
+ids = a, b, c = [p.open(m, 4000) for _ in range(3)]
+fake.late_copies(0)
+p.append([a], [4000], at, 0)
+fake.late_copies(1)
+p.fork([a], [b], None, 0)
+evict(b, 4000, 2400)
+p.fork([b], [c], None, 0)
+evict(b, 2400, 2000)
+""",
+    "drafted rows on the way are dropped, and placed on other pages": """
+ids = a, b = [p.open(m, 400) for _ in range(2)]
+fake.late_copies(0)
+p.append([a, b], [4, 4], at, 0)
+fake.late_copies(1)
+for _ in range(LAYERS):
+    p.extend_step([a, b], [9, 9], at, at, at, at, 0)
+p.truncate([a, b], [4, 4], 0)
+for _ in range(LAYERS):
+    p.extend_step([b, a], [9, 9], at, at, at, at, 0)
+""",
+    "an append on the way is dropped, and its pages are another's then": """
+ids = a, b = [p.open(m, 2000) for _ in range(2)]
+p.append([a], [2000], at, 0)
+p.truncate([a], [0], 0)
+p.append([b], [2000], at, 0)
+p.append([a], [2000], at, 0)
+""",
+}
+
+
+@pytest.mark.parametrize("case", sorted(REWRITES))
+def test_page_table_entries_on_the_way_do_not_change(case, queued):
+    """New entries go to the device by copies that run behind the stream's earlier work, from
+    memory that the host fills again for later calls."""
+    run(MORE + STAGED + REWRITES[case] + """
+fake.hipDeviceSynchronize()
+assert fake.copies() > 1
+assert fake.changed_copies() == 0, fake.changed_copies()
+""" + CLOSE, queued)
+
+
+BIG = STAGED.replace("64 << 20", "1 << 30") + """
+ids = [p.open(m, 4000) for _ in range(40)]
+waited = fake.host_waits()
+"""
+
+
+def test_copies_on_the_way_wait_for_memory_alone(queued):
+    run(MORE + BIG + """
+for n in (1600, 800, 800):
+    for r in ids:
+        p.append([r], [n], at, 0)
+    if n == 1600:  # 56,000 entries on the way, of 65,536 that there is memory for
+        assert (fake.copies(), fake.host_waits()) == (40, waited)
+assert fake.copies() == 120 and fake.host_waits() > waited and fake.changed_copies() == 0
+fake.hipDeviceSynchronize()
+waited = fake.host_waits()
+for order in (ids, ids[::-1], ids):  # one copy over every plane: memory grows once
+    p.truncate(ids, [1600] * 40, 0)
+    p.append(order, [2400] * 40, at, 0)
+assert (fake.copies(), fake.host_waits()) == (123, waited)
+fake.hipDeviceSynchronize()
+assert fake.changed_copies() == 0
+""" + CLOSE, queued)
+
+
+def test_without_memory_a_copy_has_run_when_the_call_returns(queued):
+    run(MORE + BIG + """
+fake.fake_no_memory(1)
+p.append(ids, [4000] * 40, at, 0)
+assert (fake.copies(), fake.host_waits()) == (1, waited + 1)
+p.truncate(ids, [0] * 40, 0)
+p.append(ids[::-1], [4000] * 40, at, 0)
+assert (fake.copies(), fake.host_waits(), fake.changed_copies()) == (2, waited + 2, 0)
+fake.fake_no_memory(0)
+""" + CLOSE, queued)
+
+
+def test_copies_into_graphs_read_the_table(queued):
+    """... as it was last copied, at every replay, and wait for nothing."""
+    run(MORE + STAGED + """
+ids = a, b = [p.open(m, 2000) for _ in range(2)]
+fake.capturing(1)
+waited = fake.host_waits()
+p.append([a], [2000], at, 0)
+fake.capturing(0)
+p.truncate([a], [0], 0)
+p.append([b], [2000], at, 0)
+p.append([a], [2000], at, 0)
+assert fake.host_waits() == waited
+fake.hipDeviceSynchronize()
+assert fake.changed_copies() == 1  # the graph's finds what is there now
+""" + CLOSE, queued)
