@@ -37,9 +37,9 @@
  *     work is enqueued; host-side metadata (context lengths, page tables) is
  *     already updated at return, so append-then-decode on one stream is
  *     ordered. (Page-table entries of many new pages are copied from memory of
- *     the pool's, which goes round: a call may wait for the copies of calls
- *     long before it.) Launch failures return CP_EHIP; device faults surface
- *     at the caller's next synchronisation.
+ *     the pool's: a call that would fill it again from the start waits for the
+ *     device.) Launch failures return CP_EHIP; device faults surface at the
+ *     caller's next synchronisation.
  *   - A pool is not thread-safe: the caller serialises calls on one pool.
  *     Decode calls on one pool must not overlap on the GPU (one stream, or
  *     the caller orders streams), because they share the pool's workspace.

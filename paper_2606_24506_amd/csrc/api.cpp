@@ -128,18 +128,12 @@ struct cp_pool {
   uint32_t *dev_pte = nullptr;
   uint32_t *pin_pte = nullptr;  // pinned page table, which copies into graphs read
   bool pin_read = false;        // there are such
-  // Pinned memory that page-table entries are copied from, filled round and round: a part
-  // again only when the copy that reads it has run.
+  // Pinned memory that page-table entries are copied from, filled round and round: again
+  // from the start only when every copy that reads it has run.
   struct Staging {
-    struct Part {
-      uint64_t lo, hi;
-      hipEvent_t done;  // NULL: none could be recorded
-    };
-    static constexpr uint64_t kLeast = 1 << 16;
+    static constexpr uint64_t kLeast = 1 << 18;
     uint32_t *at = nullptr;
     uint64_t cap = 0, next = 0;  // entries
-    std::vector<Part> parts;     // of copies that may still be on their way
-    std::vector<hipEvent_t> events;   // not in use
     std::vector<uint32_t *> outgrown;  // freed with the pool
   } stage;
   uint32_t *queue = nullptr;    // work-queue counters
@@ -500,9 +494,6 @@ cp_status cp_pool_destroy(cp_pool *p) {
     if (p->pin_pte) (void)hipHostFree(p->pin_pte);
     if (p->stage.at) (void)hipHostFree(p->stage.at);
     for (uint32_t *x : p->stage.outgrown) (void)hipHostFree(x);
-    for (const cp_pool::Staging::Part &x : p->stage.parts)
-      if (x.done) (void)hipEventDestroy(x.done);
-    for (hipEvent_t e : p->stage.events) (void)hipEventDestroy(e);
     if (p->queue) (void)hipFree(p->queue);
     for (void *b : {(void *)p->dev_stack, (void *)p->dev_top, (void *)p->dev_pop, (void *)p->dev_geo,
                     (void *)p->dev_layer, (void *)p->dev_entry})
@@ -814,77 +805,30 @@ cp_status check_ids(cp_pool *p, int32_t n, const int32_t *ids) {
   return CP_OK;
 }
 
-// Forgets parts whose copies have run. Asked of the events, but not while an error of the
-// caller's waits to be read: an event that is not ready would replace it.
-void forget_parts(cp_pool::Staging *t) {
-  const hipError_t waits = hipPeekAtLastError();
-  if (waits != hipSuccess && waits != hipErrorNotReady) return;
-  size_t kept = 0;
-  for (const cp_pool::Staging::Part &x : t->parts) {
-    if (x.done && hipEventQuery(x.done) == hipSuccess)
-      t->events.push_back(x.done);
-    else
-      t->parts[kept++] = x;
-  }
-  t->parts.resize(kept);
-  (void)hipGetLastError();
-}
-
-// Room for n entries to be copied from, once the copies of those there before have run.
-// NULL: there is none.
+// Room for n entries to be copied from, which no copy reads. NULL: there is none. Once
+// round waits for the device; sixteen of the largest copies fit a round (two where
+// those would take more than 64 MiB). (An event behind every copy instead cost an append
+// of 25 K tokens 4 of 94 us.)
 uint32_t *stage_room(cp_pool::Staging *t, uint64_t n) {
-  constexpr uint64_t kCopies = 4;  // of one size, on their way at once
-  if (kCopies * n > t->cap) {
-    const uint64_t cap = kCopies * n;
+  const uint64_t round = std::max(2 * n, std::min<uint64_t>(16 * n, 1 << 24));
+  if (round > t->cap) {
     uint32_t *at = nullptr;
-    if (hipHostMalloc((void **)&at, cap * 4, hipHostMallocDefault) == hipSuccess) {
+    if (hipHostMalloc((void **)&at, round * 4, hipHostMallocDefault) == hipSuccess) {
       if (t->at) t->outgrown.push_back(t->at);
-      for (const cp_pool::Staging::Part &x : t->parts)
-        if (x.done) t->events.push_back(x.done);
-      t->parts.clear();
       t->at = at;
-      t->cap = cap;
+      t->cap = round;
       t->next = 0;
     } else {
       (void)hipGetLastError();
       if (n > t->cap) return nullptr;
     }
   }
-  constexpr size_t kLook = 16;  // parts that are not worth a question
-  if (t->parts.size() >= kLook) forget_parts(t);
-  if (t->next + n > t->cap) t->next = 0;
-  const uint64_t lo = t->next, hi = lo + n;
-  for (size_t i = 0; i < t->parts.size();) {
-    const cp_pool::Staging::Part x = t->parts[i];
-    if (x.hi <= lo || hi <= x.lo) {
-      ++i;
-      continue;
-    }
-    if ((x.done ? hipEventSynchronize(x.done) : hipDeviceSynchronize()) != hipSuccess) return nullptr;
-    if (x.done) t->events.push_back(x.done);
-    t->parts.erase(t->parts.begin() + (ptrdiff_t)i);
+  if (t->next + n > t->cap) {
+    if (hipDeviceSynchronize() != hipSuccess) return nullptr;
+    t->next = 0;
   }
-  t->next = hi;
-  return t->at + lo;
-}
-
-// Behind the copy that reads `n` entries at `at`.
-void stage_copied(cp_pool::Staging *t, const uint32_t *at, uint64_t n, hipStream_t s) {
-  hipEvent_t done = nullptr;
-  if (!t->events.empty()) {
-    done = t->events.back();
-    t->events.pop_back();
-  } else if (hipEventCreateWithFlags(&done, hipEventDisableTiming) != hipSuccess) {
-    (void)hipGetLastError();
-    done = nullptr;
-  }
-  if (done && hipEventRecord(done, s) != hipSuccess) {
-    (void)hipGetLastError();
-    (void)hipEventDestroy(done);
-    done = nullptr;
-  }
-  const uint64_t lo = (uint64_t)(at - t->at);
-  t->parts.push_back(cp_pool::Staging::Part{lo, lo + n, done});
+  t->next += n;
+  return t->at + (t->next - n);
 }
 
 // Copies page-table entries [lo, hi) to the device, as they are now: the copy runs behind
@@ -907,7 +851,6 @@ cp_status push_ptes(cp_pool *p, uint64_t lo, uint64_t hi, hipStream_t s) {
   if (at) std::memcpy(at, now, (size_t)n * 4);
   if (!at || p->pin_read) std::memcpy(p->pin_pte + lo, now, (size_t)n * 4);
   hipError_t e = hipMemcpyAsync(p->dev_pte + lo, at ? at : p->pin_pte + lo, (size_t)n * 4, hipMemcpyHostToDevice, s);
-  if (e == hipSuccess && at) stage_copied(&p->stage, at, n, s);
   if (e == hipSuccess && !at && eager) e = hipStreamSynchronize(s);  // (no memory of its own)
   return e == hipSuccess ? CP_OK : hip_fail(e, "page-table copy");
 }

@@ -53,15 +53,6 @@ hipError_t hipMemcpyAsync(void *d, const void *s, size_t n, int kind, hipStream_
 hipError_t hipDeviceSynchronize() { return ++g_waits, run_to(g_enqueued), 0; }
 hipError_t hipStreamSynchronize(hipStream_t) { return ++g_waits, run_to(g_enqueued), 0; }
 hipError_t hipStreamIsCapturing(hipStream_t, int *status) { return *status = g_capturing, 0; }
-hipError_t hipEventCreateWithFlags(void **e, unsigned) { return *e = new long(0), 0; }
-hipError_t hipEventRecord(void *e, hipStream_t) { return *static_cast<long *>(e) = g_enqueued, 0; }
-hipError_t hipEventSynchronize(void *e) { return ++g_waits, run_to(*static_cast<long *>(e)), 0; }
-hipError_t hipEventQuery(void *e) {
-  const bool done = g_queue.empty() || g_queue.front().number > *static_cast<long *>(e);
-  return done ? 0 : g_last = 600;  // hipErrorNotReady
-}
-hipError_t hipPeekAtLastError() { return g_last; }
-hipError_t hipEventDestroy(void *e) { return delete static_cast<long *>(e), 0; }
 hipError_t hipLaunchKernel(const void *, dim3_t, dim3_t, void **args, size_t, hipStream_t) {
   ++g_launches;
   if (g_launched) g_launched(args[0]);

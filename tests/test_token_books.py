@@ -165,7 +165,7 @@ assert fake.changed_copies() == 0, fake.changed_copies()
 """ + CLOSE, queued)
 
 
-BIG = STAGED.replace("64 << 20", "1 << 30") + """
+BIG = STAGED.replace("64 << 20", "2 << 30") + """
 ids = [p.open(m, 4000) for _ in range(40)]
 waited = fake.host_waits()
 """
@@ -173,30 +173,33 @@ waited = fake.host_waits()
 
 def test_copies_on_the_way_wait_for_memory_alone(queued):
     run(MORE + BIG + """
-for n in (1600, 800, 800):
+def fill(n):
     for r in ids:
         p.append([r], [n], at, 0)
-    if n == 1600:  # 56,000 entries on the way, of 65,536 that there is memory for
-        assert (fake.copies(), fake.host_waits()) == (40, waited)
-assert fake.copies() == 120 and fake.host_waits() > waited and fake.changed_copies() == 0
-fake.hipDeviceSynchronize()
-waited = fake.host_waits()
+fill(1600)
+assert (fake.copies(), fake.host_waits()) == (40, waited)
+for i in range(1, 12):  # 56,000 entries each time, of 262,144 that there is memory for
+    p.truncate(ids, [0] * 40, 0)
+    fill(1600)
+assert fake.copies() == 480 and waited + 2 <= fake.host_waits() <= waited + 3
 for order in (ids, ids[::-1], ids):  # one copy over every plane: memory grows once
+    waited = fake.host_waits()
     p.truncate(ids, [1600] * 40, 0)
     p.append(order, [2400] * 40, at, 0)
-assert (fake.copies(), fake.host_waits()) == (123, waited)
+    assert fake.host_waits() == waited
 fake.hipDeviceSynchronize()
-assert fake.changed_copies() == 0
+assert (fake.copies(), fake.changed_copies()) == (483, 0)
 """ + CLOSE, queued)
 
 
 def test_without_memory_a_copy_has_run_when_the_call_returns(queued):
     run(MORE + BIG + """
+ids += [p.open(m, 4000) for _ in range(120)]  # 320,000 entries
 fake.fake_no_memory(1)
-p.append(ids, [4000] * 40, at, 0)
+p.append(ids, [4000] * 160, at, 0)
 assert (fake.copies(), fake.host_waits()) == (1, waited + 1)
-p.truncate(ids, [0] * 40, 0)
-p.append(ids[::-1], [4000] * 40, at, 0)
+p.truncate(ids, [0] * 160, 0)
+p.append(ids[::-1], [4000] * 160, at, 0)
 assert (fake.copies(), fake.host_waits(), fake.changed_copies()) == (2, waited + 2, 0)
 fake.fake_no_memory(0)
 """ + CLOSE, queued)
