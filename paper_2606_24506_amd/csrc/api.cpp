@@ -807,8 +807,8 @@ cp_status check_ids(cp_pool *p, int32_t n, const int32_t *ids) {
 
 // Room for n entries to be copied from, which no copy reads. NULL: there is none. Once
 // round waits for the device; sixteen of the largest copies fit a round (two where
-// those would take more than 64 MiB). (An event behind every copy instead cost an append
-// of 25 K tokens 4 of 94 us.)
+// those would take more than 64 MiB). (An append of 25 K tokens: 92 us, with an event behind
+// every copy 94, from memory that is always the same 90.)
 uint32_t *stage_room(cp_pool::Staging *t, uint64_t n) {
   const uint64_t round = std::max(2 * n, std::min<uint64_t>(16 * n, 1 << 24));
   if (round > t->cap) {
@@ -2911,13 +2911,19 @@ namespace {
 // taken, on success.
 cp_status prepare_cut(cp_pool *p, int32_t n, const int32_t *ids, const int64_t *from, const int64_t *new_len) {
   std::vector<int64_t> more, pages;
-  p->st.cut_cost(n, ids, from, new_len, p->st.virt(), &more, &pages);
-  bool exact = p->st.virt();  // (the bound first; a chunk is taken only for pages that fill it)
-  for (int32_t m = 0; m < p->st.n_models() && !exact; ++m) exact = pages[(size_t)m] > p->st.free_slots(m);
-  if (!p->st.virt() && (exact || !p->st.fits_budget(more))) p->st.cut_cost(n, ids, from, new_len, true, &more, &pages);
+  bool exact = p->st.virt() || p->dev_pages;  // (the bound first; a chunk is taken only for pages that fill it)
+  p->st.cut_cost(n, ids, from, new_len, exact, &more, &pages);
+  if (!exact) {
+    for (int32_t m = 0; m < p->st.n_models() && !exact; ++m) exact = pages[(size_t)m] > p->st.free_slots(m);
+    if (exact || !p->st.fits_budget(more)) p->st.cut_cost(n, ids, from, new_len, true, &more, &pages);
+  }
   if (!p->st.fits_budget(more)) return fail(CP_ENOSPC, "the pool page budget cannot take pages in the place of shared ones");
   std::vector<int32_t> carved;
   for (int32_t m = 0; m < p->st.n_models(); ++m) {
+    if (p->dev_pages && pages[(size_t)m] > 0) {  // the stack keeps what requests may take beside these
+      const cp_status rc = drain_stack(p, m, p->st.room_to_grow(m) - pages[(size_t)m]);
+      if (rc) return rc;
+    }
     const int64_t slots = p->st.virt() && more[(size_t)m] ? p->st.reserved(m) + more[(size_t)m] - p->st.allocated(m)
                                                           : pages[(size_t)m];
     if (!p->st.ensure_slots(m, slots, &carved)) {

@@ -552,6 +552,7 @@ void PoolState::cut_cost(int32_t n, const int32_t *ids, const int64_t *from, con
                          std::vector<int64_t> *reserved, std::vector<int64_t> *pages) const {
   reserved->assign(models_.size(), 0);
   pages->assign(models_.size(), 0);
+  std::vector<uint32_t> given;  // shared pages, for each request that gives them up
   for (int32_t i = 0; i < n; ++i) {
     const Request &r = reqs_[ids[i]];
     const int64_t keep = ceil_div(new_len[i], P_), k0 = std::min(from[i] / P_, keep);
@@ -561,12 +562,25 @@ void PoolState::cut_cost(int32_t n, const int32_t *ids, const int64_t *from, con
       own += (keep - k0) * r.layers;
       continue;
     }
-    for (int32_t l = 0; l < r.layers; ++l)
-      each_shared(pte_.data() + r.plane_base(l) + k0, r.pages_used - k0, [&](int64_t k) {
+    for (int32_t l = 0; l < r.layers; ++l) {
+      const uint32_t *const pt = pte_.data() + r.plane_base(l) + k0;
+      each_shared(pt, r.pages_used - k0, [&](int64_t k) {
         more += 1;
         own += k < keep - k0;
+        if (n > 1) given.push_back(pt[k]);
       });
+    }
   }
+  if (!exact) return;
+  // a page that every user gives up is freed, and owes nothing
+  std::sort(given.begin(), given.end());
+  for (size_t i = 0, j; i < given.size(); i = j) {
+    for (j = i + 1; j < given.size() && given[j] == given[i];) ++j;
+    if (j - i > sharers(given[i])) (*reserved)[(size_t)chunks_[given[i] / (chunk_bytes_ >> 8)].model] -= 1;
+  }
+  // ... but stands beside its replacements before
+  for (size_t m = 0; m < models_.size(); ++m)
+    (*reserved)[m] = std::max((*reserved)[m], acct_[m].used - acct_[m].in_stack + (*pages)[m] - acct_[m].reserved);
 }
 
 void PoolState::cut_own(int32_t id, int64_t from, int64_t new_len, std::vector<OwnPage> *copies) {

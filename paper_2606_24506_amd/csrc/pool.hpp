@@ -219,8 +219,10 @@ class PoolState {
   // call began are replaced (other requests of the call read them too). First, for all of
   // a call's: pages of their own (after ensure_slots); appends one record for each. Then
   // the old pages are given up, and each request truncated.
-  // cut_cost: what this adds to each model's `reserved` at most, before anything is given
-  // up, and the pages it allocates; not exact: at most that (as if every page were shared).
+  // cut_cost: the room beside each model's `reserved` that this needs, for what is promised
+  // behind it and for replaced pages beside their replacements (with a device stack that
+  // holds no more than it may then), and the pages it allocates; not exact: at most that
+  // (as if every page were shared, and every one with others).
   void cut_cost(int32_t n, const int32_t *ids, const int64_t *from, const int64_t *new_len, bool exact,
                 std::vector<int64_t> *reserved, std::vector<int64_t> *pages) const;
   void cut_own(int32_t id, int64_t from, int64_t new_len, std::vector<OwnPage> *copies);

@@ -2,12 +2,15 @@
 neighbours in the call, earlier work of the stream or its size could change (a
 stand-in for the HIP runtime, tests/c/queued_hip.cpp, or a host-only pool)."""
 import os
+import random
 import shutil
 import subprocess
 
 import pytest
 
 from paper_2606_24506_amd import build
+from paper_2606_24506_amd import crosspool as cpl
+from test_fork_truncate import P, ROW, grow, pool
 from test_token_calls import MORE, run
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -220,3 +223,109 @@ assert fake.host_waits() == waited
 fake.hipDeviceSynchronize()
 assert fake.changed_copies() == 1  # the graph's finds what is there now
 """ + CLOSE, queued)
+
+
+# ------------------------------------------------------- budgets of a call
+
+
+def test_a_prompt_and_its_fork_are_cut_in_one_call():
+    """Pages that only the call's requests show go back to the pool, and owe nothing."""
+    p = pool(chunks=2, pages_per_chunk=8)  # 16 pages
+    m = p.register(**ROW)
+    a, b = p.open(m, 8 * P), p.open(m, 8 * P)
+    for cut in ("keep", "truncate"):
+        grow(p, a, 8 * P)
+        p.fork([a], [b])
+        if cut == "keep":
+            p.keep([a, b], [0, 0], [P, P], [*range(P)] * 2)
+        else:
+            p.truncate([a, b], [P, P])
+        assert p.pages(a).tolist() == p.pages(b).tolist()
+        assert (p.stats()["pages_used"], p.stats()["pages_reserved"]) == (1, 15)
+        p.truncate([a, b], [0, 0])
+    grow(p, a, 8 * P)
+    p.fork([a], [b])
+    p.keep([a, b], [0, 0], [2, 3], [0, 9, 1, 2, 31])  # a page of its own each, beside the eight
+    assert not set(p.pages(a)) & set(p.pages(b)) and p.stats()["pages_reserved"] == 16
+    for r in (a, b):
+        grow(p, r, 8 * P - p.ctx_len(r))
+        p.close(r)
+    p.destroy()
+
+
+def cut_books(pages, reserve, first, lists):
+    """(pages promised after a call, pages that stand beside one another in it) from the pages
+    of every request, for the requests that the call cuts."""
+    users = {}
+    for x in pages.values():
+        for page in x:
+            users[page] = users.get(page, 0) + 1
+    had, own, shown = dict(users), 0, sum(len(x) for x in pages.values())
+    for r, f, keep in zip(lists, first, lists.values()):
+        stay = sum(t == k for k, t in enumerate(keep))
+        last = -(-(f + len(keep)) // P)
+        k0 = min((f + stay) // P, last)
+        moved = [page for page in pages[r][k0:last] if had[page] > 1]
+        own += len(moved)
+        shown -= len(pages[r]) - last
+        for page in moved + pages[r][last:]:
+            users[page] -= 1
+    return sum(n > 0 for n in users.values()) + own + reserve * len(pages) - shown, len(users) + own
+
+
+def test_only_calls_that_the_budget_cannot_hold_are_refused():
+    refused, together = (sum(x) for x in zip(*map(random_cuts, range(12))))
+    assert refused > 20 and together > 100
+
+
+def random_cuts(seed):
+    """(calls refused, calls that cut several requests that share)"""
+    rng = random.Random(seed)
+    total, reserve = 24, 10
+    p = pool(chunks=total // 8, pages_per_chunk=8)
+    m = p.register(**ROW)
+    ids, refused, together = [], 0, 0
+    for _ in range(400):
+        op = rng.random()
+        if op < 0.3 and len(ids) < 6:
+            try:
+                ids.append(p.open(m, reserve * P))
+                if len(ids) > 1:
+                    a = max(ids[:-1], key=p.ctx_len)
+                    p.fork([a], [ids[-1]], [p.ctx_len(a) // P * P])
+            except cpl.CrossPoolError as e:
+                assert e.status == cpl.CP_ENOSPC
+        elif not ids:
+            continue
+        elif op < 0.5:
+            r = rng.choice(ids)
+            grow(p, r, rng.randint(0, reserve * P - p.ctx_len(r)))
+        elif op < 0.65 and len(ids) > 1:
+            a, b = rng.sample(ids, 2)
+            if p.ctx_len(b) == 0:
+                p.fork([a], [b], [p.ctx_len(a) // P * P])
+        elif op < 0.7:
+            p.close(ids.pop(rng.randrange(len(ids))))
+        else:
+            some = rng.sample(ids, rng.randint(1, len(ids)))
+            n = {r: p.ctx_len(r) for r in some}
+            first = [rng.randint(0, n[r]) if rng.random() < 0.5 else 0 for r in some]
+            lists = {r: sorted(rng.sample(range(n[r] - f), rng.randint(0, n[r] - f))) if rng.random() < 0.6 else
+                     list(range(rng.randint(0, n[r] - f))) for r, f in zip(some, first)}
+            pages, before = {r: p.pages(r).tolist() for r in ids}, p.stats()
+            after, beside = cut_books(pages, reserve, first, lists)
+            try:
+                p.keep(some, first, [len(x) for x in lists.values()], [t for x in lists.values() for t in x])
+                assert max(after, beside) <= total and p.stats()["pages_reserved"] == after
+                together += len(some) > 1 and before["pages_used"] < sum(map(len, pages.values()))
+            except cpl.CrossPoolError as e:
+                assert e.status == cpl.CP_ENOSPC and max(after, beside) > total
+                assert (p.stats(), {r: p.pages(r).tolist() for r in ids}) == (before, pages)
+                refused += 1
+    for r in ids:  # what was admitted can be filled
+        grow(p, r, reserve * P - p.ctx_len(r))
+    for r in ids:
+        p.close(r)
+    assert p.stats()["pages_used"] == p.stats()["pages_reserved"] == 0
+    p.destroy()
+    return refused, together
