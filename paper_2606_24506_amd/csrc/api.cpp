@@ -806,12 +806,14 @@ cp_status check_ids(cp_pool *p, int32_t n, const int32_t *ids) {
 }
 
 // Room for n entries to be copied from, which no copy reads. NULL: there is none. Once
-// round waits for the device; sixteen of the largest copies fit a round (two where
-// those would take more than 64 MiB). (An append of 25 K tokens: 92 us, with an event behind
-// every copy 94, from memory that is always the same 90.)
+// round waits for the device; at least four of the largest copies fit a round (two
+// where those would take more than 64 MiB), and sixteen where it had to grow for them. (An
+// append of 25 K tokens: 92 us, with an event behind every copy 94, from memory that is
+// always the same 90.)
 uint32_t *stage_room(cp_pool::Staging *t, uint64_t n) {
-  const uint64_t round = std::max(2 * n, std::min<uint64_t>(16 * n, 1 << 24));
-  if (round > t->cap) {
+  constexpr uint64_t kEnough = 1 << 24;
+  if (std::max(2 * n, std::min(4 * n, kEnough)) > t->cap) {
+    const uint64_t round = std::max({2 * n, std::min(16 * n, kEnough), 2 * t->cap});
     uint32_t *at = nullptr;
     if (hipHostMalloc((void **)&at, round * 4, hipHostMallocDefault) == hipSuccess) {
       if (t->at) t->outgrown.push_back(t->at);
