@@ -69,6 +69,31 @@ struct EvictArgs {
   EvictReq req[kEvictMaxReq];
   uint32_t ent[kEvictEntMax];
 };
+
+// The choice's search for the k-th largest of a row's numbers (32 bits each, in the order
+// of the weights): those that it may still be, and which of them it is from the largest on.
+struct Search {
+  uint32_t lo, hi, need;
+};
+constexpr int kBins = 2048;  // counters of a pass: number x is counted by (x - lo) >> search_shift
+constexpr int search_shift(const Search &x) {
+  const int bits = 32 - __builtin_clz(x.hi - x.lo);  // lo < hi
+  return bits > 11 ? bits - 11 : 0;
+}
+// Behind a pass that found it in counter `bin`, which holds `in_bin`, as the left-th largest of
+// those. Does another pass have to follow? Each leaves a 2^11-th of the range, so that three are
+// the most whatever they count: none found it (in_bin 0) in a row that is written
+// meanwhile, and the search ends with what it has.
+constexpr bool search_narrow(Search *x, uint32_t bin, uint32_t left, uint32_t in_bin) {
+  if (in_bin == 0) return false;
+  const uint32_t rest = (1u << search_shift(*x)) - 1u, lo = x->lo + bin * (rest + 1);
+  if (left == in_bin) {  // every number of the counter is among the k: all above lo - 1 are
+    *x = Search{lo - 1, lo - 1, 0};
+    return false;
+  }
+  *x = Search{lo, x->hi - lo < rest ? x->hi : lo + rest, left};
+  return x->lo < x->hi;
+}
 static_assert(sizeof(MoveArgs) <= 3776 && sizeof(EvictArgs) <= 3776, "compaction kernel arguments too large");
 
 }  // namespace cp

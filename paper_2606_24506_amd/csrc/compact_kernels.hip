@@ -16,7 +16,6 @@ typedef unsigned int u32x4m __attribute__((ext_vector_type(4)));
 namespace {
 
 constexpr int kSelWaves = kSelectThreads / 64;
-constexpr int kBins = 2048;
 constexpr uint32_t kCands = 2048;  // numbers still possible that fit LDS
 
 // Numbers in the order of floats, from 1 on: NaN (1) below all, -0 as 0. 0 is no number.
@@ -38,8 +37,9 @@ struct Cut {
 // the middle's sums is found by counting: each pass spreads the numbers between the
 // smallest and the largest that are still possible over 2,048 counters (in the order of
 // floats, which spreads sums of any scale) and keeps the counter that holds the k-th; after
-// at most three passes it holds one value. Then every wave writes the numbers of its piece
-// that stay, in their order.
+// at most three passes it holds one value (compact.h: also of a row that is written
+// meanwhile, which gives some list, in bounds). Then every wave writes the numbers of its
+// piece that stay, in their order.
 // R > 0: the row in registers, R numbers a thread (rows of up to 1,024 R); 0: read again in
 // each pass, eight loads in flight. Bound by the passes of one workgroup: rows of 5,000 numbers
 // 12 us, of 16 K 14, of 64 K 35 (107 when each pass read them all again), of 128 K, which are
@@ -48,7 +48,7 @@ template <int R>
 __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(const EvictArgs a) {
   __shared__ uint32_t hist[kBins];
   __shared__ uint32_t part[2][kSelWaves];
-  __shared__ uint32_t found[5];  // lo, hi, still needed, as many in the counter; candidates
+  __shared__ uint32_t found[4];  // the counter, which of its numbers, how many it holds (0: no counter); candidates
   __shared__ uint32_t cand[kCands];
   const int r = sorted_search(a.n_req, blockIdx.x, [&](int i) { return a.req[i].block_begin; });
   const EvictReq &rq = a.req[r];
@@ -128,22 +128,23 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(const Evic
   hi = __builtin_amdgcn_readfirstlane(hi);
   Cut cut{need0 == m ? 0u : hi, 0u};  // (nothing to find where none, or all, of the middle stay)
   if (need0 > 0 && need0 < m) {
-    uint32_t need = need0;
-    bool few = false;  // the numbers still possible are `cand`, n_cand of them
-    while (lo < hi) {
-      const int bits = 32 - __builtin_clz(hi - lo), s = bits > 11 ? bits - 11 : 0;
+    Search x{lo, hi, need0};
+    bool few = false;  // the numbers still possible are `cand`, found[3] of them
+    for (bool more = lo < hi; more;) {
+      const int s = search_shift(x);
       for (uint32_t i = tid; i < kBins; i += kSelectThreads) hist[i] = 0;
+      if (tid == 0) found[2] = 0;
       __syncthreads();
       // (as many may be the smallest, tokens that nothing looked at: counted by the wave)
       if (few) {
-        for (uint32_t i = tid; i < found[4]; i += kSelectThreads)
-          if (cand[i] - lo <= hi - lo) atomicAdd(&hist[(cand[i] - lo) >> s], 1u);
+        for (uint32_t i = tid; i < min(found[3], kCands); i += kSelectThreads)
+          if (cand[i] - x.lo <= x.hi - x.lo) atomicAdd(&hist[(cand[i] - x.lo) >> s], 1u);
       } else {
         uint32_t least = 0;
         each_of([&](uint32_t, uint32_t k) {
-          const uint32_t off = k - lo;
+          const uint32_t off = k - x.lo;
           least += (uint32_t)__builtin_popcountll(__builtin_amdgcn_ballot_w64(off == 0));
-          if (off - 1 < hi - lo) atomicAdd(&hist[off >> s], 1u);
+          if (off - 1 < x.hi - x.lo) atomicAdd(&hist[off >> s], 1u);
         });
         if (lane == 0 && least) atomicAdd(&hist[0], least);
       }
@@ -153,41 +154,33 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(const Evic
       uint32_t sum = h0 + h1;
 #pragma unroll
       for (int o = 1; o < 64; o <<= 1) {
-        const uint32_t x = (uint32_t)__shfl_up((int)sum, o, 64);
-        if (lane >= o) sum += x;
+        const uint32_t y = (uint32_t)__shfl_up((int)sum, o, 64);
+        if (lane >= o) sum += y;
       }
       if (lane == 63) part[0][wave] = sum;
       __syncthreads();
       uint32_t before = sum - h0 - h1;
       for (int i = 0; i < wave; ++i) before += part[0][i];
-      if (before < need && need <= before + h0 + h1) {
-        const bool first = need <= before + h0;
-        const uint32_t bin = kBins - 1 - 2 * tid - (first ? 0u : 1u), left = need - before - (first ? 0u : h0);
-        const uint32_t nlo = lo + (bin << s);
-        found[0] = nlo;
-        found[1] = min(hi, nlo + ((1u << s) - 1u));
-        found[2] = left;
-        found[3] = first ? h0 : h1;
+      if (before < x.need && x.need <= before + h0 + h1) {
+        const bool first = x.need <= before + h0;
+        found[0] = kBins - 1 - 2 * tid - (first ? 0u : 1u);
+        found[1] = x.need - before - (first ? 0u : h0);
+        found[2] = first ? h0 : h1;
       }
       __syncthreads();
-      lo = __builtin_amdgcn_readfirstlane(found[0]);
-      hi = __builtin_amdgcn_readfirstlane(found[1]);
-      need = __builtin_amdgcn_readfirstlane(found[2]);
-      const uint32_t in_bin = __builtin_amdgcn_readfirstlane(found[3]);
-      if (need == in_bin) {  // every number of the counter is among them
-        lo = hi = lo - 1;
-        need = 0;
-      } else if (!few && lo < hi && in_bin <= kCands) {  // those of the counter, in any order
-        if (tid == 0) found[4] = 0;
+      const uint32_t in_bin = __builtin_amdgcn_readfirstlane(found[2]);
+      more = search_narrow(&x, __builtin_amdgcn_readfirstlane(found[0]), __builtin_amdgcn_readfirstlane(found[1]), in_bin);
+      if (more && !few && in_bin <= kCands) {  // those of the counter, in any order
+        if (tid == 0) found[3] = 0;
         __syncthreads();
         each_of([&](uint32_t, uint32_t k) {
-          if (k - lo <= hi - lo) cand[atomicAdd(&found[4], 1u) % kCands] = k;
+          if (k - x.lo <= x.hi - x.lo) cand[atomicAdd(&found[3], 1u) % kCands] = k;
         });
         few = true;
       }
       __syncthreads();
     }
-    cut = Cut{lo, need};
+    cut = Cut{x.lo, x.need};
   }
 
   // ---- the numbers that stay, in order
@@ -242,7 +235,7 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(const Evic
 #pragma unroll
     for (int u = 0; u < U; ++u) from[u] = list[min(c + u * kSelectThreads + tid, rq.keep - 1)];
 #pragma unroll
-    for (int u = 0; u < U; ++u) v[u] = w[from[u]];
+    for (int u = 0; u < U; ++u) v[u] = w[min((uint32_t)from[u], rq.n - 1)];  // (all written, unless the sums change)
     __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);
     __syncthreads();
 #pragma unroll
