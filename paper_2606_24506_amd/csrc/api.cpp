@@ -8,6 +8,7 @@
 #include <cstdio>
 #include <cstring>
 #include <string>
+#include <tuple>
 #include <type_traits>
 #include <unordered_map>
 #include <vector>
@@ -2641,6 +2642,7 @@ struct RowSpan {
   uint64_t lo, hi;
   int32_t kind, entry;  // kind: an argument of the call
   const cp_token_rows *rows;
+  bool same;  // sums in the place of their old ones
 };
 
 // Checks one argument: room for len[i] tokens of every KV head and layer, rows that do not
@@ -2660,40 +2662,95 @@ cp_status check_token_rows(const char *what, int32_t kind, int32_t n, const cp_t
       return fail(CP_EINVAL, "%s of entry %d: rows of layers overlap", what, i);
     const uint64_t at = (uint64_t)(uintptr_t)r.data + (layer > 0 ? 4 * (uint64_t)(layer * r.layer) : 0);
     const int32_t n_layers = layer < 0 ? layers : 1;
-    spans->push_back(RowSpan{at, at + 4 * (uint64_t)((n_layers > 1 ? (n_layers - 1) * r.layer : 0) + one), kind, i, &r});
+    spans->push_back(RowSpan{at, at + 4 * (uint64_t)((n_layers > 1 ? (n_layers - 1) * r.layer : 0) + one), kind, i, &r, false});
   }
   return CP_OK;
 }
 
-// Do rows of x and y, each in rising places, meet? (Slices of one tensor may lie between
-// one another's rows.)
-bool rows_meet(const RowSpan &x, const RowSpan &y, int32_t hkv, int32_t layers) {
-  auto row = [&](const RowSpan &s, int64_t i) {
-    return s.lo + 4 * (uint64_t)((layers > 1 ? i / hkv * s.rows->layer : 0) + (hkv > 1 ? i % hkv * s.rows->head : 0));
+// Looks through the rows of spans that overlap one another (slices of one tensor may lie
+// between one another's rows), in the order of their places: of those before a row the one
+// that ends last says whether it meets any.
+cp_status check_rows_between(const std::vector<RowSpan> &spans, size_t from, size_t to, int32_t hkv, int32_t layers) {
+  struct Piece {
+    uint64_t lo, hi;
+    const RowSpan *of;
   };
-  const int64_t n = (int64_t)hkv * layers;
-  for (int64_t i = 0, j = 0; i < n && j < n;) {
-    const uint64_t a = row(x, i), b = row(y, j);
-    if (a < b + 4 * (uint64_t)y.rows->len && b < a + 4 * (uint64_t)x.rows->len) return true;
-    if (a < b) ++i;
-    else ++j;
+  std::vector<Piece> rows;
+  rows.reserve((to - from) * (size_t)hkv * (size_t)layers);
+  auto put = [&](const RowSpan &s, int32_t l, int32_t h) {
+    const uint64_t lo = s.lo + 4 * (uint64_t)((layers > 1 ? l * s.rows->layer : 0) + (hkv > 1 ? h * s.rows->head : 0));
+    rows.push_back(Piece{lo, lo + 4 * (uint64_t)s.rows->len, &s});
+  };
+  auto before = [](const Piece &x, const Piece &y) { return x.lo < y.lo; };
+  // (spans are in order, and their rows where all have one layout: requests beside one
+  // another for each head, or heads for each request)
+  for (int32_t l = 0; l < layers; ++l)
+    for (int32_t h = 0; h < hkv; ++h)
+      for (size_t k = from; k < to; ++k) put(spans[k], l, h);
+  if (!std::is_sorted(rows.begin(), rows.end(), before)) {
+    rows.clear();
+    for (int32_t l = 0; l < layers; ++l)
+      for (size_t k = from; k < to; ++k)
+        for (int32_t h = 0; h < hkv; ++h) put(spans[k], l, h);
+    if (!std::is_sorted(rows.begin(), rows.end(), before)) std::sort(rows.begin(), rows.end(), before);
   }
-  return false;
+  const Piece none{0, 0, nullptr};
+  Piece written = none, read = none, other = none;  // those that end last; other: of another entry than `read`
+  for (const Piece &x : rows) {
+    const bool own = read.of && read.of->entry == x.of->entry;
+    const Piece *hit = nullptr;
+    if (x.of->kind == 0) {
+      if (written.hi > x.lo && !(x.of->same && written.of->same && written.of->entry == x.of->entry)) hit = &written;
+    } else {
+      if (written.hi > x.lo) hit = &written;
+      else if ((own ? other : read).hi > x.lo) hit = own ? &other : &read;
+      else if (own && read.hi > x.lo && !x.of->same) hit = &read;
+    }
+    if (hit)
+      return fail(CP_EINVAL, "rows per token of entries %d and %d overlap without being the same", hit->of->entry, x.of->entry);
+    if (x.of->kind != 0) {
+      written = x;
+    } else if (x.hi >= read.hi) {
+      if (!own) other = read;
+      read = x;
+    } else if (!own && x.hi > other.hi) {
+      other = x;
+    }
+  }
+  return CP_OK;
 }
 
 // Arguments 0 are read, those of other kinds written. What is written overlaps nothing, but
-// that an entry of argument 1 may be the same as its entry of argument 0.
+// that an entry of argument 1 may be the same as its entry of argument 0. (128 requests of
+// 32 layers and 8 KV heads in one tensor: 0.2 ms; a tensor each 25 us.)
 cp_status check_rows_apart(std::vector<RowSpan> *spans, int32_t hkv, int32_t layers) {
-  std::sort(spans->begin(), spans->end(), [](const RowSpan &x, const RowSpan &y) { return x.lo < y.lo; });
-  for (size_t k = 0; k < spans->size(); ++k)
-    for (size_t j = k + 1; j < spans->size() && (*spans)[j].lo < (*spans)[k].hi; ++j) {
-      const RowSpan &x = (*spans)[k], &y = (*spans)[j];
-      if (x.kind == 0 && y.kind == 0) continue;
-      const bool same = x.kind + y.kind == 1 && x.entry == y.entry && x.lo == y.lo &&
-                        (hkv == 1 || x.rows->head == y.rows->head) && (layers == 1 || x.rows->layer == y.rows->layer);
-      if (!same && rows_meet(x, y, hkv, layers))
-        return fail(CP_EINVAL, "rows per token of entries %d and %d overlap without being the same", x.entry, y.entry);
+  std::sort(spans->begin(), spans->end(), [](const RowSpan &x, const RowSpan &y) {
+    return std::tie(x.lo, x.entry, x.kind) < std::tie(y.lo, y.entry, y.kind);
+  });
+  size_t n = 0;
+  for (size_t k = 0; k < spans->size(); ++k) {
+    RowSpan &x = (*spans)[k];
+    if (x.kind == 0 && k + 1 < spans->size()) {
+      RowSpan &y = (*spans)[k + 1];
+      x.same = y.same = y.kind == 1 && y.entry == x.entry && y.lo == x.lo && (hkv == 1 || y.rows->head == x.rows->head) &&
+                        (layers == 1 || y.rows->layer == x.rows->layer);
+      if (x.same && x.rows->len == y.rows->len) continue;  // the written ones stand for both
     }
+    (*spans)[n++] = x;
+  }
+  spans->resize(n);
+  for (size_t k = 0, j; k < n; k = j) {
+    uint64_t hi = (*spans)[k].hi;
+    bool writes = (*spans)[k].kind != 0;
+    for (j = k + 1; j < n && (*spans)[j].lo < hi; ++j) {
+      hi = std::max(hi, (*spans)[j].hi);
+      writes = writes || (*spans)[j].kind != 0;
+    }
+    if (j > k + 1 && writes) {
+      const cp_status rc = check_rows_between(*spans, k, j, hkv, layers);
+      if (rc) return rc;
+    }
+  }
   return CP_OK;
 }
 

@@ -329,3 +329,122 @@ def random_cuts(seed):
     assert p.stats()["pages_used"] == p.stats()["pages_reserved"] == 0
     p.destroy()
     return refused, together
+
+
+# ------------------------------------- rows per token in one another's memory
+
+ROWS = """
+import random, time
+T = 16
+def books(n, layers, heads):
+    p = cpl.Pool(page_tokens=P, pool_bytes=4 << 30, chunk_bytes=1 << 20, device=0)
+    m = p.register(cpl.CP_KIND_GQA, heads, heads, head_dim=64, n_layers=layers)
+    ids = [p.open(m, T) for _ in range(n)]
+    p.append(ids, [T] * n, at, 0)
+    return p, ids
+def weights(p, ids, layer, old, new):
+    n = len(ids)
+    return LIB.cp_attn_weights(p.handle, n, I32(*ids), I32(*[0] * n), None, None, layer, 0.5, old, new, None, None)
+def evict(p, ids, w, new, kept):  # of nothing: requests are left as they are
+    n = len(ids)
+    o = cp_evict_opts(0, 0, *(None if x is None else ctypes.addressof(x) for x in (new, kept)))
+    return LIB.cp_kv_evict(p.handle, n, I32(*ids), I64(*[T] * n), w, by(o), None)
+BASE = 1 << 30
+"""
+
+
+def test_overlaps_of_rows_against_every_pair(queued):
+    """Records of all kinds in a small memory: a call is refused where a row that it writes
+    has an element of another's, but for sums in the place of their own old ones."""
+    run(MORE + ROWS + """
+rng = random.Random(7)
+tally = {}
+for layers, heads in ((1, 1), (1, 3), (2, 1), (3, 2)):
+    p, ids = books(4, layers, heads)
+    for trial in range(1500):
+        n = rng.randint(1, 4)
+        grid = rng.random() < 0.6  # one layout for all, or each its own
+        def strides():
+            head = rng.choice([T, T + 3, 2 * T, 4 * T, 5 * T])
+            one = (heads - 1) * head + T
+            return head, rng.choice([one, one + 5, one + T, 4 * heads * T, 8 * heads * T])
+        shared = strides()
+        def record():
+            head, layer = shared if grid else strides()
+            longest = min(head if heads > 1 else 99, layer - (heads - 1) * head if layers > 1 else 99)
+            length = T if rng.random() < 0.7 else rng.randint(T, max(T, min(longest, T + 6)))
+            start = rng.randrange(64) * T if rng.random() < 0.8 else rng.randrange(64 * T)
+            return cp_token_rows(BASE + 4 * start, length, head, max(layer, (heads - 1) * head + length))
+        first, second, third = ([record() for _ in range(n)] for _ in range(3))
+        for i in range(n):
+            if rng.random() < 0.6:
+                x = first[i]
+                second[i] = cp_token_rows(x.data, x.len if rng.random() < 0.8 else T, x.head, x.layer)
+        third = third if rng.random() < 0.3 else None
+        of_layer = rng.randrange(layers)
+        for call in ("weights", "evict"):
+            some = [of_layer] if call == "weights" else range(layers)
+            cells = []  # (argument, entry, element, row)
+            for a, recs in enumerate((first, second, third if call == "evict" else None)):
+                for i, x in enumerate(recs or ()):
+                    for l in some:
+                        for h in range(heads):
+                            at0 = (x.data - BASE) // 4 + (l * x.layer if layers > 1 else 0) + (h * x.head if heads > 1 else 0)
+                            cells += [(a, i, at0 + t) for t in range(x.len)]
+            def same(i):
+                x, y = first[i], second[i]
+                return x.data + (4 * of_layer * (x.layer - y.layer) if call == "weights" and layers > 1 else 0) == y.data and (
+                    heads == 1 or x.head == y.head) and (call == "weights" or layers == 1 or x.layer == y.layer)
+            by_cell, clash = {}, False
+            for a, i, c in cells:
+                for b, j in by_cell.setdefault(c, []):
+                    if a == b == 0 or (a + b == 1 and i == j and same(i)):
+                        continue
+                    clash = True
+                by_cell[c].append((a, i))
+            if call == "weights":
+                rc = weights(p, ids[:n], of_layer, rows(*first), rows(*second))
+            else:
+                rc = evict(p, ids[:n], rows(*first), rows(*second), rows(*third) if third else None)
+            text = LIB.cp_last_error().decode()
+            assert rc == (cpl.CP_EINVAL if clash else cpl.CP_OK), (rc, text, clash, trial, call, layers, heads)
+            assert not clash or "overlap without being the same" in text
+            tally[call, clash] = tally.get((call, clash), 0) + 1
+    for r in ids:
+        p.close(r)
+    p.destroy()
+assert min(tally.values()) > 800 and len(tally) == 4, tally
+""", queued)
+
+
+LAYOUTS = {  # (start, from head to head, from layer to layer) of request r's rows, in one tensor
+    "[layer][request][head][token]": "(r * H * T, T, n * H * T)",
+    "[layer][head][request][token]": "(r * T, n * T, n * H * T)",
+    "[request][layer][head][token]": "(r * n_layers * H * T, T, H * T)",
+    "half of the requests each way": "(r * T, n * T // 2, n * H * T) if r < n // 2 else (r * H * T, T, n * H * T)",
+    "layers apart by the request": "(r * T, 2 * n * T, 2 * n * H * T + r)",
+}
+
+
+@pytest.mark.parametrize("layout", sorted(LAYOUTS))
+def test_many_requests_in_one_tensor_are_looked_through_once(layout, queued):
+    """512 requests of 16 layers and 8 KV heads (a second and more where every pair of
+    requests was compared, row by row)."""
+    run(MORE + ROWS + f"""
+n, n_layers, H = 512, 16, 8
+place = lambda r: {LAYOUTS[layout]}
+p, ids = books(n, n_layers, H)
+recs = [cp_token_rows(BASE + 4 * a, T, h, l) for a, h, l in map(place, range(n))]
+W = rows(*recs)
+t0 = time.perf_counter()
+assert evict(p, ids, W, W, None) == cpl.CP_OK, LIB.cp_last_error()
+assert weights(p, ids, 3, W, W) == cpl.CP_OK
+took = time.perf_counter() - t0
+assert took < 0.5, took
+x = recs[200]
+recs[200] = cp_token_rows(x.data + 4, x.len, x.head, x.layer)  # some last element is another's first
+assert evict(p, ids, rows(*recs), rows(*recs), None) == cpl.CP_EINVAL
+for r in ids:
+    p.close(r)
+p.destroy()
+""", queued)
