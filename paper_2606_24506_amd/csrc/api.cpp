@@ -2970,13 +2970,22 @@ namespace {
 // taken, on success.
 cp_status prepare_cut(cp_pool *p, int32_t n, const int32_t *ids, const int64_t *from, const int64_t *new_len) {
   std::vector<int64_t> more, pages;
-  bool exact = p->st.virt() || p->dev_pages;  // (the bound first; a chunk is taken only for pages that fill it)
-  p->st.cut_cost(n, ids, from, new_len, exact, &more, &pages);
-  if (!exact) {
-    for (int32_t m = 0; m < p->st.n_models() && !exact; ++m) exact = pages[(size_t)m] > p->st.free_slots(m);
-    if (exact || !p->st.fits_budget(more)) p->st.cut_cost(n, ids, from, new_len, true, &more, &pages);
+  // The bound first: what the pages' users say is asked only where it decides (a chunk is
+  // taken for pages that fill it, a virtual pool's memory for what is promised, and a
+  // stack's pages for those that take them).
+  using Cut = PoolState::Cut;
+  bool enough = !p->st.virt() && !p->dev_pages;
+  auto count = [&](Cut how) { p->st.cut_cost(n, ids, from, new_len, how, &more, &pages); };
+  if (enough) {
+    count(Cut::kBound);
+    for (int32_t m = 0; m < p->st.n_models() && enough; ++m) enough = pages[(size_t)m] <= p->st.free_slots(m);
+    if (!enough || !p->st.fits_budget(more)) count(Cut::kShared);
+    enough = p->st.fits_budget(more);
   }
-  if (!p->st.fits_budget(more)) return fail(CP_ENOSPC, "the pool page budget cannot take pages in the place of shared ones");
+  if (!enough) {
+    count(Cut::kExact);
+    if (!p->st.fits_budget(more)) return fail(CP_ENOSPC, "the pool page budget cannot take pages in the place of shared ones");
+  }
   std::vector<int32_t> carved;
   for (int32_t m = 0; m < p->st.n_models(); ++m) {
     if (p->dev_pages && pages[(size_t)m] > 0) {  // the stack keeps what requests may take beside these

@@ -548,7 +548,7 @@ void PoolState::truncate(int32_t id, int64_t new_len) {
   if (new_len == 0) r.dropped = 0;
 }
 
-void PoolState::cut_cost(int32_t n, const int32_t *ids, const int64_t *from, const int64_t *new_len, bool exact,
+void PoolState::cut_cost(int32_t n, const int32_t *ids, const int64_t *from, const int64_t *new_len, Cut how,
                          std::vector<int64_t> *reserved, std::vector<int64_t> *pages) const {
   reserved->assign(models_.size(), 0);
   pages->assign(models_.size(), 0);
@@ -557,7 +557,7 @@ void PoolState::cut_cost(int32_t n, const int32_t *ids, const int64_t *from, con
     const Request &r = reqs_[ids[i]];
     const int64_t keep = ceil_div(new_len[i], P_), k0 = std::min(from[i] / P_, keep);
     int64_t &more = (*reserved)[(size_t)r.model], &own = (*pages)[(size_t)r.model];
-    if (!exact) {
+    if (how == Cut::kBound) {
       more += (r.pages_used - k0) * r.layers;
       own += (keep - k0) * r.layers;
       continue;
@@ -567,11 +567,11 @@ void PoolState::cut_cost(int32_t n, const int32_t *ids, const int64_t *from, con
       each_shared(pt, r.pages_used - k0, [&](int64_t k) {
         more += 1;
         own += k < keep - k0;
-        if (n > 1) given.push_back(pt[k]);
+        if (how == Cut::kExact) given.push_back(pt[k]);
       });
     }
   }
-  if (!exact) return;
+  if (how != Cut::kExact) return;
   // a page that every user gives up is freed, and owes nothing
   std::sort(given.begin(), given.end());
   for (size_t i = 0, j; i < given.size(); i = j) {

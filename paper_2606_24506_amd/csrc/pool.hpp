@@ -221,9 +221,10 @@ class PoolState {
   // the old pages are given up, and each request truncated.
   // cut_cost: the room beside each model's `reserved` that this needs, for what is promised
   // behind it and for replaced pages beside their replacements (with a device stack that
-  // holds no more than it may then), and the pages it allocates; not exact: at most that
-  // (as if every page were shared, and every one with others).
-  void cut_cost(int32_t n, const int32_t *ids, const int64_t *from, const int64_t *new_len, bool exact,
+  // holds no more than it may then), and the pages it allocates. kBound: at most that, as if
+  // every page were shared; kShared: as if every shared page had users outside the call.
+  enum class Cut { kBound, kShared, kExact };
+  void cut_cost(int32_t n, const int32_t *ids, const int64_t *from, const int64_t *new_len, Cut how,
                 std::vector<int64_t> *reserved, std::vector<int64_t> *pages) const;
   void cut_own(int32_t id, int64_t from, int64_t new_len, std::vector<OwnPage> *copies);
   // (*scratch: room for as many entries as copies)
