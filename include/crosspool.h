@@ -26,9 +26,10 @@
  *     (CP_EHIP from a copy or launch of an append or decode step) leaves
  *     the host tables updated as if the call had succeeded; the device
  *     state is then undefined and the pool should be closed. After such a
- *     failure of cp_request_fork, cp_request_truncate or cp_attn_extend_step
- *     the pool refuses work on its device memory (CP_ESTATE); requests can
- *     still be closed and the pool destroyed.
+ *     failure of cp_request_fork, cp_request_truncate, cp_request_keep,
+ *     cp_kv_evict, cp_attn_extend_step or cp_attn_tree_step the pool refuses
+ *     work on its device memory (CP_ESTATE); requests can still be closed and
+ *     the pool destroyed.
  *   - Device-memory arguments are device pointers on the pool's device;
  *     host arguments are ordinary host pointers and are not retained after
  *     the call returns. Streams are hipStream_t passed as void* (NULL = the
@@ -723,6 +724,9 @@ typedef struct {
  *            tree, less than its own; any other value (-1 is usual): a child of
  *            the context's last token, depth 0.
  *   mask     device, out, [sum n_tok][words]; depth: device, out, [sum n_tok].
+ * A mask names every ancestor. A tree deeper than a sliding window would see
+ * further back along its branches than cp_attn_extend does along the accepted
+ * one: bits of ancestors `window` or more positions back are the caller's to clear.
  * Errors: CP_EINVAL, CP_EHIP. */
 cp_status cp_tree_build(int32_t device, int32_t n, const int32_t *n_tok, const int32_t *parents, int32_t words,
                         uint32_t *mask, int32_t *depth, void *hip_stream);
@@ -765,7 +769,10 @@ typedef struct {
  * cp_attn_extend, and lse what that call (or a decode) gave for the same
  * queries and options. Rows whose lse is -inf give nothing; NaN in an lse gives NaN
  * to what its row sees. Sums are held in 32 bits, added in an order that the
- * call's arguments decide.
+ * call's arguments decide. Behind a tree and cp_request_keep the accepted tokens
+ * are the context's last, and saw there what they see here: their rows of q and of
+ * the tree's lse, packed in the path's order, are what this call takes. (Weights of a
+ * tree itself, branches that may go among it, there are none.)
  *   n_q    host, 0 <= n_q[i] <= context (0: the old sums decay).
  *   q, lse device, as in cp_attn_extend.
  *   layer  whose KV is read (and whose rows of old and sum are); the context is

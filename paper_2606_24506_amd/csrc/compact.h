@@ -15,8 +15,12 @@ constexpr int kEvictEntMax = 448;  // new page-table entries that one launch of 
 constexpr int kSelectThreads = 1024;
 constexpr int kKeepThreads = 256, kKeepCols = 16, kKeepUnroll = 4;     // cp_request_keep
 constexpr int kMoveThreads = 1024, kMoveCols = 8, kMoveUnroll = 8;     // evictions in place
-// ... where workgroups of kMoveCols columns are at most a quarter of the card's CUs (64 of them
-// 11.7 us, with half of the columns 10.0; 36 11.4 and 9.0; but 192 26 and 28, 224 26 and 32)
+// ... where workgroups of kMoveCols columns are at most a quarter of the card's CUs: twice as
+// many read every line twice, and pay only while CUs are idle. (Evictions of 16 K to 2 K
+// tokens, 8 heads of 128, by requests, us with eight columns and with four: one, 32 workgroups,
+// 33.4 and 30.9; two, 64, 35.5 and 34.4; three, 96, 42.3 and 43.6; four 49 and 49; six 51 and
+// 62. In 4 layers of 4 heads of 64, 4 K tokens: 32 23.8 and 23.8; 96 26.3 and 26.3; 192 29.4
+// and 32.5.)
 constexpr int kMoveFewCols = 4;
 constexpr int kApartThreads = 256, kApartUnroll = 4;                   // ... into pages of their own
 // Rows of a workgroup of those (segs: 16-byte pieces of a row).

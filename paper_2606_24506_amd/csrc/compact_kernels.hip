@@ -270,7 +270,7 @@ CP_DEV Column column_of(const GeomK &g, uint32_t seg) {
 // and those of later steps lie behind what this one writes (list entries rise: entry k is at
 // least k). So no workgroup waits for another. Bound by the round trips of a step (list,
 // page table, row), each asked for by all of a thread's rows at once: 2,048 of 16 K and 1,125
-// of 9 K tokens, 8 heads of 128, 10 us (13 MB read and written; 142 with one row in flight),
+// of 9 K tokens, 8 heads of 128, 11 us (13 MB, read twice and written; 142 with one row in flight),
 // half of four 4 K contexts in 16 layers 205 (5.2 TB/s);
 // accepted paths of 4 requests 3 us, 31 with the lists' loads in a row.
 template <int THREADS, int COLS, int UNROLL>
