@@ -693,7 +693,7 @@ def token_rows(tensors):
         arr[i] = cp_token_rows(t.data_ptr(), t.shape[-1], t.stride(-2), t.stride(0) if t.dim() == 3 else 0)
     arr.keep = tensors
     arr.shapes = {(t.shape[0] if t.dim() == 3 else 1, t.shape[-2]) for t in tensors}  # (layers, KV heads)
-    arr.floats = not tensors or str(tensors[0].dtype) == "torch.float32"
+    arr.floats = str(tensors[0].dtype) == "torch.float32" if tensors else None
     arr.device = tensors[0].device.index if tensors else None
     return arr
 
@@ -708,7 +708,7 @@ def _rows_arg(pool, req_ids, rows, floats: bool):
     known = _POOLS.get(pool)
     if len(rows) != len(req_ids):
         raise ValueError("one record of rows per request")
-    if rows.floats != floats:
+    if rows.floats not in (None, floats):
         raise ValueError("sums are float32, token numbers int32")
     if known is not None:
         if rows.device not in (None, known.device):

@@ -448,3 +448,14 @@ for r in ids:
     p.close(r)
 p.destroy()
 """, queued)
+
+
+def test_an_eviction_of_no_request(queued):
+    """Empty lists of rows are of either type."""
+    run(MORE + """
+p, m = heads_pool()
+p.evict([], [], [], 0, new=[], kept=[])
+none = cpl.token_rows([])
+p.evict([], [], none, 0, new=none, kept=none)
+p.destroy()
+""", queued)
