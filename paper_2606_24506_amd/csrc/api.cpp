@@ -332,7 +332,7 @@ cp_status refill_stacks(cp_pool *p, const std::vector<int64_t> &need, hipStream_
 // other models. Waits for the device.
 cp_status drain_stack(cp_pool *p, int32_t m, int64_t room) {
   std::vector<uint32_t> &st = p->stk[(size_t)m];
-  if ((int64_t)st.size() <= room) return CP_OK;
+  if ((int64_t)st.size() <= std::max<int64_t>(0, room)) return CP_OK;
   DeviceGuard g(p->device);
   hipError_t e = hipDeviceSynchronize();
   if (e != hipSuccess) return hip_fail(e, "waiting for the device before draining a page stack");

@@ -253,6 +253,20 @@ def test_a_prompt_and_its_fork_are_cut_in_one_call():
     p.destroy()
 
 
+def test_an_empty_stack_has_nothing_to_give_back():
+    """Replacements beyond what open requests may still take ask no device for pages."""
+    p = pool(chunks=2, pages_per_chunk=8, device_pages=1)
+    m = p.register(**ROW)
+    a, b = p.open(m, 3 * P), p.open(m, 3 * P)
+    grow(p, a, 3 * P)
+    p.fork([a], [b])
+    p.keep([a, b], [0, 0], [11, 11], [*range(1, 12)] * 2)
+    assert not set(p.pages(a)) & set(p.pages(b)) and p.stats()["pages_used"] == p.stats()["pages_reserved"] == 6
+    for r in (a, b):
+        p.close(r)
+    p.destroy()
+
+
 def cut_books(pages, reserve, first, lists):
     """(pages promised after a call, pages that stand beside one another in it) from the pages
     of every request, for the requests that the call cuts."""
