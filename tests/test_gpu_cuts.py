@@ -30,7 +30,7 @@ def behind():
 
 
 def test_a_fork_keeps_a_prompt_that_is_evicted_behind_other_work():
-    """The entries of 2,000 new pages are on their way while the pages are shared, replaced
+    """The entries of 2,000 new pages (1,000 in each layer) are on their way while the pages are shared, replaced
     and shared again."""
     print("[case] append, fork, evict, fork, evict behind other work", flush=True)
     layers, n = 2, 4000
@@ -135,4 +135,32 @@ def test_pages_that_wait_in_a_device_stack_make_room(call):
     for r in (a, b, c):
         p.close(r)
     assert p.stats()["pages_used"] == p.stats()["pages_reserved"] == 0
+    p.destroy()
+
+
+def test_entries_go_round_their_memory():
+    """Appends of 1,000 entries each, dropped and placed again in another order, with no
+    waiting in between: more of them than the memory that they are copied from holds."""
+    print("[case] entries round and round", flush=True)
+    layers, n, rounds = 2, 2000, 160
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    chunk = 16 * P * 2 * ROW
+    p = cpl.Pool(page_tokens=P, pool_bytes=300 * chunk, chunk_bytes=chunk, device=0)
+    m = p.register(**GEOMS[NAME], n_layers=layers)
+    ids = [p.open(m, n) for _ in range(2)]
+    rows = [normal(gen, layers, n, ROW) for _ in range(3)]
+    wrong = torch.zeros(rounds, 2, dtype=torch.int64, device="cuda")
+    out = torch.zeros(layers, n, ROW, dtype=torch.bfloat16, device="cuda")
+    torch.cuda.synchronize()
+    behind()
+    for i in range(rounds):
+        for k in ((0, 1), (1, 0))[i % 2]:
+            p.append([ids[k]], [n], rows[(i + k) % 3])
+        for k in range(2):
+            p.gather(ids[k], 0, n, out)
+            wrong[i, k] = (out != rows[(i + k) % 3]).sum()
+        p.truncate(ids, [0, 0])
+    assert (wrong == 0).all(), wrong.nonzero()
+    for r in ids:
+        p.close(r)
     p.destroy()
